@@ -290,6 +290,110 @@ int grouter_moe_step_host(grouter_ctx* ctx, const void* idx_host, const void* ga
  * (No counterpart in the paper: host-side plumbing of the step call.) */
 int grouter_host_wait(grouter_ctx* ctx, int32_t steps_in_flight);
 
+/* ---- Operators around the expert layer in a training step (no counterpart in the paper, which takes the block's other
+ * parts as given) ----
+ * These calls need no context.  Unlike the calls above they accept any pointer that is aligned to its element type
+ * (16-byte-aligned rows take the faster accesses) where the comment says "any alignment". */
+enum { GROUTER_BF16 = 0, GROUTER_F32 = 1 };
+
+/* Layer norm of every row:  y = (x - mean) * rstd * w + b  with mean = (1/d) sum x, rstd = ((1/d) sum (x-mean)^2 + eps)^(-1/2).
+ *   x  [rows, d] of dtype, row r at x + r*ldx elements (ldx >= d)      y [rows, d] of dtype, contiguous
+ *   w, b [d] of w_dtype (b may be NULL)       mean, rstd [rows] f32 out (either may be NULL)
+ * Sums and statistics are fp32; y is rounded once.  d <= 16384.  Any alignment.  rows = 0 does nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+int grouter_layernorm_fwd(const void* x, int64_t ldx, const void* w, const void* b, int32_t rows, int32_t d, int32_t dtype, int32_t w_dtype,
+                          float eps, void* y, float* mean, float* rstd, void* stream);
+/* Its backward pass, from the saved mean and rstd:  with h = (x - mean) * rstd and g = dy * w,
+ *   dx = rstd * (g - (1/d) sum g - h * (1/d) sum g*h)  [rows, d] of dtype
+ *   dw = sum over rows of dy * h,  db = sum over rows of dy   [d] f32 (db may be NULL)
+ * dy and dx are contiguous and must not overlap the inputs.  workspace: grouter_layernorm_bwd_workspace_bytes(rows, d) bytes (of
+ * the current device).  All sums run in a fixed order: results are bit-reproducible.  rows = 0 zeroes dw and db.
+ * Errors as above. */
+size_t grouter_layernorm_bwd_workspace_bytes(int32_t rows, int32_t d);
+int grouter_layernorm_bwd(const void* dy, const void* x, int64_t ldx, const void* w, const float* mean, const float* rstd, int32_t rows,
+                          int32_t d, int32_t dtype, int32_t w_dtype, void* dx, float* dw, float* db, void* workspace, void* stream);
+
+/* Linear layer:  z = x W^T + bias,  y = act(z) + residual   (all tensors bf16, contiguous, 16-byte aligned).
+ *   x [T,K]   W [N,K]   bias [N] or NULL   residual [T,N] or NULL   y [T,N] out   pre [T,N] out: z, or NULL
+ *   act: GROUTER_ACT_*; GELU in its tanh form, z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2
+ *   status: device int32 the kernels OR bits into (2 = a bounded wait ran out); the caller zeroes it
+ * bf16 tensor cores with fp32 accumulators; bias, activation and residual in fp32, y and pre rounded once.  Required: K and N
+ * multiples of 8, T >= 0.  residual may be y itself.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+enum { GROUTER_ACT_NONE = 0, GROUTER_ACT_RELU = 1, GROUTER_ACT_SILU = 2, GROUTER_ACT_GELU = 3 };
+int grouter_linear_fwd(const void* x, const void* W, const void* bias, const void* residual, int32_t T, int32_t K, int32_t N, int32_t act, void* y,
+                       void* pre, int32_t* status, void* stream);
+/* Its backward pass:  dz = dy * act'(pre) (relu'(0) = 0),  dx = dz W [T,K] bf16,  dW = dz^T x [N,K] of dW_dtype,
+ * db = sum over tokens of dz [N] f32.  Outputs that are not wanted are NULL (at least one is wanted); the residual's gradient is
+ * dy.  pre: the forward's z, needed with an activation.  dz enters the products rounded to bf16, db is summed from the unrounded
+ * values.  Results are bit-reproducible.  workspace: grouter_linear_bwd_workspace_bytes(T, K, N, act) bytes (of the current
+ * device), 256-byte aligned.  T = 0 zeroes dW and db.  Errors as above. */
+size_t grouter_linear_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N, int32_t act);
+int grouter_linear_bwd(const void* dy, const void* x, const void* W, const void* pre, int32_t T, int32_t K, int32_t N, int32_t act, void* dx,
+                       void* dW, int32_t dW_dtype, float* db, void* workspace, int32_t* status, void* stream);
+
+/* Tokens per expert, the f of the balance loss:  counts[e] = #{(t,j): idx[t,j] = e, mask[t] != 0},  n_tokens[0] = #{t: mask[t] != 0}.
+ *   idx [T,k] uint8 or int32 (idx_dtype), values in [0,E), 16-byte aligned     mask [T] bytes, or NULL: every token counts
+ *   counts [E] int32 out     n_tokens [1] int32 out
+ *   status: optional device int32, bit 1 ORed in when an id of a counted token is out of range (it is skipped); caller zeroes it
+ * E <= 1024 (256 for uint8 ids), k <= 32, T*k < 2^31.  T = 0 zeroes the outputs.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mask, int32_t T, int32_t k, int32_t E, int32_t* counts,
+                          int32_t* n_tokens, int32_t* status, void* stream);
+/* Balance and z losses of the router's scores, and their gradient.  With p = softmax of a row, lse = log sum exp of it,
+ * f_e = E counts_e / sum counts, n = n_tokens, sums over the tokens whose mask byte is set:
+ *   loss[1] = (1/n) sum_t sum_e f_e p_te        loss[2] = (1/n) sum_t lse_t^2        loss[0] = balance_coef loss[1] + z_coef loss[2]
+ *   dlogits = dloss * d loss[0] / d logits (the counts are constants), plus, with dgates, what comes back through the gates
+ *   r = g(kept scores) of grouter_route:  softmax over the k kept: q_j (dg_j - sum_i q_i dg_i);  sigmoid of each: q_j (1 - q_j) dg_j
+ *   logits [T,E] of dtype, row t at logits + t*ld elements; any alignment      dlogits [T,E] of dtype, contiguous, or NULL
+ *   counts [E], n_tokens [1]: of grouter_expert_counts, or summed over several ranks (counts: the share f is then global)
+ *   idx [T,k], dgates [T,k] f32: needed together (idx may be NULL without dgates)      dloss: device scalar or NULL (1)
+ *   loss [3] f32 out or NULL (not both NULL)      workspace: grouter_balance_loss_workspace_bytes() bytes, for the loss
+ *   status: optional device int32, bit 1: an id is out of range (its gate's gradient is left out)
+ * A masked token has a zero gradient row, whatever its scores.  A score of -inf has p = 0; a row of nothing but -inf has p = 0
+ * and lse = 0.  n = 0: losses are 0.  Coefficients of zero drop their term, finite or not.  E <= 1024 (256 for uint8 ids),
+ * k <= 32.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+size_t grouter_balance_loss_workspace_bytes(void);
+int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const void* idx, int32_t idx_dtype, const uint8_t* mask,
+                         const int32_t* counts, const int32_t* n_tokens, const float* dgates, int32_t norm, int32_t T, int32_t E, int32_t k,
+                         float balance_coef, float z_coef, const float* dloss, float* loss, void* dlogits, void* workspace, int32_t* status,
+                         void* stream);
+
+/* AdamW over a list of tensors in one launch, decoupled weight decay.  With g' = grad_scale * grad (grad_scale: device scalar or
+ * NULL) and c1 = 1 - beta1^step, c2 = 1 - beta2^step:
+ *   m = beta1 m + (1 - beta1) g'     v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr weight_decay) - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps)
+ * Every operation is rounded to f32 by itself.  A parameter is f32, or bf16 with an f32 master copy that is updated and rounded
+ * into it.  Moments and masters of all tensors lie in flat buffers; tensor i starts at the sum of the sizes before it, each rounded
+ * up to a multiple of 32 elements.  state_bits 32: m, v f32.  state_bits 8: m and sqrt(v) as one e4m3 byte an element and a
+ * power-of-two scale (exponent + 127, one byte) for 32 elements in m_exp, v_exp; a root that is not zero never rounds to zero.
+ * All-zero buffers are the state before the first step.
+ *
+ * grouter_adamw_layout_host (host): sizes of the flat buffers and of the table the step reads; with table_host (table_bytes
+ *   bytes) it also fills the table, which the caller copies to the device once.  The table holds the tensors' addresses.
+ * grouter_adamw_step: one step (step counts from 1).  The layout and the scalars are host values and are read before it returns.
+ *   Any alignment of parameters and gradients; flat buffers and the device's table 16-byte aligned.
+ * grouter_adamw_moments: the values that 8-bit moments stand for, as f32 (m_out = m, v_out = the root's square).
+ * Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+typedef struct {
+  void* param;
+  const void* grad;
+  int64_t n;
+  double weight_decay;
+  int32_t param_dtype, grad_dtype;    /* GROUTER_BF16 or GROUTER_F32 */
+} grouter_adamw_tensor;
+typedef struct {
+  int64_t state_elements;   /* of the flat buffers, a multiple of 32 */
+  uint64_t table_bytes;
+  int32_t n_tensors, n_chunks;
+  int32_t needs_master;     /* some parameter is bf16 */
+  int32_t reserved;
+} grouter_adamw_layout;
+int grouter_adamw_layout_host(const grouter_adamw_tensor* tensors, int32_t n_tensors, grouter_adamw_layout* layout, void* table_host);
+int grouter_adamw_step(const grouter_adamw_layout* layout, const void* table, int32_t state_bits, float* master, void* m, void* v,
+                       uint8_t* m_exp, uint8_t* v_exp, double lr, double beta1, double beta2, double eps, int64_t step, const float* grad_scale,
+                       void* stream);
+int grouter_adamw_moments(const void* m, const void* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t elements, float* m_out,
+                          float* v_out, void* stream);
+
 /* Synchronises `stream` and returns the sticky device status (GROUTER_OK,
  * GROUTER_ERR_BAD_INDEX, GROUTER_ERR_TIMEOUT) or GROUTER_ERR_CUDA; clears it. */
 int grouter_status(grouter_ctx* ctx, void* stream);

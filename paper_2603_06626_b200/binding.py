@@ -20,19 +20,35 @@ FLAG_ACCUMULATE_DW = 1
 FLAG_FUSED_COMBINE = 2
 NORM_SOFTMAX, NORM_SIGMOID = 0, 1
 GATE_BF16, GATE_F32 = 0, 1
+BF16, F32 = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 EXPORTS = ["grouter_create", "grouter_destroy", "grouter_workspace_bytes", "grouter_host_staging_bytes", "grouter_plan",
            "grouter_moe_fwd", "grouter_moe_bwd", "grouter_moe_step_host", "grouter_status", "grouter_strerror",
            "grouter_dense_gemm", "grouter_timing_enable", "grouter_timing_read", "grouter_plan_noalloc", "grouter_host_wait", "grouter_route", "grouter_route_workspace_bytes", "grouter_routing_stats",
            "grouter_fold_greedy_host", "grouter_timing_gap", "grouter_wgrad_chunk_rows", "grouter_gemm_cycles_enable", "grouter_gemm_cycles_read", "grouter_set_wait_limit", "grouter_wait_selftest", "grouter_set_overlap", "grouter_set_active_tokens",
            "grouter_checked_build",
-           "grouter_ep_relabel_host", "grouter_ep_layout_host", "grouter_ep_expand_ids", "grouter_ep_dispatch_rows", "grouter_ep_combine_rows"]
+           "grouter_ep_relabel_host", "grouter_ep_layout_host", "grouter_ep_expand_ids", "grouter_ep_dispatch_rows", "grouter_ep_combine_rows",
+           "grouter_layernorm_fwd", "grouter_layernorm_bwd", "grouter_layernorm_bwd_workspace_bytes",
+           "grouter_linear_fwd", "grouter_linear_bwd", "grouter_linear_bwd_workspace_bytes",
+           "grouter_expert_counts", "grouter_balance_loss", "grouter_balance_loss_workspace_bytes",
+           "grouter_adamw_layout_host", "grouter_adamw_step", "grouter_adamw_moments"]
 KERNEL_SLOTS = ["plan_hist", "plan_permute", "gather_X", "gemm_up_swiglu", "gemm_down", "combine_Y", "gather_dY", "gemm_dH",
                 "wgrad_down", "gemm_dX", "wgrad_gate_up", "reduce_dX", "zero_split_dW", "plan_scan"]
 
 
 class GrouterDims(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "ffn", "E_src", "E_tgt", "k", "idx_dtype", "gate_dtype", "flags")]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double),
+                ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class AdamwLayout(ctypes.Structure):
+    _fields_ = [("state_elements", ctypes.c_int64), ("table_bytes", ctypes.c_uint64), ("n_tensors", ctypes.c_int32), ("n_chunks", ctypes.c_int32),
+                ("needs_master", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class GrouterError(RuntimeError):
@@ -127,6 +143,32 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.grouter_timing_read.restype = ctypes.c_int
     lib.grouter_checked_build.argtypes = []
     lib.grouter_checked_build.restype = ctypes.c_int
+    i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    lib.grouter_layernorm_fwd.argtypes = [vp, i64, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp]
+    lib.grouter_layernorm_fwd.restype = ctypes.c_int
+    lib.grouter_layernorm_bwd_workspace_bytes.argtypes = [i32, i32]
+    lib.grouter_layernorm_bwd_workspace_bytes.restype = ctypes.c_size_t
+    lib.grouter_layernorm_bwd.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.grouter_layernorm_bwd.restype = ctypes.c_int
+    lib.grouter_linear_fwd.argtypes = [vp] * 4 + [i32] * 4 + [vp] * 4
+    lib.grouter_linear_fwd.restype = ctypes.c_int
+    lib.grouter_linear_bwd_workspace_bytes.argtypes = [i32] * 4
+    lib.grouter_linear_bwd_workspace_bytes.restype = ctypes.c_size_t
+    lib.grouter_linear_bwd.argtypes = [vp] * 4 + [i32] * 4 + [vp, vp, i32] + [vp] * 4
+    lib.grouter_linear_bwd.restype = ctypes.c_int
+    lib.grouter_expert_counts.argtypes = [vp, i32, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.grouter_expert_counts.restype = ctypes.c_int
+    lib.grouter_balance_loss_workspace_bytes.argtypes = []
+    lib.grouter_balance_loss_workspace_bytes.restype = ctypes.c_size_t
+    lib.grouter_balance_loss.argtypes = [vp, i64, i32, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, f32, f32, vp, vp, vp, vp, vp, vp]
+    lib.grouter_balance_loss.restype = ctypes.c_int
+    f64 = ctypes.c_double
+    lib.grouter_adamw_layout_host.argtypes = [ctypes.POINTER(AdamwTensor), i32, ctypes.POINTER(AdamwLayout), vp]
+    lib.grouter_adamw_layout_host.restype = ctypes.c_int
+    lib.grouter_adamw_step.argtypes = [ctypes.POINTER(AdamwLayout), vp, i32] + [vp] * 5 + [f64] * 4 + [i64, vp, vp]
+    lib.grouter_adamw_step.restype = ctypes.c_int
+    lib.grouter_adamw_moments.argtypes = [vp] * 4 + [i64, vp, vp, vp]
+    lib.grouter_adamw_moments.restype = ctypes.c_int
     if path == _build.LIB:
         _lib = lib
     return lib
@@ -403,6 +445,316 @@ def plan_noalloc(idx: torch.Tensor, fold_map: Optional[torch.Tensor], E_src: int
         _check(lib.grouter_plan_noalloc(_ptr(idx), dt, _ptr(fold_map), T, k, E_src, E_tgt, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
                                         _ptr(out[3]), _ptr(status), _stream()), "grouter_plan_noalloc")
     return (*out, status)
+
+
+def _elt(t: torch.Tensor, what: str) -> int:
+    """GROUTER_BF16 / GROUTER_F32 of a tensor; other types raise."""
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise TypeError(f"{what}: bfloat16 or float32 expected, got {t.dtype}")
+
+
+def _expect(what: str, t: Optional[torch.Tensor], shape, dtype=None, like: Optional[torch.Tensor] = None) -> None:
+    """Raises unless t (None passes) is a contiguous tensor of this shape (and type), on the same device as `like`."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous tensor is expected")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{what}: on {t.device}, the other arguments are on {like.device}")
+
+
+def _row_stride(what: str, x: torch.Tensor) -> int:
+    """Elements between the rows of a matrix whose rows are contiguous; other layouts raise."""
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is expected")
+    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        raise ValueError(f"{what}: rows that overlap")
+    return max(x.stride(0), x.shape[1]) if x.shape[0] > 1 else x.shape[1]
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5):
+    """grouter_layernorm_fwd: x [T,d] bf16/f32 (rows may be strided), weight and bias [d] bf16/f32 -> (y, mean f32 [T], rstd f32 [T])."""
+    lib = load_library()
+    ldx = _row_stride("x", x)
+    T, d = x.shape
+    _expect("weight", weight, (d,), like=x)
+    _expect("bias", bias, (d,), weight.dtype, like=x)
+    dt, wt = _elt(x, "x"), _elt(weight, "weight")
+    dev = x.device
+    with torch.cuda.device(dev):
+        y = torch.empty((T, d), dtype=x.dtype, device=dev)
+        stats = torch.empty((2, T), dtype=torch.float32, device=dev)
+        mean, rstd = stats[0], stats[1]
+        _check(lib.grouter_layernorm_fwd(x.data_ptr(), ldx, _ptr(weight), _ptr(bias), T, d, dt, wt, eps, _ptr(y), _ptr(mean), _ptr(rstd),
+                                         _stream()), "grouter_layernorm_fwd")
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, want_bias: bool = True):
+    """grouter_layernorm_bwd, from the forward's mean and rstd -> (dx like x, dw f32 [d], db f32 [d] or None)."""
+    lib = load_library()
+    ldx = _row_stride("x", x)
+    T, d = x.shape
+    _expect("dy", dy, (T, d), x.dtype, like=x)
+    _expect("weight", weight, (d,), like=x)
+    _expect("mean", mean, (T,), torch.float32, like=x)
+    _expect("rstd", rstd, (T,), torch.float32, like=x)
+    dt, wt = _elt(x, "x"), _elt(weight, "weight")
+    dev = x.device
+    with torch.cuda.device(dev):
+        dx = torch.empty((T, d), dtype=x.dtype, device=dev)
+        dw = torch.empty(d, dtype=torch.float32, device=dev)
+        db = torch.empty(d, dtype=torch.float32, device=dev) if want_bias else None
+        ws = torch.empty(max(1, lib.grouter_layernorm_bwd_workspace_bytes(T, d)), dtype=torch.uint8, device=dev)
+        _check(lib.grouter_layernorm_bwd(_ptr(dy), x.data_ptr(), ldx, _ptr(weight), _ptr(mean), _ptr(rstd), T, d, dt, wt, _ptr(dx), _ptr(dw),
+                                         _ptr(db), _ptr(ws), _stream()), "grouter_layernorm_bwd")
+    return dx, dw, db
+
+
+_status_words = {}
+
+
+def _status_word(dev: torch.device) -> torch.Tensor:
+    """The status word of a device that the calls without one of their own share."""
+    key = dev.index if dev.index is not None else torch.cuda.current_device()
+    if key not in _status_words:
+        _status_words[key] = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", key))
+        torch.cuda.synchronize(key)      # zeroed before a kernel on any stream can set a bit in it
+    return _status_words[key]
+
+
+def check_status(device="cuda:0") -> None:
+    """Waits for the device; raises when a linear, linear_backward, expert_counts or balance_loss call without a status word of its own
+    met a bounded wait that ran out or an expert id out of range since the last check, and clears the word."""
+    dev = torch.device(device)
+    torch.cuda.synchronize(dev)
+    word = _status_word(dev)
+    st = int(word.item())
+    word.zero_()
+    torch.cuda.synchronize(dev)
+    if st != 0:
+        raise GrouterError(-7 if st & 2 else -6, "device status")
+
+
+def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
+           save_pre: bool = False, status: Optional[torch.Tensor] = None):
+    """grouter_linear_fwd: act(x W^T + bias) + residual, x [T,K], W [N,K], all bf16 -> (y [T,N], x W^T + bias [T,N] or None)."""
+    lib = load_library()
+    if x.dim() != 2 or W.dim() != 2:
+        raise ValueError("x and W: matrices are expected")
+    T, K = x.shape
+    N = W.shape[0]
+    bf = torch.bfloat16
+    _expect("x", x, (T, K), bf)
+    _expect("W", W, (N, K), bf, like=x)
+    _expect("bias", bias, (N,), bf, like=x)
+    _expect("residual", residual, (T, N), bf, like=x)
+    _expect("status", status, (1,), torch.int32, like=x)
+    dev = x.device
+    with torch.cuda.device(dev):
+        y = torch.empty((T, N), dtype=bf, device=dev)
+        pre = torch.empty((T, N), dtype=bf, device=dev) if save_pre else None
+        _check(lib.grouter_linear_fwd(_ptr(x), _ptr(W), _ptr(bias), _ptr(residual), T, K, N, act, _ptr(y), _ptr(pre),
+                                      _ptr(_status_word(dev) if status is None else status), _stream()), "grouter_linear_fwd")
+    return y, pre
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+                    want_dx: bool = True, want_dW: bool = True, want_bias: bool = False, dW_dtype: torch.dtype = torch.bfloat16,
+                    status: Optional[torch.Tensor] = None):
+    """grouter_linear_bwd; pre: the forward's x W^T + bias, needed with an activation -> (dx bf16 [T,K], dW [N,K] of dW_dtype,
+    db f32 [N]), None for what is not wanted.  The residual's gradient is dy."""
+    lib = load_library()
+    if x.dim() != 2 or W.dim() != 2:
+        raise ValueError("x and W: matrices are expected")
+    T, K = x.shape
+    N = W.shape[0]
+    bf = torch.bfloat16
+    _expect("x", x, (T, K), bf)
+    _expect("W", W, (N, K), bf, like=x)
+    _expect("dy", dy, (T, N), bf, like=x)
+    _expect("pre", pre, (T, N), bf, like=x)
+    _expect("status", status, (1,), torch.int32, like=x)
+    if act != ACT_NONE and pre is None:
+        raise ValueError("pre: needed with an activation")
+    if dW_dtype not in (bf, torch.float32):
+        raise TypeError(f"dW_dtype: bfloat16 or float32 expected, got {dW_dtype}")
+    dev = x.device
+    with torch.cuda.device(dev):
+        dx = torch.empty((T, K), dtype=bf, device=dev) if want_dx else None
+        dW = torch.empty((N, K), dtype=dW_dtype, device=dev) if want_dW else None
+        db = torch.empty(N, dtype=torch.float32, device=dev) if want_bias else None
+        ws = torch.empty(max(256, lib.grouter_linear_bwd_workspace_bytes(T, K, N, act)), dtype=torch.uint8, device=dev)
+        _check(lib.grouter_linear_bwd(_ptr(dy), _ptr(x), _ptr(W), _ptr(pre), T, K, N, act, _ptr(dx), _ptr(dW),
+                                      F32 if dW_dtype == torch.float32 else BF16, _ptr(db), _ptr(ws),
+                                      _ptr(_status_word(dev) if status is None else status), _stream()), "grouter_linear_bwd")
+    return dx, dW, db
+
+
+def _idx_dtype(idx: torch.Tensor) -> int:
+    if idx.dtype == torch.uint8:
+        return IDX_U8
+    if idx.dtype == torch.int32:
+        return IDX_I32
+    raise TypeError(f"idx: uint8 or int32 expected, got {idx.dtype}")
+
+
+def _mask_of(mask: Optional[torch.Tensor], T: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+    if mask is not None and mask.dtype not in (torch.uint8, torch.bool):
+        raise TypeError(f"mask: uint8 or bool expected, got {mask.dtype}")
+    _expect("mask", mask, (T,), like=like)
+    return mask
+
+
+def expert_counts(idx: torch.Tensor, E: int, mask: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """grouter_expert_counts: idx [T,k] uint8/int32, mask [T] uint8/bool (zero: the token does not count) -> (counts int32 [E],
+    counted tokens int32 [1])."""
+    lib = load_library()
+    if idx.dim() != 2:
+        raise ValueError("idx: a matrix is expected")
+    T, k = idx.shape
+    _expect("idx", idx, (T, k))
+    _expect("status", status, (1,), torch.int32, like=idx)
+    mask = _mask_of(mask, T, idx)
+    dt = _idx_dtype(idx)
+    dev = idx.device
+    with torch.cuda.device(dev):
+        out = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        counts, n = out[:E], out[E:]
+        _check(lib.grouter_expert_counts(_ptr(idx), dt, _ptr(mask), T, k, E, _ptr(counts), _ptr(n),
+                                         _ptr(_status_word(dev) if status is None else status), _stream()), "grouter_expert_counts")
+    return counts, n
+
+
+def balance_loss(logits: torch.Tensor, idx: Optional[torch.Tensor], counts: torch.Tensor, n_tokens: torch.Tensor,
+                 mask: Optional[torch.Tensor] = None, balance_coef: float = 1e-2, z_coef: float = 0.0, dgates: Optional[torch.Tensor] = None,
+                 norm: int = NORM_SOFTMAX, want_loss: bool = True, want_grad: bool = True, dloss: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None):
+    """grouter_balance_loss: logits [T,E] bf16/f32 (rows may be strided), counts and n_tokens of expert_counts -> (loss f32 [3]:
+    sum, balance, z; dlogits like logits), None for what is not wanted.  With dgates f32 [T,k] (GrouterLayer.backward) and idx [T,k]
+    the gradient that comes back through the gates is added to dlogits."""
+    lib = load_library()
+    ld = _row_stride("logits", logits)
+    T, E = logits.shape
+    dt = _elt(logits, "logits")
+    if dgates is not None and idx is None:
+        raise ValueError("idx: needed with dgates")
+    k = 1
+    if idx is not None:
+        if idx.dim() != 2:
+            raise ValueError("idx: a matrix is expected")
+        k = idx.shape[1]
+        _expect("idx", idx, (T, k), like=logits)
+    _expect("counts", counts, (E,), torch.int32, like=logits)
+    _expect("n_tokens", n_tokens, (1,), torch.int32, like=logits)
+    _expect("dgates", dgates, (T, k), torch.float32, like=logits)
+    if dloss is not None and dloss.numel() != 1:
+        raise ValueError("dloss: one number is expected")
+    _expect("dloss", None if dloss is None else dloss.reshape(1), (1,), torch.float32, like=logits)
+    _expect("status", status, (1,), torch.int32, like=logits)
+    mask = _mask_of(mask, T, logits)
+    dev = logits.device
+    with torch.cuda.device(dev):
+        loss = torch.empty(3, dtype=torch.float32, device=dev) if want_loss else None
+        d = torch.empty((T, E), dtype=logits.dtype, device=dev) if want_grad else None
+        ws = torch.empty(lib.grouter_balance_loss_workspace_bytes(), dtype=torch.uint8, device=dev) if want_loss else None
+        _check(lib.grouter_balance_loss(logits.data_ptr(), ld, dt, _ptr(idx), IDX_U8 if idx is None else _idx_dtype(idx), _ptr(mask),
+                                        _ptr(counts), _ptr(n_tokens), _ptr(dgates), norm, T, E, k, balance_coef, z_coef, _ptr(dloss),
+                                        _ptr(loss), _ptr(d), _ptr(ws), _ptr(_status_word(dev) if status is None else status), _stream()),
+               "grouter_balance_loss")
+    return loss, d
+
+
+class AdamW:
+    """AdamW over a list of tensors, one launch a step (grouter_adamw_*).
+
+    params: contiguous f32 tensors, updated in place, or bf16 tensors with an f32 master copy that this object keeps; grads: one
+    contiguous f32 or bf16 tensor for each, whose memory every step reads (the layer's backward writes its gradients into
+    caller-owned tensors: keep writing the same ones).  weight_decay: a number, or one for each tensor.  Moments (and masters) lie in
+    flat tensors m, v (and master), tensor i from element offsets[i] on: f32 with state_bits 32; with state_bits 8 one byte an element
+    (m, and the root of v) plus m_exp, v_exp, one byte for 32 elements.  state: those tensors of a run to be continued, with
+    steps_done; without it the moments start at zero and the masters at the parameters' values."""
+
+    GROUP = 32
+
+    def __init__(self, params, grads, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, state_bits: int = 32,
+                 state: Optional[dict] = None, steps_done: int = 0):
+        self.lib = load_library()
+        self.params, self.grads = list(params), list(grads)
+        if not self.params or len(self.params) != len(self.grads):
+            raise ValueError("one gradient for every parameter is expected, and at least one")
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits: 8 or 32 expected, got {state_bits}")
+        n = len(self.params)
+        wd = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        if len(wd) != n:
+            raise ValueError("weight_decay: a number, or one for each tensor")
+        self.device = self.params[0].device
+        self.state_bits, self.steps_done = state_bits, int(steps_done)
+        self.lr, self.betas, self.eps = lr, tuple(betas), eps
+        desc = (AdamwTensor * n)()
+        self.offsets, at = [], 0
+        for i, (p, g) in enumerate(zip(self.params, self.grads)):
+            _expect(f"gradient {i}", g, p.shape, like=self.params[0])
+            _expect(f"parameter {i}", p, p.shape, like=self.params[0])
+            desc[i] = AdamwTensor(p.data_ptr(), g.data_ptr(), p.numel(), wd[i], _elt(p, f"parameter {i}"), _elt(g, f"gradient {i}"))
+            self.offsets.append(at)
+            at += (p.numel() + self.GROUP - 1) // self.GROUP * self.GROUP
+        self._layout = AdamwLayout()
+        _check(self.lib.grouter_adamw_layout_host(desc, n, ctypes.byref(self._layout), None), "grouter_adamw_layout_host")
+        size = self._layout.state_elements
+        assert size == at
+        dev, u8, f32 = self.device, torch.uint8, torch.float32
+        given = dict(state or {})
+        kinds = dict(m=f32, v=f32) if state_bits == 32 else dict(m=u8, v=u8, m_exp=u8, v_exp=u8)
+        if self._layout.needs_master:
+            kinds["master"] = f32
+        for name in given:
+            if name not in kinds:
+                raise ValueError(f"state: no {name} is kept here")
+        for name, kind in kinds.items():
+            shape = (size // self.GROUP if name.endswith("_exp") else size,)
+            t = given.get(name)
+            if t is None:
+                t = torch.zeros(shape, dtype=kind, device=dev)
+                if name == "master":
+                    for p, o in zip(self.params, self.offsets):
+                        t[o:o + p.numel()] = p.reshape(-1)
+            _expect(name, t, shape, kind, like=self.params[0])
+            setattr(self, name, t)
+        host = torch.zeros(max(16, self._layout.table_bytes), dtype=u8)
+        _check(self.lib.grouter_adamw_layout_host(desc, n, ctypes.byref(self._layout), host.data_ptr()), "grouter_adamw_layout_host")
+        self._table = host.to(dev)
+
+    def step(self, grad_scale: Optional[torch.Tensor] = None, lr: Optional[float] = None) -> None:
+        """One update from the gradients as they are now.  grad_scale: f32 device scalar every gradient is multiplied by."""
+        if grad_scale is not None and (grad_scale.numel() != 1 or grad_scale.dtype != torch.float32 or grad_scale.device != self.device):
+            raise ValueError("grad_scale: one f32 number on the parameters' device is expected")
+        if lr is not None:
+            self.lr = lr
+        with torch.cuda.device(self.device):
+            _check(self.lib.grouter_adamw_step(ctypes.byref(self._layout), _ptr(self._table), self.state_bits, _ptr(getattr(self, "master", None)),
+                                               _ptr(self.m), _ptr(self.v), _ptr(getattr(self, "m_exp", None)), _ptr(getattr(self, "v_exp", None)),
+                                               self.lr, self.betas[0], self.betas[1], self.eps, self.steps_done + 1, _ptr(grad_scale), _stream()),
+                   "grouter_adamw_step")
+        self.steps_done += 1
+
+    def moments(self):
+        """(m, v) as flat f32 tensors: the state itself with 32 bits, the values that the codes stand for with 8."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        out = torch.empty((2, self.m.numel()), dtype=torch.float32, device=self.device)
+        with torch.cuda.device(self.device):
+            _check(self.lib.grouter_adamw_moments(_ptr(self.m), _ptr(self.v), _ptr(self.m_exp), _ptr(self.v_exp), self.m.numel(),
+                                                  out.data_ptr(), out[1].data_ptr(), _stream()), "grouter_adamw_moments")
+        return out[0], out[1]
 
 
 def dense_gemm(A: torch.Tensor, a_mn_major: bool, B: torch.Tensor, b_mn_major: bool, M: int, N: int, K: int) -> torch.Tensor:

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libgrouter.so")
 LIB_DEBUG = os.path.join(PKG, "libgrouter_debug.so")
-SOURCES = ["api.cu", "plan.cu", "permute.cu", "gemm.cu", "route.cu", "stats.cu", "ep.cu"]
+SOURCES = ["api.cu", "plan.cu", "permute.cu", "gemm.cu", "route.cu", "stats.cu", "ep.cu", "norm.cu", "balance.cu", "linear.cu", "adamw.cu"]
 
 
 def _newest_source_mtime() -> float:
@@ -26,7 +26,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = f"{lib}.{os.getpid()}.tmp"      # several processes may build at once: each writes its own file, then renames it
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo", "-shared",
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo", "-shared", "-t", "0",
            "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp]
     if debug:
         cmd += ["-DGROUTER_DEBUG_BOUNDS"]

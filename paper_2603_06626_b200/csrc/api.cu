@@ -620,7 +620,7 @@ int grouter_dense_gemm(const void* A, int a_mn_major, const void* B, int b_mn_ma
   if (!A || !B || !C || !status || M < 1 || N < 1 || K < 1) return GROUTER_ERR_INVALID_ARG;
   if (M % 8 || N % 8 || K % 8) return GROUTER_ERR_UNSUPPORTED;
   if (!aligned16(A) || !aligned16(B) || !aligned16(C)) return GROUTER_ERR_MISALIGNED;
-  if (launch_dense_gemm(A, a_mn_major, B, b_mn_major, C, M, N, K, status, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+  if (launch_dense_gemm(A, a_mn_major, B, b_mn_major, C, M, N, K, (K + 63) / 64 * 64, status, static_cast<cudaStream_t>(stream)) != cudaSuccess)
     return GROUTER_ERR_CUDA;
   return GROUTER_OK;
 }

@@ -1,0 +1,414 @@
+// Per-expert counts, the router's balance and z losses, and the gradient of its scores.
+//
+//   c_e  = #{(t, j): idx[t,j] = e, token t counts}         f_e = E c_e / sum_e' c_e'         n = tokens that count
+//   p_te = softmax of row t of the scores                   lse_t = log sum_e exp s_te
+//   balance = sum_e f_e (1/n) sum_t p_te = (1/n) sum_t a_t      with a_t = sum_e f_e p_te
+//   z       = (1/n) sum_t lse_t^2                               loss = ca balance + cz z
+//   d loss / d s_te = (ca/n) p_te (f_e - a_t) + (2 cz/n) lse_t p_te              (the counts do not depend on the scores)
+// and, joined in the same pass, what comes back through the gates r(x) = g(kept scores):
+//   softmax over the kept k: q_j (dg_j - sum_i q_i dg_i)        sigmoid of each: q_j (1 - q_j) dg_j
+//
+// The counts are known before the scores are read, so the loss needs no column sums of p: one number a token (a_t) carries
+// it, and one pass over the scores gives the loss and its gradient.  Bound by HBM: scores read once, gradient written once.
+// LPT neighbouring lanes hold a token's row in registers, 16 bytes at a time; a block's token sums are added in a fixed
+// order, and the last step (one block) adds the blocks' sums in double precision.
+//
+// A score of -inf takes its expert out (p = 0, no gradient).  A row of nothing but -inf has p = 0 throughout and no
+// z-loss term.  A token whose mask byte is zero contributes nothing and gets a zero gradient row, whatever its scores are.
+#include <math.h>
+
+#include "vec.cuh"
+
+namespace grouter {
+
+constexpr int BAL_THREADS = 256;
+constexpr int BAL_WARPS = BAL_THREADS / 32;
+constexpr int BAL_MAX_E = 1024;
+constexpr int COUNT_THREADS = 256;
+constexpr int COUNT_SLOTS = 4096;       // counters a block of the histogram keeps (several copies of few experts)
+
+// counts += histogram of this block's share of the ids.  A thread takes 16 bytes of ids at a time (IPT of them).  Lanes
+// spread over `copies` copies of the counters, so that few experts do not queue up at the same word.
+template <typename Id>
+__global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* __restrict__ idx, int64_t slots, int k, int E, int copies,
+                                                                      const uint8_t* __restrict__ mask, int32_t* __restrict__ counts,
+                                                                      int32_t* __restrict__ n_tokens, int32_t* __restrict__ status, int direct) {
+  constexpr int IPT = 16 / (int)sizeof(Id);
+  __shared__ int32_t s_cnt[COUNT_SLOTS];
+  __shared__ int32_t s_tok;
+  for (int i = threadIdx.x; i < E * copies; i += COUNT_THREADS) s_cnt[i] = 0;
+  if (threadIdx.x == 0) s_tok = 0;
+  __syncthreads();
+  int32_t* mine = s_cnt + (threadIdx.x % copies) * E;
+  int tokens = 0;
+  bool bad = false;
+  const int64_t stride = (int64_t)gridDim.x * COUNT_THREADS * IPT;
+  for (int64_t s0 = ((int64_t)blockIdx.x * COUNT_THREADS + threadIdx.x) * IPT; s0 < slots; s0 += stride) {
+    alignas(16) Id ids[IPT];
+    if (s0 + IPT <= slots) {
+      *reinterpret_cast<uint4*>(ids) = ld_stream16(idx + s0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < IPT; ++i) ids[i] = s0 + i < slots ? idx[s0 + i] : Id(0);
+    }
+    int64_t t = s0 / k;
+    int j = (int)(s0 - t * k);
+    bool live = mask == nullptr || mask[t] != 0;
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+      if (s0 + i < slots) {
+        if (live) {
+          tokens += j == 0;
+          const int e = (int)ids[i];
+          if ((unsigned)e < (unsigned)E) atomicAdd(mine + e, 1);
+          else bad = true;
+        }
+        if (++j == k) {
+          j = 0;
+          ++t;
+          if (mask != nullptr && s0 + i + 1 < slots) live = mask[t] != 0;
+        }
+      }
+    }
+  }
+  if (bad && status) atomicOr(status, STATUS_BAD_INDEX);
+  if (tokens) atomicAdd(&s_tok, tokens);
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += COUNT_THREADS) {
+    int32_t c = 0;
+    for (int q = 0; q < copies; ++q) c += s_cnt[q * E + e];
+    if (direct) counts[e] = c;
+    else if (c) atomicAdd(counts + e, c);
+  }
+  if (threadIdx.x == 0) {
+    if (direct) *n_tokens = s_tok;
+    else if (s_tok) atomicAdd(n_tokens, s_tok);
+  }
+}
+
+struct BalanceParams {
+  const void* logits;
+  int64_t ld;
+  const void* idx;
+  int idx_i32;
+  const uint8_t* mask;
+  const int32_t *counts, *n_tokens;
+  const float* dgates;
+  int sigmoid;
+  int T, E, k;
+  float ca, cz;
+  const float* dloss;
+  float* loss;
+  void* dlogits;
+  double2* partial;     // [blocks] sums of a_t and lse_t^2 (loss wanted)
+  int32_t* status;
+};
+
+__device__ __forceinline__ void write_loss(const BalanceParams& p, double a, double z, int n) {
+  const double per = n > 0 ? 1.0 / (double)n : 0.0;
+  const float balance = (float)(a * per), zl = (float)(z * per);
+  // a loss that does not count (coefficient zero) does not spoil the sum either when it is not finite
+  p.loss[0] = (p.ca != 0.f ? p.ca * balance : 0.f) + (p.cz != 0.f ? p.cz * zl : 0.f);
+  p.loss[1] = balance;
+  p.loss[2] = zl;
+}
+
+// VE elements an access, LPT lanes a token, NV accesses a lane: LPT * NV * VE >= E.
+// Dynamic shared memory: f [E], then (with dgates) one row of E sums for every lane group.
+template <typename T, int VE, int LPT, int NV, bool GATES>
+__global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParams p) {
+  extern __shared__ float s_f[];
+  __shared__ double s_part[2][BAL_WARPS];
+  __shared__ unsigned long long s_total;
+  constexpr int TPW = 32 / LPT;                       // tokens a warp works on at a time
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int sl = lane & (LPT - 1), grp = lane / LPT;
+  const int E = p.E;
+  // f_e = E c_e / sum c, and one row of zeros for every lane group
+  if (threadIdx.x == 0) s_total = 0ull;
+  __syncthreads();
+  {
+    unsigned long long sum = 0;       // counts may come summed over many ranks
+    for (int e = threadIdx.x; e < E; e += BAL_THREADS) sum += (unsigned)__ldg(p.counts + e);
+    if (sum) atomicAdd(&s_total, sum);
+  }
+  __syncthreads();
+  const float per_count = s_total > 0 ? (float)E / (float)s_total : 0.f;
+  for (int e = threadIdx.x; e < E; e += BAL_THREADS) s_f[e] = (float)__ldg(p.counts + e) * per_count;
+  float* s_gate = s_f + ((E + 3) & ~3) + (size_t)(warp * TPW + grp) * ((E + 3) & ~3);
+  if (GATES)
+    for (int e = sl; e < E; e += LPT) s_gate[e] = 0.f;
+  __syncthreads();
+  float f[NV][VE];
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      const int c = (n * LPT + sl) * VE + i;
+      f[n][i] = c < E ? s_f[c] : 0.f;
+    }
+  const int n_tok = __ldg(p.n_tokens);
+  const float per = n_tok > 0 ? 1.f / (float)n_tok : 0.f;
+  const float up = p.dloss ? __ldg(p.dloss) : 1.f;
+  const float ka = p.ca * per * up, kz = 2.f * p.cz * per * up;
+  float sum_a = 0.f, sum_z = 0.f;
+  const int step = gridDim.x * BAL_WARPS * TPW;
+  for (int t0 = (blockIdx.x * BAL_WARPS + warp) * TPW; t0 < p.T; t0 += step) {
+    const int t = t0 + grp;
+    const bool here = t < p.T;
+    const bool live = here && (p.mask == nullptr || p.mask[t] != 0);
+    const T* row = reinterpret_cast<const T*>(p.logits) + (int64_t)t * p.ld;
+    float v[NV][VE];
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = (n * LPT + sl) * VE;
+      if (live && c < E) {
+        const Pack<T, VE> q = ld_pack<T, VE>(row + c);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[n][i] = to_f32(q.v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[n][i] = -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < VE; ++i) top = fmaxf(top, v[n][i]);
+    }
+    top = lanes_max<LPT>(top);
+    const float base = top == -INFINITY ? 0.f : top;      // a row without a score: every exp below is 0
+    float z = 0.f, a = 0.f;
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        v[n][i] = __expf(v[n][i] - base);
+        z += v[n][i];
+        a += v[n][i] * f[n][i];
+      }
+    z = lanes_sum<LPT>(z);
+    a = lanes_sum<LPT>(a);
+    const bool some = top != -INFINITY;
+    const float inv_z = some ? 1.f / z : 0.f;
+    const float lse = some ? base + logf(z) : 0.f;
+    a *= inv_z;
+    if (sl == 0 && live) {
+      sum_a += a;
+      sum_z += lse * lse;
+    }
+    if (p.dlogits == nullptr) continue;
+    if (GATES) {
+      // lane j < k of the group has the token's j-th kept expert (LPT >= k)
+      const bool kept = live && sl < p.k;
+      int e = 0;
+      float s = -INFINITY, dg = 0.f;
+      bool ok = false;
+      if (kept) {
+        const int64_t at = (int64_t)t * p.k + sl;
+        e = p.idx_i32 ? __ldg(reinterpret_cast<const int32_t*>(p.idx) + at) : (int)__ldg(reinterpret_cast<const uint8_t*>(p.idx) + at);
+        ok = (unsigned)e < (unsigned)E;
+        if (ok) {
+          s = to_f32(row[e]);
+          dg = __ldg(p.dgates + at);
+        } else if (p.status) {
+          atomicOr(p.status, STATUS_BAD_INDEX);
+        }
+      }
+      float back;
+      if (p.sigmoid) {
+        // q (1 - q) with 1 - q = 1 / (1 + exp(s)), not by subtraction
+        const float x = __expf(-fabsf(s));
+        back = ok ? x / ((1.f + x) * (1.f + x)) * dg : 0.f;
+      } else {
+        const float m = lanes_max<LPT>(s);
+        const float q = s == -INFINITY ? 0.f : __expf(s - m);
+        const float qs = lanes_sum<LPT>(q), qd = lanes_sum<LPT>(q * dg);
+        const float inv = qs > 0.f ? 1.f / qs : 0.f;
+        back = q * inv * (dg - qd * inv);
+        if (!ok) back = 0.f;
+      }
+      if (ok) atomicAdd(s_gate + e, back);      // of this token alone; a second addend only where an id repeats
+      __syncwarp();
+    }
+    T* out = reinterpret_cast<T*>(p.dlogits) + (int64_t)t * E;
+    const float shift = kz * lse;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = (n * LPT + sl) * VE;
+      if (here && c < E) {
+        float o[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          o[i] = live ? v[n][i] * inv_z * (ka * (f[n][i] - a) + shift) : 0.f;
+          if (GATES) {
+            o[i] += s_gate[c + i];
+            s_gate[c + i] = 0.f;
+          }
+        }
+        st_pack<T, VE>(out + c, o);
+      }
+    }
+    if (GATES) __syncwarp();
+  }
+  if (p.loss == nullptr) return;
+  sum_a = lanes_sum<32>(sum_a);
+  sum_z = lanes_sum<32>(sum_z);
+  if (lane == 0) {
+    s_part[0][warp] = sum_a;
+    s_part[1][warp] = sum_z;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double a = 0, z = 0;
+    for (int w = 0; w < BAL_WARPS; ++w) {
+      a += s_part[0][w];
+      z += s_part[1][w];
+    }
+    if (gridDim.x == 1) write_loss(p, a, z, n_tok);
+    else p.partial[blockIdx.x] = make_double2(a, z);
+  }
+}
+
+__global__ void __launch_bounds__(256) balance_finish_kernel(const BalanceParams p, int n_part) {
+  __shared__ double s[2][256];
+  double a = 0, z = 0;
+  for (int i = threadIdx.x; i < n_part; i += 256) {
+    const double2 v = p.partial[i];
+    a += v.x;
+    z += v.y;
+  }
+  s[0][threadIdx.x] = a;
+  s[1][threadIdx.x] = z;
+  __syncthreads();
+  for (int o = 128; o > 0; o >>= 1) {
+    if (threadIdx.x < o) {
+      s[0][threadIdx.x] += s[0][threadIdx.x + o];
+      s[1][threadIdx.x] += s[1][threadIdx.x + o];
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) write_loss(p, s[0][0], s[1][0], __ldg(p.n_tokens));
+}
+
+namespace {
+
+constexpr int BAL_MAX_BLOCKS_PER_SM = 8;
+
+template <typename T, int VE, int LPT, int NV, bool GATES>
+cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
+  constexpr int TPB = BAL_WARPS * (32 / LPT);
+  const int epad = (p.E + 3) & ~3;
+  const size_t smem = sizeof(float) * epad * (1 + (GATES ? TPB : 0));
+  const int64_t want = ((int64_t)p.T + TPB - 1) / TPB;
+  const int cap = current_sms() * BAL_MAX_BLOCKS_PER_SM;
+  const int grid = (int)(want < cap ? want : cap);
+  balance_kernel<T, VE, LPT, NV, GATES><<<grid, BAL_THREADS, smem, st>>>(p);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && p.loss && grid > 1) {
+    balance_finish_kernel<<<1, 256, 0, st>>>(p, grid);
+    e = cudaGetLastError();
+  }
+  return e;
+}
+
+template <typename T, int VE, int LPT, int NV>
+cudaError_t balance_launch(const BalanceParams& p, cudaStream_t st) {
+  return p.dgates ? balance_launch_g<T, VE, LPT, NV, true>(p, st) : balance_launch_g<T, VE, LPT, NV, false>(p, st);
+}
+
+// Lanes a token: as few as hold the row, but one for every kept expert where the gates' gradient is joined in.
+template <typename T, int VE>
+cudaError_t balance_by_width(const BalanceParams& p, cudaStream_t st) {
+  int lpt = 1;
+  while (lpt < 32 && (lpt * VE < p.E || (p.dgates && lpt < p.k))) lpt *= 2;
+  const int nv = (p.E + lpt * VE - 1) / (lpt * VE);
+  switch (lpt) {
+    case 1: return balance_launch<T, VE, 1, 1>(p, st);
+    case 2: return balance_launch<T, VE, 2, 1>(p, st);
+    case 4: return balance_launch<T, VE, 4, 1>(p, st);
+    case 8: return balance_launch<T, VE, 8, 1>(p, st);
+    case 16: return balance_launch<T, VE, 16, 1>(p, st);
+    default: break;
+  }
+  if (nv <= 1) return balance_launch<T, VE, 32, 1>(p, st);
+  if (nv <= 2) return balance_launch<T, VE, 32, 2>(p, st);
+  if (nv <= 4) return balance_launch<T, VE, 32, 4>(p, st);
+  if constexpr (VE <= 4) {
+    if (nv <= 8) return balance_launch<T, VE, 32, 8>(p, st);
+  }
+  if constexpr (VE == 1) return nv <= 16 ? balance_launch<T, VE, 32, 16>(p, st) : balance_launch<T, VE, 32, 32>(p, st);
+  return cudaErrorInvalidValue;       // E <= 1024 fits the forms above
+}
+
+}  // namespace
+}  // namespace grouter
+
+using namespace grouter;
+
+extern "C" {
+
+int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mask, int32_t T, int32_t k, int32_t E, int32_t* counts,
+                          int32_t* n_tokens, int32_t* status, void* stream) {
+  if (!counts || !n_tokens || T < 0 || k < 1 || E < 1 || (T > 0 && !idx)) return GROUTER_ERR_INVALID_ARG;
+  if (idx_dtype != GROUTER_IDX_U8 && idx_dtype != GROUTER_IDX_I32) return GROUTER_ERR_INVALID_ARG;
+  if (E > BAL_MAX_E || k > 32 || (int64_t)T * k > INT32_MAX || (idx_dtype == GROUTER_IDX_U8 && E > 256)) return GROUTER_ERR_UNSUPPORTED;
+  if (!aligned_to(idx, 16) || !aligned_to(counts, 4) || !aligned_to(n_tokens, 4) || !aligned_to(status, 4)) return GROUTER_ERR_MISALIGNED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int64_t slots = (int64_t)T * k;
+  const int ipt = idx_dtype == GROUTER_IDX_U8 ? 16 : 4;
+  const int64_t per_block = (int64_t)COUNT_THREADS * ipt;
+  const int64_t want = (slots + per_block - 1) / per_block;
+  const int cap = current_sms() * 4;
+  const int grid = (int)(want < 1 ? 1 : want < cap ? want : cap);
+  int copies = COUNT_SLOTS / E;
+  if (copies > 32) copies = 32;
+  if (grid > 1) {       // several blocks add up in place
+    if (cudaMemsetAsync(counts, 0, sizeof(int32_t) * E, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (cudaMemsetAsync(n_tokens, 0, sizeof(int32_t), st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  }
+  if (idx_dtype == GROUTER_IDX_U8)
+    expert_counts_kernel<uint8_t><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts, n_tokens,
+                                                                 status, grid == 1);
+  else
+    expert_counts_kernel<int32_t><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const int32_t*>(idx), slots, k, E, copies, mask, counts, n_tokens,
+                                                                 status, grid == 1);
+  return cudaGetLastError() == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+}
+
+size_t grouter_balance_loss_workspace_bytes(void) { return sizeof(double2) * current_sms() * BAL_MAX_BLOCKS_PER_SM; }
+
+int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const void* idx, int32_t idx_dtype, const uint8_t* mask,
+                         const int32_t* counts, const int32_t* n_tokens, const float* dgates, int32_t norm, int32_t T, int32_t E, int32_t k,
+                         float balance_coef, float z_coef, const float* dloss, float* loss, void* dlogits, void* workspace, int32_t* status,
+                         void* stream) {
+  if (!counts || !n_tokens || T < 0 || E < 1 || k < 1 || ld < E || (!loss && !dlogits)) return GROUTER_ERR_INVALID_ARG;
+  if (T > 0 && (!logits || (dgates && (!idx || !dlogits)))) return GROUTER_ERR_INVALID_ARG;
+  if (loss && !workspace) return GROUTER_ERR_INVALID_ARG;
+  if ((dtype != GROUTER_BF16 && dtype != GROUTER_F32) || (idx_dtype != GROUTER_IDX_U8 && idx_dtype != GROUTER_IDX_I32) ||
+      (norm != GROUTER_NORM_SOFTMAX && norm != GROUTER_NORM_SIGMOID))
+    return GROUTER_ERR_INVALID_ARG;
+  if (E > BAL_MAX_E || k > 32 || (int64_t)T * k > INT32_MAX || T > INT32_MAX - (1 << 20) || (idx_dtype == GROUTER_IDX_U8 && E > 256))
+    return GROUTER_ERR_UNSUPPORTED;
+  const size_t el = dtype == GROUTER_F32 ? 4 : 2;
+  if (!aligned_to(logits, el) || !aligned_to(dlogits, el) || !aligned_to(dgates, 4) || !aligned_to(counts, 4) || !aligned_to(n_tokens, 4) ||
+      !aligned_to(dloss, 4) || !aligned_to(loss, 4) || !aligned_to(status, 4) || !aligned_to(workspace, 16) ||
+      (idx_dtype == GROUTER_IDX_I32 && !aligned_to(idx, 4)))
+    return GROUTER_ERR_MISALIGNED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (T == 0) {
+    if (loss && cudaMemsetAsync(loss, 0, 3 * sizeof(float), st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    return GROUTER_OK;
+  }
+  BalanceParams p{};
+  p.logits = logits; p.ld = ld; p.idx = idx; p.idx_i32 = idx_dtype == GROUTER_IDX_I32; p.mask = mask; p.counts = counts; p.n_tokens = n_tokens;
+  p.dgates = dgates; p.sigmoid = norm == GROUTER_NORM_SIGMOID; p.T = T; p.E = E; p.k = k; p.ca = balance_coef; p.cz = z_coef; p.dloss = dloss;
+  p.loss = loss; p.dlogits = dlogits; p.partial = static_cast<double2*>(workspace); p.status = status;
+  // 16-byte accesses where every row starts on a 16-byte boundary, single elements otherwise
+  const int ve = dtype == GROUTER_F32 ? vec16<float>() : vec16<__nv_bfloat16>();
+  const bool vec = E % ve == 0 && ld % ve == 0 && aligned_to(logits, 16) && aligned_to(dlogits, 16);
+  cudaError_t e;
+  if (dtype == GROUTER_F32) e = vec ? balance_by_width<float, vec16<float>()>(p, st) : balance_by_width<float, 1>(p, st);
+  else e = vec ? balance_by_width<__nv_bfloat16, vec16<__nv_bfloat16>()>(p, st) : balance_by_width<__nv_bfloat16, 1>(p, st);
+  return e == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+}
+
+}  // extern "C"

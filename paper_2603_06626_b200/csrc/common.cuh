@@ -176,7 +176,7 @@ cudaError_t launch_reduce_rows(grouter_ctx* ctx, const __nv_bfloat16* src, __nv_
                                int n_part, float* dgates, cudaStream_t st);
 
 // MODE_DOWN_ADD: the down product with the combine folded into its epilogue (fp32 reductions into a [T, d] accumulator).
-enum GemmMode { MODE_UP = 0, MODE_DOWN = 1, MODE_DH = 2, MODE_DX = 3, MODE_WGRAD_D = 4, MODE_WGRAD_GU = 5, MODE_DENSE = 6, MODE_DOWN_ADD = 7 };
+enum GemmMode { MODE_UP = 0, MODE_DOWN = 1, MODE_DH = 2, MODE_DX = 3, MODE_WGRAD_D = 4, MODE_WGRAD_GU = 5, MODE_DENSE = 6, MODE_DOWN_ADD = 7, MODE_LINEAR = 8 };
 
 cudaError_t launch_grouped_gemm(grouter_ctx* ctx, GemmMode mode, const Workspace& ws, const void* gates, const void* W_gu,
                                 const void* W_d, float* dW_gu, float* dW_d, cudaStream_t st);
@@ -188,7 +188,18 @@ cudaError_t launch_idle(int microseconds, cudaStream_t st);
 bool make_bf16_tile_map(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 // Measures one bounded wait that cannot succeed (see grouter_wait_selftest).
 cudaError_t launch_wait_selftest(grouter_ctx* ctx, unsigned long long limit_ns, unsigned long long* d_waited_ns, cudaStream_t st);
-cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, float* C, int M, int N, int K, int32_t* status,
+// C = A * B (fp32).  A contraction longer than k_chunk (a multiple of 64) is cut into ceil(K / k_chunk) partial products, stored
+// one after the other as M x N matrices from C on.
+cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, float* C, int M, int N, int K, int k_chunk, int32_t* status,
                               cudaStream_t st);
+// C = act(A * B + bias) + residual (bf16); pre: A * B + bias (bf16) or null.  Operands as for launch_dense_gemm; an MN-major A
+// goes with an MN-major B only.
+struct LinearGemm {
+  const void *A, *B, *bias, *residual;
+  void *C, *pre;
+  int a_mn, b_mn, M, N, K, act;
+  int32_t* status;
+};
+cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st);
 
 }  // namespace grouter

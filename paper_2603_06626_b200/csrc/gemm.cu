@@ -7,7 +7,8 @@
 //   DX        dXp   = [dG|dU] * W_gu[e]
 //   WGRAD_D   dW_d[e]  = dYp_e^T * H'_e     (contraction over the expert's rows)
 //   WGRAD_GU  dW_gu[e] = [dG|dU]_e^T * Xp_e
-//   DENSE     C = A * B on plain matrices (component check)
+//   DENSE     C = A * B on plain matrices, fp32 out (component check; partial products of a linear layer's weight gradient)
+//   LINEAR    C = act(A * B + bias) + residual on plain matrices, bf16 out (the linear layer's forward pass and gradients)
 //
 // Tile: 256 x 256 x 64 per CTA pair (a cluster of two CTAs on neighbouring SMs, one pair-wide tcgen05.mma with
 // M = 256).  Each CTA owns 128 rows of the tile and half of B's 256 columns, so per 64-deep k-step it stages
@@ -24,13 +25,15 @@
 // Operands may be K-major (rows of the stored matrix run along K) or MN-major (rows run along M/N); both are
 // described to the MMA by shared-memory descriptors, so no operand is ever transposed in memory.
 //
-// Tiles are handed out by a grid-wide counter (all products but DENSE): a pair takes the next tile of the list when it
+// Tiles are handed out by a grid-wide counter (all products but DENSE and LINEAR): a pair takes the next tile of the list when it
 // is ready for one, so the pairs always work on neighbouring tiles and the operand rows they share are in L2 together.
 //
 // Every wait (mbarriers, tile queue) is bounded; on give-up the CTA raises an abort flag, ORs STATUS_TIMEOUT into the status
 // word, leaves its loops, and the pair meets at a cluster barrier before freeing TMEM and exiting.
+#include "act.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
+#include "vec.cuh"
 
 namespace grouter {
 
@@ -61,7 +64,9 @@ struct GemmParams {
   int32_t E, d, F, k;
   int32_t n_slots;             // routed slots of the plan in use (tokens * k)
   int32_t accumulate;          // weight-gradient modes: add every tile into the caller's gradient
-  int32_t M, N, K;             // DENSE: problem; WGRAD: per-expert output M x N
+  int32_t M, N, K;             // DENSE, LINEAR: problem; WGRAD: per-expert output M x N
+  int32_t k_chunk;             // DENSE: longest contraction of one tile, a multiple of 64; longer ones are cut into several partial
+                               // products, each stored as an M x N matrix of its own
   int32_t tiles_m, tiles_n;    // output tiles per problem (tiles_m unused by row-parallel modes)
   int64_t R_pad_max;
   // epilogue
@@ -72,6 +77,10 @@ struct GemmParams {
   int32_t gate_is_f32;
   const __nv_bfloat16* in_G;   // DH
   const __nv_bfloat16* in_U;   // DH
+  const __nv_bfloat16* bias;   // LINEAR: [N] or null
+  const __nv_bfloat16* residual;   // LINEAR: [M, N] or null
+  int32_t act;                 // LINEAR: GROUTER_ACT_*
+  int32_t save_pre;            // LINEAR: also store A * B + bias (tensor map C1)
   float* out_f;                // DH: dgate_part; weight gradients / DENSE: the fp32 output [E, M, N]; DOWN_ADD: Y accumulator [T, d]
   int32_t* status;
   unsigned int* tile_counter;  // device scalar, zero at launch (unused by DENSE, which has no context to keep one)
@@ -79,9 +88,12 @@ struct GemmParams {
   unsigned long long wait_limit_ns;   // how long any one wait (barrier, tile queue) may last before the CTA gives up
 };
 
+constexpr int RASTER_ROWS = 8;
+
 struct Tile {     // one CTA's share of a pair tile
   int a_x, a_y;   // TMA coordinates of this CTA's A rows at k-step 0
   int b_x, b_y;   // ... and of this CTA's half of B
+  int k_base;     // DENSE: first index of the contraction
   int num_k;      // k-steps that contribute to the result
   int steps;      // k-steps that pass through the operand ring: max(num_k, 1)
   int row0, col0; // origin of this CTA's 128 x 256 output block within the output matrix of this problem
@@ -93,7 +105,8 @@ struct Tile {     // one CTA's share of a pair tile
 template <int MODE>
 __device__ __forceinline__ int total_tiles(const GemmParams& p) {
   if (MODE == MODE_WGRAD_D || MODE == MODE_WGRAD_GU) return __ldg(p.n_wchunks) * p.tiles_m * p.tiles_n;
-  if (MODE == MODE_DENSE) return p.tiles_m * p.tiles_n;
+  if (MODE == MODE_DENSE) return p.tiles_m * p.tiles_n * ((p.K + p.k_chunk - 1) / p.k_chunk);
+  if (MODE == MODE_LINEAR) return p.tiles_m * p.tiles_n;
   return __ldg(p.n_pair_tiles) * p.tiles_n;
 }
 
@@ -102,6 +115,7 @@ template <int MODE>
 __device__ __forceinline__ Tile decode_tile(const GemmParams& p, int t, int rank) {
   Tile ti;
   ti.add = false;
+  ti.k_base = 0;
   if (MODE == MODE_UP || MODE == MODE_DOWN || MODE == MODE_DOWN_ADD || MODE == MODE_DH || MODE == MODE_DX) {
     const int mt = t / p.tiles_n, nt = t - mt * p.tiles_n;
     const int pe = __ldg(p.pair_expert + mt);
@@ -168,9 +182,15 @@ __device__ __forceinline__ Tile decode_tile(const GemmParams& p, int t, int rank
     // barriers: its boxes lie beyond the last row, where TMA fills zeros without touching memory, and the epilogue
     // ignores the accumulator.
     ti.a_y = ti.b_y = ti.num_k > 0 ? k0 : (int)p.R_pad_max;
-  } else {  // DENSE
-    const int mt = t / p.tiles_n, nt = t - mt * p.tiles_n;
-    ti.e = 0;
+  } else {  // DENSE, LINEAR
+    // Tiles in bands of RASTER_ROWS tile rows, down the band first: the pairs in flight then share a few tile rows of A and
+    // a few tile columns of B, whichever of the two matrices is the larger one.
+    const int per = p.tiles_m * p.tiles_n;
+    const int piece = MODE == MODE_DENSE ? t / per : 0, r = t - piece * per;
+    const int band = r / (RASTER_ROWS * p.tiles_n), in_band = r - band * RASTER_ROWS * p.tiles_n;
+    const int rows = min(RASTER_ROWS, p.tiles_m - band * RASTER_ROWS);
+    const int nt = in_band / rows, mt = band * RASTER_ROWS + (in_band - nt * rows);
+    ti.e = piece;                     // DENSE: which of the partial products (their matrices follow one another)
     ti.row0 = mt * PM + rank * BM;
     ti.col0 = nt * BN;
     ti.m_valid = min(BM, p.M - ti.row0);
@@ -179,7 +199,8 @@ __device__ __forceinline__ Tile decode_tile(const GemmParams& p, int t, int rank
     ti.a_y = ti.row0;
     ti.b_x = ti.col0 + rank * BNH;    // MN-major B: x; K-major B: y
     ti.b_y = ti.col0 + rank * BNH;
-    ti.num_k = (p.K + BK - 1) / BK;
+    ti.k_base = MODE == MODE_DENSE ? piece * p.k_chunk : 0;
+    ti.num_k = ((MODE == MODE_DENSE ? min(p.k_chunk, p.K - ti.k_base) : p.K) + BK - 1) / BK;
   }
   ti.steps = ti.num_k > 0 ? ti.num_k : 1;
   return ti;
@@ -228,7 +249,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
   auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + a); };
   auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + 2 + a); };
-  // Tile queue (all modes but DENSE).  The pair takes its tiles from a grid-wide counter instead of a fixed stride: the
+  // Tile queue (all modes but DENSE and LINEAR).  The pair takes its tiles from a grid-wide counter instead of a fixed stride: the
   // pairs then always work on neighbouring tiles of the list, whatever their individual pace, so the operand rows the
   // neighbours share are fetched from DRAM once.  The leader's producer draws the numbers (two tiles ahead, so the
   // round trip of the atomic is never waited for) and writes them into a ring of TQ 8-byte slots {sequence, tile} in
@@ -237,7 +258,8 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   // stage through the operand ring (the producer is at most STAGES tiles ahead of the issuer), and the issuer starts a
   // tile only after every epilogue warp has finished the tile two before it, so the oldest number still unread is at
   // most STAGES + 3 tiles older than the newest one written (STAGES + 4 <= TQ slots in use).
-  constexpr bool DYN = MODE != MODE_DENSE;
+  constexpr bool PLAIN = MODE == MODE_DENSE || MODE == MODE_LINEAR;   // plain matrices, no context to keep a tile counter in
+  constexpr bool DYN = !PLAIN;
   constexpr int TQ = 16;
   static_assert(STAGES + 4 <= TQ && (TQ & (TQ - 1)) == 0, "tile queue too short for the operand ring");
   auto tq_slot = [&](int i) { return bar_base + 8u * (2 * STAGES + 4) + 8u * (uint32_t)(i & (TQ - 1)); };
@@ -265,7 +287,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     ptx::prefetch_tensormap(&tmA);
     ptx::prefetch_tensormap(&tmB);
     ptx::prefetch_tensormap(&tmC0);
-    if (MODE == MODE_UP || MODE == MODE_DH) ptx::prefetch_tensormap(&tmC1);
+    if (MODE == MODE_UP || MODE == MODE_DH || MODE == MODE_LINEAR) ptx::prefetch_tensormap(&tmC1);
     if (MODE == MODE_UP) ptx::prefetch_tensormap(&tmC2);
   }
   if (warp == 1) {
@@ -349,18 +371,18 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           const uint32_t sb = sa + A_BYTES;
           if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), 2 * STAGE_BYTES);
           const uint32_t fb = ptx::map_to_cta(full_bar(s), 0);   // both CTAs' bytes complete on the leader's barrier
-          const int k0 = ks * BK;
+          const int k0 = ti.k_base + ks * BK;
           if (!A_MN) {
             ptx::tma_load_2d_pair(sa, &tmA, fb, k0, ti.a_y, keep_a);                       // box {64 k, 128 rows}
           } else {
-            const int ay = (MODE == MODE_DENSE ? 0 : ti.a_y) + k0;
+            const int ay = (PLAIN ? 0 : ti.a_y) + k0;
             ptx::tma_load_2d_pair(sa, &tmA, fb, ti.a_x, ay, keep_a);                       // 2 x box {64 m, 64 k}
             ptx::tma_load_2d_pair(sa + ATOM_BYTES, &tmA, fb, ti.a_x + 64, ay, keep_a);
           }
           if (!B_MN) {
             ptx::tma_load_2d_pair(sb, &tmB, fb, k0, ti.b_y, keep_b);                       // box {64 k, 128 rows}
           } else {
-            const int by = (MODE == MODE_DENSE ? 0 : ti.b_y) + k0;
+            const int by = (PLAIN ? 0 : ti.b_y) + k0;
             ptx::tma_load_2d_pair(sb, &tmB, fb, ti.b_x, by, keep_b);                       // 2 x box {64 n, 64 k}
             ptx::tma_load_2d_pair(sb + ATOM_BYTES, &tmB, fb, ti.b_x + 64, by, keep_b);
           }
@@ -517,6 +539,15 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         }
       }
     };
+    // LINEAR: residual of one 32-column chunk of this thread's row (zeros where there is none)
+    auto load_residual = [&](const Tile& ti, int c, uint4 (&q4)[4]) {
+      const int c0 = half * 128 + c * 32;
+      const int n_left = r < ti.m_valid ? ti.n_valid - c0 : 0;
+      const size_t at = ((size_t)ti.row0 + r) * p.N + ti.col0 + c0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        q4[q] = q * 8 < n_left ? *reinterpret_cast<const uint4*>(p.residual + at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
+    };
     const uint32_t leader_tempty[2] = {ptx::map_to_cta(tempty_bar(0), 0), ptx::map_to_cta(tempty_bar(1), 0)};
     int acc = 0;
     uint32_t acc_ph = 0;
@@ -526,6 +557,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const bool live = ti.m_valid > 0;    // false: this CTA only lent its half of B to the pair
       uint4 g4[4], u4[4];
       if (MODE == MODE_DH) load_gu(ti, 0, g4, u4);   // in flight while the main loop of this tile finishes
+      if (MODE == MODE_LINEAR && p.residual != nullptr) load_residual(ti, 0, g4);
       if (!ptx::mbar_wait_bounded(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)acc * BN + ((uint32_t)(quad * 32) << 16);
@@ -668,6 +700,69 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           const int nt = ti.col0 / BN;
           p.out_f[(size_t)(nt * 2 + half) * p.R_pad_max + (size_t)ti.row0 + r] = dgate;
         }
+      } else if (MODE == MODE_LINEAR) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {                // four 32-column chunks; chunks 2c, 2c+1 fill one staging block
+          const int cb = half * 128 + (c >> 1) * 64;
+          const int c0 = half * 128 + c * 32;
+          const int n_left = ti.n_valid - c0;
+          const bool any = ti.m_valid > quad * 32 && ti.n_valid - cb > 0;      // warp-uniform: the block holds results
+          uint4 res[4];
+          if (p.residual != nullptr) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) res[q] = g4[q];
+            if (c < 3) load_residual(ti, c + 1, g4); // next chunk's loads fly during this chunk's arithmetic
+          }
+          if (any) {
+            if ((c & 1) == 0) {
+              if (p.save_pre) stage_wait_all();      // both blocks are written: y through one, A * B + bias through the other
+              else { flip ^= 1u; stage_wait_older(); }
+            }
+            const uint32_t sb = p.save_pre || flip ? blk_a : blk_b;
+            uint32_t ra[32];
+            ptx::tmem_ld32(t_row + c0, ra);
+            ptx::tmem_ld_wait();
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(ra[i]);
+            if (p.bias != nullptr) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if (q * 8 < n_left) {
+                  float f[8];
+                  unpack8(__ldg(reinterpret_cast<const uint4*>(p.bias + ti.col0 + c0 + q * 8)), f);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) v[q * 8 + i] += f[i];
+                }
+              }
+            }
+            if (p.save_pre) stage_put_bf16(blk_b, (c & 1) * 4, v);
+            if (p.act == GROUTER_ACT_RELU) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = act_value<GROUTER_ACT_RELU>(v[i]);
+            } else if (p.act == GROUTER_ACT_SILU) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = act_value<GROUTER_ACT_SILU>(v[i]);
+            } else if (p.act == GROUTER_ACT_GELU) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = act_value<GROUTER_ACT_GELU>(v[i]);
+            }
+            if (p.residual != nullptr) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                float f[8];
+                unpack8(res[q], f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[q * 8 + i] += f[i];
+              }
+            }
+            stage_put_bf16(sb, (c & 1) * 4, v);
+            if ((c & 1) == 1) {
+              stage_send_2d(sb, &tmC0, ti.col0 + cb, y0);
+              if (p.save_pre) stage_send_2d(blk_b, &tmC1, ti.col0 + cb, y0);
+            }
+          }
+        }
       } else {  // WGRAD_D, WGRAD_GU, DENSE: fp32 tile straight from TMEM to global memory (stored, or added for a partial sum)
         if (ti.m_valid > quad * 32 && (have_acc || !ti.add)) {
 #pragma unroll
@@ -796,7 +891,7 @@ static cudaError_t launch_tc(const Maps& m, const GemmParams& p, int grid, cudaS
 
 template <int MODE, bool A_MN, bool B_MN>
 static cudaError_t launch_t(const Maps& m, const GemmParams& p, int grid, cudaStream_t st) {
-  if constexpr (MODE != MODE_DENSE) {
+  if constexpr (MODE != MODE_DENSE && MODE != MODE_LINEAR) {
     if (p.cycles != nullptr) return launch_tc<MODE, A_MN, B_MN, true>(m, p, grid, st);
   }
   return launch_tc<MODE, A_MN, B_MN, false>(m, p, grid, st);
@@ -968,10 +1063,17 @@ cudaError_t launch_wait_selftest(grouter_ctx* ctx, unsigned long long limit_ns, 
   return cudaGetLastError();
 }
 
-cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, float* C, int M, int N, int K, int32_t* status,
+// One CTA pair per tile, at most one CTA per SM.
+static int plain_grid(int64_t tiles) {
+  const int cap = current_sms() & ~1;
+  return 2 * tiles < cap ? (int)(2 * tiles) : cap;
+}
+
+cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, float* C, int M, int N, int K, int k_chunk, int32_t* status,
                               cudaStream_t st) {
   GemmParams p{};
   p.M = M; p.N = N; p.K = K;
+  p.k_chunk = k_chunk;
   p.tiles_m = cdiv(M, PM);
   p.tiles_n = cdiv(N, BN);
   p.status = status;
@@ -982,15 +1084,34 @@ cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, 
                   (b_mn ? make_map(&m.B, B, K, N, 64) : make_map(&m.B, B, N, K, 128));
   if (!ok) return cudaErrorInvalidValue;
   m.C0 = m.C1 = m.C2 = m.A;
-  int dev = 0, sms = 0;
-  cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  int grid = 2 * p.tiles_m * p.tiles_n;   // one CTA pair per tile, at most one CTA per SM
-  if (grid > (sms & ~1)) grid = sms & ~1;
+  const int grid = plain_grid((int64_t)p.tiles_m * p.tiles_n * cdiv(K, k_chunk));
   if (a_mn && b_mn) return launch_t<MODE_DENSE, true, true>(m, p, grid, st);
   if (a_mn) return launch_t<MODE_DENSE, true, false>(m, p, grid, st);
   if (b_mn) return launch_t<MODE_DENSE, false, true>(m, p, grid, st);
   return launch_t<MODE_DENSE, false, false>(m, p, grid, st);
+}
+
+cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st) {
+  GemmParams p{};
+  p.M = g.M; p.N = g.N; p.K = g.K;
+  p.tiles_m = cdiv(g.M, PM);
+  p.tiles_n = cdiv(g.N, BN);
+  p.status = g.status;
+  p.bias = static_cast<const __nv_bfloat16*>(g.bias);
+  p.residual = static_cast<const __nv_bfloat16*>(g.residual);
+  p.act = g.act;
+  p.save_pre = g.pre != nullptr;
+  p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
+  Maps m;
+  const bool ok = (g.a_mn ? make_map(&m.A, g.A, g.K, g.M, 64) : make_map(&m.A, g.A, g.M, g.K, 128)) &&
+                  (g.b_mn ? make_map(&m.B, g.B, g.K, g.N, 64) : make_map(&m.B, g.B, g.N, g.K, 128)) && make_map(&m.C0, g.C, g.M, g.N, 32) &&
+                  make_map(&m.C1, g.pre ? g.pre : g.C, g.M, g.N, 32);
+  if (!ok) return cudaErrorInvalidValue;
+  m.C2 = m.C0;
+  const int grid = plain_grid((int64_t)p.tiles_m * p.tiles_n);
+  if (g.a_mn) return g.b_mn ? launch_t<MODE_LINEAR, true, true>(m, p, grid, st) : cudaErrorInvalidValue;
+  if (g.b_mn) return launch_t<MODE_LINEAR, false, true>(m, p, grid, st);
+  return launch_t<MODE_LINEAR, false, false>(m, p, grid, st);
 }
 
 }  // namespace grouter

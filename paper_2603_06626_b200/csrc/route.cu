@@ -479,7 +479,7 @@ int grouter_route(const void* H, const void* W_s, const int32_t* fold_map, int32
     return cudaGetLastError() == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
   }
   // ---- two-kernel form: source scores [T, d_h] x [E_src, d_h]^T on the tensor cores, fp32 out ----
-  if (launch_dense_gemm(H, 0, W_s, 0, S_src, T, E_src, d_h, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (launch_dense_gemm(H, 0, W_s, 0, S_src, T, E_src, d_h, (d_h + 63) / 64 * 64, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   if (fold_map) {
     route_groups_kernel<<<1, ROUTE_THREADS, 0, st>>>(fold_map, E_src, E_tgt, grp_off, grp_src, status);
     if (cudaGetLastError() != cudaSuccess) return GROUTER_ERR_CUDA;

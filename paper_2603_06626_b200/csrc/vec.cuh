@@ -1,0 +1,82 @@
+// Typed loads and stores of a few consecutive elements, shared by the kernels around the expert layer (layer norm,
+// balance loss, optimizer): bf16 or f32 in memory, f32 in registers, 16 bytes at a time where VE elements fill them.
+#pragma once
+#include "common.cuh"
+
+namespace grouter {
+
+// Streaming multiprocessors of the current device (0 without one); looked up once a device.
+inline int current_sms() {
+  static int sms[64] = {};
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  if (dev >= 0 && dev < 64 && sms[dev]) return sms[dev];
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  if (dev >= 0 && dev < 64) sms[dev] = n;
+  return n;
+}
+
+inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// Elements of T in one 16-byte access.
+template <typename T>
+constexpr int vec16() { return 16 / (int)sizeof(T); }
+
+// VE elements as they lie in memory, fetched in one access where that is a power-of-two size up to 16 bytes.
+template <typename T, int VE>
+struct alignas(VE * sizeof(T) <= 16 ? VE * sizeof(T) : 16) Pack {
+  T v[VE];
+};
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// Streamed once: read-only path, no L1 line kept.
+__device__ __forceinline__ uint4 ld_stream16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+template <typename T, int VE>
+__device__ __forceinline__ Pack<T, VE> ld_pack(const T* p) {
+  Pack<T, VE> r;
+  if constexpr (VE * sizeof(T) == 16) {
+    *reinterpret_cast<uint4*>(&r) = ld_stream16(p);
+  } else {
+    static_assert(VE == 1, "whole 16-byte accesses or single elements");
+    r.v[0] = __ldg(p);
+  }
+  return r;
+}
+template <typename T, int VE>
+__device__ __forceinline__ void st_pack(T* p, const float (&f)[VE]) {
+  Pack<T, VE> r;
+#pragma unroll
+  for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(f[i]);
+  *reinterpret_cast<Pack<T, VE>*>(p) = r;
+}
+
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// Column sums of n_part rows of `cols` values in a fixed order; the first n0 columns go to out0, the others to out1 (or nowhere).
+cudaError_t launch_sum_rows(const float* partial, int n_part, int cols, float* out0, int n0, float* out1, cudaStream_t st);
+
+}  // namespace grouter
