@@ -315,11 +315,12 @@ cudaError_t balance_launch(const BalanceParams& p, cudaStream_t st) {
   return p.dgates ? balance_launch_g<T, VE, LPT, NV, true>(p, st) : balance_launch_g<T, VE, LPT, NV, false>(p, st);
 }
 
-// Lanes a token: as few as hold the row, but one for every kept expert where the gates' gradient is joined in.
+// Lanes a token: as few as hold the row, but one for every kept expert, whose gates they differentiate.  (With or without gates:
+// the sums of a row then run in the same order and the losses are the same bits.)
 template <typename T, int VE>
 cudaError_t balance_by_width(const BalanceParams& p, cudaStream_t st) {
   int lpt = 1;
-  while (lpt < 32 && (lpt * VE < p.E || (p.dgates && lpt < p.k))) lpt *= 2;
+  while (lpt < 32 && (lpt * VE < p.E || lpt < p.k)) lpt *= 2;
   const int nv = (p.E + lpt * VE - 1) / (lpt * VE);
   switch (lpt) {
     case 1: return balance_launch<T, VE, 1, 1>(p, st);
