@@ -460,7 +460,7 @@ def _expect(what: str, t: Optional[torch.Tensor], shape, dtype=None, like: Optio
     """Raises unless t (None passes) is a contiguous tensor of this shape (and type), on the same device as `like`."""
     if t is None:
         return
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
@@ -468,6 +468,29 @@ def _expect(what: str, t: Optional[torch.Tensor], shape, dtype=None, like: Optio
         raise ValueError(f"{what}: a contiguous tensor is expected")
     if like is not None and t.device != like.device:
         raise ValueError(f"{what}: on {t.device}, the other arguments are on {like.device}")
+
+
+def _device_index(dev: torch.device) -> int:
+    """Index of a CUDA device; other devices raise."""
+    if dev.type != "cuda":
+        raise ValueError(f"a CUDA tensor is expected, got one on {dev}")
+    return dev.index if dev.index is not None else torch.cuda.current_device()
+
+
+def _raw_stream(index: int) -> int:
+    """Handle of the device's current torch stream, without building a torch.cuda.Stream around it (3 us of a call of 10)."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _call(fn, what: str, index: int, *args) -> None:
+    """Calls the library with the arguments and the current stream, on the given device; raises on an error code."""
+    if torch._C._cuda_getDevice() == index:
+        code = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args, _raw_stream(index))
+    if code != 0:
+        raise GrouterError(code, what)
 
 
 def _row_stride(what: str, x: torch.Tensor) -> int:
@@ -487,13 +510,12 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     _expect("weight", weight, (d,), like=x)
     _expect("bias", bias, (d,), weight.dtype, like=x)
     dt, wt = _elt(x, "x"), _elt(weight, "weight")
-    dev = x.device
-    with torch.cuda.device(dev):
-        y = torch.empty((T, d), dtype=x.dtype, device=dev)
-        stats = torch.empty((2, T), dtype=torch.float32, device=dev)
-        mean, rstd = stats[0], stats[1]
-        _check(lib.grouter_layernorm_fwd(x.data_ptr(), ldx, _ptr(weight), _ptr(bias), T, d, dt, wt, eps, _ptr(y), _ptr(mean), _ptr(rstd),
-                                         _stream()), "grouter_layernorm_fwd")
+    dev = _device_index(x.device)
+    y = x.new_empty((T, d))
+    mean = x.new_empty(T, dtype=torch.float32)
+    rstd = x.new_empty(T, dtype=torch.float32)
+    _call(lib.grouter_layernorm_fwd, "grouter_layernorm_fwd", dev, x.data_ptr(), ldx, weight.data_ptr(), _ptr(bias), T, d, dt, wt, eps, y.data_ptr(),
+          mean.data_ptr(), rstd.data_ptr())
     return y, mean, rstd
 
 
@@ -507,40 +529,51 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     _expect("mean", mean, (T,), torch.float32, like=x)
     _expect("rstd", rstd, (T,), torch.float32, like=x)
     dt, wt = _elt(x, "x"), _elt(weight, "weight")
-    dev = x.device
-    with torch.cuda.device(dev):
-        dx = torch.empty((T, d), dtype=x.dtype, device=dev)
-        dw = torch.empty(d, dtype=torch.float32, device=dev)
-        db = torch.empty(d, dtype=torch.float32, device=dev) if want_bias else None
-        ws = torch.empty(max(1, lib.grouter_layernorm_bwd_workspace_bytes(T, d)), dtype=torch.uint8, device=dev)
-        _check(lib.grouter_layernorm_bwd(_ptr(dy), x.data_ptr(), ldx, _ptr(weight), _ptr(mean), _ptr(rstd), T, d, dt, wt, _ptr(dx), _ptr(dw),
-                                         _ptr(db), _ptr(ws), _stream()), "grouter_layernorm_bwd")
+    dev = _device_index(x.device)
+    dx = x.new_empty((T, d))
+    dw = x.new_empty(d, dtype=torch.float32)
+    db = x.new_empty(d, dtype=torch.float32) if want_bias else None
+    ws = x.new_empty(_bytes(lib.grouter_layernorm_bwd_workspace_bytes, dev, T, d), dtype=torch.uint8)
+    _call(lib.grouter_layernorm_bwd, "grouter_layernorm_bwd", dev, dy.data_ptr(), x.data_ptr(), ldx, weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+          T, d, dt, wt, dx.data_ptr(), dw.data_ptr(), _ptr(db), ws.data_ptr())
     return dx, dw, db
+
+
+def _bytes(fn, index: int, *args) -> int:
+    """Workspace bytes, which depend on the device they are for; never an empty tensor's 0."""
+    if torch._C._cuda_getDevice() == index:
+        return fn(*args) or 256
+    with torch.cuda.device(index):
+        return fn(*args) or 256
 
 
 _status_words = {}
 
 
-def _status_word(dev: torch.device) -> torch.Tensor:
+def _status_word(index: int) -> torch.Tensor:
     """The status word of a device that the calls without one of their own share."""
-    key = dev.index if dev.index is not None else torch.cuda.current_device()
-    if key not in _status_words:
-        _status_words[key] = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", key))
-        torch.cuda.synchronize(key)      # zeroed before a kernel on any stream can set a bit in it
-    return _status_words[key]
+    word = _status_words.get(index)
+    if word is None:
+        word = _status_words[index] = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
+        torch.cuda.synchronize(index)      # zeroed before a kernel on any stream can set a bit in it
+    return word
 
 
 def check_status(device="cuda:0") -> None:
     """Waits for the device; raises when a linear, linear_backward, expert_counts or balance_loss call without a status word of its own
     met a bounded wait that ran out or an expert id out of range since the last check, and clears the word."""
-    dev = torch.device(device)
-    torch.cuda.synchronize(dev)
-    word = _status_word(dev)
+    index = _device_index(torch.device(device))
+    torch.cuda.synchronize(index)
+    word = _status_word(index)
     st = int(word.item())
     word.zero_()
-    torch.cuda.synchronize(dev)
+    torch.cuda.synchronize(index)
     if st != 0:
         raise GrouterError(-7 if st & 2 else -6, "device status")
+
+
+def _status_ptr(status: Optional[torch.Tensor], index: int) -> int:
+    return (_status_word(index) if status is None else status).data_ptr()
 
 
 def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
@@ -557,12 +590,11 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     _expect("bias", bias, (N,), bf, like=x)
     _expect("residual", residual, (T, N), bf, like=x)
     _expect("status", status, (1,), torch.int32, like=x)
-    dev = x.device
-    with torch.cuda.device(dev):
-        y = torch.empty((T, N), dtype=bf, device=dev)
-        pre = torch.empty((T, N), dtype=bf, device=dev) if save_pre else None
-        _check(lib.grouter_linear_fwd(_ptr(x), _ptr(W), _ptr(bias), _ptr(residual), T, K, N, act, _ptr(y), _ptr(pre),
-                                      _ptr(_status_word(dev) if status is None else status), _stream()), "grouter_linear_fwd")
+    dev = _device_index(x.device)
+    y = x.new_empty((T, N))
+    pre = x.new_empty((T, N)) if save_pre else None
+    _call(lib.grouter_linear_fwd, "grouter_linear_fwd", dev, x.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), T, K, N, act, y.data_ptr(),
+          _ptr(pre), _status_ptr(status, dev))
     return y, pre
 
 
@@ -586,15 +618,13 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Opt
         raise ValueError("pre: needed with an activation")
     if dW_dtype not in (bf, torch.float32):
         raise TypeError(f"dW_dtype: bfloat16 or float32 expected, got {dW_dtype}")
-    dev = x.device
-    with torch.cuda.device(dev):
-        dx = torch.empty((T, K), dtype=bf, device=dev) if want_dx else None
-        dW = torch.empty((N, K), dtype=dW_dtype, device=dev) if want_dW else None
-        db = torch.empty(N, dtype=torch.float32, device=dev) if want_bias else None
-        ws = torch.empty(max(256, lib.grouter_linear_bwd_workspace_bytes(T, K, N, act)), dtype=torch.uint8, device=dev)
-        _check(lib.grouter_linear_bwd(_ptr(dy), _ptr(x), _ptr(W), _ptr(pre), T, K, N, act, _ptr(dx), _ptr(dW),
-                                      F32 if dW_dtype == torch.float32 else BF16, _ptr(db), _ptr(ws),
-                                      _ptr(_status_word(dev) if status is None else status), _stream()), "grouter_linear_bwd")
+    dev = _device_index(x.device)
+    dx = x.new_empty((T, K)) if want_dx else None
+    dW = x.new_empty((N, K), dtype=dW_dtype) if want_dW else None
+    db = x.new_empty(N, dtype=torch.float32) if want_bias else None
+    ws = x.new_empty(_bytes(lib.grouter_linear_bwd_workspace_bytes, dev, T, K, N, act), dtype=torch.uint8)
+    _call(lib.grouter_linear_bwd, "grouter_linear_bwd", dev, dy.data_ptr(), x.data_ptr(), W.data_ptr(), _ptr(pre), T, K, N, act, _ptr(dx), _ptr(dW),
+          F32 if dW_dtype == torch.float32 else BF16, _ptr(db), ws.data_ptr(), _status_ptr(status, dev))
     return dx, dW, db
 
 
@@ -606,11 +636,12 @@ def _idx_dtype(idx: torch.Tensor) -> int:
     raise TypeError(f"idx: uint8 or int32 expected, got {idx.dtype}")
 
 
-def _mask_of(mask: Optional[torch.Tensor], T: int, like: torch.Tensor) -> Optional[torch.Tensor]:
-    if mask is not None and mask.dtype not in (torch.uint8, torch.bool):
+def _check_mask(mask: Optional[torch.Tensor], T: int, like: torch.Tensor) -> None:
+    if mask is None:
+        return
+    if mask.dtype != torch.uint8 and mask.dtype != torch.bool:
         raise TypeError(f"mask: uint8 or bool expected, got {mask.dtype}")
     _expect("mask", mask, (T,), like=like)
-    return mask
 
 
 def expert_counts(idx: torch.Tensor, E: int, mask: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
@@ -622,14 +653,13 @@ def expert_counts(idx: torch.Tensor, E: int, mask: Optional[torch.Tensor] = None
     T, k = idx.shape
     _expect("idx", idx, (T, k))
     _expect("status", status, (1,), torch.int32, like=idx)
-    mask = _mask_of(mask, T, idx)
+    _check_mask(mask, T, idx)
     dt = _idx_dtype(idx)
-    dev = idx.device
-    with torch.cuda.device(dev):
-        out = torch.empty(E + 1, dtype=torch.int32, device=dev)
-        counts, n = out[:E], out[E:]
-        _check(lib.grouter_expert_counts(_ptr(idx), dt, _ptr(mask), T, k, E, _ptr(counts), _ptr(n),
-                                         _ptr(_status_word(dev) if status is None else status), _stream()), "grouter_expert_counts")
+    dev = _device_index(idx.device)
+    counts = idx.new_empty(E, dtype=torch.int32)
+    n = idx.new_empty(1, dtype=torch.int32)
+    _call(lib.grouter_expert_counts, "grouter_expert_counts", dev, idx.data_ptr(), dt, _ptr(mask), T, k, E, counts.data_ptr(), n.data_ptr(),
+          _status_ptr(status, dev))
     return counts, n
 
 
@@ -646,29 +676,28 @@ def balance_loss(logits: torch.Tensor, idx: Optional[torch.Tensor], counts: torc
     dt = _elt(logits, "logits")
     if dgates is not None and idx is None:
         raise ValueError("idx: needed with dgates")
-    k = 1
+    k, it = 1, IDX_U8
     if idx is not None:
         if idx.dim() != 2:
             raise ValueError("idx: a matrix is expected")
-        k = idx.shape[1]
+        k, it = idx.shape[1], _idx_dtype(idx)
         _expect("idx", idx, (T, k), like=logits)
     _expect("counts", counts, (E,), torch.int32, like=logits)
     _expect("n_tokens", n_tokens, (1,), torch.int32, like=logits)
     _expect("dgates", dgates, (T, k), torch.float32, like=logits)
-    if dloss is not None and dloss.numel() != 1:
-        raise ValueError("dloss: one number is expected")
-    _expect("dloss", None if dloss is None else dloss.reshape(1), (1,), torch.float32, like=logits)
+    if dloss is not None:
+        if dloss.numel() != 1:
+            raise ValueError("dloss: one number is expected")
+        _expect("dloss", dloss.reshape(1), (1,), torch.float32, like=logits)
     _expect("status", status, (1,), torch.int32, like=logits)
-    mask = _mask_of(mask, T, logits)
-    dev = logits.device
-    with torch.cuda.device(dev):
-        loss = torch.empty(3, dtype=torch.float32, device=dev) if want_loss else None
-        d = torch.empty((T, E), dtype=logits.dtype, device=dev) if want_grad else None
-        ws = torch.empty(lib.grouter_balance_loss_workspace_bytes(), dtype=torch.uint8, device=dev) if want_loss else None
-        _check(lib.grouter_balance_loss(logits.data_ptr(), ld, dt, _ptr(idx), IDX_U8 if idx is None else _idx_dtype(idx), _ptr(mask),
-                                        _ptr(counts), _ptr(n_tokens), _ptr(dgates), norm, T, E, k, balance_coef, z_coef, _ptr(dloss),
-                                        _ptr(loss), _ptr(d), _ptr(ws), _ptr(_status_word(dev) if status is None else status), _stream()),
-               "grouter_balance_loss")
+    _check_mask(mask, T, logits)
+    dev = _device_index(logits.device)
+    loss = logits.new_empty(3, dtype=torch.float32) if want_loss else None
+    d = logits.new_empty((T, E)) if want_grad else None
+    ws = logits.new_empty(_bytes(lib.grouter_balance_loss_workspace_bytes, dev), dtype=torch.uint8) if want_loss else None
+    _call(lib.grouter_balance_loss, "grouter_balance_loss", dev, logits.data_ptr(), ld, dt, _ptr(idx), it, _ptr(mask), counts.data_ptr(),
+          n_tokens.data_ptr(), _ptr(dgates), norm, T, E, k, balance_coef, z_coef, _ptr(dloss), _ptr(loss), _ptr(d), _ptr(ws),
+          _status_ptr(status, dev))
     return loss, d
 
 
@@ -732,6 +761,10 @@ class AdamW:
         host = torch.zeros(max(16, self._layout.table_bytes), dtype=u8)
         _check(self.lib.grouter_adamw_layout_host(desc, n, ctypes.byref(self._layout), host.data_ptr()), "grouter_adamw_layout_host")
         self._table = host.to(dev)
+        self._index = _device_index(dev)
+        # the addresses of the state, which this object keeps for good
+        self._args = (ctypes.byref(self._layout), self._table.data_ptr(), state_bits, _ptr(getattr(self, "master", None)), self.m.data_ptr(),
+                      self.v.data_ptr(), _ptr(getattr(self, "m_exp", None)), _ptr(getattr(self, "v_exp", None)))
 
     def step(self, grad_scale: Optional[torch.Tensor] = None, lr: Optional[float] = None) -> None:
         """One update from the gradients as they are now.  grad_scale: f32 device scalar every gradient is multiplied by."""
@@ -739,22 +772,18 @@ class AdamW:
             raise ValueError("grad_scale: one f32 number on the parameters' device is expected")
         if lr is not None:
             self.lr = lr
-        with torch.cuda.device(self.device):
-            _check(self.lib.grouter_adamw_step(ctypes.byref(self._layout), _ptr(self._table), self.state_bits, _ptr(getattr(self, "master", None)),
-                                               _ptr(self.m), _ptr(self.v), _ptr(getattr(self, "m_exp", None)), _ptr(getattr(self, "v_exp", None)),
-                                               self.lr, self.betas[0], self.betas[1], self.eps, self.steps_done + 1, _ptr(grad_scale), _stream()),
-                   "grouter_adamw_step")
+        _call(self.lib.grouter_adamw_step, "grouter_adamw_step", self._index, *self._args, self.lr, self.betas[0], self.betas[1], self.eps,
+              self.steps_done + 1, _ptr(grad_scale))
         self.steps_done += 1
 
     def moments(self):
         """(m, v) as flat f32 tensors: the state itself with 32 bits, the values that the codes stand for with 8."""
         if self.state_bits == 32:
             return self.m, self.v
-        out = torch.empty((2, self.m.numel()), dtype=torch.float32, device=self.device)
-        with torch.cuda.device(self.device):
-            _check(self.lib.grouter_adamw_moments(_ptr(self.m), _ptr(self.v), _ptr(self.m_exp), _ptr(self.v_exp), self.m.numel(),
-                                                  out.data_ptr(), out[1].data_ptr(), _stream()), "grouter_adamw_moments")
-        return out[0], out[1]
+        m, v = self.m.new_empty(self.m.shape, dtype=torch.float32), self.m.new_empty(self.m.shape, dtype=torch.float32)
+        _call(self.lib.grouter_adamw_moments, "grouter_adamw_moments", self._index, self.m.data_ptr(), self.v.data_ptr(), self.m_exp.data_ptr(),
+              self.v_exp.data_ptr(), self.m.numel(), m.data_ptr(), v.data_ptr())
+        return m, v
 
 
 def dense_gemm(A: torch.Tensor, a_mn_major: bool, B: torch.Tensor, b_mn_major: bool, M: int, N: int, K: int) -> torch.Tensor:

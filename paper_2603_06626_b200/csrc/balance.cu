@@ -15,6 +15,7 @@
 //
 // A score of -inf takes its expert out (p = 0, no gradient).  A row of nothing but -inf has p = 0 throughout and no
 // z-loss term.  A token whose mask byte is zero contributes nothing and gets a zero gradient row, whatever its scores are.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "vec.cuh"
@@ -24,20 +25,25 @@ namespace grouter {
 constexpr int BAL_THREADS = 256;
 constexpr int BAL_WARPS = BAL_THREADS / 32;
 constexpr int BAL_MAX_E = 1024;
-constexpr int COUNT_THREADS = 256;
+constexpr int COUNT_THREADS = 512;
+constexpr int COUNT_CLUSTER = 8;
+// Up to this many ids one cluster counts them all and writes the sums itself: one launch instead of two zeroings and a kernel.
+constexpr int64_t COUNT_CLUSTER_SLOTS = 1 << 19;
 constexpr int COUNT_SLOTS = 4096;       // counters a block of the histogram keeps (several copies of few experts)
 
-// counts += histogram of this block's share of the ids.  A thread takes 16 bytes of ids at a time (IPT of them).  Lanes
-// spread over `copies` copies of the counters, so that few experts do not queue up at the same word.
-template <typename Id>
+// Histogram of the ids.  A thread takes 16 bytes of ids at a time (IPT of them).  Lanes spread over `copies` copies of the
+// counters, so that few experts do not queue up at the same word.
+// CLUSTER: the grid is one cluster of COUNT_CLUSTER blocks, which add up their counters through each other's shared memory and
+// store the sums; otherwise any number of blocks adds to outputs that were zeroed before.
+template <typename Id, bool CLUSTER>
 __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* __restrict__ idx, int64_t slots, int k, int E, int copies,
                                                                       const uint8_t* __restrict__ mask, int32_t* __restrict__ counts,
-                                                                      int32_t* __restrict__ n_tokens, int32_t* __restrict__ status, int direct) {
+                                                                      int32_t* __restrict__ n_tokens, int32_t* __restrict__ status) {
   constexpr int IPT = 16 / (int)sizeof(Id);
   __shared__ int32_t s_cnt[COUNT_SLOTS];
-  __shared__ int32_t s_tok;
+  __shared__ int32_t s_sum[BAL_MAX_E + 1];        // this block's counts, then its tokens
   for (int i = threadIdx.x; i < E * copies; i += COUNT_THREADS) s_cnt[i] = 0;
-  if (threadIdx.x == 0) s_tok = 0;
+  if (threadIdx.x == 0) s_sum[E] = 0;
   __syncthreads();
   int32_t* mine = s_cnt + (threadIdx.x % copies) * E;
   int tokens = 0;
@@ -72,17 +78,30 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
     }
   }
   if (bad && status) atomicOr(status, STATUS_BAD_INDEX);
-  if (tokens) atomicAdd(&s_tok, tokens);
+  if (tokens) atomicAdd(s_sum + E, tokens);
   __syncthreads();
   for (int e = threadIdx.x; e < E; e += COUNT_THREADS) {
     int32_t c = 0;
     for (int q = 0; q < copies; ++q) c += s_cnt[q * E + e];
-    if (direct) counts[e] = c;
-    else if (c) atomicAdd(counts + e, c);
+    s_sum[e] = c;
   }
-  if (threadIdx.x == 0) {
-    if (direct) *n_tokens = s_tok;
-    else if (s_tok) atomicAdd(n_tokens, s_tok);
+  if constexpr (CLUSTER) {
+    cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+    cl.sync();
+    for (int e = cl.block_rank() * COUNT_THREADS + threadIdx.x; e <= E; e += COUNT_CLUSTER * COUNT_THREADS) {
+      int32_t c = 0;
+#pragma unroll
+      for (int r = 0; r < COUNT_CLUSTER; ++r) c += cl.map_shared_rank(s_sum, r)[e];
+      if (e < E) counts[e] = c;
+      else *n_tokens = c;
+    }
+    cl.sync();                                    // nobody leaves while its counters are read
+  } else {
+    __syncthreads();
+    for (int e = threadIdx.x; e <= E; e += COUNT_THREADS) {
+      const int32_t c = s_sum[e];
+      if (c) atomicAdd(e < E ? counts + e : n_tokens, c);
+    }
   }
 }
 
@@ -250,6 +269,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     if (GATES) __syncwarp();
   }
   if (p.loss == nullptr) return;
+  let_next_kernel_start();
   sum_a = lanes_sum<32>(sum_a);
   sum_z = lanes_sum<32>(sum_z);
   if (lane == 0) {
@@ -271,6 +291,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
 __global__ void __launch_bounds__(256) balance_finish_kernel(const BalanceParams p, int n_part) {
   __shared__ double s[2][256];
   double a = 0, z = 0;
+  after_previous_kernel();
   for (int i = threadIdx.x; i < n_part; i += 256) {
     const double2 v = p.partial[i];
     a += v.x;
@@ -293,6 +314,22 @@ namespace {
 
 constexpr int BAL_MAX_BLOCKS_PER_SM = 8;
 
+template <typename Id>
+cudaError_t count_in_cluster(const Id* idx, int64_t slots, int k, int E, int copies, const uint8_t* mask, int32_t* counts, int32_t* n_tokens,
+                             int32_t* status, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(COUNT_CLUSTER);
+  cfg.blockDim = dim3(COUNT_THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = COUNT_CLUSTER;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, expert_counts_kernel<Id, true>, idx, slots, k, E, copies, mask, counts, n_tokens, status);
+}
+
 template <typename T, int VE, int LPT, int NV, bool GATES>
 cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
   constexpr int TPB = BAL_WARPS * (32 / LPT);
@@ -303,10 +340,7 @@ cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
   const int grid = (int)(want < cap ? want : cap);
   balance_kernel<T, VE, LPT, NV, GATES><<<grid, BAL_THREADS, smem, st>>>(p);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess && p.loss && grid > 1) {
-    balance_finish_kernel<<<1, 256, 0, st>>>(p, grid);
-    e = cudaGetLastError();
-  }
+  if (e == cudaSuccess && p.loss && grid > 1) e = launch_dependent(balance_finish_kernel, dim3(1), dim3(256), 0, st, p, grid);
   return e;
 }
 
@@ -355,24 +389,27 @@ int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mas
   if (!aligned_to(idx, 16) || !aligned_to(counts, 4) || !aligned_to(n_tokens, 4) || !aligned_to(status, 4)) return GROUTER_ERR_MISALIGNED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int64_t slots = (int64_t)T * k;
-  const int ipt = idx_dtype == GROUTER_IDX_U8 ? 16 : 4;
-  const int64_t per_block = (int64_t)COUNT_THREADS * ipt;
-  const int64_t want = (slots + per_block - 1) / per_block;
-  const int cap = current_sms() * 4;
-  const int grid = (int)(want < 1 ? 1 : want < cap ? want : cap);
+  const bool u8 = idx_dtype == GROUTER_IDX_U8;
   int copies = COUNT_SLOTS / E;
   if (copies > 32) copies = 32;
-  if (grid > 1) {       // several blocks add up in place
-    if (cudaMemsetAsync(counts, 0, sizeof(int32_t) * E, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-    if (cudaMemsetAsync(n_tokens, 0, sizeof(int32_t), st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  cudaError_t e;
+  if (slots <= COUNT_CLUSTER_SLOTS) {
+    e = u8 ? count_in_cluster(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts, n_tokens, status, st)
+           : count_in_cluster(static_cast<const int32_t*>(idx), slots, k, E, copies, mask, counts, n_tokens, status, st);
+  } else {
+    if (cudaMemsetAsync(counts, 0, sizeof(int32_t) * E, st) != cudaSuccess || cudaMemsetAsync(n_tokens, 0, sizeof(int32_t), st) != cudaSuccess)
+      return GROUTER_ERR_CUDA;
+    const int64_t per_block = (int64_t)COUNT_THREADS * (u8 ? 16 : 4), want = (slots + per_block - 1) / per_block;
+    const int cap = current_sms() * 4, grid = (int)(want < cap ? want : cap);
+    if (u8)
+      expert_counts_kernel<uint8_t, false><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts,
+                                                                          n_tokens, status);
+    else
+      expert_counts_kernel<int32_t, false><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const int32_t*>(idx), slots, k, E, copies, mask, counts,
+                                                                          n_tokens, status);
+    e = cudaGetLastError();
   }
-  if (idx_dtype == GROUTER_IDX_U8)
-    expert_counts_kernel<uint8_t><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts, n_tokens,
-                                                                 status, grid == 1);
-  else
-    expert_counts_kernel<int32_t><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const int32_t*>(idx), slots, k, E, copies, mask, counts, n_tokens,
-                                                                 status, grid == 1);
-  return cudaGetLastError() == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+  return e == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
 size_t grouter_balance_loss_workspace_bytes(void) { return sizeof(double2) * current_sms() * BAL_MAX_BLOCKS_PER_SM; }

@@ -47,6 +47,7 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
     }
   }
   if constexpr (SUM) {
+    let_next_kernel_start();
 #pragma unroll
     for (int i = 0; i < 8; ++i) s_sum[rl][ct + 32 * i] = acc[i];
     __syncthreads();

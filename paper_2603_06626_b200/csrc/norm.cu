@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
       }
     }
   }
+  let_next_kernel_start();
   // this block's partial row: [dw | db]
   float* pw = partial + (int64_t)blockIdx.x * 2 * d;
   if constexpr (WIDE) {
@@ -286,6 +287,7 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* __restrict_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;
   float a = 0.f;
+  after_previous_kernel();
   if (c < cols) {
 #pragma unroll 8
     for (int r = warp; r < n_part; r += 32) a += partial[(int64_t)r * cols + c];
@@ -301,8 +303,7 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* __restrict_
 }
 
 cudaError_t launch_sum_rows(const float* partial, int n_part, int cols, float* out0, int n0, float* out1, cudaStream_t st) {
-  sum_rows_kernel<<<(cols + 31) / 32, 1024, 0, st>>>(partial, n_part, cols, out0, n0, out1);
-  return cudaGetLastError();
+  return launch_dependent(sum_rows_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, partial, n_part, cols, out0, n0, out1);
 }
 
 namespace {

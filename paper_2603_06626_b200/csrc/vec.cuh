@@ -16,6 +16,27 @@ inline int current_sms() {
   return n;
 }
 
+// Launches a kernel that reads what the kernel before it on the stream wrote: it may be scheduled while that one still runs
+// (programmatic dependent launch), so it has to call after_previous_kernel() before it touches anything.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
+}
+// Waits until the kernel before this one has ended and its writes are visible.
+__device__ __forceinline__ void after_previous_kernel() { cudaGridDependencySynchronize(); }
+// From here on the next kernel's blocks may be scheduled (they still wait for this kernel's end before they read).
+__device__ __forceinline__ void let_next_kernel_start() { cudaTriggerProgrammaticLaunchCompletion(); }
+
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // Elements of T in one 16-byte access.
