@@ -10,7 +10,7 @@
 //
 // The counts are known before the scores are read, so the loss needs no column sums of p: one number a token (a_t) carries
 // it, and one pass over the scores gives the loss and its gradient.  Bound by HBM: scores read once, gradient written once.
-// LPT neighbouring lanes hold a token's row in registers, 16 bytes at a time; a block's token sums are added in a fixed
+// Neighbouring lanes hold a token's row in registers, 16 bytes at a time; a block's token sums are added in a fixed
 // order, and the last step (one block) adds the blocks' sums in double precision.
 //
 // A score of -inf takes its expert out (p = 0, no gradient).  A row of nothing but -inf has p = 0 throughout and no
@@ -132,81 +132,129 @@ __device__ __forceinline__ void write_loss(const BalanceParams& p, double a, dou
   p.loss[2] = zl;
 }
 
-// VE elements an access, LPT lanes a token, NV accesses a lane: LPT * NV * VE >= E.
-// Dynamic shared memory: f [E], then (with dgates) one row of E sums for every lane group.
-template <typename T, int VE, int LPT, int NV, bool GATES>
+// exp(d) of a difference of scores; results below the normal range of f32 are zero
+__device__ __forceinline__ float exp_of(float d) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d * 1.4426950408889634f));
+  return r;
+}
+
+// LPT neighbouring lanes hold a token's row, EPL elements each, VE to an access.  Few lanes and many elements: the three
+// reductions over a row cost log2(LPT) shuffles each for a whole warp's 32 / LPT tokens, which is what bounded one warp a token
+// (326 instructions a token of 256 scores).  A token's loads are issued one round before they are used.
+// Dynamic shared memory: f [E], then (with dgates) one row of E sums for every lane group, zero between tokens.
+template <typename T, int VE, int LPT, int EPL, bool GATES>
 __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParams p) {
   extern __shared__ float s_f[];
   __shared__ double s_part[2][BAL_WARPS];
-  __shared__ unsigned long long s_total;
+  __shared__ unsigned long long s_count[BAL_WARPS];
+  constexpr int NV = EPL / VE;
   constexpr int TPW = 32 / LPT;                       // tokens a warp works on at a time
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sl = lane & (LPT - 1), grp = lane / LPT;
-  const int E = p.E;
-  // f_e = E c_e / sum c, and one row of zeros for every lane group
-  if (threadIdx.x == 0) s_total = 0ull;
-  __syncthreads();
+  const int E = p.E, epad = (E + 3) & ~3;
+
+  struct Row {                                        // what a lane needs of its token, as loaded
+    Pack<T, VE> q[NV];
+    int e;                                            // GATES: expert of the token's sl-th slot, and its gate's gradient
+    float dg;
+    bool live;
+  };
+  auto load = [&](int64_t t, Row& r) {
+    r.live = t < p.T;
+    r.e = -1;
+    r.dg = 0.f;
+    if (!r.live) return;
+    const T* row = reinterpret_cast<const T*>(p.logits) + t * p.ld;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = (n * LPT + sl) * VE;
+      if (c < E) r.q[n] = ld_pack<T, VE>(row + c);
+    }
+    if (GATES && sl < p.k) {                          // LPT >= k
+      const int64_t at = t * p.k + sl;
+      r.e = p.idx_i32 ? __ldg(reinterpret_cast<const int32_t*>(p.idx) + at) : (int)__ldg(reinterpret_cast<const uint8_t*>(p.idx) + at);
+      r.dg = __ldg(p.dgates + at);
+    }
+    if (p.mask != nullptr) r.live = __ldg(p.mask + t) != 0;
+  };
+
+  const int64_t step = (int64_t)gridDim.x * BAL_WARPS * TPW;
+  int64_t t = ((int64_t)blockIdx.x * BAL_WARPS + warp) * TPW + grp;
+  Row cur;
+  load(t, cur);                                       // on its way while the shares are worked out
+
+  // f_e = E c_e / sum c, and a row of zeros for every lane group
   {
-    unsigned long long sum = 0;       // counts may come summed over many ranks
-    for (int e = threadIdx.x; e < E; e += BAL_THREADS) sum += (unsigned)__ldg(p.counts + e);
-    if (sum) atomicAdd(&s_total, sum);
+    unsigned long long sum = 0;                       // counts may come summed over many ranks
+    for (int e = threadIdx.x; e < E; e += BAL_THREADS) {
+      const unsigned c = (unsigned)__ldg(p.counts + e);
+      s_f[e] = (float)c;
+      sum += c;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_count[warp] = sum;
   }
-  __syncthreads();
-  const float per_count = s_total > 0 ? (float)E / (float)s_total : 0.f;
-  for (int e = threadIdx.x; e < E; e += BAL_THREADS) s_f[e] = (float)__ldg(p.counts + e) * per_count;
-  float* s_gate = s_f + ((E + 3) & ~3) + (size_t)(warp * TPW + grp) * ((E + 3) & ~3);
+  float* s_gate = s_f + epad + (size_t)(warp * TPW + grp) * epad;
   if (GATES)
     for (int e = sl; e < E; e += LPT) s_gate[e] = 0.f;
   __syncthreads();
+  unsigned long long total = 0;
+#pragma unroll
+  for (int w = 0; w < BAL_WARPS; ++w) total += s_count[w];
+  const float per_count = total > 0 ? (float)E / (float)total : 0.f;
   float f[NV][VE];
 #pragma unroll
   for (int n = 0; n < NV; ++n)
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
       const int c = (n * LPT + sl) * VE + i;
-      f[n][i] = c < E ? s_f[c] : 0.f;
+      f[n][i] = c < E ? s_f[c] * per_count : 0.f;
     }
   const int n_tok = __ldg(p.n_tokens);
   const float per = n_tok > 0 ? 1.f / (float)n_tok : 0.f;
   const float up = p.dloss ? __ldg(p.dloss) : 1.f;
   const float ka = p.ca * per * up, kz = 2.f * p.cz * per * up;
   float sum_a = 0.f, sum_z = 0.f;
-  const int step = gridDim.x * BAL_WARPS * TPW;
-  for (int t0 = (blockIdx.x * BAL_WARPS + warp) * TPW; t0 < p.T; t0 += step) {
-    const int t = t0 + grp;
-    const bool here = t < p.T;
-    const bool live = here && (p.mask == nullptr || p.mask[t] != 0);
-    const T* row = reinterpret_cast<const T*>(p.logits) + (int64_t)t * p.ld;
+
+  for (; t - grp < p.T; t += step) {                  // the warp's tokens start at t - grp: the same trips for all its lanes
+    const bool here = t < p.T, live = cur.live;
+    const int e = cur.e;
+    const float dg = cur.dg;
     float v[NV][VE];
     float top = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      const int c = (n * LPT + sl) * VE;
-      if (live && c < E) {
-        const Pack<T, VE> q = ld_pack<T, VE>(row + c);
+      const bool in = live && (n * LPT + sl) * VE < E;
 #pragma unroll
-        for (int i = 0; i < VE; ++i) v[n][i] = to_f32(q.v[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VE; ++i) v[n][i] = -INFINITY;
+      for (int i = 0; i < VE; ++i) {
+        v[n][i] = in ? to_f32(cur.q[n].v[i]) : -INFINITY;
+        top = fmaxf(top, v[n][i]);
       }
-#pragma unroll
-      for (int i = 0; i < VE; ++i) top = fmaxf(top, v[n][i]);
     }
+    float s = -INFINITY;                              // GATES: the score of this lane's slot
+    const bool kept = GATES && live && sl < p.k;
+    const bool ok = kept && (unsigned)e < (unsigned)E;
+    if (GATES) {
+      if (ok) s = to_f32(reinterpret_cast<const T*>(p.logits)[t * p.ld + e]);
+      else if (kept && p.status) atomicOr(p.status, STATUS_BAD_INDEX);
+    }
+    load(t + step, cur);
     top = lanes_max<LPT>(top);
-    const float base = top == -INFINITY ? 0.f : top;      // a row without a score: every exp below is 0
+    const bool some = top != -INFINITY;
+    const float base = some ? top : 0.f;              // a row without a score: every exp below is 0
     float z = 0.f, a = 0.f;
 #pragma unroll
     for (int n = 0; n < NV; ++n)
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        v[n][i] = __expf(v[n][i] - base);
+        v[n][i] = exp_of(v[n][i] - base);
         z += v[n][i];
         a += v[n][i] * f[n][i];
       }
     z = lanes_sum<LPT>(z);
     a = lanes_sum<LPT>(a);
-    const bool some = top != -INFINITY;
     const float inv_z = some ? 1.f / z : 0.f;
     const float lse = some ? base + logf(z) : 0.f;
     a *= inv_z;
@@ -216,40 +264,35 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     }
     if (p.dlogits == nullptr) continue;
     if (GATES) {
-      // lane j < k of the group has the token's j-th kept expert (LPT >= k)
-      const bool kept = live && sl < p.k;
-      int e = 0;
-      float s = -INFINITY, dg = 0.f;
-      bool ok = false;
-      if (kept) {
-        const int64_t at = (int64_t)t * p.k + sl;
-        e = p.idx_i32 ? __ldg(reinterpret_cast<const int32_t*>(p.idx) + at) : (int)__ldg(reinterpret_cast<const uint8_t*>(p.idx) + at);
-        ok = (unsigned)e < (unsigned)E;
-        if (ok) {
-          s = to_f32(row[e]);
-          dg = __ldg(p.dgates + at);
-        } else if (p.status) {
-          atomicOr(p.status, STATUS_BAD_INDEX);
-        }
-      }
       float back;
       if (p.sigmoid) {
         // q (1 - q) with 1 - q = 1 / (1 + exp(s)), not by subtraction
-        const float x = __expf(-fabsf(s));
-        back = ok ? x / ((1.f + x) * (1.f + x)) * dg : 0.f;
+        const float x = exp_of(-fabsf(s));
+        back = x / ((1.f + x) * (1.f + x)) * dg;
       } else {
         const float m = lanes_max<LPT>(s);
-        const float q = s == -INFINITY ? 0.f : __expf(s - m);
-        const float qs = lanes_sum<LPT>(q), qd = lanes_sum<LPT>(q * dg);
-        const float inv = qs > 0.f ? 1.f / qs : 0.f;
+        const float q = s == -INFINITY ? 0.f : exp_of(s - m);
+        const float qs = lanes_sum<LPT>(q), qd = lanes_sum<LPT>(ok ? q * dg : 0.f);
+        const float inv = qs > 0.f || qs != qs ? 1.f / qs : 0.f;
         back = q * inv * (dg - qd * inv);
-        if (!ok) back = 0.f;
       }
-      if (ok) atomicAdd(s_gate + e, back);      // of this token alone; a second addend only where an id repeats
+      // The slots' terms meet the row's elements in shared memory.  Where a token names an expert twice (ids folded after the
+      // choice), the first of its slots brings the sum, added up in slot order.
+      const unsigned same = __match_any_sync(0xffffffffu, ok ? (grp << 16) + e : (1 << 30) + lane);
+      if (__any_sync(0xffffffffu, (same & (same - 1)) != 0)) {
+        const float mine = back;
+        back = 0.f;
+        for (int j = 0; j < 32; ++j) {
+          const float other = __shfl_sync(0xffffffffu, mine, j);
+          if (same >> j & 1) back += other;
+        }
+      }
+      if (ok && lane == __ffs(same) - 1) s_gate[e] = back;
       __syncwarp();
     }
-    T* out = reinterpret_cast<T*>(p.dlogits) + (int64_t)t * E;
-    const float shift = kz * lse;
+    T* out = reinterpret_cast<T*>(p.dlogits) + t * E;
+    // p (ka (f - a) + kz lse) = v (k1 f + k0)
+    const float k1 = inv_z * ka, k0 = inv_z * (kz * lse - ka * a);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = (n * LPT + sl) * VE;
@@ -257,16 +300,17 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
         float o[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-          o[i] = live ? v[n][i] * inv_z * (ka * (f[n][i] - a) + shift) : 0.f;
-          if (GATES) {
-            o[i] += s_gate[c + i];
-            s_gate[c + i] = 0.f;
-          }
+          o[i] = live ? v[n][i] * (k1 * f[n][i] + k0) : 0.f;
+          if (GATES) o[i] += s_gate[c + i];
         }
         st_pack<T, VE>(out + c, o);
       }
     }
-    if (GATES) __syncwarp();
+    if (GATES) {
+      __syncwarp();
+      if (ok) s_gate[e] = 0.f;
+      __syncwarp();
+    }
   }
   if (p.loss == nullptr) return;
   let_next_kernel_start();
@@ -330,48 +374,48 @@ cudaError_t count_in_cluster(const Id* idx, int64_t slots, int k, int E, int cop
   return cudaLaunchKernelEx(&cfg, expert_counts_kernel<Id, true>, idx, slots, k, E, copies, mask, counts, n_tokens, status);
 }
 
-template <typename T, int VE, int LPT, int NV, bool GATES>
+template <typename T, int VE, int LPT, int EPL, bool GATES>
 cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
   constexpr int TPB = BAL_WARPS * (32 / LPT);
   const int epad = (p.E + 3) & ~3;
-  const size_t smem = sizeof(float) * epad * (1 + (GATES ? TPB : 0));
+  const size_t smem = sizeof(float) * epad * (1 + (GATES ? TPB : 0));       // at most 37 KB: E <= LPT * EPL
   const int64_t want = ((int64_t)p.T + TPB - 1) / TPB;
   const int cap = current_sms() * BAL_MAX_BLOCKS_PER_SM;
   const int grid = (int)(want < cap ? want : cap);
-  balance_kernel<T, VE, LPT, NV, GATES><<<grid, BAL_THREADS, smem, st>>>(p);
+  balance_kernel<T, VE, LPT, EPL, GATES><<<grid, BAL_THREADS, smem, st>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && p.loss && grid > 1) e = launch_dependent(balance_finish_kernel, dim3(1), dim3(256), 0, st, p, grid);
   return e;
 }
 
-template <typename T, int VE, int LPT, int NV>
+template <typename T, int VE, int LPT, int EPL>
 cudaError_t balance_launch(const BalanceParams& p, cudaStream_t st) {
-  return p.dgates ? balance_launch_g<T, VE, LPT, NV, true>(p, st) : balance_launch_g<T, VE, LPT, NV, false>(p, st);
+  return p.dgates ? balance_launch_g<T, VE, LPT, EPL, true>(p, st) : balance_launch_g<T, VE, LPT, EPL, false>(p, st);
 }
 
-// Lanes a token: as few as hold the row, but one for every kept expert, whose gates they differentiate.  (With or without gates:
-// the sums of a row then run in the same order and the losses are the same bits.)
+template <typename T, int VE, int EPL>
+cudaError_t balance_by_lanes(const BalanceParams& p, int lpt, cudaStream_t st) {
+  switch (lpt) {
+    case 1: return balance_launch<T, VE, 1, EPL>(p, st);
+    case 2: return balance_launch<T, VE, 2, EPL>(p, st);
+    case 4: return balance_launch<T, VE, 4, EPL>(p, st);
+    case 8: return balance_launch<T, VE, 8, EPL>(p, st);
+    case 16: return balance_launch<T, VE, 16, EPL>(p, st);
+    default: return balance_launch<T, VE, 32, EPL>(p, st);
+  }
+}
+
+// Lanes a token: enough for 16 elements each and for one of the kept experts each.  (With or without gates: the sums of a row then
+// run in the same order and the losses are the same bits.)
 template <typename T, int VE>
 cudaError_t balance_by_width(const BalanceParams& p, cudaStream_t st) {
   int lpt = 1;
-  while (lpt < 32 && (lpt * VE < p.E || lpt < p.k)) lpt *= 2;
-  const int nv = (p.E + lpt * VE - 1) / (lpt * VE);
-  switch (lpt) {
-    case 1: return balance_launch<T, VE, 1, 1>(p, st);
-    case 2: return balance_launch<T, VE, 2, 1>(p, st);
-    case 4: return balance_launch<T, VE, 4, 1>(p, st);
-    case 8: return balance_launch<T, VE, 8, 1>(p, st);
-    case 16: return balance_launch<T, VE, 16, 1>(p, st);
-    default: break;
+  while (lpt < 32 && (lpt * 16 < p.E || lpt < p.k)) lpt *= 2;
+  if (lpt * 16 < p.E) return balance_launch<T, VE, 32, 32>(p, st);
+  if constexpr (VE > 1) {
+    if (lpt * 8 >= p.E) return balance_by_lanes<T, VE, 8>(p, lpt, st);
   }
-  if (nv <= 1) return balance_launch<T, VE, 32, 1>(p, st);
-  if (nv <= 2) return balance_launch<T, VE, 32, 2>(p, st);
-  if (nv <= 4) return balance_launch<T, VE, 32, 4>(p, st);
-  if constexpr (VE <= 4) {
-    if (nv <= 8) return balance_launch<T, VE, 32, 8>(p, st);
-  }
-  if constexpr (VE == 1) return nv <= 16 ? balance_launch<T, VE, 32, 16>(p, st) : balance_launch<T, VE, 32, 32>(p, st);
-  return cudaErrorInvalidValue;       // E <= 1024 fits the forms above
+  return balance_by_lanes<T, VE, 16>(p, lpt, st);
 }
 
 }  // namespace
