@@ -6,32 +6,49 @@
 //              dx_tj = rstd_t (g_tj - (1/d) sum_i g_ti - h_tj (1/d) sum_i g_ti h_ti)
 //              dw_j = sum_t dy_tj h_tj       db_j = sum_t dy_tj
 //
-// Both passes touch every element once and are bound by HBM.  A row is held in registers, NORM_EPT elements a thread, by a
-// warp (narrow rows) or a whole block; sums are taken in fp32 from the registers, the variance from the centred values
-// (never as a difference of large sums).  Blocks are resident and walk over the rows, so a thread always sees the same
-// columns: the weights are read once per block, and the backward pass adds up dw and db of its columns in registers and
-// writes one partial row per block, which a second small kernel adds up in a fixed order (bit-reproducible, no atomics).
+// Both passes touch every element once and are bound by HBM, but only if they are lean: at 6.4 TB/s an SM has some 20 (forward)
+// and 30 (backward) instruction slots for an element of bf16, so the arithmetic is done two elements to an instruction (f32x2).
+// Sums are taken in fp32, the variance from the centred values (never as a difference of large sums).
+//   Forward: a row lies in the registers of one warp as it was loaded (up to 256 bytes a lane, eight KB a row in flight), or of
+//     several for wide rows; nothing is kept from row to row.
+//   Backward: the running dw and db of a column have to stay with one thread, so a row is spread over enough threads for 16
+//     elements each; blocks are resident and walk over the rows (the coming ones on their way into shared memory), write one
+//     partial row each, and a second small kernel adds those up in a fixed order (bit-reproducible, no atomics).
+#include <algorithm>
+
 #include "vec.cuh"
 
 namespace grouter {
 
-constexpr int NORM_EPT = 16;            // elements of a row that a thread holds
-constexpr int NORM_MAX_D = 1024 * NORM_EPT;
-constexpr int NORM_WARP_ROWS = 8;       // rows of a block that gives every row one warp
+constexpr int NORM_MAX_D = 16384;
 
-template <int TPR>
-constexpr int norm_threads() { return TPR == 32 ? 32 * NORM_WARP_ROWS : TPR; }
+// VE consecutive weights from column c on (which exist), as f32.
+template <typename W, int VE>
+__device__ __forceinline__ void load_weights(const W* __restrict__ w, int c, float (&f)[VE]) {
+  if constexpr (VE == 1) {
+    f[0] = to_f32(__ldg(w + c));
+  } else {
+    constexpr int PER = VE * sizeof(W) >= 16 ? 16 / (int)sizeof(W) : VE;       // 16- or 8-byte accesses
+#pragma unroll
+    for (int q = 0; q < VE; q += PER) {
+      Pack<W, PER> p;
+      if constexpr (PER * sizeof(W) == 16) *reinterpret_cast<uint4*>(&p) = __ldg(reinterpret_cast<const uint4*>(w + c + q));
+      else *reinterpret_cast<uint2*>(&p) = __ldg(reinterpret_cast<const uint2*>(w + c + q));
+#pragma unroll
+      for (int i = 0; i < PER; ++i) f[q + i] = to_f32(p.v[i]);
+    }
+  }
+}
 
-// Sum over the TPR threads of a row, the same value in each of them.  `red` has two halves used in turn: a warp may still
-// read one while the others already write the next sum into the other, and the barrier in between keeps the third away.
-template <int TPR, int N>
+// Sums of N values over the NW warps of a row, the same value in each of their threads.  `red` has two halves used in turn: a warp
+// may still read one while the others already write the next sums into the other, and the barrier in between keeps the third away.
+template <int NW, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& half) {
 #pragma unroll
   for (int n = 0; n < N; ++n) v[n] = lanes_sum<32>(v[n]);
-  if constexpr (TPR > 32) {
-    constexpr int NW = TPR / 32;
+  if constexpr (NW > 1) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float* buf = red + half * (2 * 32);
+    float* buf = red + half * (N * 32);
     half ^= 1;
     if (lane == 0) {
 #pragma unroll
@@ -43,219 +60,294 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& half) {
   }
 }
 
-// VE consecutive weights from column c on (zeros without weights or beyond d), of either type; in whole 16- or 8-byte
-// accesses where VE > 1, which the host only picks when the weights start on a 16-byte boundary.
-template <int VE>
-__device__ __forceinline__ void load_weights(const void* w, int w_f32, int c, int d, float (&f)[VE]) {
+// Nothing about these registers is known from here on: the compiler converts them again where they are used next, instead of
+// carrying twice as many converted values along (164 registers a thread, where the row as loaded and the arithmetic take half).
+template <typename T, int VE, int NP>
+__device__ __forceinline__ void forget(Pack<T, VE> (&p)[NP]) {
+  if constexpr (VE > 1 && sizeof(T) == 2) {
 #pragma unroll
-  for (int i = 0; i < VE; ++i) f[i] = 0.f;
-  if (w == nullptr || c >= d) return;
-  if (w_f32) {
-    const float* p = reinterpret_cast<const float*>(w) + c;
-    if constexpr (VE == 1) {
-      f[0] = __ldg(p);
-    } else {
+    for (int n = 0; n < NP; ++n) {
+      uint32_t* r = reinterpret_cast<uint32_t*>(&p[n]);
 #pragma unroll
-      for (int q = 0; q < VE; q += 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(p + q));
-        f[q] = v.x;
-        f[q + 1] = v.y;
-        f[q + 2] = v.z;
-        f[q + 3] = v.w;
-      }
-    }
-  } else {
-    const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(w) + c;
-    if constexpr (VE == 1) {
-      f[0] = __bfloat162float(*p);
-    } else {
-#pragma unroll
-      for (int q = 0; q < VE; q += 4) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p + q));
-        const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x));
-        const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
-        f[q] = lo.x;
-        f[q + 1] = lo.y;
-        f[q + 2] = hi.x;
-        f[q + 3] = hi.y;
-      }
+      for (int i = 0; i < VE / 2; ++i) asm volatile("" : "+r"(r[i]));
     }
   }
 }
 
-template <typename T, int VE, int TPR>
-__global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w,
-                                                                           const void* __restrict__ b, int w_f32, int rows, int d, float eps,
-                                                                           T* __restrict__ y, float* __restrict__ mean_out,
-                                                                           float* __restrict__ rstd_out) {
-  constexpr int NV = NORM_EPT / VE;
-  constexpr int RPB = TPR == 32 ? NORM_WARP_ROWS : 1;
-  __shared__ float red[2 * 2 * 32];
-  const int lane = threadIdx.x & (TPR - 1);
-  const int sub = TPR == 32 ? threadIdx.x >> 5 : 0;
-  const float inv_d = 1.f / (float)d;
-  float wv[NV][VE], bv[NV][VE];
+// ---- forward: NW warps a row, NP accesses of VE elements a lane ----
+__host__ __device__ constexpr int norm_forward_threads(int nw) { return nw == 1 ? 128 : 32 * nw; }
+
+template <typename T, typename W, int VE, int NP, int NW>
+__global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(const T* __restrict__ x, int64_t ldx, const W* __restrict__ w,
+                                                                                const W* __restrict__ b, int rows, int d, float eps,
+                                                                                T* __restrict__ y, float* __restrict__ mean_out,
+                                                                                float* __restrict__ rstd_out) {
+  constexpr int RPB = NW == 1 ? norm_forward_threads(1) / 32 : 1;
+  __shared__ float red[2 * 32];
+  const int64_t row = (int64_t)blockIdx.x * RPB + (NW == 1 ? threadIdx.x >> 5 : 0);
+  const int at = NW == 1 ? threadIdx.x & 31 : threadIdx.x;
+  if (row >= rows) return;                 // whole warps, and whole blocks where a row has several
+  const T* xr = x + row * ldx;
+  Pack<T, VE> p[NP];
 #pragma unroll
-  for (int n = 0; n < NV; ++n) {
-    const int c = (n * TPR + lane) * VE;
-    load_weights<VE>(w, w_f32, c, d, wv[n]);
-    load_weights<VE>(b, w_f32, c, d, bv[n]);
+  for (int n = 0; n < NP; ++n) {
+    const int c = (n * (32 * NW) + at) * VE;
+    if (c < d) p[n] = ld_pack<T, VE>(xr + c);
   }
+  const float inv_d = 1.f / (float)d;
   int half = 0;
-  for (int row = blockIdx.x * RPB + sub; row < rows; row += gridDim.x * RPB) {
-    const T* xr = x + (int64_t)row * ldx;
-    float v[NV][VE];
-    float s[1] = {0.f};
+  float s[1] = {0.f};
+  if constexpr (VE > 1) {
+    float2 s2 = both(0.f);
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int c = (n * TPR + lane) * VE;
-      if (c < d) {
-        const Pack<T, VE> p = ld_pack<T, VE>(xr + c);
+    for (int n = 0; n < NP; ++n)
+      if ((n * (32 * NW) + at) * VE < d) {
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          v[n][i] = to_f32(p.v[i]);
-          s[0] += v[n][i];
+        for (int i = 0; i < VE; i += 2) s2 = add2(s2, make_float2(to_f32(p[n].v[i]), to_f32(p[n].v[i + 1])));
+      }
+    s[0] = s2.x + s2.y;
+  } else {
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+      if (n * (32 * NW) + at < d) s[0] += to_f32(p[n].v[0]);
+  }
+  row_sums<NW, 1>(s, red, half);
+  forget<T, VE, NP>(p);
+  const float mean = s[0] * inv_d;
+  float q[1] = {0.f};
+  if constexpr (VE > 1) {
+    float2 q2 = both(0.f);
+    const float2 m2 = both(-mean);
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+      if ((n * (32 * NW) + at) * VE < d) {
+#pragma unroll
+        for (int i = 0; i < VE; i += 2) {
+          const float2 c2 = add2(make_float2(to_f32(p[n].v[i]), to_f32(p[n].v[i + 1])), m2);
+          q2 = fma2(c2, c2, q2);
         }
       }
-    }
-    row_sums<TPR, 1>(s, red, half);
-    const float mean = s[0] * inv_d;
-    float q[1] = {0.f};
+    q[0] = q2.x + q2.y;
+  } else {
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      if ((n * TPR + lane) * VE < d) {
+    for (int n = 0; n < NP; ++n)
+      if (n * (32 * NW) + at < d) {
+        const float c1 = to_f32(p[n].v[0]) - mean;
+        q[0] += c1 * c1;
+      }
+  }
+  row_sums<NW, 1>(q, red, half);
+  forget<T, VE, NP>(p);
+  const float rstd = 1.f / sqrtf(q[0] * inv_d + eps);
+  T* yr = y + row * d;
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          v[n][i] -= mean;
-          q[0] += v[n][i] * v[n][i];
+  for (int n = 0; n < NP; ++n) {
+    const int c = (n * (32 * NW) + at) * VE;
+    if (c < d) {
+      float wl[VE], bl[VE], o[VE];
+      load_weights<W, VE>(w, c, wl);
+      if (b != nullptr) {
+        load_weights<W, VE>(b, c, bl);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) bl[i] = 0.f;
+      }
+      if constexpr (VE > 1) {
+#pragma unroll
+        for (int i = 0; i < VE; i += 2) {
+          const float2 h = mul2(add2(make_float2(to_f32(p[n].v[i]), to_f32(p[n].v[i + 1])), both(-mean)), both(rstd));
+          const float2 v = fma2(h, make_float2(wl[i], wl[i + 1]), make_float2(bl[i], bl[i + 1]));
+          o[i] = v.x;
+          o[i + 1] = v.y;
         }
+      } else {
+        o[0] = (to_f32(p[n].v[0]) - mean) * rstd * wl[0] + bl[0];
       }
+      st_pack<T, VE>(yr + c, o);
     }
-    row_sums<TPR, 1>(q, red, half);
-    const float rstd = 1.f / sqrtf(q[0] * inv_d + eps);
-    T* yr = y + (int64_t)row * d;
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int c = (n * TPR + lane) * VE;
-      if (c < d) {
-        float o[VE];
-#pragma unroll
-        for (int i = 0; i < VE; ++i) o[i] = v[n][i] * rstd * wv[n][i] + bv[n][i];
-        st_pack<T, VE>(yr + c, o);
-      }
-    }
-    if (lane == 0) {
-      if (mean_out) mean_out[row] = mean;
-      if (rstd_out) rstd_out[row] = rstd;
-    }
+  }
+  if (at == 0) {
+    if (mean_out) mean_out[row] = mean;
+    if (rstd_out) rstd_out[row] = rstd;
   }
 }
 
-// WIDE (1024 threads a row, 64 registers each): the running dw and db live in shared memory instead of registers, each
-// thread touching only its own columns, and the weights are read again for every row (they stay in L1 / L2).
-template <typename T, int VE, int TPR>
-__global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t ldx,
-                                                                            const void* __restrict__ w, int w_f32, const float* __restrict__ mean_in,
-                                                                            const float* __restrict__ rstd_in, int rows, int d, T* __restrict__ dx,
-                                                                            float* __restrict__ partial) {
-  constexpr int NV = NORM_EPT / VE;
-  constexpr int RPB = TPR == 32 ? NORM_WARP_ROWS : 1;
-  constexpr bool WIDE = TPR == 1024;
-  extern __shared__ float s_cols[];     // WIDE: [2][NORM_EPT][TPR], a column of it for each thread;  one warp per row: [NORM_WARP_ROWS][32 * NORM_EPT]
+// ---- backward: TPR threads a row, NORM_EPT elements each ----
+constexpr int NORM_EPT = 16;
+constexpr int NORM_WARP_ROWS = 8;       // rows of a block that gives every row one warp
+__host__ __device__ constexpr int norm_backward_threads(int tpr) { return tpr == 32 ? 32 * NORM_WARP_ROWS : tpr; }
+__host__ __device__ constexpr int norm_backward_per_sm(int tpr) { return tpr >= 512 ? 1 : 512 / norm_backward_threads(tpr); }
+// Rows (x and dy) that a block has on their way or in use: what keeps HBM busy (rows held one ahead in registers were 32 KB an SM
+// and 3.6 TB/s).  As many as shared memory takes: an SM holds 512 threads' rows, 1024 for the widest.
+__host__ __device__ constexpr int norm_ring(int bytes, int tpr) { return tpr == 1024 ? (bytes == 2 ? 3 : 1) : bytes == 2 ? 4 : 3; }
+
+__device__ __forceinline__ void copy16_async(void* smem, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Every thread copies its own elements of the coming rows into shared memory and reads back only those, so the ring needs no
+// barrier: the one barrier a row is that of its two sums.  VE = 1 (rows that are not 16-byte aligned): plain loads, no ring.
+template <typename T, typename W, int VE, int TPR>
+__global__ void __launch_bounds__(norm_backward_threads(TPR), norm_backward_per_sm(TPR))
+norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t ldx, const W* __restrict__ w, const float* __restrict__ mean_in,
+                     const float* __restrict__ rstd_in, int rows, int d, T* __restrict__ dx, float* __restrict__ partial) {
+  constexpr int NV = NORM_EPT / VE, PAIRS = NORM_EPT / 2;
+  constexpr int RPB = TPR == 32 ? NORM_WARP_ROWS : 1, THREADS = norm_backward_threads(TPR);
+  constexpr bool RING = VE > 1;
+  constexpr int S = norm_ring(sizeof(T), TPR);
+  constexpr bool HOLD = TPR < 1024;     // the weights stay in registers (1024 threads have 64 each: there they are read from L1)
+  extern __shared__ uint4 s_ring[];     // RING: [S][x, dy][NV][THREADS]
   __shared__ float red[2 * 2 * 32];
+  __shared__ float s_cols[TPR == 32 ? NORM_WARP_ROWS * 32 * NORM_EPT : 1];
   const int lane = threadIdx.x & (TPR - 1);
   const int sub = TPR == 32 ? threadIdx.x >> 5 : 0;
   const float inv_d = 1.f / (float)d;
-  float wv[WIDE ? 1 : NV][VE], aw[WIDE ? 1 : NV][VE], ab[WIDE ? 1 : NV][VE];
-  if constexpr (WIDE) {
-#pragma unroll
-    for (int i = 0; i < 2 * NORM_EPT; ++i) s_cols[i * TPR + lane] = 0.f;
-  } else {
+  // a thread's elements in pairs: pair j holds elements 2j and 2j + 1 of its [NV][VE]; columns beyond d hold zeros throughout
+  auto col = [&](int k) { return ((k / VE) * TPR + lane) * VE + k % VE; };
+  auto weights = [&](float2 (&f)[PAIRS]) {
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      load_weights<VE>(w, w_f32, (n * TPR + lane) * VE, d, wv[n]);
+      float t[VE];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) aw[n][i] = ab[n][i] = 0.f;
+      for (int i = 0; i < VE; ++i) t[i] = 0.f;
+      const int c = (n * TPR + lane) * VE;
+      if (c < d) load_weights<W, VE>(w, c, t);
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const int k = n * VE + i;
+        if (k & 1) f[k / 2].y = t[i];
+        else f[k / 2].x = t[i];
+      }
     }
+  };
+  float2 wv[PAIRS], aw[PAIRS], ab[PAIRS];
+  if constexpr (HOLD) weights(wv);
+#pragma unroll
+  for (int j = 0; j < PAIRS; ++j) aw[j] = ab[j] = both(0.f);
+
+  auto slot = [&](int s, int which, int n) { return s_ring + ((s * 2 + which) * NV + n) * THREADS + threadIdx.x; };
+  auto fetch = [&](int64_t r, int s) {
+    if (r < rows) {
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const int c = (n * TPR + lane) * VE;
+        if (c < d) {
+          copy16_async(slot(s, 0, n), x + r * ldx + c);
+          copy16_async(slot(s, 1, n), dy + r * d + c);
+        }
+      }
+    }
+    copies_commit();
+  };
+  int64_t row = (int64_t)blockIdx.x * RPB + sub;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  float nmean = 0.f, nrstd = 0.f;
+  auto stats = [&](int64_t r) {
+    if (r < rows) {
+      nmean = __ldg(mean_in + r);
+      nrstd = __ldg(rstd_in + r);
+    }
+  };
+  stats(row);
+  if constexpr (RING) {
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if ((n * TPR + lane) * VE >= d)
+        for (int s = 0; s < S; ++s) *slot(s, 0, n) = *slot(s, 1, n) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int s = 0; s < S; ++s) fetch(row + s * step, s);
   }
-  int half = 0;
-  for (int row = blockIdx.x * RPB + sub; row < rows; row += gridDim.x * RPB) {
-    const T* xr = x + (int64_t)row * ldx;
-    const T* gr = dy + (int64_t)row * d;
-    const float mean = __ldg(mean_in + row), rstd = __ldg(rstd_in + row);
+  int half = 0, s_at = 0;
+  for (; row < rows; row += step) {
+    const float mean = nmean, rstd = nrstd;
+    stats(row + step);
     Pack<T, VE> px[NV], pg[NV];
+    auto take = [&]() {                 // this row's elements
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int c = (n * TPR + lane) * VE;
-      if (c < d) {
-        px[n] = ld_pack<T, VE>(xr + c);
-        pg[n] = ld_pack<T, VE>(gr + c);
-      }
-    }
-    float s[2] = {0.f, 0.f};            // sum of g, sum of g h
+      for (int n = 0; n < NV; ++n) {
+        if constexpr (RING) {
+          *reinterpret_cast<uint4*>(&px[n]) = *slot(s_at, 0, n);
+          *reinterpret_cast<uint4*>(&pg[n]) = *slot(s_at, 1, n);
+        } else {
+          const int c = (n * TPR + lane) * VE;
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int c = (n * TPR + lane) * VE;
-      if (c < d) {
-        float wl[VE];
-        if constexpr (WIDE) load_weights<VE>(w, w_f32, c, d, wl);
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          const float g0 = to_f32(pg[n].v[i]), h = (to_f32(px[n].v[i]) - mean) * rstd;
-          if constexpr (WIDE) {
-            s_cols[(n * VE + i) * TPR + lane] += g0 * h;
-            s_cols[(NORM_EPT + n * VE + i) * TPR + lane] += g0;
-          } else {
-            aw[n][i] += g0 * h;
-            ab[n][i] += g0;
-            wl[i] = wv[n][i];
+          for (int i = 0; i < VE; ++i) px[n].v[i] = pg[n].v[i] = from_f32<T>(0.f);
+          if (c < d) {
+            px[n] = ld_pack<T, VE>(x + row * ldx + c);
+            pg[n] = ld_pack<T, VE>(dy + row * d + c);
           }
-          s[0] += g0 * wl[i];
-          s[1] += g0 * wl[i] * h;
         }
       }
+    };
+    auto x_of = [&](int j) { return make_float2(to_f32(px[2 * j / VE].v[2 * j % VE]), to_f32(px[(2 * j + 1) / VE].v[(2 * j + 1) % VE])); };
+    auto g_of = [&](int j) { return make_float2(to_f32(pg[2 * j / VE].v[2 * j % VE]), to_f32(pg[(2 * j + 1) / VE].v[(2 * j + 1) % VE])); };
+    if constexpr (RING) copies_wait<S - 1>();
+    take();
+    if constexpr (!HOLD) weights(wv);
+    float2 s1 = both(0.f), s2 = both(0.f);            // sums of g and of g h
+#pragma unroll
+    for (int j = 0; j < PAIRS; ++j) {
+      const float2 g0 = g_of(j), h = mul2(add2(x_of(j), both(-mean)), both(rstd));
+      aw[j] = fma2(g0, h, aw[j]);
+      ab[j] = add2(ab[j], g0);
+      const float2 g = mul2(g0, wv[j]);
+      s1 = add2(s1, g);
+      s2 = fma2(g, h, s2);
     }
-    row_sums<TPR, 2>(s, red, half);
-    const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
-    T* dr = dx + (int64_t)row * d;
+    float s[2] = {s1.x + s1.y, s2.x + s2.y};
+    row_sums<TPR / 32, 2>(s, red, half);
+    const float2 c1 = both(-s[0] * inv_d), c2 = both(-s[1] * inv_d);
+    if constexpr (!HOLD) {
+      asm volatile("" ::: "memory");                  // read again rather than kept over the sums
+      weights(wv);
+    }
+    if constexpr (RING) {
+      asm volatile("" ::: "memory");
+      take();
+    } else {
+      forget<T, VE, NV>(px);
+      forget<T, VE, NV>(pg);
+    }
+    T* dr = dx + row * d;
+    float o[NORM_EPT];
+#pragma unroll
+    for (int j = 0; j < PAIRS; ++j) {
+      const float2 h = mul2(add2(x_of(j), both(-mean)), both(rstd));
+      const float2 v = mul2(fma2(h, c2, fma2(g_of(j), wv[j], c1)), both(rstd));
+      o[2 * j] = v.x;
+      o[2 * j + 1] = v.y;
+    }
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = (n * TPR + lane) * VE;
       if (c < d) {
-        float wl[VE], o[VE];
-        if constexpr (WIDE) load_weights<VE>(w, w_f32, c, d, wl);
+        float t[VE];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          if constexpr (!WIDE) wl[i] = wv[n][i];
-          const float h = (to_f32(px[n].v[i]) - mean) * rstd;
-          o[i] = rstd * (to_f32(pg[n].v[i]) * wl[i] - c1 - h * c2);
-        }
-        st_pack<T, VE>(dr + c, o);
+        for (int i = 0; i < VE; ++i) t[i] = o[n * VE + i];
+        st_pack<T, VE>(dr + c, t);
       }
+    }
+    if constexpr (RING) {
+      fetch(row + S * step, s_at);
+      s_at = s_at + 1 == S ? 0 : s_at + 1;
     }
   }
   let_next_kernel_start();
   // this block's partial row: [dw | db]
   float* pw = partial + (int64_t)blockIdx.x * 2 * d;
-  if constexpr (WIDE) {
-#pragma unroll
-    for (int n = 0; n < NV; ++n)
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const int c = (n * TPR + lane) * VE + i;
-        if (c < d) {
-          pw[c] = s_cols[(n * VE + i) * TPR + lane];
-          pw[d + c] = s_cols[(NORM_EPT + n * VE + i) * TPR + lane];
-        }
-      }
-  } else if constexpr (TPR == 32) {
+  if constexpr (TPR == 32) {
     constexpr int COLS = 32 * NORM_EPT;
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
-      for (int n = 0; n < NV; ++n)
-#pragma unroll
-        for (int i = 0; i < VE; ++i) s_cols[sub * COLS + (n * 32 + lane) * VE + i] = pass == 0 ? aw[n][i] : ab[n][i];
+      for (int j = 0; j < PAIRS; ++j) {
+        const float2 v = pass == 0 ? aw[j] : ab[j];
+        s_cols[sub * COLS + col(2 * j)] = v.x;
+        s_cols[sub * COLS + col(2 * j + 1)] = v.y;
+      }
       __syncthreads();
       for (int c = threadIdx.x; c < d; c += 32 * NORM_WARP_ROWS) {
         float a = 0.f;
@@ -267,15 +359,16 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
     }
   } else {
 #pragma unroll
-    for (int n = 0; n < NV; ++n)
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const int c = (n * TPR + lane) * VE + i;
-        if (c < d) {
-          pw[c] = aw[n][i];
-          pw[d + c] = ab[n][i];
-        }
+    for (int j = 0; j < PAIRS; ++j) {
+      if (col(2 * j) < d) {
+        pw[col(2 * j)] = aw[j].x;
+        pw[d + col(2 * j)] = ab[j].x;
       }
+      if (col(2 * j + 1) < d) {
+        pw[col(2 * j + 1)] = aw[j].y;
+        pw[d + col(2 * j + 1)] = ab[j].y;
+      }
+    }
   }
 }
 
@@ -289,7 +382,7 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* __restrict_
   float a = 0.f;
   after_previous_kernel();
   if (c < cols) {
-#pragma unroll 8
+#pragma unroll 16
     for (int r = warp; r < n_part; r += 32) a += partial[(int64_t)r * cols + c];
   }
   s[warp][lane] = a;
@@ -319,77 +412,98 @@ struct NormArgs {
   cudaStream_t st;
 };
 
-// Threads that hold a row of d elements.
+// Threads that hold a row of d elements in the backward pass.
 int norm_tpr(int d) {
-  if (d <= 32 * NORM_EPT) return 32;
-  if (d <= 128 * NORM_EPT) return 128;
-  if (d <= 256 * NORM_EPT) return 256;
-  if (d <= 512 * NORM_EPT) return 512;
-  return 1024;
+  int tpr = 32;
+  while (tpr * NORM_EPT < d) tpr *= 2;
+  return tpr;
 }
 
-// Blocks of the backward pass: enough to fill the GPU at the registers the kernels take, and no more than there are
-// rows, since every block leaves a partial row behind.
+// Blocks of the backward pass: enough to fill the GPU, and no more than there are rows, since every block leaves a partial row.
 int norm_backward_blocks(int rows, int d) {
-  const int sms = current_sms();
-  const int tpr = norm_tpr(d);
-  const int rpb = tpr == 32 ? NORM_WARP_ROWS : 1;
-  const int per_sm = tpr <= 128 ? (tpr == 32 ? 2 : 4) : tpr == 256 ? 2 : 1;
-  const int want = (rows + rpb - 1) / rpb;
-  return want < sms * per_sm ? want : sms * per_sm;
+  const int tpr = norm_tpr(d), rpb = tpr == 32 ? NORM_WARP_ROWS : 1;
+  const int want = (rows + rpb - 1) / rpb, cap = current_sms() * norm_backward_per_sm(tpr);
+  return want < cap ? want : cap;
 }
 
-template <typename T, int VE, int TPR>
+template <typename T, typename W, int VE, int NP, int NW>
 cudaError_t forward_launch(const NormArgs& a) {
-  constexpr int RPB = TPR == 32 ? NORM_WARP_ROWS : 1;
-  const int per_sm = 2048 / norm_threads<TPR>();
-  const int want = (a.rows + RPB - 1) / RPB, cap = current_sms() * per_sm;
-  norm_forward_kernel<T, VE, TPR><<<want < cap ? want : cap, norm_threads<TPR>(), 0, a.st>>>(
-      static_cast<const T*>(a.x), a.ldx, a.w, a.b, a.w_f32, a.rows, a.d, a.eps, static_cast<T*>(a.y), a.mean_out, a.rstd_out);
+  constexpr int RPB = NW == 1 ? norm_forward_threads(1) / 32 : 1;
+  norm_forward_kernel<T, W, VE, NP, NW><<<(a.rows + RPB - 1) / RPB, norm_forward_threads(NW), 0, a.st>>>(
+      static_cast<const T*>(a.x), a.ldx, static_cast<const W*>(a.w), static_cast<const W*>(a.b), a.rows, a.d, a.eps, static_cast<T*>(a.y), a.mean_out,
+      a.rstd_out);
   return cudaGetLastError();
 }
 
-template <typename T, int VE, int TPR>
+// One warp a row while its lanes hold it in at most 16 accesses each, then as many warps as that takes.
+template <typename T, typename W, int VE>
+cudaError_t forward_by_width(const NormArgs& a) {
+  const int per_lane = (a.d + 32 * VE - 1) / (32 * VE);
+  if (per_lane <= 1) return forward_launch<T, W, VE, 1, 1>(a);
+  if (per_lane <= 2) return forward_launch<T, W, VE, 2, 1>(a);
+  if (per_lane <= 4) return forward_launch<T, W, VE, 4, 1>(a);
+  if (per_lane <= 8) return forward_launch<T, W, VE, 8, 1>(a);
+  if (per_lane <= 16) return forward_launch<T, W, VE, 16, 1>(a);
+  if (per_lane <= 32) return forward_launch<T, W, VE, 16, 2>(a);
+  if (per_lane <= 64) return forward_launch<T, W, VE, 16, 4>(a);
+  if constexpr (VE < 8) {      // 16384 elements in 64 accesses of eight
+    if (per_lane <= 128) return forward_launch<T, W, VE, 16, 8>(a);
+  }
+  if constexpr (VE == 1) return per_lane <= 256 ? forward_launch<T, W, VE, 16, 16>(a) : forward_launch<T, W, VE, 16, 32>(a);
+  return cudaErrorInvalidValue;
+}
+
+template <typename T, typename W, int VE, int TPR>
 cudaError_t backward_launch(const NormArgs& a) {
   const int nblk = norm_backward_blocks(a.rows, a.d);
-  const size_t smem = TPR == 1024 ? sizeof(float) * 2 * NORM_EPT * TPR : TPR == 32 ? sizeof(float) * NORM_WARP_ROWS * 32 * NORM_EPT : 0;
-  auto kern = norm_backward_kernel<T, VE, TPR>;
-  if (TPR == 1024) {      // up to 128 KB: the opt-in is a per-device setting
+  constexpr int threads = norm_backward_threads(TPR), smem = VE > 1 ? norm_ring(sizeof(T), TPR) * 2 * (NORM_EPT / VE) * threads * 16 : 0;
+  auto kern = norm_backward_kernel<T, W, VE, TPR>;
+  if (smem > 0) {      // up to 192 KB: the opt-in is a per-device setting
     static bool configured[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64 || !configured[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e != cudaSuccess) return e;
       if (dev >= 0 && dev < 64) configured[dev] = true;
     }
   }
-  kern<<<nblk, norm_threads<TPR>(), smem, a.st>>>(static_cast<const T*>(a.dy), static_cast<const T*>(a.x), a.ldx, a.w, a.w_f32, a.mean_in,
-                                                  a.rstd_in, a.rows, a.d, static_cast<T*>(a.dx), a.partial);
+  kern<<<nblk, threads, smem, a.st>>>(static_cast<const T*>(a.dy), static_cast<const T*>(a.x), a.ldx, static_cast<const W*>(a.w), a.mean_in,
+                                      a.rstd_in, a.rows, a.d, static_cast<T*>(a.dx), a.partial);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   return launch_sum_rows(a.partial, nblk, 2 * a.d, a.dw, a.d, a.db, a.st);
 }
 
-template <typename T, int VE, bool BACKWARD>
-cudaError_t norm_by_width(const NormArgs& a) {
+template <typename T, typename W, int VE>
+cudaError_t backward_by_width(const NormArgs& a) {
   switch (norm_tpr(a.d)) {
-    case 32: return BACKWARD ? backward_launch<T, VE, 32>(a) : forward_launch<T, VE, 32>(a);
-    case 128: return BACKWARD ? backward_launch<T, VE, 128>(a) : forward_launch<T, VE, 128>(a);
-    case 256: return BACKWARD ? backward_launch<T, VE, 256>(a) : forward_launch<T, VE, 256>(a);
-    case 512: return BACKWARD ? backward_launch<T, VE, 512>(a) : forward_launch<T, VE, 512>(a);
-    default: return BACKWARD ? backward_launch<T, VE, 1024>(a) : forward_launch<T, VE, 1024>(a);
+    case 32: return backward_launch<T, W, VE, 32>(a);
+    case 64: return backward_launch<T, W, VE, 64>(a);
+    case 128: return backward_launch<T, W, VE, 128>(a);
+    case 256: return backward_launch<T, W, VE, 256>(a);
+    case 512: return backward_launch<T, W, VE, 512>(a);
+    default: return backward_launch<T, W, VE, 1024>(a);
   }
 }
 
-// 16-byte accesses where every row of every activation and the weights start on a 16-byte boundary, single elements otherwise.
+template <bool BACKWARD, typename T, typename W, int VE>
+cudaError_t norm_by_width(const NormArgs& a) {
+  if constexpr (BACKWARD) return backward_by_width<T, W, VE>(a);
+  else return forward_by_width<T, W, VE>(a);
+}
+template <bool BACKWARD, typename T>
+cudaError_t norm_by_type(const NormArgs& a) {
+  // 16-byte accesses where every row of every activation and the weights start on a 16-byte boundary, single elements otherwise
+  constexpr int VE = vec16<T>();
+  const bool vec = a.d % VE == 0 && a.ldx % VE == 0 && aligned_to(a.x, 16) && aligned_to(BACKWARD ? a.dy : a.y, 16) &&
+                   (!BACKWARD || aligned_to(a.dx, 16)) && aligned_to(a.w, 16) && aligned_to(a.b, 16);
+  if (a.w_f32) return vec ? norm_by_width<BACKWARD, T, float, VE>(a) : norm_by_width<BACKWARD, T, float, 1>(a);
+  return vec ? norm_by_width<BACKWARD, T, __nv_bfloat16, VE>(a) : norm_by_width<BACKWARD, T, __nv_bfloat16, 1>(a);
+}
 template <bool BACKWARD>
 cudaError_t norm_dispatch(const NormArgs& a, int dtype) {
-  const int ve = dtype == GROUTER_F32 ? vec16<float>() : vec16<__nv_bfloat16>();
-  const bool vec = a.d % ve == 0 && a.ldx % ve == 0 && aligned_to(a.x, 16) && aligned_to(BACKWARD ? a.dy : a.y, 16) &&
-                   (!BACKWARD || aligned_to(a.dx, 16)) && aligned_to(a.w, 16) && aligned_to(a.b, 16);
-  if (dtype == GROUTER_F32) return vec ? norm_by_width<float, vec16<float>(), BACKWARD>(a) : norm_by_width<float, 1, BACKWARD>(a);
-  return vec ? norm_by_width<__nv_bfloat16, vec16<__nv_bfloat16>(), BACKWARD>(a) : norm_by_width<__nv_bfloat16, 1, BACKWARD>(a);
+  return dtype == GROUTER_F32 ? norm_by_type<BACKWARD, float>(a) : norm_by_type<BACKWARD, __nv_bfloat16>(a);
 }
 
 int norm_check(int32_t rows, int32_t d, int64_t ldx, int32_t dtype, int32_t w_dtype) {
@@ -422,7 +536,7 @@ int grouter_layernorm_fwd(const void* x, int64_t ldx, const void* w, const void*
 
 size_t grouter_layernorm_bwd_workspace_bytes(int32_t rows, int32_t d) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
-  return (size_t)(rows ? norm_backward_blocks(rows, d) : 1) * 2 * d * sizeof(float);
+  return (size_t)std::max(norm_backward_blocks(rows, d), 1) * 2 * d * sizeof(float);
 }
 
 int grouter_layernorm_bwd(const void* dy, const void* x, int64_t ldx, const void* w, const float* mean, const float* rstd, int32_t rows,
