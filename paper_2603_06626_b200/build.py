@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libgrouter.so")
 LIB_DEBUG = os.path.join(PKG, "libgrouter_debug.so")
-SOURCES = ["api.cu", "plan.cu", "permute.cu", "gemm.cu", "route.cu", "stats.cu", "ep.cu", "norm.cu", "balance.cu", "linear.cu", "adamw.cu"]
+SOURCES = ["api.cu", "plan.cu", "permute.cu", "gemm.cu", "route.cu", "stats.cu", "ep.cu", "norm.cu", "balance.cu", "linear.cu", "linear_small.cu", "adamw.cu"]
 
 
 def _newest_source_mtime() -> float:

@@ -201,5 +201,8 @@ struct LinearGemm {
   int32_t* status;
 };
 cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st);
+// The same product for few rows of A (tokens; K-major): the contraction cut over a cluster of `splits` CTAs (linear_small_splits).
+int linear_small_splits(int T, int N, int K);
+cudaError_t launch_linear_small(const LinearGemm& g, int splits, cudaStream_t st);
 
 }  // namespace grouter

@@ -18,10 +18,12 @@ constexpr int DZ_THREADS = 256;
 constexpr int DZ_COLS = 256;            // columns of a block: 32 threads of 8
 constexpr int DZ_LANES = DZ_THREADS * 8 / DZ_COLS;      // rows it works on at a time
 
-// dz = dy act'(z) (WRITE), and the column sums of this block's rows (SUM) as row blockIdx.y of `partial` [gridDim.y][N].
+// dz = dy act'(z) (WRITE), and the column sums of this block's rows (SUM) as row blockIdx.y of `partial` [gridDim.y][N].  A thread has
+// DZ_AHEAD rows' loads on their way at a time.
 template <int ACT, bool WRITE, bool SUM>
 __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat16* __restrict__ dy, const __nv_bfloat16* __restrict__ z, int T,
                                                                int N, __nv_bfloat16* __restrict__ dz, float* __restrict__ partial) {
+  constexpr int DZ_AHEAD = 4;
   __shared__ float s_sum[SUM ? DZ_LANES : 1][DZ_COLS + 1];
   const int ct = threadIdx.x & 31, rl = threadIdx.x >> 5;
   const int c = blockIdx.x * DZ_COLS + ct * 8;
@@ -29,21 +31,31 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
   if (c < N) {
-#pragma unroll 2
-    for (int64_t t = (int64_t)blockIdx.y * DZ_LANES + rl; t < T; t += (int64_t)gridDim.y * DZ_LANES) {
-      const int64_t at = t * N + c;
-      const Pack<__nv_bfloat16, 8> g = ld_pack<__nv_bfloat16, 8>(dy + at);
-      float v[8];
+    const int64_t step = (int64_t)gridDim.y * DZ_LANES;
+    for (int64_t t0 = (int64_t)blockIdx.y * DZ_LANES + rl; t0 < T; t0 += step * DZ_AHEAD) {
+      Pack<__nv_bfloat16, 8> g[DZ_AHEAD], q[DZ_AHEAD];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = to_f32(g.v[i]);
-      if (ACT != GROUTER_ACT_NONE) {
-        const Pack<__nv_bfloat16, 8> p = ld_pack<__nv_bfloat16, 8>(z + at);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= act_slope<ACT>(to_f32(p.v[i]));
+      for (int u = 0; u < DZ_AHEAD; ++u) {
+        const int64_t t = t0 + u * step;
+        if (t < T) {
+          g[u] = ld_pack<__nv_bfloat16, 8>(dy + t * N + c);
+          if (ACT != GROUTER_ACT_NONE) q[u] = ld_pack<__nv_bfloat16, 8>(z + t * N + c);
+        }
       }
-      if (WRITE) st_pack<__nv_bfloat16, 8>(dz + at, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+      for (int u = 0; u < DZ_AHEAD; ++u) {
+        const int64_t t = t0 + u * step;
+        if (t < T) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            v[i] = to_f32(g[u].v[i]);
+            if (ACT != GROUTER_ACT_NONE) v[i] *= act_slope<ACT>(to_f32(q[u].v[i]));
+            if (SUM) acc[i] += v[i];
+          }
+          if (WRITE) st_pack<__nv_bfloat16, 8>(dz + t * N + c, v);
+        }
+      }
     }
   }
   if constexpr (SUM) {
@@ -148,6 +160,20 @@ cudaError_t launch_dz(int act, const void* dy, const void* z, int T, int N, void
   }
 }
 
+// y or dx: the CTA-pair core, or the kernel for few tokens.  Both sides in rounds of the machine times 64-deep steps a round,
+// measured over T = 1 .. 4096 and weights of 128 x 128 to 4096 x 4096: a step takes 0.33 us on 256 x 256 tiles (5.7 us around them)
+// and 0.45 us on two 128 x 128 tiles an SM (7.5 us around them, and as much again for every further round); up to 64 tokens the
+// tiles are narrower and their kernel ahead throughout (one token, 4096 x 4096: 9.2 against 38 us; 128 tokens, 512 -> 4096: 9.8
+// against 8.9; 512 tokens, 4096 x 4096: 23.5 against 26.8; 1024: 34.5 against 28.4).
+cudaError_t launch_product(const LinearGemm& g, cudaStream_t st) {
+  const int sms = current_sms(), splits = linear_small_splits(g.M, g.N, g.K), steps = cdiv(g.K, 64);
+  const int big_rounds = cdiv((int64_t)cdiv(g.M, 256) * cdiv(g.N, 256), sms / 2 > 0 ? sms / 2 : 1);
+  const int small_rounds = cdiv((int64_t)cdiv(g.M, 128) * cdiv(g.N, 128) * splits, 2 * sms > 0 ? 2 * sms : 1);
+  const float big = 5.7f + 0.33f * big_rounds * steps, small = small_rounds * (7.5f + 0.45f * cdiv(steps, splits));
+  if (g.M <= 64 || small < big) return launch_linear_small(g, splits, st);
+  return launch_linear_gemm(g, st);
+}
+
 int linear_check(int32_t T, int32_t K, int32_t N, int32_t act) {
   if (T < 0 || K < 1 || N < 1 || act < GROUTER_ACT_NONE || act > GROUTER_ACT_GELU) return GROUTER_ERR_INVALID_ARG;
   if (K % 8 || N % 8 || T > INT32_MAX - 256 || K > INT32_MAX - 256 || N > INT32_MAX - 256) return GROUTER_ERR_UNSUPPORTED;
@@ -172,7 +198,7 @@ int grouter_linear_fwd(const void* x, const void* W, const void* bias, const voi
   LinearGemm g{};
   g.A = x; g.B = W; g.bias = bias; g.residual = residual; g.C = y; g.pre = pre;
   g.M = T; g.N = N; g.K = K; g.act = act; g.status = status;
-  return launch_linear_gemm(g, static_cast<cudaStream_t>(stream)) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+  return launch_product(g, static_cast<cudaStream_t>(stream)) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
 size_t grouter_linear_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N, int32_t act) {
@@ -206,7 +232,7 @@ int grouter_linear_bwd(const void* dy, const void* x, const void* W, const void*
   if (dx) {
     LinearGemm g{};
     g.A = dz; g.B = W; g.b_mn = 1; g.C = dx; g.M = T; g.N = K; g.K = N; g.act = GROUTER_ACT_NONE; g.status = status;
-    if (launch_linear_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (launch_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   if (dW) {
     const int pieces = dw_pieces(T, K, N);
