@@ -225,9 +225,10 @@ int grouter_linear_bwd(const void* dy, const void* x, const void* W, const void*
   const void* dz = act == GROUTER_ACT_NONE ? dy : ws + w.dz;
   if (act != GROUTER_ACT_NONE || db) {
     const int rb = dz_row_blocks(T, N);
-    float* partial = db ? reinterpret_cast<float*>(ws + w.sums) : nullptr;
+    // a single block of rows leaves the sums themselves
+    float* partial = db ? (rb == 1 ? db : reinterpret_cast<float*>(ws + w.sums)) : nullptr;
     if (launch_dz(act, dy, pre, T, N, ws + w.dz, partial, rb, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-    if (db && launch_sum_rows(partial, rb, N, db, N, nullptr, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (db && rb > 1 && launch_sum_rows(partial, rb, N, db, N, nullptr, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   if (dx) {
     LinearGemm g{};
