@@ -132,57 +132,101 @@ __device__ __forceinline__ void write_loss(const BalanceParams& p, double a, dou
   p.loss[2] = zl;
 }
 
-// exp(d) of a difference of scores; results below the normal range of f32 are zero
-__device__ __forceinline__ float exp_of(float d) {
+// 2^d; results below the normal range of f32 are zero
+__device__ __forceinline__ float exp2_of(float d) {
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d * 1.4426950408889634f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  return r;
+}
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * 1.4426950408889634f); }
+// the largest of three (a NaN only if all are)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
+// Rounds whose scores a thread has on their way or in use: 128 to 192 bytes of them.
+__host__ __device__ constexpr int balance_ring(int bytes, int epl) { return bytes * epl >= 64 ? (bytes * epl >= 128 ? 2 : 3) : bytes * epl >= 32 ? 4 : 6; }
+
 // LPT neighbouring lanes hold a token's row, EPL elements each, VE to an access.  Few lanes and many elements: the three
 // reductions over a row cost log2(LPT) shuffles each for a whole warp's 32 / LPT tokens, which is what bounded one warp a token
-// (326 instructions a token of 256 scores).  A token's loads are issued one round before they are used.
-// Dynamic shared memory: f [E], then (with dgates) one row of E sums for every lane group, zero between tokens.
+// (326 instructions a token of 256 scores).  The arithmetic is done two elements to an instruction where there is one for it.
+// Blocks are resident and walk over the tokens; the scores of the next rounds are on their way into shared memory (one round ahead
+// in registers was 24 KB an SM and 3.8 TB/s), every thread copying and reading back its own, so that no barrier is needed.
+// Dynamic shared memory: that ring, f [E], then (with dgates) one row of E sums for every lane group, zero between tokens.
 template <typename T, int VE, int LPT, int EPL, bool GATES>
 __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParams p) {
-  extern __shared__ float s_f[];
+  constexpr bool RING = VE > 1;                       // rows that are not 16-byte aligned: plain loads, one round ahead
+  constexpr int S = balance_ring(sizeof(T), EPL);
+  extern __shared__ uint4 s_ring[];                   // RING: [S][NV][BAL_THREADS]
+  float* s_f = reinterpret_cast<float*>(s_ring + (RING ? S * (EPL / VE) * BAL_THREADS : 0));
   __shared__ double s_part[2][BAL_WARPS];
   __shared__ unsigned long long s_count[BAL_WARPS];
-  constexpr int NV = EPL / VE;
+  constexpr int NV = EPL / VE, PAIRS = EPL / 2;
   constexpr int TPW = 32 / LPT;                       // tokens a warp works on at a time
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sl = lane & (LPT - 1), grp = lane / LPT;
   const int E = p.E, epad = (E + 3) & ~3;
 
-  struct Row {                                        // what a lane needs of its token, as loaded
-    Pack<T, VE> q[NV];
-    int e;                                            // GATES: expert of the token's sl-th slot, and its gate's gradient
+  // Columns beyond E are never loaded and stay -inf: p = 0.  What a masked token's row holds is computed along and dropped.
+  Pack<T, VE> q[NV];
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+#pragma unroll
+    for (int i = 0; i < VE; ++i) q[n].v[i] = from_f32<T>(-INFINITY);
+  auto slot = [&](int s, int n) { return s_ring + (s * NV + n) * BAL_THREADS + threadIdx.x; };
+  auto fetch = [&](int64_t t, int s) {
+    if (t < p.T) {
+      const T* row = reinterpret_cast<const T*>(p.logits) + t * p.ld;
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const int c = (n * LPT + sl) * VE;
+        if (c < E) {
+          if constexpr (RING) copy16_async(slot(s, n), row + c);
+          else q[n] = ld_pack<T, VE>(row + c);
+        }
+      }
+    }
+    if constexpr (RING) copies_commit();
+  };
+  // What else a lane needs of its token: whether it counts, and (GATES, lane j < k of the group: LPT >= k) its j-th kept expert with
+  // the gradient of its gate, two rounds ahead, and that expert's score one round ahead.
+  struct Side {
+    int e;
     float dg;
     bool live;
   };
-  auto load = [&](int64_t t, Row& r) {
-    r.live = t < p.T;
-    r.e = -1;
-    r.dg = 0.f;
-    if (!r.live) return;
-    const T* row = reinterpret_cast<const T*>(p.logits) + t * p.ld;
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int c = (n * LPT + sl) * VE;
-      if (c < E) r.q[n] = ld_pack<T, VE>(row + c);
-    }
-    if (GATES && sl < p.k) {                          // LPT >= k
+  auto side = [&](int64_t t) {
+    Side r{-1, 0.f, t < p.T};
+    if (!r.live) return r;
+    if (GATES && sl < p.k) {
       const int64_t at = t * p.k + sl;
       r.e = p.idx_i32 ? __ldg(reinterpret_cast<const int32_t*>(p.idx) + at) : (int)__ldg(reinterpret_cast<const uint8_t*>(p.idx) + at);
       r.dg = __ldg(p.dgates + at);
     }
     if (p.mask != nullptr) r.live = __ldg(p.mask + t) != 0;
+    return r;
+  };
+  auto score = [&](int64_t t, const Side& r) {
+    return GATES && r.live && sl < p.k && (unsigned)r.e < (unsigned)E ? to_f32(reinterpret_cast<const T*>(p.logits)[t * p.ld + r.e]) : -INFINITY;
   };
 
   const int64_t step = (int64_t)gridDim.x * BAL_WARPS * TPW;
   int64_t t = ((int64_t)blockIdx.x * BAL_WARPS + warp) * TPW + grp;
-  Row cur;
-  load(t, cur);                                       // on its way while the shares are worked out
+  if constexpr (RING) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        if ((n * LPT + sl) * VE >= E) *reinterpret_cast<Pack<T, VE>*>(slot(s, n)) = q[n];
+      fetch(t + s * step, s);
+    }
+  } else {
+    fetch(t, 0);
+  }
+  Side next = side(t), after = side(t + step);
+  float next_s = score(t, next);
 
   // f_e = E c_e / sum c, and a row of zeros for every lane group
   {
@@ -204,55 +248,61 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
 #pragma unroll
   for (int w = 0; w < BAL_WARPS; ++w) total += s_count[w];
   const float per_count = total > 0 ? (float)E / (float)total : 0.f;
-  float f[NV][VE];
+  // a lane's elements in pairs: pair j holds elements 2j and 2j + 1 of its [NV][VE]
+  auto col = [&](int k) { return ((k / VE) * LPT + sl) * VE + k % VE; };
+  float2 f[PAIRS];
 #pragma unroll
-  for (int n = 0; n < NV; ++n)
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const int c = (n * LPT + sl) * VE + i;
-      f[n][i] = c < E ? s_f[c] * per_count : 0.f;
-    }
+  for (int j = 0; j < PAIRS; ++j) {
+    f[j].x = col(2 * j) < E ? s_f[col(2 * j)] * per_count : 0.f;
+    f[j].y = col(2 * j + 1) < E ? s_f[col(2 * j + 1)] * per_count : 0.f;
+  }
   const int n_tok = __ldg(p.n_tokens);
   const float per = n_tok > 0 ? 1.f / (float)n_tok : 0.f;
   const float up = p.dloss ? __ldg(p.dloss) : 1.f;
   const float ka = p.ca * per * up, kz = 2.f * p.cz * per * up;
   float sum_a = 0.f, sum_z = 0.f;
 
+  int s_at = 0;
   for (; t - grp < p.T; t += step) {                  // the warp's tokens start at t - grp: the same trips for all its lanes
-    const bool here = t < p.T, live = cur.live;
-    const int e = cur.e;
-    const float dg = cur.dg;
-    float v[NV][VE];
+    const bool here = t < p.T, live = next.live;
+    const int e = next.e;
+    const float dg = next.dg, s = next_s;             // GATES: of this lane's slot
+    next = after;
+    next_s = score(t + step, next);
+    after = side(t + 2 * step);
+    if constexpr (RING) {
+      copies_wait<S - 1>();
+#pragma unroll
+      for (int n = 0; n < NV; ++n) *reinterpret_cast<uint4*>(&q[n]) = *slot(s_at, n);
+    }
+    float2 v[PAIRS];
+#pragma unroll
+    for (int j = 0; j < PAIRS; ++j)
+      v[j] = make_float2(to_f32(q[2 * j / VE].v[2 * j % VE]), to_f32(q[(2 * j + 1) / VE].v[(2 * j + 1) % VE]));
+    if constexpr (!RING) fetch(t + step, 0);
     float top = -INFINITY;
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const bool in = live && (n * LPT + sl) * VE < E;
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        v[n][i] = in ? to_f32(cur.q[n].v[i]) : -INFINITY;
-        top = fmaxf(top, v[n][i]);
-      }
-    }
-    float s = -INFINITY;                              // GATES: the score of this lane's slot
+    for (int j = 0; j < PAIRS; ++j) top = max3(top, v[j].x, v[j].y);
     const bool kept = GATES && live && sl < p.k;
     const bool ok = kept && (unsigned)e < (unsigned)E;
-    if (GATES) {
-      if (ok) s = to_f32(reinterpret_cast<const T*>(p.logits)[t * p.ld + e]);
-      else if (kept && p.status) atomicOr(p.status, STATUS_BAD_INDEX);
-    }
-    load(t + step, cur);
+    if (GATES && kept && !ok && p.status) atomicOr(p.status, STATUS_BAD_INDEX);
     top = lanes_max<LPT>(top);
     const bool some = top != -INFINITY;
     const float base = some ? top : 0.f;              // a row without a score: every exp below is 0
-    float z = 0.f, a = 0.f;
+    float2 z2 = both(0.f), a2 = both(0.f);
 #pragma unroll
-    for (int n = 0; n < NV; ++n)
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        v[n][i] = exp_of(v[n][i] - base);
-        z += v[n][i];
-        a += v[n][i] * f[n][i];
-      }
+    for (int j = 0; j < PAIRS; ++j) {
+      // the difference first: its rounding is relative to it, and scores of any size stay in range
+      const float2 d = mul2(add2(v[j], both(-base)), both(1.4426950408889634f));
+      v[j] = make_float2(exp2_of(d.x), exp2_of(d.y));
+      z2 = add2(z2, v[j]);
+      a2 = fma2(v[j], f[j], a2);
+    }
+    float z = z2.x + z2.y, a = a2.x + a2.y;
+    if constexpr (RING) {                             // the slot has been read: v comes from it
+      fetch(t + S * step, s_at);
+      s_at = s_at + 1 == S ? 0 : s_at + 1;
+    }
     z = lanes_sum<LPT>(z);
     a = lanes_sum<LPT>(a);
     const float inv_z = some ? 1.f / z : 0.f;
@@ -292,18 +342,32 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     }
     T* out = reinterpret_cast<T*>(p.dlogits) + t * E;
     // p (ka (f - a) + kz lse) = v (k1 f + k0)
-    const float k1 = inv_z * ka, k0 = inv_z * (kz * lse - ka * a);
+    const float2 k1 = both(inv_z * ka), k0 = both(inv_z * (kz * lse - ka * a));
+    float o[EPL];
+#pragma unroll
+    for (int j = 0; j < PAIRS; ++j) {
+      const float2 d = mul2(v[j], fma2(k1, f[j], k0));
+      o[2 * j] = d.x;
+      o[2 * j + 1] = d.y;
+    }
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = (n * LPT + sl) * VE;
       if (here && c < E) {
-        float o[VE];
+        float w[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-          o[i] = live ? v[n][i] * (k1 * f[n][i] + k0) : 0.f;
-          if (GATES) o[i] += s_gate[c + i];
+          w[i] = o[n * VE + i];
+          if (GATES) w[i] += s_gate[c + i];
         }
-        st_pack<T, VE>(out + c, o);
+        Pack<T, VE> r;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(w[i]);
+        if (!live) {
+#pragma unroll
+          for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(0.f);
+        }
+        *reinterpret_cast<Pack<T, VE>*>(out + c) = r;
       }
     }
     if (GATES) {
@@ -378,11 +442,25 @@ template <typename T, int VE, int LPT, int EPL, bool GATES>
 cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
   constexpr int TPB = BAL_WARPS * (32 / LPT);
   const int epad = (p.E + 3) & ~3;
-  const size_t smem = sizeof(float) * epad * (1 + (GATES ? TPB : 0));       // at most 37 KB: E <= LPT * EPL
+  constexpr int RING = VE > 1 ? balance_ring(sizeof(T), EPL) * EPL * (int)sizeof(T) * BAL_THREADS : 0;      // at most 64 KB
+  constexpr int MAX_SMEM = RING + (int)sizeof(float) * LPT * EPL * (1 + (GATES ? TPB : 0));                // E <= LPT * EPL: 37 KB more
+  const size_t smem = RING + sizeof(float) * epad * (1 + (GATES ? TPB : 0));
+  auto kern = balance_kernel<T, VE, LPT, EPL, GATES>;
   const int64_t want = ((int64_t)p.T + TPB - 1) / TPB;
-  const int cap = current_sms() * BAL_MAX_BLOCKS_PER_SM;
+  static int resident[64] = {};       // blocks an SM holds, which is what walks over the tokens; asked once per device
+  int dev = 0, per_sm = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 0 && dev < 64) per_sm = resident[dev];
+  if (per_sm == 0) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, BAL_THREADS, MAX_SMEM);
+    if (e != cudaSuccess) return e;
+    per_sm = per_sm < 1 ? 1 : per_sm > BAL_MAX_BLOCKS_PER_SM ? BAL_MAX_BLOCKS_PER_SM : per_sm;
+    if (dev >= 0 && dev < 64) resident[dev] = per_sm;
+  }
+  const int cap = current_sms() * per_sm;
   const int grid = (int)(want < cap ? want : cap);
-  balance_kernel<T, VE, LPT, EPL, GATES><<<grid, BAL_THREADS, smem, st>>>(p);
+  kern<<<grid, BAL_THREADS, smem, st>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && p.loss && grid > 1) e = launch_dependent(balance_finish_kernel, dim3(1), dim3(256), 0, st, p, grid);
   return e;

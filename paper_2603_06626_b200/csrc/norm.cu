@@ -181,13 +181,6 @@ __host__ __device__ constexpr int norm_backward_per_sm(int tpr) { return tpr >= 
 // and 3.6 TB/s).  As many as shared memory takes: an SM holds 512 threads' rows, 1024 for the widest.
 __host__ __device__ constexpr int norm_ring(int bytes, int tpr) { return tpr == 1024 ? (bytes == 2 ? 3 : 1) : bytes == 2 ? 4 : 3; }
 
-__device__ __forceinline__ void copy16_async(void* smem, const void* global) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // Every thread copies its own elements of the coming rows into shared memory and reads back only those, so the ring needs no
 // barrier: the one barrier a row is that of its two sums.  VE = 1 (rows that are not 16-byte aligned): plain loads, no ring.
 template <typename T, typename W, int VE, int TPR>

@@ -65,6 +65,14 @@ __device__ __forceinline__ uint4 ld_stream16(const void* p) {
   return v;
 }
 
+// Asynchronous copies of 16 bytes from global to shared memory, in groups of the issuing thread.
+__device__ __forceinline__ void copy16_async(void* smem, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 template <typename T, int VE>
 __device__ __forceinline__ Pack<T, VE> ld_pack(const T* p) {
   Pack<T, VE> r;
