@@ -519,8 +519,10 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     return y, mean, rstd
 
 
-def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, want_bias: bool = True):
-    """grouter_layernorm_bwd, from the forward's mean and rstd -> (dx like x, dw f32 [d], db f32 [d] or None)."""
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, want_bias: bool = True,
+                        dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None):
+    """grouter_layernorm_bwd, from the forward's mean and rstd -> (dx like x, dw f32 [d], db f32 [d] or None).  dw, db: tensors to
+    write the gradients into, e.g. those an AdamW object reads."""
     lib = load_library()
     ldx = _row_stride("x", x)
     T, d = x.shape
@@ -530,9 +532,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     _expect("rstd", rstd, (T,), torch.float32, like=x)
     dt, wt = _elt(x, "x"), _elt(weight, "weight")
     dev = _device_index(x.device)
+    _expect("dw", dw, (d,), torch.float32, like=x)
+    _expect("db", db, (d,), torch.float32, like=x)
     dx = x.new_empty((T, d))
-    dw = x.new_empty(d, dtype=torch.float32)
-    db = x.new_empty(d, dtype=torch.float32) if want_bias else None
+    if dw is None:
+        dw = x.new_empty(d, dtype=torch.float32)
+    if db is None and want_bias:
+        db = x.new_empty(d, dtype=torch.float32)
     ws = x.new_empty(_bytes(lib.grouter_layernorm_bwd_workspace_bytes, dev, T, d), dtype=torch.uint8)
     _call(lib.grouter_layernorm_bwd, "grouter_layernorm_bwd", dev, dy.data_ptr(), x.data_ptr(), ldx, weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
           T, d, dt, wt, dx.data_ptr(), dw.data_ptr(), _ptr(db), ws.data_ptr())
@@ -600,9 +606,10 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
 
 def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Optional[torch.Tensor] = None, act: int = ACT_NONE,
                     want_dx: bool = True, want_dW: bool = True, want_bias: bool = False, dW_dtype: torch.dtype = torch.bfloat16,
-                    status: Optional[torch.Tensor] = None):
+                    dW: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """grouter_linear_bwd; pre: the forward's x W^T + bias, needed with an activation -> (dx bf16 [T,K], dW [N,K] of dW_dtype,
-    db f32 [N]), None for what is not wanted.  The residual's gradient is dy."""
+    db f32 [N]), None for what is not wanted.  The residual's gradient is dy.  dW, db: tensors to write the gradients into (dW bf16
+    or f32), e.g. those an AdamW object reads."""
     lib = load_library()
     if x.dim() != 2 or W.dim() != 2:
         raise ValueError("x and W: matrices are expected")
@@ -616,12 +623,18 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Opt
     _expect("status", status, (1,), torch.int32, like=x)
     if act != ACT_NONE and pre is None:
         raise ValueError("pre: needed with an activation")
-    if dW_dtype not in (bf, torch.float32):
-        raise TypeError(f"dW_dtype: bfloat16 or float32 expected, got {dW_dtype}")
+    if dW is not None:
+        dW_dtype = dW.dtype
+        _expect("dW", dW, (N, K), like=x)
+    if dW_dtype != bf and dW_dtype != torch.float32:
+        raise TypeError(f"dW: bfloat16 or float32 expected, got {dW_dtype}")
+    _expect("db", db, (N,), torch.float32, like=x)
     dev = _device_index(x.device)
     dx = x.new_empty((T, K)) if want_dx else None
-    dW = x.new_empty((N, K), dtype=dW_dtype) if want_dW else None
-    db = x.new_empty(N, dtype=torch.float32) if want_bias else None
+    if dW is None and want_dW:
+        dW = x.new_empty((N, K), dtype=dW_dtype)
+    if db is None and want_bias:
+        db = x.new_empty(N, dtype=torch.float32)
     ws = x.new_empty(_bytes(lib.grouter_linear_bwd_workspace_bytes, dev, T, K, N, act), dtype=torch.uint8)
     _call(lib.grouter_linear_bwd, "grouter_linear_bwd", dev, dy.data_ptr(), x.data_ptr(), W.data_ptr(), _ptr(pre), T, K, N, act, _ptr(dx), _ptr(dW),
           F32 if dW_dtype == torch.float32 else BF16, _ptr(db), ws.data_ptr(), _status_ptr(status, dev))

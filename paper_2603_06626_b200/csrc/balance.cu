@@ -25,48 +25,59 @@ namespace grouter {
 constexpr int BAL_THREADS = 256;
 constexpr int BAL_WARPS = BAL_THREADS / 32;
 constexpr int BAL_MAX_E = 1024;
-constexpr int COUNT_THREADS = 512;
+constexpr int COUNT_THREADS = 1024;
 constexpr int COUNT_CLUSTER = 8;
 // Up to this many ids one cluster counts them all and writes the sums itself: one launch instead of two zeroings and a kernel.
-constexpr int64_t COUNT_CLUSTER_SLOTS = 1 << 19;
+constexpr uint32_t COUNT_CLUSTER_SLOTS = 1 << 19;
 constexpr int COUNT_SLOTS = 4096;       // counters a block of the histogram keeps (several copies of few experts)
 
-// Histogram of the ids.  A thread takes 16 bytes of ids at a time (IPT of them).  Lanes spread over `copies` copies of the
-// counters, so that few experts do not queue up at the same word.
+// Histogram of the ids.  A thread takes 16 bytes of ids at a time (IPT of them).  Lanes spread over `copies` (a power of two up to
+// 32) copies of the counters, the copies of one expert side by side: with 32 of them every lane has a bank of its own, whatever
+// the ids are.
 // CLUSTER: the grid is one cluster of COUNT_CLUSTER blocks, which add up their counters through each other's shared memory and
 // store the sums; otherwise any number of blocks adds to outputs that were zeroed before.
 template <typename Id, bool CLUSTER>
-__global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* __restrict__ idx, int64_t slots, int k, int E, int copies,
-                                                                      const uint8_t* __restrict__ mask, int32_t* __restrict__ counts,
-                                                                      int32_t* __restrict__ n_tokens, int32_t* __restrict__ status) {
+__global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* __restrict__ idx, uint32_t slots, uint32_t k, int E,
+                                                                      int copies, const uint8_t* __restrict__ mask,
+                                                                      int32_t* __restrict__ counts, int32_t* __restrict__ n_tokens,
+                                                                      int32_t* __restrict__ status) {
   constexpr int IPT = 16 / (int)sizeof(Id);
   __shared__ int32_t s_cnt[COUNT_SLOTS];
   __shared__ int32_t s_sum[BAL_MAX_E + 1];        // this block's counts, then its tokens
   for (int i = threadIdx.x; i < E * copies; i += COUNT_THREADS) s_cnt[i] = 0;
   if (threadIdx.x == 0) s_sum[E] = 0;
   __syncthreads();
-  int32_t* mine = s_cnt + (threadIdx.x % copies) * E;
+  int32_t* mine = s_cnt + (threadIdx.x & (copies - 1));
   int tokens = 0;
   bool bad = false;
-  const int64_t stride = (int64_t)gridDim.x * COUNT_THREADS * IPT;
-  for (int64_t s0 = ((int64_t)blockIdx.x * COUNT_THREADS + threadIdx.x) * IPT; s0 < slots; s0 += stride) {
+  const uint32_t stride = gridDim.x * COUNT_THREADS * IPT;      // slots + stride < 2^32: slots < 2^31, stride < 2^24
+  struct Piece {
     alignas(16) Id ids[IPT];
+  };
+  auto load = [&](uint32_t s0) {
+    Piece r;
     if (s0 + IPT <= slots) {
-      *reinterpret_cast<uint4*>(ids) = ld_stream16(idx + s0);
+      *reinterpret_cast<uint4*>(r.ids) = ld_stream16(idx + s0);
     } else {
 #pragma unroll
-      for (int i = 0; i < IPT; ++i) ids[i] = s0 + i < slots ? idx[s0 + i] : Id(0);
+      for (int i = 0; i < IPT; ++i) r.ids[i] = s0 + i < slots ? idx[s0 + i] : Id(0);
     }
-    int64_t t = s0 / k;
-    int j = (int)(s0 - t * k);
+    return r;
+  };
+  uint32_t s0 = (blockIdx.x * COUNT_THREADS + threadIdx.x) * IPT;
+  Piece next = load(s0);
+  for (; s0 < slots; s0 += stride) {
+    const Piece cur = next;
+    next = load(s0 + stride);                                   // on its way while these are counted
+    uint32_t t = s0 / k, j = s0 - t * k;
     bool live = mask == nullptr || mask[t] != 0;
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
       if (s0 + i < slots) {
         if (live) {
           tokens += j == 0;
-          const int e = (int)ids[i];
-          if ((unsigned)e < (unsigned)E) atomicAdd(mine + e, 1);
+          const int e = (int)cur.ids[i];
+          if ((unsigned)e < (unsigned)E) atomicAdd(mine + e * copies, 1);
           else bad = true;
         }
         if (++j == k) {
@@ -80,10 +91,12 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
   if (bad && status) atomicOr(status, STATUS_BAD_INDEX);
   if (tokens) atomicAdd(s_sum + E, tokens);
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += COUNT_THREADS) {
-    int32_t c = 0;
-    for (int q = 0; q < copies; ++q) c += s_cnt[q * E + e];
-    s_sum[e] = c;
+  // `copies` neighbouring lanes add up an expert
+  for (int i0 = 0; i0 < E * copies; i0 += COUNT_THREADS) {
+    const int i = i0 + threadIdx.x;
+    int32_t c = i < E * copies ? s_cnt[i] : 0;
+    for (int o = copies / 2; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    if (i < E * copies && (i & (copies - 1)) == 0) s_sum[i / copies] = c;
   }
   if constexpr (CLUSTER) {
     cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
@@ -159,7 +172,8 @@ template <typename T, int VE, int LPT, int EPL, bool GATES>
 __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParams p) {
   constexpr bool RING = VE > 1;                       // rows that are not 16-byte aligned: plain loads, one round ahead
   constexpr int S = balance_ring(sizeof(T), EPL);
-  extern __shared__ uint4 s_ring[];                   // RING: [S][NV][BAL_THREADS]
+  extern __shared__ uint4 s_dyn[];
+  Pack<T, VE>* s_ring = reinterpret_cast<Pack<T, VE>*>(s_dyn);      // RING: [S][NV][BAL_THREADS]
   float* s_f = reinterpret_cast<float*>(s_ring + (RING ? S * (EPL / VE) * BAL_THREADS : 0));
   __shared__ double s_part[2][BAL_WARPS];
   __shared__ unsigned long long s_count[BAL_WARPS];
@@ -183,7 +197,8 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
       for (int n = 0; n < NV; ++n) {
         const int c = (n * LPT + sl) * VE;
         if (c < E) {
-          if constexpr (RING) copy16_async(slot(s, n), row + c);
+          if constexpr (RING && VE * sizeof(T) == 16) copy16_async(slot(s, n), row + c);
+          else if constexpr (RING) copy8_async(slot(s, n), row + c);
           else q[n] = ld_pack<T, VE>(row + c);
         }
       }
@@ -219,7 +234,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     for (int s = 0; s < S; ++s) {
 #pragma unroll
       for (int n = 0; n < NV; ++n)
-        if ((n * LPT + sl) * VE >= E) *reinterpret_cast<Pack<T, VE>*>(slot(s, n)) = q[n];
+        if ((n * LPT + sl) * VE >= E) *slot(s, n) = q[n];
       fetch(t + s * step, s);
     }
   } else {
@@ -273,7 +288,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     if constexpr (RING) {
       copies_wait<S - 1>();
 #pragma unroll
-      for (int n = 0; n < NV; ++n) *reinterpret_cast<uint4*>(&q[n]) = *slot(s_at, n);
+      for (int n = 0; n < NV; ++n) q[n] = *slot(s_at, n);
     }
     float2 v[PAIRS];
 #pragma unroll
@@ -306,7 +321,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     z = lanes_sum<LPT>(z);
     a = lanes_sum<LPT>(a);
     const float inv_z = some ? 1.f / z : 0.f;
-    const float lse = some ? base + logf(z) : 0.f;
+    const float lse = some ? base + __logf(z) : 0.f;          // z >= 1: within 2^-21
     a *= inv_z;
     if (sl == 0 && live) {
       sum_a += a;
@@ -356,9 +371,20 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
       if (here && c < E) {
         float w[VE];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          w[i] = o[n * VE + i];
-          if (GATES) w[i] += s_gate[c + i];
+        for (int i = 0; i < VE; ++i) w[i] = o[n * VE + i];
+        if (GATES) {
+          if constexpr (VE == 1) {
+            w[0] += s_gate[c];
+          } else {
+#pragma unroll
+            for (int i = 0; i < VE; i += 4) {
+              const float4 g = *reinterpret_cast<const float4*>(s_gate + c + i);
+              w[i] += g.x;
+              w[i + 1] += g.y;
+              w[i + 2] += g.z;
+              w[i + 3] += g.w;
+            }
+          }
         }
         Pack<T, VE> r;
 #pragma unroll
@@ -423,7 +449,7 @@ namespace {
 constexpr int BAL_MAX_BLOCKS_PER_SM = 8;
 
 template <typename Id>
-cudaError_t count_in_cluster(const Id* idx, int64_t slots, int k, int E, int copies, const uint8_t* mask, int32_t* counts, int32_t* n_tokens,
+cudaError_t count_in_cluster(const Id* idx, uint32_t slots, uint32_t k, int E, int copies, const uint8_t* mask, int32_t* counts, int32_t* n_tokens,
                              int32_t* status, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(COUNT_CLUSTER);
@@ -510,10 +536,10 @@ int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mas
   if (E > BAL_MAX_E || k > 32 || (int64_t)T * k > INT32_MAX || (idx_dtype == GROUTER_IDX_U8 && E > 256)) return GROUTER_ERR_UNSUPPORTED;
   if (!aligned_to(idx, 16) || !aligned_to(counts, 4) || !aligned_to(n_tokens, 4) || !aligned_to(status, 4)) return GROUTER_ERR_MISALIGNED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t slots = (int64_t)T * k;
+  const uint32_t slots = (uint32_t)T * (uint32_t)k;
   const bool u8 = idx_dtype == GROUTER_IDX_U8;
-  int copies = COUNT_SLOTS / E;
-  if (copies > 32) copies = 32;
+  int copies = 32;
+  while (copies * E > COUNT_SLOTS) copies /= 2;
   cudaError_t e;
   if (slots <= COUNT_CLUSTER_SLOTS) {
     e = u8 ? count_in_cluster(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts, n_tokens, status, st)
@@ -521,8 +547,8 @@ int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mas
   } else {
     if (cudaMemsetAsync(counts, 0, sizeof(int32_t) * E, st) != cudaSuccess || cudaMemsetAsync(n_tokens, 0, sizeof(int32_t), st) != cudaSuccess)
       return GROUTER_ERR_CUDA;
-    const int64_t per_block = (int64_t)COUNT_THREADS * (u8 ? 16 : 4), want = (slots + per_block - 1) / per_block;
-    const int cap = current_sms() * 4, grid = (int)(want < cap ? want : cap);
+    const int64_t per_block = (int64_t)COUNT_THREADS * (u8 ? 16 : 4), want = ((int64_t)slots + per_block - 1) / per_block;
+    const int cap = current_sms() * 2, grid = (int)(want < cap ? want : cap);
     if (u8)
       expert_counts_kernel<uint8_t, false><<<grid, COUNT_THREADS, 0, st>>>(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts,
                                                                           n_tokens, status);
@@ -562,12 +588,15 @@ int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const vo
   p.logits = logits; p.ld = ld; p.idx = idx; p.idx_i32 = idx_dtype == GROUTER_IDX_I32; p.mask = mask; p.counts = counts; p.n_tokens = n_tokens;
   p.dgates = dgates; p.sigmoid = norm == GROUTER_NORM_SIGMOID; p.T = T; p.E = E; p.k = k; p.ca = balance_coef; p.cz = z_coef; p.dloss = dloss;
   p.loss = loss; p.dlogits = dlogits; p.partial = static_cast<double2*>(workspace); p.status = status;
-  // 16-byte accesses where every row starts on a 16-byte boundary, single elements otherwise
+  // 16-byte accesses where every row starts on a 16-byte boundary (8-byte ones for bf16 on such a boundary: 60 experts), single
+  // elements otherwise
   const int ve = dtype == GROUTER_F32 ? vec16<float>() : vec16<__nv_bfloat16>();
   const bool vec = E % ve == 0 && ld % ve == 0 && aligned_to(logits, 16) && aligned_to(dlogits, 16);
   cudaError_t e;
   if (dtype == GROUTER_F32) e = vec ? balance_by_width<float, vec16<float>()>(p, st) : balance_by_width<float, 1>(p, st);
-  else e = vec ? balance_by_width<__nv_bfloat16, vec16<__nv_bfloat16>()>(p, st) : balance_by_width<__nv_bfloat16, 1>(p, st);
+  else if (vec) e = balance_by_width<__nv_bfloat16, vec16<__nv_bfloat16>()>(p, st);
+  else if (E % 4 == 0 && ld % 4 == 0 && aligned_to(logits, 8) && aligned_to(dlogits, 8)) e = balance_by_width<__nv_bfloat16, 4>(p, st);
+  else e = balance_by_width<__nv_bfloat16, 1>(p, st);
   return e == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
