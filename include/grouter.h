@@ -346,12 +346,12 @@ int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mas
  *   logits [T,E] of dtype, row t at logits + t*ld elements; any alignment      dlogits [T,E] of dtype, contiguous, or NULL
  *   counts [E], n_tokens [1]: of grouter_expert_counts, or summed over several ranks (counts: the share f is then global)
  *   idx [T,k], dgates [T,k] f32: needed together (idx may be NULL without dgates)      dloss: device scalar or NULL (1)
- *   loss [3] f32 out or NULL (not both NULL)      workspace: grouter_balance_loss_workspace_bytes() bytes, for the loss
+ *   loss [3] f32 out or NULL (not both NULL)      workspace: grouter_balance_loss_workspace_bytes(T, E, k) bytes, for the loss
  *   status: optional device int32, bit 1: an id is out of range (its gate's gradient is left out)
  * A masked token has a zero gradient row, whatever its scores.  A score of -inf has p = 0; a row of nothing but -inf has p = 0
  * and lse = 0.  n = 0: losses are 0.  Coefficients of zero drop their term, finite or not.  E <= 1024 (256 for uint8 ids),
  * k <= 32.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
-size_t grouter_balance_loss_workspace_bytes(void);
+size_t grouter_balance_loss_workspace_bytes(int32_t T, int32_t E, int32_t k);   /* 0 for few tokens: none is needed */
 int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const void* idx, int32_t idx_dtype, const uint8_t* mask,
                          const int32_t* counts, const int32_t* n_tokens, const float* dgates, int32_t norm, int32_t T, int32_t E, int32_t k,
                          float balance_coef, float z_coef, const float* dloss, float* loss, void* dlogits, void* workspace, int32_t* status,

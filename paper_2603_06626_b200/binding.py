@@ -158,7 +158,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.grouter_linear_bwd.restype = ctypes.c_int
     lib.grouter_expert_counts.argtypes = [vp, i32, vp, i32, i32, i32, vp, vp, vp, vp]
     lib.grouter_expert_counts.restype = ctypes.c_int
-    lib.grouter_balance_loss_workspace_bytes.argtypes = []
+    lib.grouter_balance_loss_workspace_bytes.argtypes = [i32] * 3
     lib.grouter_balance_loss_workspace_bytes.restype = ctypes.c_size_t
     lib.grouter_balance_loss.argtypes = [vp, i64, i32, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, f32, f32, vp, vp, vp, vp, vp, vp]
     lib.grouter_balance_loss.restype = ctypes.c_int
@@ -495,11 +495,20 @@ def _call(fn, what: str, index: int, *args) -> None:
 
 def _row_stride(what: str, x: torch.Tensor) -> int:
     """Elements between the rows of a matrix whose rows are contiguous; other layouts raise."""
+    if x.dim() == 2 and x.is_contiguous():
+        return x.shape[1]
     if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{what}: a matrix with contiguous rows is expected")
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+    if x.shape[0] <= 1:
+        return x.shape[1]
+    if x.stride(0) < x.shape[1]:
         raise ValueError(f"{what}: rows that overlap")
-    return max(x.stride(0), x.shape[1]) if x.shape[0] > 1 else x.shape[1]
+    return x.stride(0)
+
+
+def _dense_like(x: torch.Tensor) -> torch.Tensor:
+    """An uninitialised contiguous tensor of x's shape and type."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
 def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5):
@@ -511,7 +520,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     _expect("bias", bias, (d,), weight.dtype, like=x)
     dt, wt = _elt(x, "x"), _elt(weight, "weight")
     dev = _device_index(x.device)
-    y = x.new_empty((T, d))
+    y = _dense_like(x)
     mean = x.new_empty(T, dtype=torch.float32)
     rstd = x.new_empty(T, dtype=torch.float32)
     _call(lib.grouter_layernorm_fwd, "grouter_layernorm_fwd", dev, x.data_ptr(), ldx, weight.data_ptr(), _ptr(bias), T, d, dt, wt, eps, y.data_ptr(),
@@ -534,7 +543,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     dev = _device_index(x.device)
     _expect("dw", dw, (d,), torch.float32, like=x)
     _expect("db", db, (d,), torch.float32, like=x)
-    dx = x.new_empty((T, d))
+    dx = torch.empty_like(dy)
     if dw is None:
         dw = x.new_empty(d, dtype=torch.float32)
     if db is None and want_bias:
@@ -546,11 +555,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
 
 
 def _bytes(fn, index: int, *args) -> int:
-    """Workspace bytes, which depend on the device they are for; never an empty tensor's 0."""
+    """Workspace bytes, which depend on the device they are for."""
     if torch._C._cuda_getDevice() == index:
-        return fn(*args) or 256
+        return fn(*args)
     with torch.cuda.device(index):
-        return fn(*args) or 256
+        return fn(*args)
 
 
 _status_words = {}
@@ -630,7 +639,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Opt
         raise TypeError(f"dW: bfloat16 or float32 expected, got {dW_dtype}")
     _expect("db", db, (N,), torch.float32, like=x)
     dev = _device_index(x.device)
-    dx = x.new_empty((T, K)) if want_dx else None
+    dx = torch.empty_like(x) if want_dx else None
     if dW is None and want_dW:
         dW = x.new_empty((N, K), dtype=dW_dtype)
     if db is None and want_bias:
@@ -706,8 +715,9 @@ def balance_loss(logits: torch.Tensor, idx: Optional[torch.Tensor], counts: torc
     _check_mask(mask, T, logits)
     dev = _device_index(logits.device)
     loss = logits.new_empty(3, dtype=torch.float32) if want_loss else None
-    d = logits.new_empty((T, E)) if want_grad else None
-    ws = logits.new_empty(_bytes(lib.grouter_balance_loss_workspace_bytes, dev), dtype=torch.uint8) if want_loss else None
+    d = _dense_like(logits) if want_grad else None
+    need = _bytes(lib.grouter_balance_loss_workspace_bytes, dev, T, E, k) if want_loss else 0
+    ws = logits.new_empty(need, dtype=torch.uint8) if need else None
     _call(lib.grouter_balance_loss, "grouter_balance_loss", dev, logits.data_ptr(), ld, dt, _ptr(idx), it, _ptr(mask), counts.data_ptr(),
           n_tokens.data_ptr(), _ptr(dgates), norm, T, E, k, balance_coef, z_coef, _ptr(dloss), _ptr(loss), _ptr(d), _ptr(ws),
           _status_ptr(status, dev))

@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
   __shared__ int32_t s_cnt[COUNT_SLOTS];
   __shared__ int32_t s_sum[BAL_MAX_E + 1];        // this block's counts, then its tokens
   for (int i = threadIdx.x; i < E * copies; i += COUNT_THREADS) s_cnt[i] = 0;
-  if (threadIdx.x == 0) s_sum[E] = 0;
+  if (threadIdx.x == 0) s_sum[E] = mask == nullptr && blockIdx.x == 0 ? (int32_t)(slots / k) : 0;      // without a mask: all tokens
   __syncthreads();
   int32_t* mine = s_cnt + (threadIdx.x & (copies - 1));
   int tokens = 0;
@@ -69,13 +69,22 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
   for (; s0 < slots; s0 += stride) {
     const Piece cur = next;
     next = load(s0 + stride);                                   // on its way while these are counted
+    if (mask == nullptr && s0 + IPT <= slots) {                 // every id counts: no need to know whose it is
+#pragma unroll
+      for (int i = 0; i < IPT; ++i) {
+        const int e = (int)cur.ids[i];
+        if ((unsigned)e < (unsigned)E) atomicAdd(mine + e * copies, 1);
+        else bad = true;
+      }
+      continue;
+    }
     uint32_t t = s0 / k, j = s0 - t * k;
     bool live = mask == nullptr || mask[t] != 0;
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
       if (s0 + i < slots) {
         if (live) {
-          tokens += j == 0;
+          tokens += j == 0 && mask != nullptr;
           const int e = (int)cur.ids[i];
           if ((unsigned)e < (unsigned)E) atomicAdd(mine + e * copies, 1);
           else bad = true;
@@ -411,14 +420,30 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     s_part[1][warp] = sum_z;
   }
   __syncthreads();
+  __shared__ double2 s_sum;
   if (threadIdx.x == 0) {
     double a = 0, z = 0;
     for (int w = 0; w < BAL_WARPS; ++w) {
       a += s_part[0][w];
       z += s_part[1][w];
     }
-    if (gridDim.x == 1) write_loss(p, a, z, n_tok);
-    else p.partial[blockIdx.x] = make_double2(a, z);
+    s_sum = make_double2(a, z);
+  }
+  cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+  if (cl.num_blocks() == gridDim.x) {                 // the whole grid is one cluster: its blocks add up among themselves
+    cl.sync();
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      double a = 0, z = 0;
+      for (unsigned r = 0; r < gridDim.x; ++r) {
+        const double2 v = *cl.map_shared_rank(&s_sum, r);
+        a += v.x;
+        z += v.y;
+      }
+      write_loss(p, a, z, n_tok);
+    }
+    cl.sync();                                        // nobody leaves while its sums are read
+  } else if (threadIdx.x == 0) {
+    p.partial[blockIdx.x] = s_sum;
   }
 }
 
@@ -446,7 +471,20 @@ __global__ void __launch_bounds__(256) balance_finish_kernel(const BalanceParams
 
 namespace {
 
-constexpr int BAL_MAX_BLOCKS_PER_SM = 8;
+constexpr int BAL_MAX_BLOCKS = 1184;   // 148 SMs x 8 blocks
+constexpr int BAL_CLUSTER = 8;         // a grid of up to so many blocks is one cluster, and needs neither workspace nor second kernel
+
+// Lanes a token: enough for 16 elements each and for one of the kept experts each.  (With or without gates: the sums of a row then
+// run in the same order and the losses are the same bits.)
+int balance_lanes(int E, int k) {
+  int lpt = 1;
+  while (lpt < 32 && (lpt * 16 < E || lpt < k)) lpt *= 2;
+  return lpt;
+}
+int64_t balance_blocks(int T, int E, int k) {
+  const int per_block = BAL_WARPS * (32 / balance_lanes(E, k));
+  return ((int64_t)T + per_block - 1) / per_block;
+}
 
 template <typename Id>
 cudaError_t count_in_cluster(const Id* idx, uint32_t slots, uint32_t k, int E, int copies, const uint8_t* mask, int32_t* counts, int32_t* n_tokens,
@@ -472,7 +510,7 @@ cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
   constexpr int MAX_SMEM = RING + (int)sizeof(float) * LPT * EPL * (1 + (GATES ? TPB : 0));                // E <= LPT * EPL: 37 KB more
   const size_t smem = RING + sizeof(float) * epad * (1 + (GATES ? TPB : 0));
   auto kern = balance_kernel<T, VE, LPT, EPL, GATES>;
-  const int64_t want = ((int64_t)p.T + TPB - 1) / TPB;
+  const int64_t want = balance_blocks(p.T, p.E, p.k);
   static int resident[64] = {};       // blocks an SM holds, which is what walks over the tokens; asked once per device
   int dev = 0, per_sm = 0;
   cudaGetDevice(&dev);
@@ -481,14 +519,25 @@ cudaError_t balance_launch_g(const BalanceParams& p, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, BAL_THREADS, MAX_SMEM);
     if (e != cudaSuccess) return e;
-    per_sm = per_sm < 1 ? 1 : per_sm > BAL_MAX_BLOCKS_PER_SM ? BAL_MAX_BLOCKS_PER_SM : per_sm;
+    if (per_sm < 1) per_sm = 1;
     if (dev >= 0 && dev < 64) resident[dev] = per_sm;
   }
-  const int cap = current_sms() * per_sm;
+  int cap = current_sms() * per_sm;
+  if (cap > BAL_MAX_BLOCKS) cap = BAL_MAX_BLOCKS;
   const int grid = (int)(want < cap ? want : cap);
-  kern<<<grid, BAL_THREADS, smem, st>>>(p);
-  cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess && p.loss && grid > 1) e = launch_dependent(balance_finish_kernel, dim3(1), dim3(256), 0, st, p, grid);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(BAL_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = grid;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = p.loss && grid <= BAL_CLUSTER ? 1 : 0;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
+  if (e == cudaSuccess && p.loss && grid > BAL_CLUSTER) e = launch_dependent(balance_finish_kernel, dim3(1), dim3(256), 0, st, p, grid);
   return e;
 }
 
@@ -509,12 +558,9 @@ cudaError_t balance_by_lanes(const BalanceParams& p, int lpt, cudaStream_t st) {
   }
 }
 
-// Lanes a token: enough for 16 elements each and for one of the kept experts each.  (With or without gates: the sums of a row then
-// run in the same order and the losses are the same bits.)
 template <typename T, int VE>
 cudaError_t balance_by_width(const BalanceParams& p, cudaStream_t st) {
-  int lpt = 1;
-  while (lpt < 32 && (lpt * 16 < p.E || lpt < p.k)) lpt *= 2;
+  const int lpt = balance_lanes(p.E, p.k);
   if (lpt * 16 < p.E) return balance_launch<T, VE, 32, 32>(p, st);
   if constexpr (VE > 1) {
     if (lpt * 8 >= p.E) return balance_by_lanes<T, VE, 8>(p, lpt, st);
@@ -560,7 +606,10 @@ int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mas
   return e == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
-size_t grouter_balance_loss_workspace_bytes(void) { return sizeof(double2) * current_sms() * BAL_MAX_BLOCKS_PER_SM; }
+size_t grouter_balance_loss_workspace_bytes(int32_t T, int32_t E, int32_t k) {
+  if (T < 1 || E < 1 || k < 1 || balance_blocks(T, E, k) <= BAL_CLUSTER) return 0;
+  return sizeof(double2) * BAL_MAX_BLOCKS;
+}
 
 int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const void* idx, int32_t idx_dtype, const uint8_t* mask,
                          const int32_t* counts, const int32_t* n_tokens, const float* dgates, int32_t norm, int32_t T, int32_t E, int32_t k,
@@ -568,12 +617,12 @@ int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const vo
                          void* stream) {
   if (!counts || !n_tokens || T < 0 || E < 1 || k < 1 || ld < E || (!loss && !dlogits)) return GROUTER_ERR_INVALID_ARG;
   if (T > 0 && (!logits || (dgates && (!idx || !dlogits)))) return GROUTER_ERR_INVALID_ARG;
-  if (loss && !workspace) return GROUTER_ERR_INVALID_ARG;
   if ((dtype != GROUTER_BF16 && dtype != GROUTER_F32) || (idx_dtype != GROUTER_IDX_U8 && idx_dtype != GROUTER_IDX_I32) ||
       (norm != GROUTER_NORM_SOFTMAX && norm != GROUTER_NORM_SIGMOID))
     return GROUTER_ERR_INVALID_ARG;
   if (E > BAL_MAX_E || k > 32 || (int64_t)T * k > INT32_MAX || T > INT32_MAX - (1 << 20) || (idx_dtype == GROUTER_IDX_U8 && E > 256))
     return GROUTER_ERR_UNSUPPORTED;
+  if (loss && !workspace && grouter_balance_loss_workspace_bytes(T, E, k) > 0) return GROUTER_ERR_INVALID_ARG;
   const size_t el = dtype == GROUTER_F32 ? 4 : 2;
   if (!aligned_to(logits, el) || !aligned_to(dlogits, el) || !aligned_to(dgates, 4) || !aligned_to(counts, 4) || !aligned_to(n_tokens, 4) ||
       !aligned_to(dloss, 4) || !aligned_to(loss, 4) || !aligned_to(status, 4) || !aligned_to(workspace, 16) ||

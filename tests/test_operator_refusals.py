@@ -58,7 +58,7 @@ def test_counts_and_balance(lib):
 
     def bal(x=A, ld=8, dt=0, idx=A, it=0, mask=None, c=A, n=A, dg=A, norm=0, T=4, E=8, k=2, dl=None, loss=A, d=A, ws=A, status=None):
         return lib.grouter_balance_loss(x, ld, dt, idx, it, mask, c, n, dg, norm, T, E, k, 0.1, 0.1, dl, loss, d, ws, status, None)
-    assert bal(x=None) == bal(c=None) == bal(n=None) == bal(idx=None) == bal(loss=None, d=None) == bal(ws=None) == INVALID
+    assert bal(x=None) == bal(c=None) == bal(n=None) == bal(idx=None) == bal(loss=None, d=None) == bal(ws=None, T=100000) == INVALID
     assert bal(d=None) == INVALID                       # a gradient of the gates has nowhere to go
     assert bal(ld=7) == bal(norm=2) == bal(dt=3) == bal(it=2) == bal(k=0) == INVALID
     assert bal(E=257, ld=257) == bal(E=1025, ld=1025, it=1) == bal(k=33) == UNSUPPORTED
