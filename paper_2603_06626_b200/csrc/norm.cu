@@ -280,36 +280,38 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
     if constexpr (RING) copies_wait<S - 1>();
     take();
     if constexpr (!HOLD) weights(wv);
-    float2 s1 = both(0.f), s2 = both(0.f);            // sums of g and of g h
+    // with 128 registers a thread the centred row and dy stay where they are; with 64 they are read again after the sums
+    float2 xc[PAIRS], g0[PAIRS];
+    auto open = [&](int j) {
+      g0[j] = g_of(j);
+      xc[j] = add2(x_of(j), both(-mean));
+    };
+    float2 s1 = both(0.f), s2 = both(0.f);            // sums of g and of g (x - mean)
 #pragma unroll
     for (int j = 0; j < PAIRS; ++j) {
-      const float2 g0 = g_of(j), h = mul2(add2(x_of(j), both(-mean)), both(rstd));
-      aw[j] = fma2(g0, h, aw[j]);
-      ab[j] = add2(ab[j], g0);
-      const float2 g = mul2(g0, wv[j]);
+      open(j);
+      aw[j] = fma2(g0[j], mul2(xc[j], both(rstd)), aw[j]);
+      ab[j] = add2(ab[j], g0[j]);
+      const float2 g = mul2(g0[j], wv[j]);
       s1 = add2(s1, g);
-      s2 = fma2(g, h, s2);
+      s2 = fma2(g, xc[j], s2);
     }
     float s[2] = {s1.x + s1.y, s2.x + s2.y};
     row_sums<TPR / 32, 2>(s, red, half);
-    const float2 c1 = both(-s[0] * inv_d), c2 = both(-s[1] * inv_d);
+    // dx = rstd g w - rstd mean(g) - (x - mean) rstd^3 mean(g (x - mean))
+    const float2 r = both(rstd), c1 = both(-s[0] * inv_d * rstd), c2 = both(-s[1] * inv_d * rstd * rstd * rstd);
     if constexpr (!HOLD) {
-      asm volatile("" ::: "memory");                  // read again rather than kept over the sums
-      weights(wv);
-    }
-    if constexpr (RING) {
       asm volatile("" ::: "memory");
-      take();
-    } else {
-      forget<T, VE, NV>(px);
-      forget<T, VE, NV>(pg);
+      weights(wv);
+      if constexpr (RING) take();
+      else forget<T, VE, NV>(px), forget<T, VE, NV>(pg);
     }
     T* dr = dx + row * d;
     float o[NORM_EPT];
 #pragma unroll
     for (int j = 0; j < PAIRS; ++j) {
-      const float2 h = mul2(add2(x_of(j), both(-mean)), both(rstd));
-      const float2 v = mul2(fma2(h, c2, fma2(g_of(j), wv[j], c1)), both(rstd));
+      if constexpr (!HOLD) open(j);
+      const float2 v = fma2(xc[j], c2, fma2(mul2(g0[j], wv[j]), r, c1));
       o[2 * j] = v.x;
       o[2 * j + 1] = v.y;
     }
