@@ -1,6 +1,6 @@
 // Activations of the linear layer and their slopes.
 #pragma once
-#include "common.cuh"
+#include "vec.cuh"
 
 namespace grouter {
 
@@ -29,19 +29,25 @@ __device__ __forceinline__ float act_value(float z) {
   }
   return z;
 }
+// g times the slope at z, two elements at a time.
 template <int ACT>
-__device__ __forceinline__ float act_slope(float z) {
-  if (ACT == GROUTER_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (ACT == GROUTER_ACT_SILU) {
-    const float s = logistic(z);
-    return s * (1.f + z * (1.f - s));
+__device__ __forceinline__ float2 act_back2(float2 g, float2 z) {
+  if (ACT == GROUTER_ACT_RELU) return make_float2(z.x > 0.f ? g.x : 0.f, z.y > 0.f ? g.y : 0.f);
+  if (ACT == GROUTER_ACT_SILU) {        // s (1 + z (1 - s))
+    const float2 s = make_float2(logistic(z.x), logistic(z.y));
+    const float2 rest = fma2(s, both(-1.f), both(1.f));
+    return mul2(g, mul2(s, fma2(z, rest, both(1.f))));
   }
-  if (ACT == GROUTER_ACT_GELU) {
-    float zc;
-    const float s = gelu_gate(z, zc);
-    return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * zc * zc);
+  if (ACT == GROUTER_ACT_GELU) {        // s + z s (1 - s) u',  u' = 2 sqrt(2/pi) (1 + 3 * 0.044715 z^2)
+    const float2 zc = make_float2(fminf(fmaxf(z.x, -12.f), 12.f), fminf(fmaxf(z.y, -12.f), 12.f));
+    const float2 q = mul2(zc, zc);
+    const float2 u = mul2(zc, fma2(q, both(1.5957691216057308f * 0.044715f), both(1.5957691216057308f)));
+    const float2 s = make_float2(logistic(u.x), logistic(u.y));
+    const float2 slope = fma2(q, both(1.5957691216057308f * 0.134145f), both(1.5957691216057308f));
+    const float2 rest = fma2(s, both(-1.f), both(1.f));
+    return mul2(g, fma2(mul2(mul2(z, s), rest), slope, s));
   }
-  return 1.f;
+  return g;
 }
 
 }  // namespace grouter

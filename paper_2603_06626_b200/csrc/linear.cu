@@ -27,9 +27,9 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
   __shared__ float s_sum[SUM ? DZ_LANES : 1][DZ_COLS + 1];
   const int ct = threadIdx.x & 31, rl = threadIdx.x >> 5;
   const int c = blockIdx.x * DZ_COLS + ct * 8;
-  float acc[8];
+  float2 acc[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  for (int i = 0; i < 4; ++i) acc[i] = both(0.f);
   if (c < N) {
     const int64_t step = (int64_t)gridDim.y * DZ_LANES;
     for (int64_t t0 = (int64_t)blockIdx.y * DZ_LANES + rl; t0 < T; t0 += step * DZ_AHEAD) {
@@ -48,10 +48,12 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
         if (t < T) {
           float v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v[i] = to_f32(g[u].v[i]);
-            if (ACT != GROUTER_ACT_NONE) v[i] *= act_slope<ACT>(to_f32(q[u].v[i]));
-            if (SUM) acc[i] += v[i];
+          for (int i = 0; i < 8; i += 2) {
+            float2 w = make_float2(to_f32(g[u].v[i]), to_f32(g[u].v[i + 1]));
+            if (ACT != GROUTER_ACT_NONE) w = act_back2<ACT>(w, make_float2(to_f32(q[u].v[i]), to_f32(q[u].v[i + 1])));
+            if (SUM) acc[i / 2] = add2(acc[i / 2], w);
+            v[i] = w.x;
+            v[i + 1] = w.y;
           }
           if (WRITE) st_pack<__nv_bfloat16, 8>(dz + t * N + c, v);
         }
@@ -61,7 +63,10 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
   if constexpr (SUM) {
     let_next_kernel_start();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s_sum[rl][ct + 32 * i] = acc[i];
+    for (int i = 0; i < 4; ++i) {
+      s_sum[rl][ct + 64 * i] = acc[i].x;
+      s_sum[rl][ct + 64 * i + 32] = acc[i].y;
+    }
     __syncthreads();
     for (int q = threadIdx.x; q < DZ_COLS; q += DZ_THREADS) {
       float a = 0.f;
