@@ -557,7 +557,10 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const bool live = ti.m_valid > 0;    // false: this CTA only lent its half of B to the pair
       uint4 g4[4], u4[4];
       if (MODE == MODE_DH) load_gu(ti, 0, g4, u4);   // in flight while the main loop of this tile finishes
-      if (MODE == MODE_LINEAR && p.residual != nullptr) load_residual(ti, 0, g4);
+      if (MODE == MODE_LINEAR && p.residual != nullptr) {
+        load_residual(ti, 0, g4);
+        load_residual(ti, 1, u4);
+      }
       if (!ptx::mbar_wait_bounded(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)acc * BN + ((uint32_t)(quad * 32) << 16);
@@ -710,8 +713,8 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           uint4 res[4];
           if (p.residual != nullptr) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) res[q] = g4[q];
-            if (c < 3) load_residual(ti, c + 1, g4); // next chunk's loads fly during this chunk's arithmetic
+            for (int q = 0; q < 4; ++q) res[q] = c & 1 ? u4[q] : g4[q];
+            if (c < 2) load_residual(ti, c + 2, c & 1 ? u4 : g4);      // two chunks ahead of the arithmetic
           }
           if (any) {
             if ((c & 1) == 0) {
