@@ -470,6 +470,11 @@ def _expect(what: str, t: Optional[torch.Tensor], shape, dtype=None, like: Optio
         raise ValueError(f"{what}: on {t.device}, the other arguments are on {like.device}")
 
 
+def _fits(t: Optional[torch.Tensor], shape, dtype, dev: torch.device) -> bool:
+    """What _expect checks, in one expression: the calls below ask this first and look for the reason only when it fails."""
+    return t is None or (t.shape == shape and t.dtype == dtype and t.device == dev and t.is_contiguous())
+
+
 def _device_index(dev: torch.device) -> int:
     """Index of a CUDA device; other devices raise."""
     if dev.type != "cuda":
@@ -516,10 +521,12 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     lib = load_library()
     ldx = _row_stride("x", x)
     T, d = x.shape
-    _expect("weight", weight, (d,), like=x)
-    _expect("bias", bias, (d,), weight.dtype, like=x)
+    on = x.device
+    if not (_fits(weight, (d,), weight.dtype, on) and _fits(bias, (d,), weight.dtype, on)):
+        _expect("weight", weight, (d,), like=x)
+        _expect("bias", bias, (d,), weight.dtype, like=x)
     dt, wt = _elt(x, "x"), _elt(weight, "weight")
-    dev = _device_index(x.device)
+    dev = _device_index(on)
     y = _dense_like(x)
     mean = x.new_empty(T, dtype=torch.float32)
     rstd = x.new_empty(T, dtype=torch.float32)
@@ -535,14 +542,15 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     lib = load_library()
     ldx = _row_stride("x", x)
     T, d = x.shape
-    _expect("dy", dy, (T, d), x.dtype, like=x)
-    _expect("weight", weight, (d,), like=x)
-    _expect("mean", mean, (T,), torch.float32, like=x)
-    _expect("rstd", rstd, (T,), torch.float32, like=x)
+    on, f32 = x.device, torch.float32
+    if not (_fits(dy, x.shape, x.dtype, on) and _fits(weight, (d,), weight.dtype, on) and _fits(mean, (T,), f32, on) and
+            _fits(rstd, (T,), f32, on) and _fits(dw, (d,), f32, on) and _fits(db, (d,), f32, on)):
+        _expect("dy", dy, (T, d), x.dtype, like=x)
+        _expect("weight", weight, (d,), like=x)
+        for name, v, n in (("mean", mean, T), ("rstd", rstd, T), ("dw", dw, d), ("db", db, d)):
+            _expect(name, v, (n,), f32, like=x)
     dt, wt = _elt(x, "x"), _elt(weight, "weight")
-    dev = _device_index(x.device)
-    _expect("dw", dw, (d,), torch.float32, like=x)
-    _expect("db", db, (d,), torch.float32, like=x)
+    dev = _device_index(on)
     dx = torch.empty_like(dy)
     if dw is None:
         dw = x.new_empty(d, dtype=torch.float32)
@@ -599,13 +607,15 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
         raise ValueError("x and W: matrices are expected")
     T, K = x.shape
     N = W.shape[0]
-    bf = torch.bfloat16
-    _expect("x", x, (T, K), bf)
-    _expect("W", W, (N, K), bf, like=x)
-    _expect("bias", bias, (N,), bf, like=x)
-    _expect("residual", residual, (T, N), bf, like=x)
-    _expect("status", status, (1,), torch.int32, like=x)
-    dev = _device_index(x.device)
+    bf, on = torch.bfloat16, x.device
+    if not (_fits(x, (T, K), bf, on) and _fits(W, (N, K), bf, on) and _fits(bias, (N,), bf, on) and _fits(residual, (T, N), bf, on) and
+            _fits(status, (1,), torch.int32, on)):
+        _expect("x", x, (T, K), bf)
+        _expect("W", W, (N, K), bf, like=x)
+        _expect("bias", bias, (N,), bf, like=x)
+        _expect("residual", residual, (T, N), bf, like=x)
+        _expect("status", status, (1,), torch.int32, like=x)
+    dev = _device_index(on)
     y = x.new_empty((T, N))
     pre = x.new_empty((T, N)) if save_pre else None
     _call(lib.grouter_linear_fwd, "grouter_linear_fwd", dev, x.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), T, K, N, act, y.data_ptr(),
@@ -624,12 +634,15 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Opt
         raise ValueError("x and W: matrices are expected")
     T, K = x.shape
     N = W.shape[0]
-    bf = torch.bfloat16
-    _expect("x", x, (T, K), bf)
-    _expect("W", W, (N, K), bf, like=x)
-    _expect("dy", dy, (T, N), bf, like=x)
-    _expect("pre", pre, (T, N), bf, like=x)
-    _expect("status", status, (1,), torch.int32, like=x)
+    bf, on = torch.bfloat16, x.device
+    if not (_fits(x, (T, K), bf, on) and _fits(W, (N, K), bf, on) and _fits(dy, (T, N), bf, on) and _fits(pre, (T, N), bf, on) and
+            _fits(db, (N,), torch.float32, on) and _fits(status, (1,), torch.int32, on)):
+        _expect("x", x, (T, K), bf)
+        _expect("W", W, (N, K), bf, like=x)
+        _expect("dy", dy, (T, N), bf, like=x)
+        _expect("pre", pre, (T, N), bf, like=x)
+        _expect("db", db, (N,), torch.float32, like=x)
+        _expect("status", status, (1,), torch.int32, like=x)
     if act != ACT_NONE and pre is None:
         raise ValueError("pre: needed with an activation")
     if dW is not None:
@@ -637,8 +650,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, pre: Opt
         _expect("dW", dW, (N, K), like=x)
     if dW_dtype != bf and dW_dtype != torch.float32:
         raise TypeError(f"dW: bfloat16 or float32 expected, got {dW_dtype}")
-    _expect("db", db, (N,), torch.float32, like=x)
-    dev = _device_index(x.device)
+    dev = _device_index(on)
     dx = torch.empty_like(x) if want_dx else None
     if dW is None and want_dW:
         dW = x.new_empty((N, K), dtype=dW_dtype)
@@ -663,7 +675,8 @@ def _check_mask(mask: Optional[torch.Tensor], T: int, like: torch.Tensor) -> Non
         return
     if mask.dtype != torch.uint8 and mask.dtype != torch.bool:
         raise TypeError(f"mask: uint8 or bool expected, got {mask.dtype}")
-    _expect("mask", mask, (T,), like=like)
+    if not _fits(mask, (T,), mask.dtype, like.device):
+        _expect("mask", mask, (T,), like=like)
 
 
 def expert_counts(idx: torch.Tensor, E: int, mask: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
@@ -673,11 +686,13 @@ def expert_counts(idx: torch.Tensor, E: int, mask: Optional[torch.Tensor] = None
     if idx.dim() != 2:
         raise ValueError("idx: a matrix is expected")
     T, k = idx.shape
-    _expect("idx", idx, (T, k))
-    _expect("status", status, (1,), torch.int32, like=idx)
+    on = idx.device
+    if not (_fits(idx, idx.shape, idx.dtype, on) and _fits(status, (1,), torch.int32, on)):
+        _expect("idx", idx, (T, k))
+        _expect("status", status, (1,), torch.int32, like=idx)
     _check_mask(mask, T, idx)
     dt = _idx_dtype(idx)
-    dev = _device_index(idx.device)
+    dev = _device_index(on)
     counts = idx.new_empty(E, dtype=torch.int32)
     n = idx.new_empty(1, dtype=torch.int32)
     _call(lib.grouter_expert_counts, "grouter_expert_counts", dev, idx.data_ptr(), dt, _ptr(mask), T, k, E, counts.data_ptr(), n.data_ptr(),
@@ -703,17 +718,20 @@ def balance_loss(logits: torch.Tensor, idx: Optional[torch.Tensor], counts: torc
         if idx.dim() != 2:
             raise ValueError("idx: a matrix is expected")
         k, it = idx.shape[1], _idx_dtype(idx)
+    on, i32 = logits.device, torch.int32
+    if not (_fits(counts, (E,), i32, on) and _fits(n_tokens, (1,), i32, on) and _fits(dgates, (T, k), torch.float32, on) and
+            _fits(status, (1,), i32, on) and (idx is None or _fits(idx, (T, k), idx.dtype, on))):
         _expect("idx", idx, (T, k), like=logits)
-    _expect("counts", counts, (E,), torch.int32, like=logits)
-    _expect("n_tokens", n_tokens, (1,), torch.int32, like=logits)
-    _expect("dgates", dgates, (T, k), torch.float32, like=logits)
+        _expect("counts", counts, (E,), i32, like=logits)
+        _expect("n_tokens", n_tokens, (1,), i32, like=logits)
+        _expect("dgates", dgates, (T, k), torch.float32, like=logits)
+        _expect("status", status, (1,), i32, like=logits)
     if dloss is not None:
         if dloss.numel() != 1:
             raise ValueError("dloss: one number is expected")
         _expect("dloss", dloss.reshape(1), (1,), torch.float32, like=logits)
-    _expect("status", status, (1,), torch.int32, like=logits)
     _check_mask(mask, T, logits)
-    dev = _device_index(logits.device)
+    dev = _device_index(on)
     loss = logits.new_empty(3, dtype=torch.float32) if want_loss else None
     d = _dense_like(logits) if want_grad else None
     need = _bytes(lib.grouter_balance_loss_workspace_bytes, dev, T, E, k) if want_loss else 0
