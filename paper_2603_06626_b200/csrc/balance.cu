@@ -301,8 +301,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     }
     float2 v[PAIRS];
 #pragma unroll
-    for (int j = 0; j < PAIRS; ++j)
-      v[j] = make_float2(to_f32(q[2 * j / VE].v[2 * j % VE]), to_f32(q[(2 * j + 1) / VE].v[(2 * j + 1) % VE]));
+    for (int j = 0; j < PAIRS; ++j) v[j] = pair_at(q, j);
     if constexpr (!RING) fetch(t + step, 0);
     float top = -INFINITY;
 #pragma unroll
@@ -395,13 +394,8 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
             }
           }
         }
-        Pack<T, VE> r;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(w[i]);
-        if (!live) {
-#pragma unroll
-          for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(0.f);
-        }
+        Pack<T, VE> r = make_pack<T, VE>(w);
+        if (!live) r = Pack<T, VE>{};                 // zeros
         *reinterpret_cast<Pack<T, VE>*>(out + c) = r;
       }
     }

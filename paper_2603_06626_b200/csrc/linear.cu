@@ -49,8 +49,8 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
           float v[8];
 #pragma unroll
           for (int i = 0; i < 8; i += 2) {
-            float2 w = make_float2(to_f32(g[u].v[i]), to_f32(g[u].v[i + 1]));
-            if (ACT != GROUTER_ACT_NONE) w = act_back2<ACT>(w, make_float2(to_f32(q[u].v[i]), to_f32(q[u].v[i + 1])));
+            float2 w = pair_at(g, 4 * u + i / 2);
+            if (ACT != GROUTER_ACT_NONE) w = act_back2<ACT>(w, pair_at(q, 4 * u + i / 2));
             if (SUM) acc[i / 2] = add2(acc[i / 2], w);
             v[i] = w.x;
             v[i + 1] = w.y;

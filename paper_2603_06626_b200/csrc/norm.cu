@@ -34,8 +34,13 @@ __device__ __forceinline__ void load_weights(const W* __restrict__ w, int c, flo
       Pack<W, PER> p;
       if constexpr (PER * sizeof(W) == 16) *reinterpret_cast<uint4*>(&p) = __ldg(reinterpret_cast<const uint4*>(w + c + q));
       else *reinterpret_cast<uint2*>(&p) = __ldg(reinterpret_cast<const uint2*>(w + c + q));
+      const Pack<W, PER> one[1] = {p};
 #pragma unroll
-      for (int i = 0; i < PER; ++i) f[q + i] = to_f32(p.v[i]);
+      for (int i = 0; i < PER; i += 2) {
+        const float2 v = pair_at(one, i / 2);
+        f[q + i] = v.x;
+        f[q + i + 1] = v.y;
+      }
     }
   }
 }
@@ -103,7 +108,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
     for (int n = 0; n < NP; ++n)
       if ((n * (32 * NW) + at) * VE < d) {
 #pragma unroll
-        for (int i = 0; i < VE; i += 2) s2 = add2(s2, make_float2(to_f32(p[n].v[i]), to_f32(p[n].v[i + 1])));
+        for (int i = 0; i < VE; i += 2) s2 = add2(s2, pair_at(p, (n * VE + i) / 2));
       }
     s[0] = s2.x + s2.y;
   } else {
@@ -123,7 +128,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
       if ((n * (32 * NW) + at) * VE < d) {
 #pragma unroll
         for (int i = 0; i < VE; i += 2) {
-          const float2 c2 = add2(make_float2(to_f32(p[n].v[i]), to_f32(p[n].v[i + 1])), m2);
+          const float2 c2 = add2(pair_at(p, (n * VE + i) / 2), m2);
           q2 = fma2(c2, c2, q2);
         }
       }
@@ -155,7 +160,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
       if constexpr (VE > 1) {
 #pragma unroll
         for (int i = 0; i < VE; i += 2) {
-          const float2 h = mul2(add2(make_float2(to_f32(p[n].v[i]), to_f32(p[n].v[i + 1])), both(-mean)), both(rstd));
+          const float2 h = mul2(add2(pair_at(p, (n * VE + i) / 2), both(-mean)), both(rstd));
           const float2 v = fma2(h, make_float2(wl[i], wl[i + 1]), make_float2(bl[i], bl[i + 1]));
           o[i] = v.x;
           o[i + 1] = v.y;
@@ -275,16 +280,14 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
         }
       }
     };
-    auto x_of = [&](int j) { return make_float2(to_f32(px[2 * j / VE].v[2 * j % VE]), to_f32(px[(2 * j + 1) / VE].v[(2 * j + 1) % VE])); };
-    auto g_of = [&](int j) { return make_float2(to_f32(pg[2 * j / VE].v[2 * j % VE]), to_f32(pg[(2 * j + 1) / VE].v[(2 * j + 1) % VE])); };
     if constexpr (RING) copies_wait<S - 1>();
     take();
     if constexpr (!HOLD) weights(wv);
     // with 128 registers a thread the centred row and dy stay where they are; with 64 they are read again after the sums
     float2 xc[PAIRS], g0[PAIRS];
     auto open = [&](int j) {
-      g0[j] = g_of(j);
-      xc[j] = add2(x_of(j), both(-mean));
+      g0[j] = pair_at(pg, j);
+      xc[j] = add2(pair_at(px, j), both(-mean));
     };
     float2 s1 = both(0.f), s2 = both(0.f);            // sums of g and of g (x - mean)
 #pragma unroll
@@ -319,10 +322,7 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
     for (int n = 0; n < NV; ++n) {
       const int c = (n * TPR + lane) * VE;
       if (c < d) {
-        float t[VE];
-#pragma unroll
-        for (int i = 0; i < VE; ++i) t[i] = o[n * VE + i];
-        st_pack<T, VE>(dr + c, t);
+        st_pack<T, VE>(dr + c, o + n * VE);
       }
     }
     if constexpr (RING) {

@@ -87,12 +87,34 @@ __device__ __forceinline__ Pack<T, VE> ld_pack(const T* p) {
   }
   return r;
 }
+// Elements 2j and 2j + 1 of an array of packs, as f32.  Two bf16 come out of their word in one instruction each.
+template <typename T, int VE, int N>
+__device__ __forceinline__ float2 pair_at(const Pack<T, VE> (&q)[N], int j) {
+  if constexpr (VE == 1) {
+    return make_float2(to_f32(q[2 * j].v[0]), to_f32(q[2 * j + 1].v[0]));
+  } else if constexpr (sizeof(T) == 2) {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&q[2 * j / VE])[(2 * j % VE) / 2];
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  } else {
+    return make_float2(q[2 * j / VE].v[2 * j % VE], q[2 * j / VE].v[2 * j % VE + 1]);
+  }
+}
+// VE values rounded to T, two bf16 to an instruction.
 template <typename T, int VE>
-__device__ __forceinline__ void st_pack(T* p, const float (&f)[VE]) {
+__device__ __forceinline__ Pack<T, VE> make_pack(const float* f) {
   Pack<T, VE> r;
+  if constexpr (VE > 1 && sizeof(T) == 2) {
 #pragma unroll
-  for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(f[i]);
-  *reinterpret_cast<Pack<T, VE>*>(p) = r;
+    for (int i = 0; i < VE; i += 2) reinterpret_cast<__nv_bfloat162*>(&r)[i / 2] = __floats2bfloat162_rn(f[i], f[i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) r.v[i] = from_f32<T>(f[i]);
+  }
+  return r;
+}
+template <typename T, int VE>
+__device__ __forceinline__ void st_pack(T* p, const float* f) {
+  *reinterpret_cast<Pack<T, VE>*>(p) = make_pack<T, VE>(f);
 }
 
 // Two f32 operations in one instruction (each rounded by itself).
