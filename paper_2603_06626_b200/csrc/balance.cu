@@ -216,24 +216,28 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
   };
   // What else a lane needs of its token: whether it counts, and (GATES, lane j < k of the group: LPT >= k) its j-th kept expert with
   // the gradient of its gate, two rounds ahead, and that expert's score one round ahead.
+  // All of it as loaded: whatever is computed from it here would wait for it here.
   struct Side {
-    int e;
+    int e, mask;
     float dg;
-    bool live;
   };
   auto side = [&](int64_t t) {
-    Side r{-1, 0.f, t < p.T};
-    if (!r.live) return r;
-    if (GATES && sl < p.k) {
-      const int64_t at = t * p.k + sl;
-      r.e = p.idx_i32 ? __ldg(reinterpret_cast<const int32_t*>(p.idx) + at) : (int)__ldg(reinterpret_cast<const uint8_t*>(p.idx) + at);
-      r.dg = __ldg(p.dgates + at);
+    Side r{-1, 0, 0.f};
+    if (t < p.T) {
+      r.mask = 1;
+      if (p.mask != nullptr) r.mask = __ldg(p.mask + t);
+      if (GATES && sl < p.k) {
+        const int64_t at = t * p.k + sl;
+        r.e = p.idx_i32 ? __ldg(reinterpret_cast<const int32_t*>(p.idx) + at) : (int)__ldg(reinterpret_cast<const uint8_t*>(p.idx) + at);
+        r.dg = __ldg(p.dgates + at);
+      }
     }
-    if (p.mask != nullptr) r.live = __ldg(p.mask + t) != 0;
     return r;
   };
   auto score = [&](int64_t t, const Side& r) {
-    return GATES && r.live && sl < p.k && (unsigned)r.e < (unsigned)E ? to_f32(reinterpret_cast<const T*>(p.logits)[t * p.ld + r.e]) : -INFINITY;
+    T s = from_f32<T>(-INFINITY);
+    if (GATES && r.mask != 0 && sl < p.k && (unsigned)r.e < (unsigned)E) s = reinterpret_cast<const T*>(p.logits)[t * p.ld + r.e];
+    return s;
   };
 
   const int64_t step = (int64_t)gridDim.x * BAL_WARPS * TPW;
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     fetch(t, 0);
   }
   Side next = side(t), after = side(t + step);
-  float next_s = score(t, next);
+  T next_s = score(t, next);
 
   // f_e = E c_e / sum c, and a row of zeros for every lane group
   {
@@ -288,9 +292,9 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
 
   int s_at = 0;
   for (; t - grp < p.T; t += step) {                  // the warp's tokens start at t - grp: the same trips for all its lanes
-    const bool here = t < p.T, live = next.live;
+    const bool here = t < p.T, live = next.mask != 0;
     const int e = next.e;
-    const float dg = next.dg, s = next_s;             // GATES: of this lane's slot
+    const float dg = next.dg, s = to_f32(next_s);     // GATES: of this lane's slot
     next = after;
     next_s = score(t + step, next);
     after = side(t + 2 * step);
