@@ -577,6 +577,8 @@ def _status_word(index: int) -> torch.Tensor:
     """The status word of a device that the calls without one of their own share."""
     word = _status_words.get(index)
     if word is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first call on a device sets up its status word: make it outside a stream capture, or pass status=")
         word = _status_words[index] = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
         torch.cuda.synchronize(index)      # zeroed before a kernel on any stream can set a bit in it
     return word

@@ -3,8 +3,10 @@
 //   forward    z = x W^T + b       y = act(z) + r                                    x [T,K], W [N,K], y, z, r [T,N]
 //   backward   dz = dy act'(z)     dx = dz W      dW = dz^T x      db = sum_t dz      (the residual's gradient is dy itself)
 //
-// The products run on the CTA-pair tcgen05 core of the grouped products (gemm.cu, MODE_LINEAR / MODE_DENSE): bf16 operands,
-// fp32 accumulators; bias, activation and residual are applied in fp32 on the accumulator and rounded once.
+// The products run on the CTA-pair tcgen05 core of the grouped products (gemm.cu, MODE_LINEAR / MODE_DENSE) or, for few tokens, on
+// the kernel of linear_small.cu: bf16 operands, fp32 accumulators; bias, activation and residual are applied in fp32 on the
+// accumulator and rounded once.  Bound by the tensor cores: 32768 x 4096 x 1536 with SiLU and both outputs takes 320-357 us, 1.29-1.15
+// PFLOP/s as the GPU goes from rested to its power limit (8192 x 8192 x 8192 plain: 1.36).
 // dz is rounded to bf16, the type the tensor cores take it in; db is summed from the unrounded values.  One pass over dy and
 // z writes dz and the partial column sums; without an activation dz is dy and the pass only sums (or is left out).
 // dW's output matrix is often too small to give every CTA pair a tile: its contraction over the tokens is then cut into
@@ -175,7 +177,8 @@ cudaError_t launch_product(const LinearGemm& g, cudaStream_t st) {
   const int big_rounds = cdiv((int64_t)cdiv(g.M, 256) * cdiv(g.N, 256), sms / 2 > 0 ? sms / 2 : 1);
   const int small_rounds = cdiv((int64_t)cdiv(g.M, 128) * cdiv(g.N, 128) * splits, 2 * sms > 0 ? 2 * sms : 1);
   const float big = 5.7f + 0.33f * big_rounds * steps, small = small_rounds * (7.5f + 0.45f * cdiv(steps, splits));
-  if (g.M <= 64 || small < big) return launch_linear_small(g, splits, st);
+  const bool fits = cdiv(g.M, 128) <= 65535;      // its grid has the token tiles in y
+  if (g.M <= 64 || (small < big && fits)) return launch_linear_small(g, splits, st);
   return launch_linear_gemm(g, st);
 }
 
