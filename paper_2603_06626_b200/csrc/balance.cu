@@ -29,11 +29,11 @@ constexpr int COUNT_THREADS = 1024;
 constexpr int COUNT_CLUSTER = 8;
 // Up to this many ids one cluster counts them all and writes the sums itself: one launch instead of two zeroings and a kernel.
 constexpr uint32_t COUNT_CLUSTER_SLOTS = 1 << 19;
-constexpr int COUNT_SLOTS = 4096;       // counters a block of the histogram keeps (several copies of few experts)
+constexpr int COUNT_SLOTS = 4224;       // counters a block of the histogram keeps: 32 copies of 128 experts and of two more
 
 // Histogram of the ids.  A thread takes 16 bytes of ids at a time (IPT of them).  Lanes spread over `copies` (a power of two up to
 // 32) copies of the counters, the copies of one expert side by side: with 32 of them every lane has a bank of its own, whatever
-// the ids are.
+// the ids are.  Two counters more, E and E + 1, take the ids that are out of range and those of masked tokens: no id is a branch.
 // CLUSTER: the grid is one cluster of COUNT_CLUSTER blocks, which add up their counters through each other's shared memory and
 // store the sums; otherwise any number of blocks adds to outputs that were zeroed before.
 template <typename Id, bool CLUSTER>
@@ -43,13 +43,14 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
                                                                       int32_t* __restrict__ status) {
   constexpr int IPT = 16 / (int)sizeof(Id);
   __shared__ int32_t s_cnt[COUNT_SLOTS];
-  __shared__ int32_t s_sum[BAL_MAX_E + 1];        // this block's counts, then its tokens
-  for (int i = threadIdx.x; i < E * copies; i += COUNT_THREADS) s_cnt[i] = 0;
-  if (threadIdx.x == 0) s_sum[E] = mask == nullptr && blockIdx.x == 0 ? (int32_t)(slots / k) : 0;      // without a mask: all tokens
+  __shared__ int32_t s_sum[BAL_MAX_E + 2];        // this block's counts
+  __shared__ int32_t s_tokens;
+  const int rows = E + 2;
+  for (int i = threadIdx.x; i < rows * copies; i += COUNT_THREADS) s_cnt[i] = 0;
+  if (threadIdx.x == 0) s_tokens = mask == nullptr && blockIdx.x == 0 ? (int32_t)(slots / k) : 0;      // without a mask: all tokens
   __syncthreads();
   int32_t* mine = s_cnt + (threadIdx.x & (copies - 1));
   int tokens = 0;
-  bool bad = false;
   const uint32_t stride = gridDim.x * COUNT_THREADS * IPT;      // slots + stride < 2^32: slots < 2^31, stride < 2^24
   struct Piece {
     alignas(16) Id ids[IPT];
@@ -71,11 +72,7 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
     next = load(s0 + stride);                                   // on its way while these are counted
     if (mask == nullptr && s0 + IPT <= slots) {                 // every id counts: no need to know whose it is
 #pragma unroll
-      for (int i = 0; i < IPT; ++i) {
-        const int e = (int)cur.ids[i];
-        if ((unsigned)e < (unsigned)E) atomicAdd(mine + e * copies, 1);
-        else bad = true;
-      }
+      for (int i = 0; i < IPT; ++i) atomicAdd(mine + min((uint32_t)cur.ids[i], (uint32_t)E) * copies, 1);
       continue;
     }
     uint32_t t = s0 / k, j = s0 - t * k;
@@ -83,12 +80,8 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
       if (s0 + i < slots) {
-        if (live) {
-          tokens += j == 0 && mask != nullptr;
-          const int e = (int)cur.ids[i];
-          if ((unsigned)e < (unsigned)E) atomicAdd(mine + e * copies, 1);
-          else bad = true;
-        }
+        tokens += live && j == 0 && mask != nullptr;
+        atomicAdd(mine + (live ? min((uint32_t)cur.ids[i], (uint32_t)E) : (uint32_t)E + 1) * copies, 1);
         if (++j == k) {
           j = 0;
           ++t;
@@ -97,15 +90,19 @@ __global__ void __launch_bounds__(COUNT_THREADS) expert_counts_kernel(const Id* 
       }
     }
   }
-  if (bad && status) atomicOr(status, STATUS_BAD_INDEX);
-  if (tokens) atomicAdd(s_sum + E, tokens);
+  if (tokens) atomicAdd(&s_tokens, tokens);
   __syncthreads();
   // `copies` neighbouring lanes add up an expert
-  for (int i0 = 0; i0 < E * copies; i0 += COUNT_THREADS) {
+  for (int i0 = 0; i0 < rows * copies; i0 += COUNT_THREADS) {
     const int i = i0 + threadIdx.x;
-    int32_t c = i < E * copies ? s_cnt[i] : 0;
+    int32_t c = i < rows * copies ? s_cnt[i] : 0;
     for (int o = copies / 2; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-    if (i < E * copies && (i & (copies - 1)) == 0) s_sum[i / copies] = c;
+    if (i < rows * copies && (i & (copies - 1)) == 0) s_sum[i / copies] = c;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (s_sum[E] != 0 && status) atomicOr(status, STATUS_BAD_INDEX);
+    s_sum[E] = s_tokens;
   }
   if constexpr (CLUSTER) {
     cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
@@ -583,7 +580,7 @@ int grouter_expert_counts(const void* idx, int32_t idx_dtype, const uint8_t* mas
   const uint32_t slots = (uint32_t)T * (uint32_t)k;
   const bool u8 = idx_dtype == GROUTER_IDX_U8;
   int copies = 32;
-  while (copies * E > COUNT_SLOTS) copies /= 2;
+  while (copies * (E + 2) > COUNT_SLOTS) copies /= 2;
   cudaError_t e;
   if (slots <= COUNT_CLUSTER_SLOTS) {
     e = u8 ? count_in_cluster(static_cast<const uint8_t*>(idx), slots, k, E, copies, mask, counts, n_tokens, status, st)
