@@ -16,6 +16,8 @@
 // Every product, sum, quotient and root is rounded separately (no contraction), in the order written above: the result of
 // an element does not depend on which code path or compiler handles it.
 // Bound by HBM: 30 bytes an element (f32 moments and gradient, bf16 parameter), 16.06 with 8-bit moments and bf16 gradient.
+// Measured: 138 M elements with f32 moments 605-615 us (6.8 TB/s, a little above a plain copy's 6.46: reads outweigh writes);
+// 69 M with 8-bit moments and bf16 gradient 200 us (5.5 TB/s), 6 M of them in 120 tensors 21 us and 10 us to read the moments back.
 // The 8-bit form spends some 60 instructions an element, most of them on the exactly rounded root and quotient and on the codes:
 // whole chunks go without any test, two groups' exponents are reduced in one word, what is rare (values below the smallest code,
 // infinities) is behind a branch.

@@ -9,6 +9,10 @@
 // Both passes touch every element once and are bound by HBM, but only if they are lean: at 6.4 TB/s an SM has some 20 (forward)
 // and 30 (backward) instruction slots for an element of bf16, so the arithmetic is done two elements to an instruction (f32x2).
 // Sums are taken in fp32, the variance from the centred values (never as a difference of large sums).
+// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 91 us (5.9 TB/s), 65536 x 512 25 us (5.3);
+// backward with both kernels 16384 x 4096 bf16 78 us (5.1), 16384 x 2048 47 us (4.3; the partial rows and the second kernel take 7
+// of them), 8192 x 4096 f32 75 us (5.3).  Rows that are not 16-byte aligned go element by element: 16384 x 4095 bf16 86 us
+// forward (3.1 TB/s), 114 us backward (3.5).
 //   Forward: a row lies in the registers of one warp as it was loaded (up to 256 bytes a lane, eight KB a row in flight), or of
 //     several for wide rows; nothing is kept from row to row.
 //   Backward: the running dw and db of a column have to stay with one thread, so a row is spread over enough threads for 16
