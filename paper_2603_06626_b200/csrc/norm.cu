@@ -10,14 +10,16 @@
 // and 30 (backward) instruction slots for an element of bf16, so the arithmetic is done two elements to an instruction (f32x2).
 // Sums are taken in fp32, the variance from the centred values (never as a difference of large sums).
 // Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 91 us (5.9 TB/s), 65536 x 512 25 us (5.3);
-// backward with both kernels 16384 x 4096 bf16 78 us (5.1), 16384 x 2048 47 us (4.3; the partial rows and the second kernel take 7
-// of them), 8192 x 4096 f32 75 us (5.3).  Rows that are not 16-byte aligned go element by element: 16384 x 4095 bf16 86 us
-// forward (3.1 TB/s), 114 us backward (3.5).
+// backward with both kernels 16384 x 4096 bf16 76 us (5.3), 16384 x 2048 44 us (4.6), 8192 x 4096 f32 75 us (5.4), 8192 x 16384 f32
+// 299 us (5.4).  Rows that are not 16-byte aligned go element by element: 16384 x 4095 bf16 86 us forward (3.1 TB/s), 119 us
+// backward (3.4).
 //   Forward: a row lies in the registers of one warp as it was loaded (up to 256 bytes a lane, eight KB a row in flight), or of
 //     several for wide rows; nothing is kept from row to row.
 //   Backward: the running dw and db of a column have to stay with one thread, so a row is spread over enough threads for 16
-//     elements each; blocks are resident and walk over the rows (the coming ones on their way into shared memory), write one
-//     partial row each, and a second small kernel adds those up in a fixed order (bit-reproducible, no atomics).
+//     elements each; blocks are resident and walk over the rows (the coming ones on their way into shared memory), every cluster
+//     of them writes one partial row, and a second small kernel adds those up in a fixed order (bit-reproducible, no atomics).
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "vec.cuh"
@@ -201,9 +203,8 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
   constexpr bool RING = VE > 1;
   constexpr int S = norm_ring(sizeof(T), TPR);
   constexpr bool HOLD = TPR < 1024;     // the weights stay in registers (1024 threads have 64 each: there they are read from L1)
-  extern __shared__ uint4 s_ring[];     // RING: [S][x, dy][NV][THREADS]
+  extern __shared__ uint4 s_ring[];     // RING: [S][x, dy][NV][THREADS]; at the end this block's columns, [dw | db]
   __shared__ float red[2 * 2 * 32];
-  __shared__ float s_cols[TPR == 32 ? NORM_WARP_ROWS * 32 * NORM_EPT : 1];
   const int lane = threadIdx.x & (TPR - 1);
   const int sub = TPR == 32 ? threadIdx.x >> 5 : 0;
   const float inv_d = 1.f / (float)d;
@@ -335,40 +336,39 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
     }
   }
   let_next_kernel_start();
-  // this block's partial row: [dw | db]
-  float* pw = partial + (int64_t)blockIdx.x * 2 * d;
-  if constexpr (TPR == 32) {
-    constexpr int COLS = 32 * NORM_EPT;
+  // this block's columns, [dw | db], take the ring's place (nothing is on its way into it any more)
+  float* cols = reinterpret_cast<float*>(s_ring);
+  __syncthreads();
+  float* mine = cols + (TPR == 32 ? sub * 2 * d : 0);      // one warp a row: each of the eight has its own
 #pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll
-      for (int j = 0; j < PAIRS; ++j) {
-        const float2 v = pass == 0 ? aw[j] : ab[j];
-        s_cols[sub * COLS + col(2 * j)] = v.x;
-        s_cols[sub * COLS + col(2 * j + 1)] = v.y;
-      }
-      __syncthreads();
-      for (int c = threadIdx.x; c < d; c += 32 * NORM_WARP_ROWS) {
-        float a = 0.f;
-#pragma unroll
-        for (int r = 0; r < NORM_WARP_ROWS; ++r) a += s_cols[r * COLS + c];
-        pw[pass * d + c] = a;
-      }
-      __syncthreads();
+  for (int k = 0; k < NORM_EPT; ++k)
+    if (col(k) < d) {
+      mine[col(k)] = k & 1 ? aw[k / 2].y : aw[k / 2].x;
+      mine[d + col(k)] = k & 1 ? ab[k / 2].y : ab[k / 2].x;
     }
-  } else {
+  if constexpr (TPR == 32) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * d; c += THREADS) {
+      float a = cols[c];
 #pragma unroll
-    for (int j = 0; j < PAIRS; ++j) {
-      if (col(2 * j) < d) {
-        pw[col(2 * j)] = aw[j].x;
-        pw[d + col(2 * j)] = ab[j].x;
-      }
-      if (col(2 * j + 1) < d) {
-        pw[col(2 * j + 1)] = aw[j].y;
-        pw[d + col(2 * j + 1)] = ab[j].y;
-      }
+      for (int r = 1; r < NORM_WARP_ROWS; ++r) a += cols[r * 2 * d + c];
+      cols[c] = a;
     }
   }
+  // the cluster's blocks add up a share of the columns each, in rank order, into one partial row
+  cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+  const int CL = (int)cl.num_blocks();
+  cl.sync();
+  float* pw = partial + (int64_t)(blockIdx.x / CL) * 2 * d;
+  for (int c = (int)cl.block_rank() * THREADS + threadIdx.x; c < 2 * d; c += CL * THREADS) {
+    float a = cols[c];
+    if (CL > 1) {
+      a = 0.f;
+      for (int r = 0; r < CL; ++r) a += cl.map_shared_rank(cols, r)[c];
+    }
+    pw[c] = a;
+  }
+  cl.sync();                            // nobody leaves while its columns are read
 }
 
 // Column sums of `n_part` rows of `cols` values, in a fixed order: a block takes 32 columns, its 32 warps share the rows.
@@ -418,11 +418,24 @@ int norm_tpr(int d) {
   return tpr;
 }
 
-// Blocks of the backward pass: enough to fill the GPU, and no more than there are rows, since every block leaves a partial row.
-int norm_backward_blocks(int rows, int d) {
+// Blocks of the backward pass: enough to fill the GPU, no more than there are rows for, and whole clusters: neighbouring blocks
+// that add up their columns through each other's shared memory and leave one partial row.
+//   A row a block: the partial rows are as large as the problem, so eight blocks join (1000 x 1024: 18 -> 9.6 us, in pairs 15), or
+//     two of the larger ones, of which an SM holds few; very few rows do without (20 x 4096: 8.0 us, in pairs 10).
+//   Many rows a block: pairs (16384 x 2048: 47 -> 44 us, 8192 x 16384 f32: 367 -> 298; clusters of eight leave places for blocks empty:
+//     55 us, 65536 x 1024 73 in pairs and 97 in eights); one warp a row gains nothing (65536 x 512: 40 us either way).
+struct NormGrid {
+  int blocks, cluster;
+  int parts() const { return blocks / cluster; }      // partial rows they leave
+};
+NormGrid norm_backward_grid(int rows, int d) {
   const int tpr = norm_tpr(d), rpb = tpr == 32 ? NORM_WARP_ROWS : 1;
   const int want = (rows + rpb - 1) / rpb, cap = current_sms() * norm_backward_per_sm(tpr);
-  return want < cap ? want : cap;
+  NormGrid g{want < cap ? want : cap, 1};
+  if (want <= cap) g.cluster = want < 64 ? 1 : tpr <= 128 ? 8 : 2;
+  else if (tpr >= 64 && want >= 8 * cap) g.cluster = 2;
+  g.blocks -= g.blocks % g.cluster;
+  return g;
 }
 
 template <typename T, typename W, int VE, int NP, int NW>
@@ -454,24 +467,34 @@ cudaError_t forward_by_width(const NormArgs& a) {
 
 template <typename T, typename W, int VE, int TPR>
 cudaError_t backward_launch(const NormArgs& a) {
-  const int nblk = norm_backward_blocks(a.rows, a.d);
-  constexpr int threads = norm_backward_threads(TPR), smem = VE > 1 ? norm_ring(sizeof(T), TPR) * 2 * (NORM_EPT / VE) * threads * 16 : 0;
+  const NormGrid g = norm_backward_grid(a.rows, a.d);
+  constexpr int threads = norm_backward_threads(TPR), ring = VE > 1 ? norm_ring(sizeof(T), TPR) * 2 * (NORM_EPT / VE) * threads * 16 : 0;
+  constexpr int cols = 2 * threads * NORM_EPT * (int)sizeof(float);
+  constexpr int smem = ring > cols ? ring : cols;      // up to 192 KB
   auto kern = norm_backward_kernel<T, W, VE, TPR>;
-  if (smem > 0) {      // up to 192 KB: the opt-in is a per-device setting
-    static bool configured[64] = {};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev < 0 || dev >= 64 || !configured[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      if (e != cudaSuccess) return e;
-      if (dev >= 0 && dev < 64) configured[dev] = true;
-    }
+  static bool configured[64] = {};                     // the opt-in is a per-device setting
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev < 0 || dev >= 64 || !configured[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  kern<<<nblk, threads, smem, a.st>>>(static_cast<const T*>(a.dy), static_cast<const T*>(a.x), a.ldx, static_cast<const W*>(a.w), a.mean_in,
-                                      a.rstd_in, a.rows, a.d, static_cast<T*>(a.dx), a.partial);
-  const cudaError_t e = cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(g.blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = a.st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = g.cluster;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<const T*>(a.dy), static_cast<const T*>(a.x), a.ldx, static_cast<const W*>(a.w),
+                                           a.mean_in, a.rstd_in, a.rows, a.d, static_cast<T*>(a.dx), a.partial);
   if (e != cudaSuccess) return e;
-  return launch_sum_rows(a.partial, nblk, 2 * a.d, a.dw, a.d, a.db, a.st);
+  return launch_sum_rows(a.partial, g.parts(), 2 * a.d, a.dw, a.d, a.db, a.st);
 }
 
 template <typename T, typename W, int VE>
@@ -535,7 +558,7 @@ int grouter_layernorm_fwd(const void* x, int64_t ldx, const void* w, const void*
 
 size_t grouter_layernorm_bwd_workspace_bytes(int32_t rows, int32_t d) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
-  return (size_t)std::max(norm_backward_blocks(rows, d), 1) * 2 * d * sizeof(float);
+  return (size_t)std::max(norm_backward_grid(rows, d).parts(), 1) * 2 * d * sizeof(float);
 }
 
 int grouter_layernorm_bwd(const void* dy, const void* x, int64_t ldx, const void* w, const float* mean, const float* rstd, int32_t rows,
