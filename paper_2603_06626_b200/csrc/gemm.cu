@@ -300,6 +300,10 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   ptx::tc_fence_after();
   const uint32_t tmem_base = s_tmem_base;
   volatile int* abort_flag = &s_abort;
+  if constexpr (PLAIN) {              // set up while the kernel before was still ending (launch_tc); from here on its results are read
+    after_previous_kernel();
+    let_next_kernel_start();
+  }
 
   const int n_tiles = total_tiles<MODE>(p);
   // L2 residency: B (an expert's weights, or the row chunk every output tile of a weight gradient reads) is
@@ -888,6 +892,8 @@ static cudaError_t launch_tc(const Maps& m, const GemmParams& p, int grid, cudaS
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
+  if constexpr (MODE == MODE_DENSE || MODE == MODE_LINEAR)
+    return launch_dependent(kern, dim3(grid), dim3(GEMM_THREADS), GEMM_SMEM, st, m.A, m.B, m.C0, m.C1, m.C2, p);
   kern<<<grid, GEMM_THREADS, GEMM_SMEM, st>>>(m.A, m.B, m.C0, m.C1, m.C2, p);
   return cudaGetLastError();
 }

@@ -32,6 +32,7 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
   float2 acc[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc[i] = both(0.f);
+  after_previous_kernel();
   if (c < N) {
     const int64_t step = (int64_t)gridDim.y * DZ_LANES;
     for (int64_t t0 = (int64_t)blockIdx.y * DZ_LANES + rl; t0 < T; t0 += step * DZ_AHEAD) {
@@ -62,8 +63,8 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
       }
     }
   }
+  let_next_kernel_start();
   if constexpr (SUM) {
-    let_next_kernel_start();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       s_sum[rl][ct + 64 * i] = acc[i].x;
@@ -83,6 +84,8 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
 // out = sum of `pieces` matrices of n4 x 4 values, in order.
 template <typename T>
 __global__ void __launch_bounds__(256) sum_pieces_kernel(const float* __restrict__ in, int pieces, int64_t n4, T* __restrict__ out) {
+  after_previous_kernel();
+  let_next_kernel_start();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
     float4 a = __ldcs(reinterpret_cast<const float4*>(in) + i);
     for (int q = 1; q < pieces; ++q) {
@@ -150,12 +153,10 @@ template <int ACT>
 cudaError_t launch_dz_act(const void* dy, const void* z, int T, int N, void* dz, float* partial, dim3 grid, cudaStream_t st) {
   const __nv_bfloat16 *g = static_cast<const __nv_bfloat16*>(dy), *p = static_cast<const __nv_bfloat16*>(z);
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(dz);
-  if (partial) {
-    linear_dz_kernel<ACT, ACT != GROUTER_ACT_NONE, true><<<grid, DZ_THREADS, 0, st>>>(g, p, T, N, o, partial);
-  } else if constexpr (ACT != GROUTER_ACT_NONE) {      // without an activation there is nothing to write either
-    linear_dz_kernel<ACT, true, false><<<grid, DZ_THREADS, 0, st>>>(g, p, T, N, o, partial);
-  }
-  return cudaGetLastError();
+  if (partial) return launch_dependent(linear_dz_kernel<ACT, ACT != GROUTER_ACT_NONE, true>, grid, dim3(DZ_THREADS), 0, st, g, p, T, N, o, partial);
+  if constexpr (ACT != GROUTER_ACT_NONE)      // without an activation there is nothing to write either
+    return launch_dependent(linear_dz_kernel<ACT, true, false>, grid, dim3(DZ_THREADS), 0, st, g, p, T, N, o, partial);
+  return cudaSuccess;
 }
 cudaError_t launch_dz(int act, const void* dy, const void* z, int T, int N, void* dz, float* partial, int row_blocks, cudaStream_t st) {
   const dim3 grid(cdiv(N, DZ_COLS), row_blocks);
@@ -256,9 +257,11 @@ int grouter_linear_bwd(const void* dy, const void* x, const void* W, const void*
       if (pieces > 1) {
         const int64_t n4 = (int64_t)N * K / 4, want = (n4 + 255) / 256, cap = (int64_t)current_sms() * 8;
         const int grid = (int)(want < cap ? want : cap), real = cdiv(T, chunk);      // whole 64-token steps may leave the last piece out
-        if (dW_dtype == GROUTER_F32) sum_pieces_kernel<float><<<grid, 256, 0, st>>>(out, real, n4, static_cast<float*>(dW));
-        else sum_pieces_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(out, real, n4, static_cast<__nv_bfloat16*>(dW));
-        if (cudaGetLastError() != cudaSuccess) return GROUTER_ERR_CUDA;
+        const cudaError_t e =
+            dW_dtype == GROUTER_F32
+                ? launch_dependent(sum_pieces_kernel<float>, dim3(grid), dim3(256), 0, st, out, real, n4, static_cast<float*>(dW))
+                : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, out, real, n4, static_cast<__nv_bfloat16*>(dW));
+        if (e != cudaSuccess) return GROUTER_ERR_CUDA;
       }
     }
   }

@@ -77,6 +77,8 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
   ptx::tc_fence_after();
   const uint32_t tmem_base = s_tmem_base;
   volatile int* abort_flag = &s_abort;
+  after_previous_kernel();           // set up while it was still ending; from here on its results are read
+  let_next_kernel_start();
 
   if (warp == 0) {
     if (lane == 0) {
@@ -267,12 +269,14 @@ cudaError_t small_launch(const LinearGemm& g, int splits, cudaStream_t st) {
   cfg.blockDim = dim3(LS_THREADS);
   cfg.dynamicSmemBytes = ls_smem(TN);
   cfg.stream = st;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = splits;
-  at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute at[2] = {};
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = splits;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kern, a, b, p);
 }
 

@@ -380,6 +380,7 @@ __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* __restrict_
   const int c = blockIdx.x * 32 + lane;
   float a = 0.f;
   after_previous_kernel();
+  let_next_kernel_start();
   if (c < cols) {
 #pragma unroll 16
     for (int r = warp; r < n_part; r += 32) a += partial[(int64_t)r * cols + c];
