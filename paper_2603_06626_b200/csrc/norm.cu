@@ -9,12 +9,12 @@
 // Both passes touch every element once and are bound by HBM, but only if they are lean: at 6.4 TB/s an SM has some 20 (forward)
 // and 30 (backward) instruction slots for an element of bf16, so the arithmetic is done two elements to an instruction (f32x2).
 // Sums are taken in fp32, the variance from the centred values (never as a difference of large sums).
-// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 91 us (5.9 TB/s), 65536 x 512 25 us (5.3);
+// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 84 us (6.4 TB/s), 65536 x 512 25 us (5.4);
 // backward with both kernels 16384 x 4096 bf16 76 us (5.3), 16384 x 2048 44 us (4.6), 8192 x 4096 f32 75 us (5.4), 8192 x 16384 f32
-// 299 us (5.4).  Rows that are not 16-byte aligned go element by element: 16384 x 4095 bf16 86 us forward (3.1 TB/s), 119 us
-// backward (3.4).
-//   Forward: a row lies in the registers of one warp as it was loaded (up to 256 bytes a lane, eight KB a row in flight), or of
-//     several for wide rows; nothing is kept from row to row.
+// 299 us (5.4).  Rows that are not 16-byte aligned go by pairs, or by single elements where even those do not fit: 16384 x 4094
+// bf16 55 us forward, 102 us backward, 16384 x 4095 87 and 119 us.
+//   Forward: a row lies in the registers of as many warps as hold it in a few accesses a lane, as it was loaded; nothing is kept
+//     from row to row.
 //   Backward: the running dw and db of a column have to stay with one thread, so a row is spread over enough threads for 16
 //     elements each; blocks are resident and walk over the rows (the coming ones on their way into shared memory), every cluster
 //     of them writes one partial row, and a second small kernel adds those up in a fixed order (bit-reproducible, no atomics).
@@ -34,12 +34,13 @@ __device__ __forceinline__ void load_weights(const W* __restrict__ w, int c, flo
   if constexpr (VE == 1) {
     f[0] = to_f32(__ldg(w + c));
   } else {
-    constexpr int PER = VE * sizeof(W) >= 16 ? 16 / (int)sizeof(W) : VE;       // 16- or 8-byte accesses
+    constexpr int PER = VE * sizeof(W) >= 16 ? 16 / (int)sizeof(W) : VE;       // accesses of 16, 8 or 4 bytes
 #pragma unroll
     for (int q = 0; q < VE; q += PER) {
       Pack<W, PER> p;
       if constexpr (PER * sizeof(W) == 16) *reinterpret_cast<uint4*>(&p) = __ldg(reinterpret_cast<const uint4*>(w + c + q));
-      else *reinterpret_cast<uint2*>(&p) = __ldg(reinterpret_cast<const uint2*>(w + c + q));
+      else if constexpr (PER * sizeof(W) == 8) *reinterpret_cast<uint2*>(&p) = __ldg(reinterpret_cast<const uint2*>(w + c + q));
+      else *reinterpret_cast<uint32_t*>(&p) = __ldg(reinterpret_cast<const uint32_t*>(w + c + q));
       const Pack<W, PER> one[1] = {p};
 #pragma unroll
       for (int i = 0; i < PER; i += 2) {
@@ -72,7 +73,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& half) {
 }
 
 // Nothing about these registers is known from here on: the compiler converts them again where they are used next, instead of
-// carrying twice as many converted values along (164 registers a thread, where the row as loaded and the arithmetic take half).
+// carrying twice as many converted values along.
 template <typename T, int VE, int NP>
 __device__ __forceinline__ void forget(Pack<T, VE> (&p)[NP]) {
   if constexpr (VE > 1 && sizeof(T) == 2) {
@@ -123,7 +124,6 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
       if (n * (32 * NW) + at < d) s[0] += to_f32(p[n].v[0]);
   }
   row_sums<NW, 1>(s, red, half);
-  forget<T, VE, NP>(p);
   const float mean = s[0] * inv_d;
   float q[1] = {0.f};
   if constexpr (VE > 1) {
@@ -148,7 +148,6 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
       }
   }
   row_sums<NW, 1>(q, red, half);
-  forget<T, VE, NP>(p);
   const float rstd = 1.f / sqrtf(q[0] * inv_d + eps);
   T* yr = y + row * d;
 #pragma unroll
@@ -193,14 +192,15 @@ __host__ __device__ constexpr int norm_backward_per_sm(int tpr) { return tpr >= 
 __host__ __device__ constexpr int norm_ring(int bytes, int tpr) { return tpr == 1024 ? (bytes == 2 ? 3 : 1) : bytes == 2 ? 4 : 3; }
 
 // Every thread copies its own elements of the coming rows into shared memory and reads back only those, so the ring needs no
-// barrier: the one barrier a row is that of its two sums.  VE = 1 (rows that are not 16-byte aligned): plain loads, no ring.
+// barrier: the one barrier a row is that of its two sums.  Rows that are not 16-byte aligned: plain loads, no ring
+// (one of 4-byte copies: 8192 x 4095 f32 78 -> 91 us).
 template <typename T, typename W, int VE, int TPR>
 __global__ void __launch_bounds__(norm_backward_threads(TPR), norm_backward_per_sm(TPR))
 norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t ldx, const W* __restrict__ w, const float* __restrict__ mean_in,
                      const float* __restrict__ rstd_in, int rows, int d, T* __restrict__ dx, float* __restrict__ partial) {
   constexpr int NV = NORM_EPT / VE, PAIRS = NORM_EPT / 2;
   constexpr int RPB = TPR == 32 ? NORM_WARP_ROWS : 1, THREADS = norm_backward_threads(TPR);
-  constexpr bool RING = VE > 1;
+  constexpr bool RING = VE * sizeof(T) == 16;
   constexpr int S = norm_ring(sizeof(T), TPR);
   constexpr bool HOLD = TPR < 1024;     // the weights stay in registers (1024 threads have 64 each: there they are read from L1)
   extern __shared__ uint4 s_ring[];     // RING: [S][x, dy][NV][THREADS]; at the end this block's columns, [dw | db]
@@ -448,28 +448,33 @@ cudaError_t forward_launch(const NormArgs& a) {
   return cudaGetLastError();
 }
 
-// One warp a row while its lanes hold it in at most 16 accesses each, then as many warps as that takes.
+// One warp a row while its lanes hold it in at most MOST accesses each, then up to 16 warps, then what is needed of both.
+template <typename T, typename W, int VE, int MOST, int NP = 1, int NW = 1>
+cudaError_t forward_spread(const NormArgs& a) {
+  constexpr int HOLDS = NP * NW * 32 * VE;
+  if constexpr (HOLDS < NORM_MAX_D) {
+    if (a.d > HOLDS) {
+      if constexpr (NP < MOST || (NW == 16 && NP < 16)) return forward_spread<T, W, VE, MOST, 2 * NP, NW>(a);
+      else return forward_spread<T, W, VE, MOST, NP, 2 * NW>(a);
+    }
+  }
+  return forward_launch<T, W, VE, NP, NW>(a);
+}
+
+// Four 16-byte accesses a lane (16384 x 4096 bf16: 44.6 us, with sixteen 52.3, with two 52.7), two where the whole matrix is small
+// and the time is that of a row (1 x 4096: 2.6 against 3.0 us, 1024 x 2048 3.3 against 4.0, but 1024 x 4096 5.3 against 4.3);
+// eight of the smaller ones (16384 x 4094: 54 us, with four 79).
+constexpr int64_t NORM_SMALL = 1 << 21;
 template <typename T, typename W, int VE>
 cudaError_t forward_by_width(const NormArgs& a) {
-  const int per_lane = (a.d + 32 * VE - 1) / (32 * VE);
-  if (per_lane <= 1) return forward_launch<T, W, VE, 1, 1>(a);
-  if (per_lane <= 2) return forward_launch<T, W, VE, 2, 1>(a);
-  if (per_lane <= 4) return forward_launch<T, W, VE, 4, 1>(a);
-  if (per_lane <= 8) return forward_launch<T, W, VE, 8, 1>(a);
-  if (per_lane <= 16) return forward_launch<T, W, VE, 16, 1>(a);
-  if (per_lane <= 32) return forward_launch<T, W, VE, 16, 2>(a);
-  if (per_lane <= 64) return forward_launch<T, W, VE, 16, 4>(a);
-  if constexpr (VE < 8) {      // 16384 elements in 64 accesses of eight
-    if (per_lane <= 128) return forward_launch<T, W, VE, 16, 8>(a);
-  }
-  if constexpr (VE == 1) return per_lane <= 256 ? forward_launch<T, W, VE, 16, 16>(a) : forward_launch<T, W, VE, 16, 32>(a);
-  return cudaErrorInvalidValue;
+  if constexpr (VE * sizeof(T) < 16) return forward_spread<T, W, VE, 8>(a);
+  else return (int64_t)a.rows * a.d <= NORM_SMALL ? forward_spread<T, W, VE, 2>(a) : forward_spread<T, W, VE, 4>(a);
 }
 
 template <typename T, typename W, int VE, int TPR>
 cudaError_t backward_launch(const NormArgs& a) {
   const NormGrid g = norm_backward_grid(a.rows, a.d);
-  constexpr int threads = norm_backward_threads(TPR), ring = VE > 1 ? norm_ring(sizeof(T), TPR) * 2 * (NORM_EPT / VE) * threads * 16 : 0;
+  constexpr int threads = norm_backward_threads(TPR), ring = VE == vec16<T>() ? norm_ring(sizeof(T), TPR) * 2 * (NORM_EPT / VE) * threads * 16 : 0;
   constexpr int cols = 2 * threads * NORM_EPT * (int)sizeof(float);
   constexpr int smem = ring > cols ? ring : cols;      // up to 192 KB
   auto kern = norm_backward_kernel<T, W, VE, TPR>;
@@ -515,14 +520,21 @@ cudaError_t norm_by_width(const NormArgs& a) {
   if constexpr (BACKWARD) return backward_by_width<T, W, VE>(a);
   else return forward_by_width<T, W, VE>(a);
 }
+template <bool BACKWARD, typename T, int VE>
+cudaError_t norm_by_weights(const NormArgs& a) {
+  return a.w_f32 ? norm_by_width<BACKWARD, T, float, VE>(a) : norm_by_width<BACKWARD, T, __nv_bfloat16, VE>(a);
+}
 template <bool BACKWARD, typename T>
 cudaError_t norm_by_type(const NormArgs& a) {
-  // 16-byte accesses where every row of every activation and the weights start on a 16-byte boundary, single elements otherwise
-  constexpr int VE = vec16<T>();
-  const bool vec = a.d % VE == 0 && a.ldx % VE == 0 && aligned_to(a.x, 16) && aligned_to(BACKWARD ? a.dy : a.y, 16) &&
-                   (!BACKWARD || aligned_to(a.dx, 16)) && aligned_to(a.w, 16) && aligned_to(a.b, 16);
-  if (a.w_f32) return vec ? norm_by_width<BACKWARD, T, float, VE>(a) : norm_by_width<BACKWARD, T, float, 1>(a);
-  return vec ? norm_by_width<BACKWARD, T, __nv_bfloat16, VE>(a) : norm_by_width<BACKWARD, T, __nv_bfloat16, 1>(a);
+  // accesses of VE elements where every row of every activation and the weights start on a boundary of them
+  auto fits = [&](int ve) {
+    const size_t b = ve * sizeof(T), wb = std::min<size_t>(ve * (a.w_f32 ? 4 : 2), 16);
+    return a.d % ve == 0 && a.ldx % ve == 0 && aligned_to(a.x, b) && aligned_to(BACKWARD ? a.dy : a.y, b) && (!BACKWARD || aligned_to(a.dx, b)) &&
+           aligned_to(a.w, wb) && aligned_to(a.b, wb);
+  };
+  if (fits(vec16<T>())) return norm_by_weights<BACKWARD, T, vec16<T>()>(a);
+  if (fits(2)) return norm_by_weights<BACKWARD, T, 2>(a);
+  return norm_by_weights<BACKWARD, T, 1>(a);
 }
 template <bool BACKWARD>
 cudaError_t norm_dispatch(const NormArgs& a, int dtype) {

@@ -81,8 +81,12 @@ __device__ __forceinline__ Pack<T, VE> ld_pack(const T* p) {
   Pack<T, VE> r;
   if constexpr (VE * sizeof(T) == 16) {
     *reinterpret_cast<uint4*>(&r) = ld_stream16(p);
+  } else if constexpr (VE * sizeof(T) == 8) {
+    *reinterpret_cast<uint2*>(&r) = __ldg(reinterpret_cast<const uint2*>(p));
+  } else if constexpr (VE == 2) {
+    *reinterpret_cast<uint32_t*>(&r) = __ldg(reinterpret_cast<const uint32_t*>(p));
   } else {
-    static_assert(VE == 1, "whole 16-byte accesses or single elements");
+    static_assert(VE == 1, "whole 16-byte accesses, pairs or single elements");
     r.v[0] = __ldg(p);
   }
   return r;

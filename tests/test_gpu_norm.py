@@ -162,3 +162,30 @@ def test_gradient_against_differences_of_the_kernel():
     ana = (dx.double() * u.double()).sum().item()
     scale = (dx.double() * u.double()).abs().sum().item()
     assert abs(num - ana) <= 1e-3 * scale
+
+
+# rows on boundaries of two elements only, and of more where the weights are not; matrices on both sides of 2^21 elements, which is
+# where aligned rows go from two accesses a lane to four: every number of warps a row
+PAIRS = [(1, 2, "bf16", "bf16", 0, 2), (37, 66, "bf16", "f32", 0, 0), (19, 514, "f32", "bf16", 0, 0), (300, 1022, "bf16", "bf16", 2, 4),
+         (65, 1026, "f32", "f32", 6, 2), (40, 2050, "bf16", "bf16", 0, 0), (17, 4094, "f32", "bf16", 0, 0), (7, 8190, "bf16", "f32", 8, 0),
+         (5, 8194, "f32", "f32", 0, 0), (3, 16382, "bf16", "bf16", 0, 0), (2, 16382, "f32", "bf16", 0, 0), (4, 4095, "bf16", "bf16", 0, 0),
+         (4, 4097, "f32", "f32", 0, 0)]
+SPREADS = [(2049, 1024, "bf16", "bf16", 0, 0), (2048, 1024, "f32", "f32", 0, 0), (2051, 1032, "bf16", "f32", 8, 0), (1025, 2048, "f32", "bf16", 0, 0),
+           (514, 4104, "bf16", "bf16", 0, 0), (257, 8200, "f32", "f32", 0, 0), (129, 16384, "bf16", "bf16", 0, 0), (130, 16384, "f32", "f32", 0, 0),
+           (9, 1024, "f32", "bf16", 0, 0), (9, 4100, "f32", "f32", 0, 0), (9, 8192, "bf16", "bf16", 0, 0)]
+
+
+@pytest.mark.parametrize("T,d,ty,wt,pad,shift", PAIRS + SPREADS)
+def test_pairs_and_spreads(T, d, ty, wt, pad, shift):
+    test_both_passes(T, d, ty, wt, pad, shift)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+def test_pairs_of_activations_over_unaligned_weights(ty):
+    rng = np.random.default_rng(2)
+    x = _matrix(rng, 33, 514, ty, 2, 2)
+    dy = _matrix(rng, 33, 514, ty, 0, 2)
+    for first in (1, 2):
+        w = torch.randn(514 + first, device="cuda:0").to(TYPES[ty])[first:]
+        _check_forward(x, w, w, ty)
+        _check_backward(dy, x, w, ty)
