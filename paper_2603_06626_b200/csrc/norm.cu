@@ -9,15 +9,16 @@
 // Both passes touch every element once and are bound by HBM, but only if they are lean: at 6.4 TB/s an SM has some 20 (forward)
 // and 30 (backward) instruction slots for an element of bf16, so the arithmetic is done two elements to an instruction (f32x2).
 // Sums are taken in fp32, the variance from the centred values (never as a difference of large sums).
-// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 84 us (6.4 TB/s), 65536 x 512 25 us (5.4);
+// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 84 us (6.4 TB/s), 65536 x 512 22 us (6.1);
 // backward with both kernels 16384 x 4096 bf16 76 us (5.3), 16384 x 2048 44 us (4.6), 8192 x 4096 f32 75 us (5.4), 8192 x 16384 f32
 // 299 us (5.4).  Rows that are not 16-byte aligned go by pairs, or by single elements where even those do not fit: 16384 x 4094
 // bf16 55 us forward, 102 us backward, 16384 x 4095 87 and 119 us.
-//   Forward: a row lies in the registers of as many warps as hold it in a few accesses a lane, as it was loaded; nothing is kept
-//     from row to row.
+//   Forward: a row lies in the registers of as many lanes (a quarter of a warp to 32 warps) as hold it in a few accesses each, as it
+//     was loaded; nothing is kept from row to row.
 //   Backward: the running dw and db of a column have to stay with one thread, so a row is spread over enough threads for 16
-//     elements each; blocks are resident and walk over the rows (the coming ones on their way into shared memory), every cluster
-//     of them writes one partial row, and a second small kernel adds those up in a fixed order (bit-reproducible, no atomics).
+//     elements each (eight for a row of 128: 262144 x 128 bf16 40 us, with a warp 87); blocks are resident and walk over the rows (the
+//     coming ones on their way into shared memory), every cluster of them writes one partial row, and a second small kernel adds
+//     those up in a fixed order (bit-reproducible, no atomics).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -52,12 +53,13 @@ __device__ __forceinline__ void load_weights(const W* __restrict__ w, int c, flo
   }
 }
 
-// Sums of N values over the NW warps of a row, the same value in each of their threads.  `red` has two halves used in turn: a warp
+// Sums of N values over the LANES threads of a row, the same value in each of them.  `red` has two halves used in turn: a warp
 // may still read one while the others already write the next sums into the other, and the barrier in between keeps the third away.
-template <int NW, int N>
+template <int LANES, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& half) {
+  constexpr int NW = LANES / 32;
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = lanes_sum<32>(v[n]);
+  for (int n = 0; n < N; ++n) v[n] = lanes_sum<(LANES < 32 ? LANES : 32)>(v[n]);
   if constexpr (NW > 1) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float* buf = red + half * (N * 32);
@@ -86,24 +88,25 @@ __device__ __forceinline__ void forget(Pack<T, VE> (&p)[NP]) {
   }
 }
 
-// ---- forward: NW warps a row, NP accesses of VE elements a lane ----
-__host__ __device__ constexpr int norm_forward_threads(int nw) { return nw == 1 ? 128 : 32 * nw; }
+// ---- forward: LANES threads a row, NP accesses of VE elements each ----
+__host__ __device__ constexpr int norm_forward_threads(int lanes) { return lanes <= 32 ? 128 : lanes; }
 
-template <typename T, typename W, int VE, int NP, int NW>
-__global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(const T* __restrict__ x, int64_t ldx, const W* __restrict__ w,
+template <typename T, typename W, int VE, int NP, int LANES>
+__global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kernel(const T* __restrict__ x, int64_t ldx, const W* __restrict__ w,
                                                                                 const W* __restrict__ b, int rows, int d, float eps,
                                                                                 T* __restrict__ y, float* __restrict__ mean_out,
                                                                                 float* __restrict__ rstd_out) {
-  constexpr int RPB = NW == 1 ? norm_forward_threads(1) / 32 : 1;
+  constexpr int RPB = norm_forward_threads(LANES) / LANES;
   __shared__ float red[2 * 32];
-  const int64_t row = (int64_t)blockIdx.x * RPB + (NW == 1 ? threadIdx.x >> 5 : 0);
-  const int at = NW == 1 ? threadIdx.x & 31 : threadIdx.x;
-  if (row >= rows) return;                 // whole warps, and whole blocks where a row has several
+  const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LANES;
+  const int at = threadIdx.x & (LANES - 1);
+  if (LANES >= 32 && row >= rows) return;  // whole warps, and whole blocks where a row has several
+  if (LANES < 32 && row >= rows) d = 0;    // stays for the sums of the rows beside it in the warp
   const T* xr = x + row * ldx;
   Pack<T, VE> p[NP];
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
-    const int c = (n * (32 * NW) + at) * VE;
+    const int c = (n * LANES + at) * VE;
     if (c < d) p[n] = ld_pack<T, VE>(xr + c);
   }
   const float inv_d = 1.f / (float)d;
@@ -113,7 +116,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
     float2 s2 = both(0.f);
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if ((n * (32 * NW) + at) * VE < d) {
+      if ((n * LANES + at) * VE < d) {
 #pragma unroll
         for (int i = 0; i < VE; i += 2) s2 = add2(s2, pair_at(p, (n * VE + i) / 2));
       }
@@ -121,9 +124,9 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
   } else {
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if (n * (32 * NW) + at < d) s[0] += to_f32(p[n].v[0]);
+      if (n * LANES + at < d) s[0] += to_f32(p[n].v[0]);
   }
-  row_sums<NW, 1>(s, red, half);
+  row_sums<LANES, 1>(s, red, half);
   const float mean = s[0] * inv_d;
   float q[1] = {0.f};
   if constexpr (VE > 1) {
@@ -131,7 +134,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
     const float2 m2 = both(-mean);
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if ((n * (32 * NW) + at) * VE < d) {
+      if ((n * LANES + at) * VE < d) {
 #pragma unroll
         for (int i = 0; i < VE; i += 2) {
           const float2 c2 = add2(pair_at(p, (n * VE + i) / 2), m2);
@@ -142,17 +145,17 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
   } else {
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if (n * (32 * NW) + at < d) {
+      if (n * LANES + at < d) {
         const float c1 = to_f32(p[n].v[0]) - mean;
         q[0] += c1 * c1;
       }
   }
-  row_sums<NW, 1>(q, red, half);
+  row_sums<LANES, 1>(q, red, half);
   const float rstd = 1.f / sqrtf(q[0] * inv_d + eps);
   T* yr = y + row * d;
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
-    const int c = (n * (32 * NW) + at) * VE;
+    const int c = (n * LANES + at) * VE;
     if (c < d) {
       float wl[VE], bl[VE], o[VE];
       load_weights<W, VE>(w, c, wl);
@@ -176,7 +179,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
       st_pack<T, VE>(yr + c, o);
     }
   }
-  if (at == 0) {
+  if (at == 0 && row < rows) {
     if (mean_out) mean_out[row] = mean;
     if (rstd_out) rstd_out[row] = rstd;
   }
@@ -184,8 +187,7 @@ __global__ void __launch_bounds__(norm_forward_threads(NW)) norm_forward_kernel(
 
 // ---- backward: TPR threads a row, NORM_EPT elements each ----
 constexpr int NORM_EPT = 16;
-constexpr int NORM_WARP_ROWS = 8;       // rows of a block that gives every row one warp
-__host__ __device__ constexpr int norm_backward_threads(int tpr) { return tpr == 32 ? 32 * NORM_WARP_ROWS : tpr; }
+__host__ __device__ constexpr int norm_backward_threads(int tpr) { return tpr <= 32 ? 256 : tpr; }
 __host__ __device__ constexpr int norm_backward_per_sm(int tpr) { return tpr >= 512 ? 1 : 512 / norm_backward_threads(tpr); }
 // Rows (x and dy) that a block has on their way or in use: what keeps HBM busy (rows held one ahead in registers were 32 KB an SM
 // and 3.6 TB/s).  As many as shared memory takes: an SM holds 512 threads' rows, 1024 for the widest.
@@ -199,14 +201,14 @@ __global__ void __launch_bounds__(norm_backward_threads(TPR), norm_backward_per_
 norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t ldx, const W* __restrict__ w, const float* __restrict__ mean_in,
                      const float* __restrict__ rstd_in, int rows, int d, T* __restrict__ dx, float* __restrict__ partial) {
   constexpr int NV = NORM_EPT / VE, PAIRS = NORM_EPT / 2;
-  constexpr int RPB = TPR == 32 ? NORM_WARP_ROWS : 1, THREADS = norm_backward_threads(TPR);
+  constexpr int THREADS = norm_backward_threads(TPR), RPB = THREADS / TPR;
   constexpr bool RING = VE * sizeof(T) == 16;
   constexpr int S = norm_ring(sizeof(T), TPR);
   constexpr bool HOLD = TPR < 1024;     // the weights stay in registers (1024 threads have 64 each: there they are read from L1)
   extern __shared__ uint4 s_ring[];     // RING: [S][x, dy][NV][THREADS]; at the end this block's columns, [dw | db]
   __shared__ float red[2 * 2 * 32];
   const int lane = threadIdx.x & (TPR - 1);
-  const int sub = TPR == 32 ? threadIdx.x >> 5 : 0;
+  const int sub = threadIdx.x / TPR;
   const float inv_d = 1.f / (float)d;
   // a thread's elements in pairs: pair j holds elements 2j and 2j + 1 of its [NV][VE]; columns beyond d hold zeros throughout
   auto col = [&](int k) { return ((k / VE) * TPR + lane) * VE + k % VE; };
@@ -264,21 +266,25 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
     for (int s = 0; s < S; ++s) fetch(row + s * step, s);
   }
   int half = 0, s_at = 0;
-  for (; row < rows; row += step) {
-    const float mean = nmean, rstd = nrstd;
+  // rows that share a warp stay together for their sums: those past the last row hold zeros
+  const int behind = TPR < 32 ? sub & (32 / TPR - 1) : 0;
+  for (; row - behind < rows; row += step) {
+    const bool live = TPR >= 32 || row < rows;
+    const float mean = live ? nmean : 0.f, rstd = live ? nrstd : 0.f;
     stats(row + step);
     Pack<T, VE> px[NV], pg[NV];
     auto take = [&]() {                 // this row's elements
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
         if constexpr (RING) {
-          *reinterpret_cast<uint4*>(&px[n]) = *slot(s_at, 0, n);
-          *reinterpret_cast<uint4*>(&pg[n]) = *slot(s_at, 1, n);
+          const uint4 zeros = make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(&px[n]) = live ? *slot(s_at, 0, n) : zeros;
+          *reinterpret_cast<uint4*>(&pg[n]) = live ? *slot(s_at, 1, n) : zeros;
         } else {
           const int c = (n * TPR + lane) * VE;
 #pragma unroll
           for (int i = 0; i < VE; ++i) px[n].v[i] = pg[n].v[i] = from_f32<T>(0.f);
-          if (c < d) {
+          if (c < d && live) {
             px[n] = ld_pack<T, VE>(x + row * ldx + c);
             pg[n] = ld_pack<T, VE>(dy + row * d + c);
           }
@@ -305,7 +311,7 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
       s2 = fma2(g, xc[j], s2);
     }
     float s[2] = {s1.x + s1.y, s2.x + s2.y};
-    row_sums<TPR / 32, 2>(s, red, half);
+    row_sums<TPR, 2>(s, red, half);
     // dx = rstd g w - rstd mean(g) - (x - mean) rstd^3 mean(g (x - mean))
     const float2 r = both(rstd), c1 = both(-s[0] * inv_d * rstd), c2 = both(-s[1] * inv_d * rstd * rstd * rstd);
     if constexpr (!HOLD) {
@@ -326,9 +332,7 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = (n * TPR + lane) * VE;
-      if (c < d) {
-        st_pack<T, VE>(dr + c, o + n * VE);
-      }
+      if (c < d && live) st_pack<T, VE>(dr + c, o + n * VE);
     }
     if constexpr (RING) {
       fetch(row + S * step, s_at);
@@ -339,19 +343,19 @@ norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, int64_t 
   // this block's columns, [dw | db], take the ring's place (nothing is on its way into it any more)
   float* cols = reinterpret_cast<float*>(s_ring);
   __syncthreads();
-  float* mine = cols + (TPR == 32 ? sub * 2 * d : 0);      // one warp a row: each of the eight has its own
+  float* mine = cols + sub * 2 * d;      // each of the rows that the block works on at a time has its own
 #pragma unroll
   for (int k = 0; k < NORM_EPT; ++k)
     if (col(k) < d) {
       mine[col(k)] = k & 1 ? aw[k / 2].y : aw[k / 2].x;
       mine[d + col(k)] = k & 1 ? ab[k / 2].y : ab[k / 2].x;
     }
-  if constexpr (TPR == 32) {
+  if constexpr (RPB > 1) {
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * d; c += THREADS) {
       float a = cols[c];
 #pragma unroll
-      for (int r = 1; r < NORM_WARP_ROWS; ++r) a += cols[r * 2 * d + c];
+      for (int r = 1; r < RPB; ++r) a += cols[r * 2 * d + c];
       cols[c] = a;
     }
   }
@@ -414,7 +418,7 @@ struct NormArgs {
 
 // Threads that hold a row of d elements in the backward pass.
 int norm_tpr(int d) {
-  int tpr = 32;
+  int tpr = 8;
   while (tpr * NORM_EPT < d) tpr *= 2;
   return tpr;
 }
@@ -430,7 +434,7 @@ struct NormGrid {
   int parts() const { return blocks / cluster; }      // partial rows they leave
 };
 NormGrid norm_backward_grid(int rows, int d) {
-  const int tpr = norm_tpr(d), rpb = tpr == 32 ? NORM_WARP_ROWS : 1;
+  const int tpr = norm_tpr(d), rpb = norm_backward_threads(tpr) / tpr;
   const int want = (rows + rpb - 1) / rpb, cap = current_sms() * norm_backward_per_sm(tpr);
   NormGrid g{want < cap ? want : cap, 1};
   if (want <= cap) g.cluster = want < 64 ? 1 : tpr <= 128 ? 8 : 2;
@@ -439,36 +443,38 @@ NormGrid norm_backward_grid(int rows, int d) {
   return g;
 }
 
-template <typename T, typename W, int VE, int NP, int NW>
+template <typename T, typename W, int VE, int NP, int LANES>
 cudaError_t forward_launch(const NormArgs& a) {
-  constexpr int RPB = NW == 1 ? norm_forward_threads(1) / 32 : 1;
-  norm_forward_kernel<T, W, VE, NP, NW><<<(a.rows + RPB - 1) / RPB, norm_forward_threads(NW), 0, a.st>>>(
+  constexpr int THREADS = norm_forward_threads(LANES), RPB = THREADS / LANES;
+  norm_forward_kernel<T, W, VE, NP, LANES><<<(a.rows + RPB - 1) / RPB, THREADS, 0, a.st>>>(
       static_cast<const T*>(a.x), a.ldx, static_cast<const W*>(a.w), static_cast<const W*>(a.b), a.rows, a.d, a.eps, static_cast<T*>(a.y), a.mean_out,
       a.rstd_out);
   return cudaGetLastError();
 }
 
-// One warp a row while its lanes hold it in at most MOST accesses each, then up to 16 warps, then what is needed of both.
-template <typename T, typename W, int VE, int MOST, int NP = 1, int NW = 1>
+// Up to FEW accesses a lane while a quarter of a warp holds a row, then more lanes; a warp's lanes then take up to MOST, more warps
+// follow up to 16, and what is still needed of both.
+template <typename T, typename W, int VE, int MOST, int FEW, int NP = 1, int LANES = 8>
 cudaError_t forward_spread(const NormArgs& a) {
-  constexpr int HOLDS = NP * NW * 32 * VE;
+  constexpr int HOLDS = NP * LANES * VE;
   if constexpr (HOLDS < NORM_MAX_D) {
     if (a.d > HOLDS) {
-      if constexpr (NP < MOST || (NW == 16 && NP < 16)) return forward_spread<T, W, VE, MOST, 2 * NP, NW>(a);
-      else return forward_spread<T, W, VE, MOST, NP, 2 * NW>(a);
+      if constexpr (NP < FEW || (LANES >= 32 && (NP < MOST || (LANES == 512 && NP < 16)))) return forward_spread<T, W, VE, MOST, FEW, 2 * NP, LANES>(a);
+      else return forward_spread<T, W, VE, MOST, FEW, NP, 2 * LANES>(a);
     }
   }
-  return forward_launch<T, W, VE, NP, NW>(a);
+  return forward_launch<T, W, VE, NP, LANES>(a);
 }
 
-// Four 16-byte accesses a lane (16384 x 4096 bf16: 44.6 us, with sixteen 52.3, with two 52.7), two where the whole matrix is small
-// and the time is that of a row (1 x 4096: 2.6 against 3.0 us, 1024 x 2048 3.3 against 4.0, but 1024 x 4096 5.3 against 4.3);
-// eight of the smaller ones (16384 x 4094: 54 us, with four 79).
+// Four 16-byte accesses a lane (16384 x 4096 bf16: 44.6 us, with sixteen 52.3, with two 52.7; 65536 x 128 7.9 us, with one access of 16
+// lanes 9.4, of a warp 16), and fewer, in more lanes, where the whole matrix is small and the time is that of a row (1 x 4096: 2.6
+// against 3.0 us, 1024 x 2048 3.3 against 4.0, but 1024 x 4096 5.3 against 4.3); eight of the smaller ones (16384 x 4094: 54 us, with
+// four 79).
 constexpr int64_t NORM_SMALL = 1 << 21;
 template <typename T, typename W, int VE>
 cudaError_t forward_by_width(const NormArgs& a) {
-  if constexpr (VE * sizeof(T) < 16) return forward_spread<T, W, VE, 8>(a);
-  else return (int64_t)a.rows * a.d <= NORM_SMALL ? forward_spread<T, W, VE, 2>(a) : forward_spread<T, W, VE, 4>(a);
+  if constexpr (VE * sizeof(T) < 16) return forward_spread<T, W, VE, 8, 4>(a);
+  else return (int64_t)a.rows * a.d <= NORM_SMALL ? forward_spread<T, W, VE, 2, 1>(a) : forward_spread<T, W, VE, 4, 4>(a);
 }
 
 template <typename T, typename W, int VE, int TPR>
@@ -506,6 +512,8 @@ cudaError_t backward_launch(const NormArgs& a) {
 template <typename T, typename W, int VE>
 cudaError_t backward_by_width(const NormArgs& a) {
   switch (norm_tpr(a.d)) {
+    case 8: return backward_launch<T, W, VE, 8>(a);
+    case 16: return backward_launch<T, W, VE, 16>(a);
     case 32: return backward_launch<T, W, VE, 32>(a);
     case 64: return backward_launch<T, W, VE, 64>(a);
     case 128: return backward_launch<T, W, VE, 128>(a);

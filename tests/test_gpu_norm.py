@@ -189,3 +189,32 @@ def test_pairs_of_activations_over_unaligned_weights(ty):
         w = torch.randn(514 + first, device="cuda:0").to(TYPES[ty])[first:]
         _check_forward(x, w, w, ty)
         _check_backward(dy, x, w, ty)
+
+
+# several rows to a warp: more than one round of resident blocks whose last round is not full, and fewer rows than a warp takes
+SHARED = [(9999, 128, "f32", "f32", 0, 0), (20001, 64, "bf16", "bf16", 0, 0), (10007, 200, "bf16", "f32", 8, 0), (9475, 100, "bf16", "bf16", 0, 0),
+          (9473, 33, "f32", "bf16", 0, 1), (9474, 255, "bf16", "bf16", 0, 0), (2, 128, "bf16", "bf16", 0, 0), (3, 256, "f32", "f32", 0, 0),
+          (5, 24, "bf16", "bf16", 0, 0), (31, 129, "f32", "f32", 0, 0), (1, 127, "bf16", "f32", 0, 0), (33, 16, "f32", "f32", 0, 0)]
+
+
+@pytest.mark.parametrize("T,d,ty,wt,pad,shift", SHARED)
+def test_rows_that_share_a_warp(T, d, ty, wt, pad, shift):
+    """Thousands of rows hold elements whose value and mean are both next to zero, where the error of the mean (a part of mean |x|,
+    not of |mean|) is what counts: 128 * 2^-24 of mean |x|, the bound of the mean itself, is added to the magnitudes."""
+    from paper_2603_06626_b200 import binding as B
+    rng = np.random.default_rng(T * 7 + d)
+    x = _matrix(rng, T, d, ty, pad, shift)
+    w = torch.from_numpy((rng.normal(size=d) * 0.3 + 1).astype(np.float32)).to("cuda:0").to(TYPES[wt])
+    b = torch.from_numpy(rng.normal(size=d).astype(np.float32)).to("cuda:0").to(TYPES[wt])
+    xr, wr = f64(x), f64(w)
+    for bias in (b, None):
+        br = 0 * wr if bias is None else f64(bias)
+        y, mean, rstd = B.layer_norm(x, w, bias, EPS)
+        yr, mr, rr = orc.layer_norm(xr, wr, br, EPS)
+        size = np.abs(xr).mean(1)
+        mags = (np.abs(xr) + np.abs(mr)[:, None] + size[:, None]) * rr[:, None] * np.abs(wr) + np.abs(br)
+        assert (np.abs(f64(y) - yr) <= _out_bound(ty, yr, mags * (1 + np.abs(mr * rr)[:, None]))).all()
+        assert (np.abs(f64(mean) - mr) <= 128 * U * size + 1e-30).all()
+        assert (np.abs(f64(rstd) - rr) <= 128 * U * rr * (1 + np.abs(mr * rr)) ** 2).all()
+    dy = torch.from_numpy(rng.normal(size=(T, d)).astype(np.float32)).to("cuda:0").to(TYPES[ty])
+    _check_backward(dy, x, w, ty)
