@@ -171,7 +171,7 @@ cudaError_t launch_dz(int act, const void* dy, const void* z, int T, int N, void
 // y or dx: the CTA-pair core, or the kernel for few tokens.  Both sides in rounds of the machine times 64-deep steps a round,
 // measured over T = 1 .. 4096 and weights of 128 x 128 to 4096 x 4096: a step takes 0.33 us on 256 x 256 tiles (5.7 us around them)
 // and 0.45 us on two 128 x 128 tiles an SM (7.5 us around them, and as much again for every further round); up to 64 tokens the
-// tiles are narrower and their kernel ahead throughout (one token, 4096 x 4096: 9.2 against 38 us; 128 tokens, 512 -> 4096: 9.8
+// tiles are narrower and their kernel ahead throughout (one token, 4096 x 4096: 8.4 against 38 us; 128 tokens, 512 -> 4096: 9.8
 // against 8.9; 512 tokens, 4096 x 4096: 23.5 against 26.8; 1024: 34.5 against 28.4).
 cudaError_t launch_product(const LinearGemm& g, cudaStream_t st) {
   const int sms = current_sms(), splits = linear_small_splits(g.M, g.N, g.K), steps = cdiv(g.K, 64);

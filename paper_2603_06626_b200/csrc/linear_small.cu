@@ -7,7 +7,7 @@
 // 90 KB of the weight on its way into each.  The CTAs then leave their fp32 partial tiles in shared memory, every one adds up
 // a share of the outputs over the S tiles in rank order (bit-reproducible), applies bias, activation and residual and writes.
 //
-// Bound by HBM (the weight).  Measured, weight 4096 x 4096 (33.5 MB, 5.2 us at a plain copy's pace): one token 9.2 us, 64 tokens
+// Bound by HBM (the weight).  Measured, weight 4096 x 4096 (33.5 MB, 5.2 us at a plain copy's pace): one token 8.4 us, 64 tokens
 // 12 us, 256 tokens 18 us; 128 x 128 with one token 4.1 us, which is what launch, set-up and the cluster's two barriers take.
 //
 // Roles in a CTA: warp 0 loads (TMA, ring of STAGES 64-deep steps), warp 1 issues the MMAs, warps 2-5 bring the accumulator to
