@@ -369,6 +369,8 @@ int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const vo
  *
  * grouter_adamw_layout_host (host): sizes of the flat buffers and of the table the step reads; with table_host (table_bytes
  *   bytes) it also fills the table, which the caller copies to the device once.  The table holds the tensors' addresses.
+ *   Tensors that share memory are INVALID_ARG: a parameter with another parameter or with a gradient.  Several parameters may have
+ *   the same gradient, and a parameter's own gradient may be the parameter itself (then of its type).
  * grouter_adamw_step: one step (step counts from 1).  The layout and the scalars are host values and are read before it returns.
  *   Any alignment of parameters and gradients; flat buffers and the device's table 16-byte aligned.
  * grouter_adamw_moments: the values that 8-bit moments stand for, as f32 (m_out = m, v_out = the root's square).

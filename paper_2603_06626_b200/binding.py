@@ -749,10 +749,11 @@ class AdamW:
 
     params: contiguous f32 tensors, updated in place, or bf16 tensors with an f32 master copy that this object keeps; grads: one
     contiguous f32 or bf16 tensor for each, whose memory every step reads (the layer's backward writes its gradients into
-    caller-owned tensors: keep writing the same ones).  weight_decay: a number, or one for each tensor.  Moments (and masters) lie in
-    flat tensors m, v (and master), tensor i from element offsets[i] on: f32 with state_bits 32; with state_bits 8 one byte an element
-    (m, and the root of v) plus m_exp, v_exp, one byte for 32 elements.  state: those tensors of a run to be continued, with
-    steps_done; without it the moments start at zero and the masters at the parameters' values."""
+    caller-owned tensors: keep writing the same ones).  A parameter shares no memory with another one or with a gradient.
+    weight_decay: a number, or one for each tensor.  Moments (and masters) lie in flat tensors m, v (and master), tensor i from element
+    offsets[i] on: f32 with state_bits 32; with state_bits 8 one byte an element (m, and the root of v) plus m_exp, v_exp, one byte for
+    32 elements.  state: those tensors of a run to be continued, with steps_done; without it the moments start at zero and the masters
+    at the parameters' values."""
 
     GROUP = 32
 
@@ -776,6 +777,8 @@ class AdamW:
         for i, (p, g) in enumerate(zip(self.params, self.grads)):
             _expect(f"gradient {i}", g, p.shape, like=self.params[0])
             _expect(f"parameter {i}", p, p.shape, like=self.params[0])
+            if p.data_ptr() == g.data_ptr() and p.dtype != g.dtype and p.numel():
+                raise ValueError(f"gradient {i}: of another type in its parameter's memory")
             desc[i] = AdamwTensor(p.data_ptr(), g.data_ptr(), p.numel(), wd[i], _elt(p, f"parameter {i}"), _elt(g, f"gradient {i}"))
             self.offsets.append(at)
             at += (p.numel() + self.GROUP - 1) // self.GROUP * self.GROUP

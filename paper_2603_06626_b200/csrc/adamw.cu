@@ -27,6 +27,10 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "vec.cuh"
 
 namespace grouter {
@@ -325,6 +329,43 @@ __global__ void __launch_bounds__(256) adamw_moments_kernel(const uint8_t* __res
   }
 }
 
+namespace {
+
+// Whether a parameter's memory is also another tensor's: another parameter (two blocks would write it), a gradient that some other
+// block reads, or its own gradient shifted against it.  A gradient that starts where its parameter does is left alone: the thread
+// that writes an element has read it (of the same type, which is the caller's to keep).
+int adamw_check_overlap(const grouter_adamw_tensor* tensors, int32_t n) {
+  struct Range {
+    uintptr_t begin, end;
+    bool written;
+  };
+  const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[2 * (size_t)n]);
+  if (!ranges) return GROUTER_ERR_CUDA;
+  size_t count = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const grouter_adamw_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(t.param), g = reinterpret_cast<uintptr_t>(t.grad);
+    const uintptr_t p_bytes = (uintptr_t)t.n * (t.param_dtype == GROUTER_BF16 ? 2 : 4), g_bytes = (uintptr_t)t.n * (t.grad_dtype == GROUTER_BF16 ? 2 : 4);
+    if (p == g) {
+      ranges[count++] = {p, p + std::max(p_bytes, g_bytes), true};
+    } else {
+      ranges[count++] = {p, p + p_bytes, true};
+      ranges[count++] = {g, g + g_bytes, false};
+    }
+  }
+  std::sort(ranges.get(), ranges.get() + count, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t written = 0, read = 0;         // where the ranges so far end
+  for (size_t i = 0; i < count; ++i) {
+    const Range& r = ranges[i];
+    if (r.begin < written || (r.written && r.begin < read)) return GROUTER_ERR_INVALID_ARG;
+    uintptr_t& end = r.written ? written : read;
+    end = std::max(end, r.end);
+  }
+  return GROUTER_OK;
+}
+
+}  // namespace
 }  // namespace grouter
 
 using namespace grouter;
@@ -348,6 +389,7 @@ int grouter_adamw_layout_host(const grouter_adamw_tensor* tensors, int32_t n_ten
     if (t.param_dtype == GROUTER_BF16) needs_master = 1;
   }
   if (chunks > INT32_MAX) return GROUTER_ERR_UNSUPPORTED;
+  if (const int e = adamw_check_overlap(tensors, n_tensors)) return e;
   layout->n_tensors = n_tensors;
   layout->n_chunks = (int32_t)chunks;
   layout->state_elements = elements;

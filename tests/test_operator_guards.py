@@ -1,0 +1,53 @@
+"""Host-side guards of the operators around the expert layer, on the CPU: what must be refused before a kernel could race on it."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2603_06626_b200 import binding as B
+
+OK, INVALID = 0, -1
+A = 1 << 20           # stands for a device address: the layout is host arithmetic
+
+
+def _layout(*tensors):
+    """Code of the layout of (param, grad, elements, param type, grad type) tuples."""
+    desc = (B.AdamwTensor * len(tensors))(*[B.AdamwTensor(p, g, n, 0.0, pt, gt) for p, g, n, pt, gt in tensors])
+    return B.load_library().grouter_adamw_layout_host(desc, len(tensors), ctypes.byref(B.AdamwLayout()), None)
+
+
+def test_adamw_refuses_parameters_that_share_memory():
+    far = A + (1 << 16)
+    one = (A, far, 100, B.F32, B.F32)
+    assert _layout(one, (A, far + 4096, 100, B.F32, B.F32)) == INVALID                  # the same tensor twice
+    assert _layout(one, (A + 396, far + 4096, 8, B.F32, B.F32)) == INVALID              # its last element
+    assert _layout(one, (A - 32, far + 4096, 9, B.F32, B.F32)) == INVALID               # its first
+    assert _layout((A, far, 10 ** 6, B.BF16, B.F32), (A + 4000, A, 0, B.F32, B.F32), (A + 8000, 1 << 40, 2, B.F32, B.F32)) == INVALID   # inside a long one
+    assert _layout(one, (A + 400, far + 4096, 8, B.F32, B.F32)) == OK                   # next to each other
+    assert _layout(one, (A, far, 0, B.F32, B.F32)) == OK                                # an empty tensor has no memory
+
+
+def test_adamw_refuses_a_parameter_over_a_gradient_that_others_read():
+    far = A + (1 << 16)
+    assert _layout((A, far, 100, B.F32, B.F32), (far + 200, far + 4096, 8, B.F32, B.F32)) == INVALID      # over another tensor's gradient
+    assert _layout((A, A + 4, 100, B.F32, B.F32)) == INVALID                                              # over its own, shifted
+    assert _layout((A, A - 8, 100, B.BF16, B.BF16)) == INVALID
+    assert _layout((A, A, 100, B.F32, B.F32)) == OK                                                       # an element reads what it writes
+    assert _layout((A, A, 100, B.BF16, B.F32), (A + 200, far, 4, B.BF16, B.BF16)) == INVALID              # its gradient goes on behind it
+    assert _layout((A, far, 100, B.F32, B.F32), (A + 400, far, 100, B.F32, B.F32)) == OK                  # a gradient that two of them read
+
+
+def test_the_binding_refuses_a_gradient_of_another_type_in_its_parameters_memory(monkeypatch):
+    monkeypatch.setattr(B, "_device_index", lambda dev: 0)
+    p, g = torch.zeros(64), torch.zeros(64)
+    B.AdamW([p], [g])
+    with pytest.raises(B.GrouterError):
+        B.AdamW([p, p], [g, torch.zeros(64)])
+    flat = torch.zeros(96)
+    with pytest.raises(B.GrouterError):
+        B.AdamW([flat[:64], flat[32:]], [g, g])
+    half = g.view(torch.bfloat16)
+    with pytest.raises(ValueError):
+        B.AdamW([half[:64]], [g])
+    with pytest.raises(ValueError):
+        B.AdamW([g], [half[:64]])
