@@ -9,6 +9,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import threading
 from typing import Optional
 
 import torch
@@ -571,16 +572,22 @@ def _bytes(fn, index: int, *args) -> int:
 
 
 _status_words = {}
+_status_lock = threading.Lock()
 
 
 def _status_word(index: int) -> torch.Tensor:
     """The status word of a device that the calls without one of their own share."""
     word = _status_words.get(index)
-    if word is None:
-        if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("the first call on a device sets up its status word: make it outside a stream capture, or pass status=")
-        word = _status_words[index] = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
-        torch.cuda.synchronize(index)      # zeroed before a kernel on any stream can set a bit in it
+    if word is not None:
+        return word
+    with _status_lock:                     # one word a device: a second one would be freed under the kernels that were given it
+        word = _status_words.get(index)
+        if word is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the first call on a device sets up its status word: make it outside a stream capture, or pass status=")
+            word = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
+            torch.cuda.synchronize(index)  # zeroed before a kernel on any stream can set a bit in it
+            _status_words[index] = word
     return word
 
 

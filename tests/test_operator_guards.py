@@ -51,3 +51,44 @@ def test_the_binding_refuses_a_gradient_of_another_type_in_its_parameters_memory
         B.AdamW([half[:64]], [g])
     with pytest.raises(ValueError):
         B.AdamW([g], [half[:64]])
+
+
+def test_threads_that_make_a_devices_first_call_together_share_one_status_word(monkeypatch):
+    """The second of two words would be freed while a kernel may still set a bit in it."""
+    import threading
+    import time
+    started = threading.Barrier(4)
+    made = []
+
+    def zeros(*shape, **kw):
+        time.sleep(0.05)                       # long enough for every other thread to come by
+        made.append(torch.empty(1, dtype=torch.int32))
+        return made[-1]
+
+    monkeypatch.setattr(B, "_status_words", {})
+    monkeypatch.setattr(B.torch, "zeros", zeros)
+    monkeypatch.setattr(B.torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(B.torch.cuda, "synchronize", lambda index: None)
+    got = [None] * 4
+
+    def first_call(i):
+        started.wait()
+        got[i] = B._status_word(0)
+
+    threads = [threading.Thread(target=first_call, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(made) == 1 and all(w is made[0] for w in got)
+
+
+def test_a_status_word_is_shared_only_once_it_is_zeroed(monkeypatch):
+    """Another thread's call must not get the word between its creation and the end of the zeroing."""
+    monkeypatch.setattr(B, "_status_words", {})
+    monkeypatch.setattr(B.torch, "zeros", lambda *shape, **kw: torch.empty(1, dtype=torch.int32))
+    monkeypatch.setattr(B.torch.cuda, "is_current_stream_capturing", lambda: False)
+    seen = []
+    monkeypatch.setattr(B.torch.cuda, "synchronize", lambda index: seen.append(B._status_words.get(0)))
+    B._status_word(0)
+    assert seen == [None] and B._status_words[0] is not None
