@@ -808,7 +808,7 @@ class AdamW:
                 t = torch.zeros(shape, dtype=kind, device=dev)
                 if name == "master":
                     for p, o in zip(self.params, self.offsets):
-                        t[o:o + p.numel()] = p.reshape(-1)
+                        t[o:o + p.numel()] = p.detach().reshape(-1)
             _expect(name, t, shape, kind, like=self.params[0])
             setattr(self, name, t)
         host = torch.zeros(max(16, self._layout.table_bytes), dtype=u8)

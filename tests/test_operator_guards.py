@@ -92,3 +92,13 @@ def test_a_status_word_is_shared_only_once_it_is_zeroed(monkeypatch):
     monkeypatch.setattr(B.torch.cuda, "synchronize", lambda index: seen.append(B._status_words.get(0)))
     B._status_word(0)
     assert seen == [None] and B._status_words[0] is not None
+
+
+def test_adamw_keeps_no_history_of_parameters_that_require_gradients(monkeypatch):
+    import copy
+    monkeypatch.setattr(B, "_device_index", lambda dev: 0)
+    p = [torch.nn.Parameter(torch.randn(5, 7).bfloat16()), torch.nn.Parameter(torch.randn(40).bfloat16())]
+    opt = B.AdamW(p, [torch.zeros(5, 7), torch.zeros(40)])
+    for t in (opt.master, opt.m, opt.v):
+        assert not t.requires_grad and t.is_leaf and t.grad_fn is None
+    assert torch.equal(copy.deepcopy(opt.master)[64:104], p[1].detach().float()) and (opt.master.numpy()[35:64] == 0).all()
