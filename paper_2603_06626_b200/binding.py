@@ -591,15 +591,18 @@ def _status_word(index: int) -> torch.Tensor:
     return word
 
 
-def check_status(device="cuda:0") -> None:
+def check_status(device="cuda:0", status: Optional[torch.Tensor] = None) -> None:
     """Waits for the device; raises when a linear, linear_backward, expert_counts or balance_loss call without a status word of its own
-    met a bounded wait that ran out or an expert id out of range since the last check, and clears the word."""
+    met a bounded wait that ran out or an expert id out of range since the last check, and clears the bits that it has seen.  That word
+    is one for all streams and threads of the process; calls that passed status= are checked by passing the same one here."""
     index = _device_index(torch.device(device))
     torch.cuda.synchronize(index)
-    word = _status_word(index)
-    st = int(word.item())
-    word.zero_()
-    torch.cuda.synchronize(index)
+    word = _status_word(index) if status is None else status
+    with _status_lock:
+        st = int(word.item())
+        if st != 0:
+            word.bitwise_and_(~st)      # what other threads' calls have found since stays for the next check
+            torch.cuda.synchronize(index)
     if st != 0:
         raise GrouterError(-7 if st & 2 else -6, "device status")
 

@@ -102,3 +102,37 @@ def test_adamw_keeps_no_history_of_parameters_that_require_gradients(monkeypatch
     for t in (opt.master, opt.m, opt.v):
         assert not t.requires_grad and t.is_leaf and t.grad_fn is None
     assert torch.equal(copy.deepcopy(opt.master)[64:104], p[1].detach().float()) and (opt.master.numpy()[35:64] == 0).all()
+
+
+class _Word:
+    """A status word on which another thread's kernel sets a bit right after it has been read."""
+
+    def __init__(self, before, after):
+        self.value, self.after = before, after
+
+    def item(self):
+        seen, self.value = self.value, self.value | self.after
+        return seen
+
+    def zero_(self):
+        self.value = 0
+
+    def bitwise_and_(self, keep):
+        self.value &= keep
+
+
+def test_a_check_clears_only_the_bits_that_it_reports(monkeypatch):
+    word = _Word(0, 2)
+    monkeypatch.setattr(B, "_device_index", lambda dev: 0)
+    monkeypatch.setattr(B, "_status_words", {0: word})
+    monkeypatch.setattr(B.torch.cuda, "synchronize", lambda index: None)
+    B.check_status()                                     # nothing had been found
+    assert word.value == 2
+    word.after = 1
+    with pytest.raises(B.GrouterError) as e:
+        B.check_status()
+    assert e.value.code == -7 and word.value == 1        # the wait that ran out is reported, the id that came after is not lost
+    word.after = 0
+    with pytest.raises(B.GrouterError) as e:
+        B.check_status()
+    assert e.value.code == -6 and word.value == 0
