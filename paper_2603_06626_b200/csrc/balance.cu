@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(BAL_THREADS) balance_kernel(const BalanceParam
     z = lanes_sum<LPT>(z);
     a = lanes_sum<LPT>(a);
     const float inv_z = some ? 1.f / z : 0.f;
-    const float lse = some ? base + __logf(z) : 0.f;          // z >= 1: within 2^-21
+    const float lse = some ? base + __logf(z) : z;            // z >= 1: within 2^-21.  No score: z = 0, or NaN if there was one
     a *= inv_z;
     if (sl == 0 && live) {
       sum_a += a;

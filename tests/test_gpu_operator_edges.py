@@ -1,0 +1,26 @@
+"""Edges of the operators around the expert layer: scores that are not numbers."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("E", [8, 60, 333])
+@pytest.mark.parametrize("ty", [torch.float32, torch.bfloat16])
+def test_a_row_without_a_number_spoils_both_losses(E, ty):
+    """Scores that are NaN throughout, or NaN beside -inf, are no empty row: the z loss is NaN as well, also where it counts alone."""
+    from paper_2603_06626_b200 import binding as B
+    for others in (float("nan"), -float("inf")):
+        s = torch.randn(50, E, device="cuda:0").to(ty)
+        s[17] = others
+        s[17, E - 1] = float("nan")
+        i = torch.zeros(50, 1, dtype=torch.int32, device="cuda:0")
+        counts, n = B.expert_counts(i, E)
+        loss, d = B.balance_loss(s, i, counts, n, balance_coef=0.0, z_coef=0.1)
+        assert torch.isnan(loss).all() and torch.isnan(d[17, E - 1])
+        rows = torch.arange(50, device="cuda:0") != 17
+        assert torch.isfinite(d[rows]).all()
+        mask = rows.to(torch.uint8)
+        counts, n = B.expert_counts(i, E, mask=mask)
+        loss, d = B.balance_loss(s, i, counts, n, mask=mask, balance_coef=0.0, z_coef=0.1)
+        assert torch.isfinite(loss).all() and torch.isfinite(d).all()
