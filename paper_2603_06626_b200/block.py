@@ -42,6 +42,8 @@ class RoutedBlock:
                 "W_2": (normal(d, hidden, std=hidden ** -0.5), bf, True), "b_2": (torch.zeros(d, dtype=bf, device=device), f32, False)}
         self.w = {n: w for n, (w, _, _) in made.items()}
         self.grad = {n: torch.zeros(w.shape, dtype=gt, device=device) for n, (w, gt, _) in made.items()}
+        # what the block's own calls find; the word that other calls on the device share is not touched
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.optimizer = B.AdamW(self.w.values(), self.grad.values(), lr=lr, betas=(0.9, 0.95), state_bits=state_bits,
                                  weight_decay=[weight_decay if decays else 0.0 for _, _, decays in made.values()])
 
@@ -50,12 +52,13 @@ class RoutedBlock:
         w = self.w
         h, mean, rstd = B.layer_norm(x, w["norm_w"], w["norm_b"])
         idx, gates, scores = B.route(h, w["W_s"], None, self.E, self.k, want_scores=True)
-        counts, n = B.expert_counts(idx, self.E, mask=mask)
-        losses, _ = B.balance_loss(scores, idx, counts, n, mask=mask, balance_coef=self.balance_coef, z_coef=self.z_coef, want_grad=False)
+        counts, n = B.expert_counts(idx, self.E, mask=mask, status=self.status)
+        losses, _ = B.balance_loss(scores, idx, counts, n, mask=mask, balance_coef=self.balance_coef, z_coef=self.z_coef, want_grad=False,
+                                   status=self.status)
         self.layer.plan(idx)
         routed = self.layer.forward(h, gates, w["W_gu"], w["W_d"])
-        u, pre = B.linear(h, w["W_1"], bias=w["b_1"], act=B.ACT_SILU, save_pre=True)
-        out, _ = B.linear(u, w["W_2"], bias=w["b_2"], residual=x)
+        u, pre = B.linear(h, w["W_1"], bias=w["b_1"], act=B.ACT_SILU, save_pre=True, status=self.status)
+        out, _ = B.linear(u, w["W_2"], bias=w["b_2"], residual=x, status=self.status)
         out += routed
         self._saved = (x, mask, h, mean, rstd, idx, gates, scores, counts, n, u, pre)
         return out, losses
@@ -65,11 +68,11 @@ class RoutedBlock:
         x, mask, h, mean, rstd, idx, gates, scores, counts, n, u, pre = self._saved
         w, g = self.w, self.grad
         dh, _, _, dgates = self.layer.backward(dout, h, gates, w["W_gu"], w["W_d"], dW_gu=g["W_gu"], dW_d=g["W_d"])
-        du, _, _ = B.linear_backward(dout, u, w["W_2"], dW=g["W_2"], db=g["b_2"])
-        dh_dense, _, _ = B.linear_backward(du, h, w["W_1"], pre=pre, act=B.ACT_SILU, dW=g["W_1"], db=g["b_1"])
+        du, _, _ = B.linear_backward(dout, u, w["W_2"], dW=g["W_2"], db=g["b_2"], status=self.status)
+        dh_dense, _, _ = B.linear_backward(du, h, w["W_1"], pre=pre, act=B.ACT_SILU, dW=g["W_1"], db=g["b_1"], status=self.status)
         _, dscores = B.balance_loss(scores, idx, counts, n, mask=mask, balance_coef=self.balance_coef, z_coef=self.z_coef, dgates=dgates,
-                                    want_loss=False)
-        dh_router, _, _ = B.linear_backward(dscores.bfloat16(), h, w["W_s"], dW=g["W_s"])
+                                    want_loss=False, status=self.status)
+        dh_router, _, _ = B.linear_backward(dscores.bfloat16(), h, w["W_s"], dW=g["W_s"], status=self.status)
         dh += dh_dense
         dh += dh_router
         dx, _, _ = B.layer_norm_backward(dh, x, w["norm_w"], mean, rstd, dw=g["norm_w"], db=g["norm_b"])
@@ -80,9 +83,9 @@ class RoutedBlock:
         self.optimizer.step(grad_scale=grad_scale)
 
     def check_status(self) -> None:
-        """Raises on what the kernels found since the last check."""
+        """Raises on what this block's kernels found since the last check."""
         self.layer.check_status()
-        B.check_status(self.layer.device)
+        B.check_status(self.layer.device, status=self.status)
 
 
 def main() -> None:

@@ -1,4 +1,4 @@
-"""Edges of the operators around the expert layer: scores that are not numbers."""
+"""Edges of the operators around the expert layer: scores that are not numbers, errors that belong to somebody else."""
 import pytest
 import torch
 
@@ -24,3 +24,24 @@ def test_a_row_without_a_number_spoils_both_losses(E, ty):
         counts, n = B.expert_counts(i, E, mask=mask)
         loss, d = B.balance_loss(s, i, counts, n, mask=mask, balance_coef=0.0, z_coef=0.1)
         assert torch.isfinite(loss).all() and torch.isfinite(d).all()
+
+
+def test_the_block_keeps_its_errors_to_itself():
+    """An error of a call elsewhere is neither raised nor cleared by the block's check, and the other way round."""
+    from paper_2603_06626_b200 import binding as B
+    from paper_2603_06626_b200.block import RoutedBlock
+    block = RoutedBlock(64, 64, 64, 8, 2, 64)
+    x = torch.randn(64, 64, device="cuda:0").bfloat16()
+    block.forward(x)
+    block.backward(x)
+    B.check_status()
+    B.expert_counts(torch.full((4, 2), 9, dtype=torch.uint8, device="cuda:0"), 8)
+    block.check_status()
+    with pytest.raises(B.GrouterError):
+        B.check_status()
+    block.forward(x)
+    block.status.fill_(2)
+    B.check_status()
+    with pytest.raises(B.GrouterError):
+        block.check_status()
+    block.check_status()
