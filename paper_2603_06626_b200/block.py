@@ -21,10 +21,14 @@ from . import binding as B
 
 
 class RoutedBlock:
-    """Weights, gradients and optimizer of one block for batches of T tokens (T a multiple of 8, as the router head takes them)."""
+    """Weights, gradients and optimizer of one block for batches of T tokens.  T, d, ffn, E and hidden are multiples of 8: the router
+    head and the products work in units of 8 of each."""
 
     def __init__(self, T: int, d: int, ffn: int, E: int, k: int, hidden: int, device: str = "cuda:0", seed: int = 0, lr: float = 1e-3,
                  weight_decay: float = 0.01, state_bits: int = 32, balance_coef: float = 1e-2, z_coef: float = 1e-3):
+        for name, size in (("T", T), ("d", d), ("ffn", ffn), ("E", E), ("hidden", hidden)):
+            if size < 1 or size % 8:
+                raise ValueError(f"{name}: a multiple of 8 is expected, got {size}")
         self.T, self.d, self.E, self.k = T, d, E, k
         self.balance_coef, self.z_coef = balance_coef, z_coef
         self.layer = B.GrouterLayer(T, d, ffn, E, k, device=device)

@@ -136,3 +136,12 @@ def test_a_check_clears_only_the_bits_that_it_reports(monkeypatch):
     with pytest.raises(B.GrouterError) as e:
         B.check_status()
     assert e.value.code == -6 and word.value == 0
+
+
+def test_the_block_says_what_its_sizes_have_to_be():
+    from paper_2603_06626_b200.block import RoutedBlock
+    for name in ("T", "d", "ffn", "E", "hidden"):
+        sizes = dict(T=64, d=64, ffn=64, E=8, k=2, hidden=64)
+        sizes[name] += 4
+        with pytest.raises(ValueError, match=f"^{name}: a multiple of 8"):
+            RoutedBlock(**sizes)
