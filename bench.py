@@ -41,17 +41,28 @@ MOVER_SLOTS = ["gather_X", "combine_Y", "gather_dY", "reduce_dX"]
 FALLBACK_PEAKS = {"hbm_gbs": 6650.0, "bf16_tflops": 1590.0, "bf16_tflops_sustained": 1400.0}
 
 
+CSRC = os.path.join(ROOT, "paper_2603_06626_b200", "csrc")
+STEP_SOURCES = ["api.cu", "gemm.cu", "permute.cu", "plan.cu"]      # what the kernels of the layer's step are compiled from
+
+
 def kernel_source_tag() -> str:
-    """Short hash of the CUDA sources (comments and blank space left out): DRAM counters taken with other code are not
-    reported."""
+    """Short hash of the CUDA sources of the layer's step and of the headers that they include (comments and blank space left out):
+    DRAM counters taken with other code are not reported."""
     import hashlib
     import re
+    files = {}
+    todo = list(STEP_SOURCES)
+    while todo:
+        name = todo.pop()
+        path = os.path.join(CSRC, name)
+        if name in files or not os.path.exists(path):              # (the public header lies elsewhere: no code)
+            continue
+        with open(path) as f:
+            files[name] = re.sub(r"//[^\n]*", "", f.read())
+        todo += re.findall(r'#include "([^"]+)"', files[name])
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2603_06626_b200", "csrc")
-    for name in sorted(os.listdir(csrc)):
-        with open(os.path.join(csrc, name)) as f:
-            code = re.sub(r"//[^\n]*", "", f.read())
-        h.update(name.encode() + b"\0" + "".join(code.split()).encode())
+    for name in sorted(files):
+        h.update(name.encode() + b"\0" + "".join(files[name].split()).encode())
     return h.hexdigest()[:12]
 
 
@@ -78,7 +89,7 @@ def recorded_traffic(w: synth.Workload, kernel: str):
     profiles/dram_traffic.txt holds one-pass ncu counters taken on a workload of a few GB (lines: workload kernel bytes
     source-tag).  A line for `w` itself is used as it stands; otherwise the small workload's figure is scaled by the
     ratio of the two workloads' algorithmic bytes (DRAM traffic of these kernels follows their operand and result sizes:
-    the capture reads within a few per cent of the algorithmic bytes).  None when the CUDA sources have changed since
+    the capture reads within a few per cent of the algorithmic bytes).  None when the step's CUDA sources have changed since
     the capture (other source tag) or there is no line for the kernel."""
     if not os.path.exists(TRAFFIC_FILE):
         return None
