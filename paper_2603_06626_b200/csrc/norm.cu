@@ -101,13 +101,15 @@ __global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kern
   const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LANES;
   const int at = threadIdx.x & (LANES - 1);
   if (LANES >= 32 && row >= rows) return;  // whole warps, and whole blocks where a row has several
-  if (LANES < 32 && row >= rows) d = 0;    // stays for the sums of the rows beside it in the warp
+  // A row that is not there stays for the sums of those beside it in the warp, without elements (end), its mean a plain 0: dividing by
+  // a d of 0 sent such lanes down the slow paths of quotient and root (1 x 128 bf16: 1.9 -> 2.1 us).
+  const int end = LANES >= 32 || row < rows ? d : 0;
   const T* xr = x + row * ldx;
   Pack<T, VE> p[NP];
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
     const int c = (n * LANES + at) * VE;
-    if (c < d) p[n] = ld_pack<T, VE>(xr + c);
+    if (c < end) p[n] = ld_pack<T, VE>(xr + c);
   }
   const float inv_d = 1.f / (float)d;
   int half = 0;
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kern
     float2 s2 = both(0.f);
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if ((n * LANES + at) * VE < d) {
+      if ((n * LANES + at) * VE < end) {
 #pragma unroll
         for (int i = 0; i < VE; i += 2) s2 = add2(s2, pair_at(p, (n * VE + i) / 2));
       }
@@ -124,7 +126,7 @@ __global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kern
   } else {
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if (n * LANES + at < d) s[0] += to_f32(p[n].v[0]);
+      if (n * LANES + at < end) s[0] += to_f32(p[n].v[0]);
   }
   row_sums<LANES, 1>(s, red, half);
   const float mean = s[0] * inv_d;
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kern
     const float2 m2 = both(-mean);
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if ((n * LANES + at) * VE < d) {
+      if ((n * LANES + at) * VE < end) {
 #pragma unroll
         for (int i = 0; i < VE; i += 2) {
           const float2 c2 = add2(pair_at(p, (n * VE + i) / 2), m2);
@@ -145,7 +147,7 @@ __global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kern
   } else {
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if (n * LANES + at < d) {
+      if (n * LANES + at < end) {
         const float c1 = to_f32(p[n].v[0]) - mean;
         q[0] += c1 * c1;
       }
@@ -156,7 +158,7 @@ __global__ void __launch_bounds__(norm_forward_threads(LANES)) norm_forward_kern
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
     const int c = (n * LANES + at) * VE;
-    if (c < d) {
+    if (c < end) {
       float wl[VE], bl[VE], o[VE];
       load_weights<W, VE>(w, c, wl);
       if (b != nullptr) {
