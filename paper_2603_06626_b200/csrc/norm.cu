@@ -462,17 +462,18 @@ int norm_tpr(int d) {
 //   A row a block: the partial rows are as large as the problem, so eight blocks join (1000 x 1024: 18 -> 9.6 us, in pairs 15), or
 //     two of the larger ones, of which an SM holds few; very few rows do without (20 x 4096: 8.0 us, in pairs 10).
 //   Many rows a block: pairs (16384 x 2048: 47 -> 44 us, 8192 x 16384 f32: 367 -> 298; clusters of eight leave places for blocks empty:
-//     55 us, 65536 x 1024 73 in pairs and 97 in eights); one warp a row gains nothing (65536 x 512: 40 us either way).
+//     55 us, 65536 x 1024 73 in pairs and 97 in eights); one warp a row gains nothing (65536 x 512: 40 us either way),
+//     and rows without a ring lose (16384 x 2047 bf16: 59 -> 64, 16384 x 4095 116 -> 119, 8192 x 4095 f32 76 -> 78).
 struct NormGrid {
   int blocks, cluster;
   int parts() const { return blocks / cluster; }      // partial rows they leave
 };
-NormGrid norm_backward_grid(int rows, int d) {
+NormGrid norm_backward_grid(int rows, int d, bool ring) {
   const int tpr = norm_tpr(d), rpb = norm_backward_threads(tpr) / tpr;
   const int want = (rows + rpb - 1) / rpb, cap = current_sms() * norm_backward_per_sm(tpr);
   NormGrid g{want < cap ? want : cap, 1};
   if (want <= cap) g.cluster = want < 64 ? 1 : tpr <= 128 ? 8 : 2;
-  else if (tpr >= 64 && want >= 8 * cap) g.cluster = 2;
+  else if (ring && tpr >= 64 && want >= 8 * cap) g.cluster = 2;
   g.blocks -= g.blocks % g.cluster;
   return g;
 }
@@ -513,7 +514,7 @@ cudaError_t forward_by_width(const NormArgs& a) {
 
 template <typename T, typename W, int VE, int TPR>
 cudaError_t backward_launch(const NormArgs& a) {
-  const NormGrid g = norm_backward_grid(a.rows, a.d);
+  const NormGrid g = norm_backward_grid(a.rows, a.d, VE == vec16<T>());
   constexpr int threads = norm_backward_threads(TPR), ring = VE == vec16<T>() ? norm_ring(sizeof(T), TPR) * 2 * (NORM_EPT / VE) * threads * 16 : 0;
   constexpr int cols = 2 * threads * NORM_EPT * (int)sizeof(float);
   constexpr int smem = ring > cols ? ring : cols;      // up to 192 KB
@@ -613,7 +614,8 @@ int grouter_layernorm_fwd(const void* x, int64_t ldx, const void* w, const void*
 
 size_t grouter_layernorm_bwd_workspace_bytes(int32_t rows, int32_t d) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
-  return (size_t)std::max(norm_backward_grid(rows, d).parts(), 1) * 2 * d * sizeof(float);
+  // alignment is not known here: as many partial rows as rows without a ring leave
+  return (size_t)std::max(norm_backward_grid(rows, d, false).parts(), 1) * 2 * d * sizeof(float);
 }
 
 int grouter_layernorm_bwd(const void* dy, const void* x, int64_t ldx, const void* w, const float* mean, const float* rstd, int32_t rows,
