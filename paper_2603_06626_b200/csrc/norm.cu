@@ -488,14 +488,15 @@ cudaError_t forward_launch(const NormArgs& a) {
 }
 
 // Up to FEW accesses a lane while a quarter of a warp holds a row, then more lanes; a warp's lanes then take up to MOST, more warps
-// follow up to 16, and what is still needed of both.
-template <typename T, typename W, int VE, int MOST, int FEW, int NP = 1, int LANES = 8>
+// follow up to LAST lanes, those take twice MOST before warps follow up to 16, and what is still needed of both.
+template <typename T, typename W, int VE, int MOST, int FEW, int LAST, int NP = 1, int LANES = 8>
 cudaError_t forward_spread(const NormArgs& a) {
   constexpr int HOLDS = NP * LANES * VE;
   if constexpr (HOLDS < NORM_MAX_D) {
     if (a.d > HOLDS) {
-      if constexpr (NP < FEW || (LANES >= 32 && (NP < MOST || (LANES == 512 && NP < 16)))) return forward_spread<T, W, VE, MOST, FEW, 2 * NP, LANES>(a);
-      else return forward_spread<T, W, VE, MOST, FEW, NP, 2 * LANES>(a);
+      constexpr bool more = NP < FEW || (LANES >= 32 && (NP < MOST || (LANES == LAST && NP < 2 * MOST) || (LANES == 512 && NP < 16)));
+      if constexpr (more) return forward_spread<T, W, VE, MOST, FEW, LAST, 2 * NP, LANES>(a);
+      else return forward_spread<T, W, VE, MOST, FEW, LAST, NP, 2 * LANES>(a);
     }
   }
   return forward_launch<T, W, VE, NP, LANES>(a);
@@ -505,11 +506,20 @@ cudaError_t forward_spread(const NormArgs& a) {
 // lanes 9.4, of a warp 16), and fewer, in more lanes, where the whole matrix is small and the time is that of a row (1 x 4096: 2.6
 // against 3.0 us, 1024 x 2048 3.3 against 4.0, but 1024 x 4096 5.3 against 4.3); eight of the smaller ones (16384 x 4094: 54 us, with
 // four 79).
+// The widest rows take eight accesses of eight warps before more warps (8192 x 16384 bf16: 107 us, four of sixteen warps 129; 8192 x 12288 84 and
+// 104; but 140 x 16384 5.8 and 5.1), large matrices of single bf16 sixteen (16384 x 4095: 85 us, with eight 90; but 1000 x 4095 10.6 and 8.6).
 constexpr int64_t NORM_SMALL = 1 << 21;
 template <typename T, typename W, int VE>
 cudaError_t forward_by_width(const NormArgs& a) {
-  if constexpr (VE * sizeof(T) < 16) return forward_spread<T, W, VE, 8, 4>(a);
-  else return (int64_t)a.rows * a.d <= NORM_SMALL ? forward_spread<T, W, VE, 2, 1>(a) : forward_spread<T, W, VE, 4, 4>(a);
+  const int64_t size = (int64_t)a.rows * a.d;
+  if constexpr (VE * sizeof(T) == 2) {
+    return size <= 8 * NORM_SMALL ? forward_spread<T, W, VE, 8, 4, 512>(a) : forward_spread<T, W, VE, 16, 4, 512>(a);
+  } else if constexpr (VE * sizeof(T) < 16) {
+    return forward_spread<T, W, VE, 8, 4, 512>(a);
+  } else {
+    if (size <= NORM_SMALL) return forward_spread<T, W, VE, 2, 1, 512>(a);
+    return size <= 2 * NORM_SMALL ? forward_spread<T, W, VE, 4, 4, 512>(a) : forward_spread<T, W, VE, 4, 4, 256>(a);
+  }
 }
 
 template <typename T, typename W, int VE, int TPR>
