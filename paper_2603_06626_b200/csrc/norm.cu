@@ -507,12 +507,13 @@ cudaError_t forward_spread(const NormArgs& a) {
 // against 3.0 us, 1024 x 2048 3.3 against 4.0, but 1024 x 4096 5.3 against 4.3); eight of the smaller ones (16384 x 4094: 54 us, with
 // four 79).
 // The widest rows take eight accesses of eight warps before more warps (8192 x 16384 bf16: 107 us, four of sixteen warps 129; 8192 x 12288 84 and
-// 104; but 140 x 16384 5.8 and 5.1), large matrices of single bf16 sixteen (16384 x 4095: 85 us, with eight 90; but 1000 x 4095 10.6 and 8.6).
+// 104; but 140 x 16384 5.8 and 5.1), large matrices of single bf16 under f32 weights sixteen (16384 x 2047: 42 us, with eight 44, 16384 x 4095
+// 85.5 and 90; but 1000 x 4095 10.6 and 8.6, and under bf16 weights 16384 x 2047 44.5 and 42).
 constexpr int64_t NORM_SMALL = 1 << 21;
 template <typename T, typename W, int VE>
 cudaError_t forward_by_width(const NormArgs& a) {
   const int64_t size = (int64_t)a.rows * a.d;
-  if constexpr (VE * sizeof(T) == 2) {
+  if constexpr (VE * sizeof(T) == 2 && sizeof(W) == 4) {
     return size <= 8 * NORM_SMALL ? forward_spread<T, W, VE, 8, 4, 512>(a) : forward_spread<T, W, VE, 16, 4, 512>(a);
   } else if constexpr (VE * sizeof(T) < 16) {
     return forward_spread<T, W, VE, 8, 4, 512>(a);
