@@ -618,7 +618,7 @@ int grouter_balance_loss(const void* logits, int64_t ld, int32_t dtype, const vo
   if ((dtype != GROUTER_BF16 && dtype != GROUTER_F32) || (idx_dtype != GROUTER_IDX_U8 && idx_dtype != GROUTER_IDX_I32) ||
       (norm != GROUTER_NORM_SOFTMAX && norm != GROUTER_NORM_SIGMOID))
     return GROUTER_ERR_INVALID_ARG;
-  if (E > BAL_MAX_E || k > 32 || (int64_t)T * k > INT32_MAX || T > INT32_MAX - (1 << 20) || (idx_dtype == GROUTER_IDX_U8 && E > 256))
+  if (E > BAL_MAX_E || k > 32 || (int64_t)T * k > INT32_MAX || T > INT32_MAX - (1 << 20) || (idx && idx_dtype == GROUTER_IDX_U8 && E > 256))
     return GROUTER_ERR_UNSUPPORTED;
   if (loss && !workspace && grouter_balance_loss_workspace_bytes(T, E, k) > 0) return GROUTER_ERR_INVALID_ARG;
   const size_t el = dtype == GROUTER_F32 ? 4 : 2;

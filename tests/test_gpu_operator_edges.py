@@ -45,3 +45,15 @@ def test_the_block_keeps_its_errors_to_itself():
     with pytest.raises(B.GrouterError):
         block.check_status()
     block.check_status()
+
+
+@pytest.mark.parametrize("E", [256, 257, 1024])
+def test_losses_without_ids(E):
+    from paper_2603_06626_b200 import binding as B
+    s = torch.randn(40, E, device="cuda:0")
+    i = s.topk(2, dim=1).indices.to(torch.int32)
+    counts, n = B.expert_counts(i, E)
+    want = B.balance_loss(s, i, counts, n, z_coef=0.1)
+    got = B.balance_loss(s, None, counts, n, z_coef=0.1)
+    B.check_status()
+    assert torch.allclose(got[0], want[0], rtol=1e-5) and torch.allclose(got[1], want[1], rtol=1e-4, atol=1e-9)

@@ -145,3 +145,12 @@ def test_the_block_says_what_its_sizes_have_to_be():
         sizes[name] += 4
         with pytest.raises(ValueError, match=f"^{name}: a multiple of 8"):
             RoutedBlock(**sizes)
+
+
+def test_losses_without_ids_are_not_held_to_the_ids_limits():
+    """E up to 1024: the limit of 256 is that of 8-bit ids, and none are given here."""
+    def bal(idx, E, T=0):
+        return B.load_library().grouter_balance_loss(A, E, B.F32, idx, B.IDX_U8, None, A, A, None, B.NORM_SOFTMAX, T, E, 1, 0.1, 0.1, None, None, A, None,
+                                                     None, None)
+    assert bal(None, 256) == OK and bal(None, 257) == OK and bal(None, 1024) == OK
+    assert bal(A, 257) == -3 and bal(None, 1025) == -3
