@@ -53,6 +53,7 @@ class RoutedBlock:
 
     def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None):
         """x [T,d] bf16; mask [T] (zero: padding, left out of the losses and the router's gradient) -> (out [T,d], losses f32 [3])."""
+        B._expect("x", x, (self.T, self.d), torch.bfloat16, like=self.status)
         w = self.w
         h, mean, rstd = B.layer_norm(x, w["norm_w"], w["norm_b"])
         idx, gates, scores = B.route(h, w["W_s"], None, self.E, self.k, want_scores=True)
@@ -69,6 +70,7 @@ class RoutedBlock:
 
     def backward(self, dout: torch.Tensor):
         """dout [T,d] bf16: gradient of the upstream loss -> dx [T,d] bf16; the weights' gradients go to self.grad."""
+        B._expect("dout", dout, (self.T, self.d), torch.bfloat16, like=self.status)
         x, mask, h, mean, rstd, idx, gates, scores, counts, n, u, pre = self._saved
         w, g = self.w, self.grad
         dh, _, _, dgates = self.layer.backward(dout, h, gates, w["W_gu"], w["W_d"], dW_gu=g["W_gu"], dW_d=g["W_d"])

@@ -154,3 +154,18 @@ def test_losses_without_ids_are_not_held_to_the_ids_limits():
                                                      None, None)
     assert bal(None, 256) == OK and bal(None, 257) == OK and bal(None, 1024) == OK
     assert bal(A, 257) == -3 and bal(None, 1025) == -3
+
+
+def test_the_block_checks_its_batch_before_a_kernel_reads_it():
+    """The plan and the layer take addresses: a shorter batch would be read past its end."""
+    from paper_2603_06626_b200.block import RoutedBlock
+    block = object.__new__(RoutedBlock)
+    block.T, block.d, block.status = 64, 32, torch.zeros(1, dtype=torch.int32)
+    for call, name in ((block.forward, "x"), (block.backward, "dout")):
+        for bad in (torch.zeros(56, 32), torch.zeros(72, 32), torch.zeros(64, 24)):
+            with pytest.raises(ValueError, match=f"^{name}: shape"):
+                call(bad.bfloat16())
+        with pytest.raises(TypeError, match=f"^{name}: torch.bfloat16"):
+            call(torch.zeros(64, 32))
+        with pytest.raises(ValueError, match=f"^{name}: a contiguous"):
+            call(torch.zeros(32, 64, dtype=torch.bfloat16).t())
