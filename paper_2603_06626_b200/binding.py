@@ -594,8 +594,9 @@ def _status_word(index: int) -> torch.Tensor:
 def check_status(device="cuda:0", status: Optional[torch.Tensor] = None) -> None:
     """Waits for the device; raises when a linear, linear_backward, expert_counts or balance_loss call without a status word of its own
     met a bounded wait that ran out or an expert id out of range since the last check, and clears the bits that it has seen.  That word
-    is one for all streams and threads of the process; calls that passed status= are checked by passing the same one here."""
-    index = _device_index(torch.device(device))
+    is one for all streams and threads of the process; calls that passed status= are checked by passing the same one here (the device
+    is then its own)."""
+    index = _device_index(torch.device(device) if status is None else status.device)
     torch.cuda.synchronize(index)
     word = _status_word(index) if status is None else status
     with _status_lock:

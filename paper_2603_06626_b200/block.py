@@ -91,7 +91,7 @@ class RoutedBlock:
     def check_status(self) -> None:
         """Raises on what this block's kernels found since the last check."""
         self.layer.check_status()
-        B.check_status(self.layer.device, status=self.status)
+        B.check_status(status=self.status)
 
 
 def main() -> None:

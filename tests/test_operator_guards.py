@@ -169,3 +169,11 @@ def test_the_block_checks_its_batch_before_a_kernel_reads_it():
             call(torch.zeros(64, 32))
         with pytest.raises(ValueError, match=f"^{name}: a contiguous"):
             call(torch.zeros(32, 64, dtype=torch.bfloat16).t())
+
+
+def test_a_check_of_a_given_word_waits_for_that_words_device(monkeypatch):
+    waited = []
+    monkeypatch.setattr(B, "_device_index", lambda dev: dev.index if dev.index is not None else 5)
+    monkeypatch.setattr(B.torch.cuda, "synchronize", lambda index: waited.append(index))
+    B.check_status(status=torch.zeros(1, dtype=torch.int32))       # stands for one on another device than the default, cuda:0
+    assert waited == [5]
