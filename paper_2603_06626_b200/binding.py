@@ -693,7 +693,7 @@ def _check_mask(mask: Optional[torch.Tensor], T: int, like: torch.Tensor) -> Non
 
 
 def expert_counts(idx: torch.Tensor, E: int, mask: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
-    """grouter_expert_counts: idx [T,k] uint8/int32, mask [T] uint8/bool (zero: the token does not count) -> (counts int32 [E],
+    """grouter_expert_counts: idx [T,k] uint8/int32 (16-byte aligned), mask [T] uint8/bool (zero: the token does not count) -> (counts int32 [E],
     counted tokens int32 [1])."""
     lib = load_library()
     if idx.dim() != 2:

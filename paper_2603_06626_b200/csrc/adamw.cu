@@ -15,12 +15,12 @@
 //
 // Every product, sum, quotient and root is rounded separately (no contraction), in the order written above: the result of
 // an element does not depend on which code path or compiler handles it.
-// Bound by HBM: 30 bytes an element (f32 moments and gradient, bf16 parameter), 16.06 with 8-bit moments and bf16 gradient.
+// Bound by HBM: 30 bytes an element (f32 moments and gradient, bf16 parameter), 16.125 with 8-bit moments and bf16 gradient.
 // Measured: 138 M elements with f32 moments 605-615 us (6.8 TB/s, a little above a plain copy's 6.46: reads outweigh writes);
 // 69 M with 8-bit moments and bf16 gradient 200 us (5.5 TB/s), 6 M of them in 120 tensors 21 us and 10 us to read the moments back.
 // The 8-bit form spends some 60 instructions an element, most of them on the exactly rounded root and quotient and on the codes:
 // whole chunks go without any test, two groups' exponents are reduced in one word, what is rare (values below the smallest code,
-// infinities) is behind a branch.
+// infinities) is behind a branch (and 8 bytes a thread are spilled, at five blocks an SM).
 // A table in device memory, built once on the host, cuts the tensors into chunks of ADAMW_CHUNK elements, one block each: small, so
 // that an SM always has blocks that load while others compute (8192 elements a block: 35 against 31 us for 6 M elements in
 // 120 small tensors with 8-bit moments, 620 against 604 us for 138 M with f32 moments).
@@ -127,9 +127,9 @@ __device__ __forceinline__ void store4(void* base, bool vec, int n, const float*
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (q < n) {
-      if constexpr (HALF) reinterpret_cast<__nv_bfloat16*>(base)[q] = __float2bfloat16_rn(f[q]);
-      else reinterpret_cast<float*>(base)[q] = f[q];
-    }
+        if constexpr (HALF) reinterpret_cast<__nv_bfloat16*>(base)[q] = __float2bfloat16_rn(f[q]);
+        else reinterpret_cast<float*>(base)[q] = f[q];
+      }
   }
 }
 
@@ -304,7 +304,7 @@ __device__ __forceinline__ void adamw_by_edge(const AdamwParams& a, const AdamwC
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(ADAMW_THREADS, BITS == 8 ? 5 : 5) adamw_kernel(const AdamwParams a) {
+__global__ void __launch_bounds__(ADAMW_THREADS, 5) adamw_kernel(const AdamwParams a) {
   const AdamwChunk ch = a.chunks[blockIdx.x];
   if (ch.flags & P_BF16) {
     if (ch.flags & G_BF16) adamw_by_edge<BITS, true, true>(a, ch);

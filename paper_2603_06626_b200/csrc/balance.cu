@@ -14,7 +14,9 @@
 // order, and the last step (one block) adds the blocks' sums in double precision.
 //
 // Measured: 1048575 tokens x 256 bf16 with a mask 190 us for losses and gradient (5.65 TB/s of 6.46), the counts 17 us before
-// them; 32768 x 128 f32 with the gates' gradient 21 us in all; 511 tokens 8.7 us (two launches).
+// them; 32768 x 128 f32 with the gates' gradient 21-22 us in all; 511 tokens 8.8 us (two launches).
+// With the gates' gradient wide routers are bound by registers and shared memory, not by HBM: 524288 x 160 bf16 194 us with the counts
+// (99 without gates), 1048575 x 60 148 us, 200000 x 333 154 us, each 3.4 to 3.6 times their bytes at a plain copy's pace.
 //
 // A score of -inf takes its expert out (p = 0, no gradient).  A row of nothing but -inf has p = 0 throughout and no
 // z-loss term.  A token whose mask byte is zero contributes nothing and gets a zero gradient row, whatever its scores are.
@@ -154,7 +156,8 @@ __device__ __forceinline__ void write_loss(const BalanceParams& p, double a, dou
   p.loss[2] = zl;
 }
 
-// 2^d; results below the normal range of f32 are zero
+// 2^d by the hardware's exponential (within 2 ulp of f32: the gradient of f32 scores is as close to the 64-bit definition as plain f32
+// operations come, 8e-8 of it); results below the normal range of f32 are zero
 __device__ __forceinline__ float exp2_of(float d) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
@@ -168,7 +171,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Rounds whose scores a thread has on their way or in use: 128 to 192 bytes of them.
+// Rounds whose scores a thread has on their way or in use: 96 to 256 bytes of them.
 __host__ __device__ constexpr int balance_ring(int bytes, int epl) { return bytes * epl >= 64 ? (bytes * epl >= 128 ? 2 : 3) : bytes * epl >= 32 ? 4 : 6; }
 
 // LPT neighbouring lanes hold a token's row, EPL elements each, VE to an access.  Few lanes and many elements: the three
@@ -473,7 +476,7 @@ constexpr int BAL_MAX_BLOCKS = 1184;   // 148 SMs x 8 blocks
 constexpr int BAL_CLUSTER = 8;         // a grid of up to so many blocks is one cluster, and needs neither workspace nor second kernel
 
 // Lanes a token: enough for 16 elements each and for one of the kept experts each.  (With or without gates: the sums of a row then
-// run in the same order and the losses are the same bits.)
+// run in the same order, and while one round of blocks holds all tokens the losses are the same bits.)
 int balance_lanes(int E, int k) {
   int lpt = 1;
   while (lpt < 32 && (lpt * 16 < E || lpt < k)) lpt *= 2;

@@ -5,8 +5,9 @@
 //
 // The products run on the CTA-pair tcgen05 core of the grouped products (gemm.cu, MODE_LINEAR / MODE_DENSE) or, for few tokens, on
 // the kernel of linear_small.cu: bf16 operands, fp32 accumulators; bias, activation and residual are applied in fp32 on the
-// accumulator and rounded once.  Bound by the tensor cores: 32768 x 4096 x 1536 with SiLU and both outputs takes 320-357 us, 1.29-1.15
-// PFLOP/s as the GPU goes from rested to its power limit (8192 x 8192 x 8192 plain: 1.36).
+// accumulator and rounded once.  Bound by the tensor cores: 32768 x 4096 x 1536 with SiLU and both outputs takes 312-353 us, 1.32-1.17
+// PFLOP/s as the GPU goes from rested to its power limit; without the epilogue 288-328, as long as a library's product of these
+// sizes (292-328).  8192 x 8192 x 8192 plain: 1.48-1.26 PFLOP/s, 8 to 9 % behind the library's 1.63-1.38.
 // dz is rounded to bf16, the type the tensor cores take it in; db is summed from the unrounded values.  One pass over dy and
 // z writes dz and the partial column sums; without an activation dz is dy and the pass only sums (or is left out).
 // dW's output matrix is often too small to give every CTA pair a tile: its contraction over the tokens is then cut into

@@ -7,8 +7,10 @@
 // 90 KB of the weight on its way into each.  The CTAs then leave their fp32 partial tiles in shared memory, every one adds up
 // a share of the outputs over the S tiles in rank order (bit-reproducible), applies bias, activation and residual and writes.
 //
-// Bound by HBM (the weight).  Measured, weight 4096 x 4096 (33.5 MB, 5.2 us at a plain copy's pace): one token 8.4 us, 64 tokens
-// 12 us, 256 tokens 18 us; 128 x 128 with one token 4.1 us, which is what launch, set-up and the cluster's two barriers take.
+// Bound by latency more than by the weight's bytes.  Measured, weight 4096 x 4096 (33.5 MB, 5.2 us at a plain copy's pace): one token
+// 9.9 us with ten weights in turn (335 MB, from HBM), 8.5 with three (100 MB, which stay in L2); with three, 64 tokens 12 us and 256
+// tokens 18; 128 x 128 with one token 4.1 us, which is what launch, set-up and the cluster's two barriers take.  A CTA has eight steps
+// and a ring of six, so its first load and its epilogue are most of its time.
 //
 // Roles in a CTA: warp 0 loads (TMA, ring of STAGES 64-deep steps), warp 1 issues the MMAs, warps 2-5 bring the accumulator to
 // shared memory; all six share the epilogue.  Every wait is bounded, as in the CTA-pair core: on give-up the CTA raises

@@ -9,14 +9,15 @@
 // Both passes touch every element once and are bound by HBM, but only if they are lean: at 6.4 TB/s an SM has some 20 (forward)
 // and 30 (backward) instruction slots for an element of bf16, so the arithmetic is done two elements to an instruction (f32x2).
 // Sums are taken in fp32, the variance from the centred values (never as a difference of large sums).
-// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 84 us (6.4 TB/s), 65536 x 512 22 us (6.1);
-// backward with both kernels 16384 x 4096 bf16 76 us (5.3), 16384 x 2048 44 us (4.6), 8192 x 4096 f32 75 us (5.4), 8192 x 16384 f32
-// 299 us (5.4).  Rows that are not 16-byte aligned go by pairs, or by single elements where even those do not fit: 16384 x 4094
-// bf16 55 us forward, 102 us backward, 16384 x 4095 87 and 119 us.
+// Measured on a B200 whose plain copy runs at 6.46 TB/s: forward 32768 x 4096 bf16 84 us (6.4 TB/s), 65536 x 512 22-25 us (6.1-5.3),
+// 8192 x 16384 85 us (6.3);  backward with both kernels 16384 x 4096 bf16 74 us (5.4), 16384 x 2048 43 us (4.7), 8192 x 4096 f32 74 us
+// (5.4), 8192 x 16384 f32 299 us (5.4) and bf16 202 us (4.0: 1024 threads a row, one row an SM).  Rows that are not 16-byte aligned go
+// by pairs, or by single elements where even those do not fit: 16384 x 4094 bf16 55 us forward, 100 us backward, 16384 x 4095 88
+// and 117 us.  Wider than 8192 such rows spill registers in the backward pass (160 to 192 bytes a thread): 8192 x 16383 bf16 395 us.
 //   Forward: a row lies in the registers of as many lanes (a quarter of a warp to 32 warps) as hold it in a few accesses each, as it
 //     was loaded; nothing is kept from row to row.
 //   Backward: the running dw and db of a column have to stay with one thread, so a row is spread over enough threads for 16
-//     elements each (eight for a row of 128: 262144 x 128 bf16 40 us, with a warp 87); blocks are resident and walk over the rows (the
+//     elements each (eight for a row of 128: 262144 x 128 bf16 39 us, with a warp 87); blocks are resident and walk over the rows (the
 //     coming ones on their way into shared memory), every cluster of them writes one partial row, and a second small kernel adds
 //     those up in a fixed order (bit-reproducible, no atomics).
 #include <cooperative_groups.h>
@@ -598,7 +599,7 @@ cudaError_t norm_dispatch(const NormArgs& a, int dtype) {
 int norm_check(int32_t rows, int32_t d, int64_t ldx, int32_t dtype, int32_t w_dtype) {
   if (rows < 0 || d < 1 || ldx < d) return GROUTER_ERR_INVALID_ARG;
   if ((dtype != GROUTER_BF16 && dtype != GROUTER_F32) || (w_dtype != GROUTER_BF16 && w_dtype != GROUTER_F32)) return GROUTER_ERR_INVALID_ARG;
-  // the row counters of the resident blocks step past the last row by up to one grid
+  // rows are rounded up to whole blocks in 32 bits
   return d > NORM_MAX_D || rows > INT32_MAX - (1 << 20) ? GROUTER_ERR_UNSUPPORTED : GROUTER_OK;
 }
 
