@@ -396,6 +396,83 @@ int grouter_adamw_step(const grouter_adamw_layout* layout, const void* table, in
 int grouter_adamw_moments(const void* m, const void* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t elements, float* m_out,
                           float* v_out, void* stream);
 
+/* Root-mean-square norm on a residual stream:  h = x + residual (rounded to dtype),  rstd = ((1/d) sum h^2 + eps)^(-1/2),  y = h * rstd * w.
+ *   x, residual [rows, d] of dtype, row r at x + r*ldx, residual + r*ldr elements (ldx, ldr >= d)      residual may be NULL: h is x
+ *   w [d] of w_dtype      h [rows, d] of dtype out, contiguous, with a residual only      rstd [rows] f32 out or NULL
+ *   scales NULL: y [rows, d] of dtype, contiguous.  Else y [rows, d] e4m3 codes, scales their scales (grouter_fp8_scale_bytes(rows, d)
+ *   bytes) as grouter_quantize_fp8 makes them; d is then a multiple of 16 and all rows, w, y and scales are 16-byte aligned.
+ * The norm is that of h as it is stored.  Sums and statistics are fp32; y is rounded once.  Outputs must not overlap the inputs.
+ * d <= 16384.  rows = 0 does nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+int grouter_rmsnorm_fwd(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* w, int32_t rows, int32_t d, int32_t dtype,
+                        int32_t w_dtype, float eps, void* h, void* y, void* scales, float* rstd, void* stream);
+/* Its backward pass, from h and the saved rstd:  with u = h * rstd and g = dy * w,
+ *   dx = dh + rstd * (g - u * (1/d) sum g*u)  [rows, d] of dtype: the gradient of x and of the residual
+ *   dw = sum over rows of dy * u  [d] f32
+ *   dh [rows, d] of dtype, contiguous: the gradient that reaches h along the stream, or NULL (0)
+ * dy and dx are contiguous; outputs must not overlap the inputs.  workspace: grouter_rmsnorm_bwd_workspace_bytes(rows, d) bytes (of
+ * the current device).  All sums run in a fixed order: results are bit-reproducible.  rows = 0 zeroes dw.  Errors as above. */
+size_t grouter_rmsnorm_bwd_workspace_bytes(int32_t rows, int32_t d);
+int grouter_rmsnorm_bwd(const void* dy, const void* h, int64_t ldh, const void* dh, const void* w, const float* rstd, int32_t rows, int32_t d,
+                        int32_t dtype, int32_t w_dtype, void* dx, float* dw, void* workspace, void* stream);
+
+/* Matrices in 8 bits: e4m3 codes and one power-of-two scale for 128 neighbours of a row.  The scale of a block is 2^e with the smallest
+ * e >= -126 for which no finite element is above 448 * 2^e in magnitude; a code is element / 2^e rounded to nearest even; infinities and NaN
+ * have the NaN code and no say in the scale.
+ *   codes [rows, grouter_fp8_pitch(cols)] bytes: rows padded to a multiple of 16 with zeros
+ *   scales: grouter_fp8_scale_bytes(rows, cols) bytes, e + 127 (1 .. 254) of row r, block b at
+ *     ((r / 128) * ceil(cols / 512) + b / 4) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4,
+ *     the order in which the tensor cores take them; the bytes of rows and blocks that are not there hold anything
+ * grouter_quantize_fp8: x [rows, cols] of dtype, row r at x + r*ldx elements, any alignment -> codes and scales of its rows (codes NULL:
+ *   not wanted) and codes_t, scales_t [cols, ...] of the transposed matrix's (NULL: not wanted), whose blocks run along x's rows.
+ *   square != 0: one scale for 128 x 128 elements, the same in both forms (weights).
+ * grouter_dequantize_fp8: y [rows, cols] of dtype, row r at y + r*ldy elements: the values that codes and scales stand for (exact
+ *   in both types; what was rounded up to 2^128 is an infinity).
+ * codes and scales are 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+size_t grouter_fp8_pitch(int32_t cols);
+size_t grouter_fp8_scale_bytes(int32_t rows, int32_t cols);
+int grouter_quantize_fp8(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t cols, int32_t square, void* codes, void* scales,
+                         void* codes_t, void* scales_t, void* stream);
+int grouter_dequantize_fp8(const void* codes, const void* scales, int32_t rows, int32_t cols, int64_t ldy, int32_t dtype, void* y, void* stream);
+
+/* Linear layer in 8 bits:  y = x W^T + bias + residual  for x [T,K], W [N,K] as codes and scales (the products of a block of 128 are
+ * multiplied by both scales and added up in fp32, bias and residual in fp32, y rounded once).
+ *   bias [N] or NULL, residual [T,N] or NULL, y [T,N] out: bf16, contiguous.  residual may be y itself.
+ *   status: device int32 the kernels OR bits into (2 = a bounded wait ran out); the caller zeroes it
+ * Required: N a multiple of 8, everything 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+int grouter_linear_fp8_fwd(const void* x, const void* x_scales, const void* W, const void* W_scales, const void* bias, const void* residual, int32_t T,
+                           int32_t K, int32_t N, void* y, int32_t* status, void* stream);
+/* Its backward pass from dy [T,N] bf16 (contiguous), which is put into 8 bits here, by rows for dx and by columns for dW:
+ *   dx = q(dy) W [T,K] bf16      dW = q(dy^T) x [N,K] of dW_dtype      db = sum over tokens of dy [N] f32 (not in 8 bits)
+ *   xt, Wt: codes and scales of the transposed matrices, x^T [K,T] for dW and W^T [K,N] for dx (grouter_quantize_fp8's codes_t)
+ * Outputs that are not wanted are NULL (at least one is wanted).  K and N multiples of 8.  Results are bit-reproducible.  workspace:
+ * grouter_linear_fp8_bwd_workspace_bytes(T, K, N) bytes (of the current device), 256-byte aligned.  T = 0 zeroes dW and db.  Errors as above. */
+size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N);
+int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales, const void* Wt, const void* Wt_scales, int32_t T, int32_t K, int32_t N,
+                           void* dx, void* dW, int32_t dW_dtype, float* db, void* workspace, int32_t* status, void* stream);
+
+/* Gated feed-forward block:  pre = x W_gu^T = [g | u],  h = act(g) * u,  y = h W_d^T + residual   (bf16, contiguous, 16-byte aligned).
+ *   x [T,d]   W_gu [2H,d], gate rows first   W_d [d,H]   residual [T,d] or NULL   h [T,H] out   y [T,d] out   pre [T,2H] out, or NULL
+ *   act: GROUTER_ACT_*      status: as for the linear layer
+ * Two launches: both projections, activation and product; the product with W_d.  fp32 accumulators; h is formed in fp32 and rounded
+ * once, pre and y too.  d and H multiples of 8, T >= 0.  residual may be y itself.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+int grouter_gated_ffn_fwd(const void* x, const void* W_gu, const void* W_d, const void* residual, int32_t T, int32_t d, int32_t H, int32_t act,
+                          void* h, void* y, void* pre, int32_t* status, void* stream);
+/* Its backward pass:  dh = dy W_d,  dpre = [dh * u * act'(g) | dh * act(g)] (relu'(0) = 0),
+ *   dx = dpre W_gu [T,d] bf16      dW_gu = dpre^T x [2H,d],  dW_d = dy^T h [d,H] of dW_dtype
+ * Outputs that are not wanted are NULL (at least one is wanted); the residual's gradient is dy.  h is formed again from pre; h and dpre
+ * enter the products rounded to bf16, dh does not leave fp32.  Results are bit-reproducible.  workspace:
+ * grouter_gated_ffn_bwd_workspace_bytes(T, d, H) bytes (of the current device), 256-byte aligned.  T = 0 zeroes dW_gu and dW_d. */
+size_t grouter_gated_ffn_bwd_workspace_bytes(int32_t T, int32_t d, int32_t H);
+int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const void* W_d, const void* pre, int32_t T, int32_t d, int32_t H,
+                          int32_t act, void* dx, void* dW_gu, void* dW_d, int32_t dW_dtype, void* workspace, int32_t* status, void* stream);
+/* The same block's forward pass in 8 bits:  h = act(x W_g^T) * (x W_u^T) in fp32, put into codes (128 columns a scale) as
+ * grouter_quantize_fp8 does,  y = h W_d^T + residual.  x [T,d], W_g, W_u [H,d], W_d [d,H], h [T,H] out: codes and scales;
+ * residual [T,d] or NULL, y [T,d]: bf16. */
+int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, const void* W_g, const void* W_g_scales, const void* W_u, const void* W_u_scales,
+                              const void* W_d, const void* W_d_scales, const void* residual, int32_t T, int32_t d, int32_t H, int32_t act, void* h,
+                              void* h_scales, void* y, int32_t* status, void* stream);
+
 /* Synchronises `stream` and returns the sticky device status (GROUTER_OK,
  * GROUTER_ERR_BAD_INDEX, GROUTER_ERR_TIMEOUT) or GROUTER_ERR_CUDA; clears it. */
 int grouter_status(grouter_ctx* ctx, void* stream);

@@ -33,7 +33,11 @@ EXPORTS = ["grouter_create", "grouter_destroy", "grouter_workspace_bytes", "grou
            "grouter_layernorm_fwd", "grouter_layernorm_bwd", "grouter_layernorm_bwd_workspace_bytes",
            "grouter_linear_fwd", "grouter_linear_bwd", "grouter_linear_bwd_workspace_bytes",
            "grouter_expert_counts", "grouter_balance_loss", "grouter_balance_loss_workspace_bytes",
-           "grouter_adamw_layout_host", "grouter_adamw_step", "grouter_adamw_moments"]
+           "grouter_adamw_layout_host", "grouter_adamw_step", "grouter_adamw_moments",
+           "grouter_rmsnorm_fwd", "grouter_rmsnorm_bwd", "grouter_rmsnorm_bwd_workspace_bytes",
+           "grouter_fp8_pitch", "grouter_fp8_scale_bytes", "grouter_quantize_fp8", "grouter_dequantize_fp8",
+           "grouter_linear_fp8_fwd", "grouter_linear_fp8_bwd", "grouter_linear_fp8_bwd_workspace_bytes",
+           "grouter_gated_ffn_fwd", "grouter_gated_ffn_bwd", "grouter_gated_ffn_bwd_workspace_bytes", "grouter_gated_ffn_fp8_fwd"]
 KERNEL_SLOTS = ["plan_hist", "plan_permute", "gather_X", "gemm_up_swiglu", "gemm_down", "combine_Y", "gather_dY", "gemm_dH",
                 "wgrad_down", "gemm_dX", "wgrad_gate_up", "reduce_dX", "zero_split_dW", "plan_scan"]
 
@@ -170,6 +174,24 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.grouter_adamw_step.restype = ctypes.c_int
     lib.grouter_adamw_moments.argtypes = [vp] * 4 + [i64, vp, vp, vp]
     lib.grouter_adamw_moments.restype = ctypes.c_int
+    size = ctypes.c_size_t
+    for name, result, args in (
+            ("rmsnorm_fwd", i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp]),
+            ("rmsnorm_bwd_workspace_bytes", size, [i32, i32]),
+            ("rmsnorm_bwd", i32, [vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
+            ("fp8_pitch", size, [i32]),
+            ("fp8_scale_bytes", size, [i32, i32]),
+            ("quantize_fp8", i32, [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp]),
+            ("dequantize_fp8", i32, [vp, vp, i32, i32, i64, i32, vp, vp]),
+            ("linear_fp8_fwd", i32, [vp] * 6 + [i32] * 3 + [vp] * 3),
+            ("linear_fp8_bwd_workspace_bytes", size, [i32] * 3),
+            ("linear_fp8_bwd", i32, [vp] * 5 + [i32] * 3 + [vp, vp, i32] + [vp] * 4),
+            ("gated_ffn_fwd", i32, [vp] * 4 + [i32] * 4 + [vp] * 5),
+            ("gated_ffn_bwd_workspace_bytes", size, [i32] * 3),
+            ("gated_ffn_bwd", i32, [vp] * 5 + [i32] * 4 + [vp] * 3 + [i32] + [vp] * 3),
+            ("gated_ffn_fp8_fwd", i32, [vp] * 9 + [i32] * 4 + [vp] * 5)):
+        fn = getattr(lib, "grouter_" + name)
+        fn.restype, fn.argtypes = result, args
     if path == _build.LIB:
         _lib = lib
     return lib
@@ -592,8 +614,8 @@ def _status_word(index: int) -> torch.Tensor:
 
 
 def check_status(device="cuda:0", status: Optional[torch.Tensor] = None) -> None:
-    """Waits for the device; raises when a linear, linear_backward, expert_counts or balance_loss call without a status word of its own
-    met a bounded wait that ran out or an expert id out of range since the last check, and clears the bits that it has seen.  That word
+    """Waits for the device; raises when a linear, linear_backward, gated_ffn, fp8 product, expert_counts or balance_loss call without a
+    status word of its own met a bounded wait that ran out or an expert id out of range since the last check, and clears the bits that it has seen.  That word
     is one for all streams and threads of the process; calls that passed status= are checked by passing the same one here (the device
     is then its own)."""
     index = _device_index(torch.device(device) if status is None else status.device)
@@ -841,6 +863,322 @@ class AdamW:
         _call(self.lib.grouter_adamw_moments, "grouter_adamw_moments", self._index, self.m.data_ptr(), self.v.data_ptr(), self.m_exp.data_ptr(),
               self.v_exp.data_ptr(), self.m.numel(), m.data_ptr(), v.data_ptr())
         return m, v
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, fp8: bool = False):
+    """grouter_rmsnorm_fwd: x, residual [T,d] bf16/f32 (rows may be strided), weight [d] bf16/f32 -> (y, h, rstd f32 [T]) with
+    h = x + residual (without a residual: x itself), y = h * rstd * weight.  fp8: y as Fp8Blocks (d a multiple of 16, rows 16-byte
+    aligned)."""
+    lib = load_library()
+    ldx = _row_stride("x", x)
+    T, d = x.shape
+    on = x.device
+    if not _fits(weight, (d,), weight.dtype, on):
+        _expect("weight", weight, (d,), like=x)
+    ldr = d
+    if residual is not None:
+        ldr = _row_stride("residual", residual)
+        if residual.shape != x.shape or residual.dtype != x.dtype or residual.device != on:
+            raise ValueError(f"residual: like x expected ({tuple(x.shape)} {x.dtype} on {on}), got {tuple(residual.shape)} {residual.dtype} on {residual.device}")
+    dt, wt = _elt(x, "x"), _elt(weight, "weight")
+    dev = _device_index(on)
+    if fp8 and d % 16:
+        raise ValueError(f"x: with fp8 rows of a multiple of 16 elements are expected, got {d}")
+    h = x if residual is None else _dense_like(x)
+    y = Fp8Blocks.empty(T, d, on) if fp8 else _dense_like(x)
+    rstd = x.new_empty(T, dtype=torch.float32)
+    _call(lib.grouter_rmsnorm_fwd, "grouter_rmsnorm_fwd", dev, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+          weight.data_ptr(), T, d, dt, wt, eps, None if residual is None else h.data_ptr(), y.codes.data_ptr() if fp8 else y.data_ptr(),
+          y.scales.data_ptr() if fp8 else None, rstd.data_ptr())
+    return y, h, rstd
+
+
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dh: Optional[torch.Tensor] = None,
+                      dw: Optional[torch.Tensor] = None):
+    """grouter_rmsnorm_bwd, from the forward's h and rstd -> (dx like h, the gradient of x and of the residual; dw f32 [d]).  dh: the
+    gradient that reaches h along the residual stream, added to dx.  dw: a tensor to write the gradient into."""
+    lib = load_library()
+    ldh = _row_stride("h", h)
+    T, d = h.shape
+    on, f32 = h.device, torch.float32
+    if not (_fits(dy, h.shape, h.dtype, on) and _fits(dh, h.shape, h.dtype, on) and _fits(weight, (d,), weight.dtype, on) and
+            _fits(rstd, (T,), f32, on) and _fits(dw, (d,), f32, on)):
+        _expect("dy", dy, (T, d), h.dtype, like=h)
+        _expect("dh", dh, (T, d), h.dtype, like=h)
+        _expect("weight", weight, (d,), like=h)
+        _expect("rstd", rstd, (T,), f32, like=h)
+        _expect("dw", dw, (d,), f32, like=h)
+    dt, wt = _elt(h, "h"), _elt(weight, "weight")
+    dev = _device_index(on)
+    dx = torch.empty_like(dy)
+    if dw is None:
+        dw = h.new_empty(d, dtype=f32)
+    ws = h.new_empty(_bytes(lib.grouter_rmsnorm_bwd_workspace_bytes, dev, T, d), dtype=torch.uint8)
+    _call(lib.grouter_rmsnorm_bwd, "grouter_rmsnorm_bwd", dev, dy.data_ptr(), h.data_ptr(), ldh, _ptr(dh), weight.data_ptr(), rstd.data_ptr(), T, d,
+          dt, wt, dx.data_ptr(), dw.data_ptr(), ws.data_ptr())
+    return dx, dw
+
+
+class Fp8Blocks:
+    """A matrix [rows, cols] in 8 bits: codes [rows, cols rounded up to 16] float8_e4m3fn, zeros behind the last column, and scales, a
+    power of two for 128 neighbours of a row, as uint8 exponents + 127 [ceil(rows / 128), ceil(cols / 512), 32, 4, 4]: the scale of row r,
+    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h)."""
+
+    __slots__ = ("codes", "scales", "cols")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
+        self.codes, self.scales, self.cols = codes, scales, int(cols)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device) -> "Fp8Blocks":
+        return cls(torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device),
+                   torch.empty(cls.scale_shape(rows, cols), dtype=torch.uint8, device=device), cols)
+
+    @staticmethod
+    def scale_shape(rows: int, cols: int):
+        return (rows + 127) // 128, (cols + 511) // 512, 32, 4, 4
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], self.cols
+
+    @property
+    def device(self) -> torch.device:
+        return self.codes.device
+
+    def scale_exponents(self) -> torch.Tensor:
+        """The scales as a matrix [rows, ceil(cols / 128)] of exponents + 127."""
+        rows, cols = self.shape
+        a, b = self.scales.shape[:2]
+        return self.scales.permute(0, 3, 2, 1, 4).reshape(128 * a, 4 * b)[:rows, :(cols + 127) // 128]
+
+
+def _expect_fp8(what: str, q: Optional[Fp8Blocks], shape, like: Optional[torch.device] = None) -> None:
+    """Raises unless q (None passes) holds a matrix of this shape in the layout that the kernels read, on the device `like`."""
+    if q is None:
+        return
+    if not isinstance(q, Fp8Blocks):
+        raise TypeError(f"{what}: Fp8Blocks expected, got {type(q).__name__}")
+    rows, cols = shape
+    on = q.codes.device if like is None else like
+    if (q.cols == cols and _fits(q.codes, (rows, (cols + 15) // 16 * 16), torch.float8_e4m3fn, on) and
+            _fits(q.scales, Fp8Blocks.scale_shape(rows, cols), torch.uint8, on)):
+        return
+    if q.cols != cols:
+        raise ValueError(f"{what}: {cols} columns expected, got {q.cols}")
+    where = torch.empty(0, device=on)
+    _expect(f"{what}: codes", q.codes, (rows, (cols + 15) // 16 * 16), torch.float8_e4m3fn, like=where)
+    _expect(f"{what}: scales", q.scales, Fp8Blocks.scale_shape(rows, cols), torch.uint8, like=where)
+
+
+def quantize_fp8(x: torch.Tensor, square: bool = False, rows: bool = True, transposed: bool = False):
+    """grouter_quantize_fp8: x [R,C] bf16/f32 (rows may be strided) -> (Fp8Blocks of x, Fp8Blocks of x transposed), None for the form that is
+    not wanted.  One scale for 128 neighbours of a row of that form; square: for 128 x 128 elements, the same in both (weights)."""
+    lib = load_library()
+    ld = _row_stride("x", x)
+    R, C = x.shape
+    dt = _elt(x, "x")
+    if not rows and not transposed:
+        raise ValueError("rows, transposed: at least one of them is expected")
+    dev = _device_index(x.device)
+    q = Fp8Blocks.empty(R, C, x.device) if rows else None
+    t = Fp8Blocks.empty(C, R, x.device) if transposed else None
+    _call(lib.grouter_quantize_fp8, "grouter_quantize_fp8", dev, x.data_ptr(), ld, dt, R, C, int(square), q.codes.data_ptr() if rows else None,
+          q.scales.data_ptr() if rows else None, t.codes.data_ptr() if transposed else None, t.scales.data_ptr() if transposed else None)
+    return q, t
+
+
+def dequantize_fp8(q: Fp8Blocks, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """grouter_dequantize_fp8: the values that codes and scales stand for, [rows, cols] bf16 or f32."""
+    lib = load_library()
+    if not isinstance(q, Fp8Blocks):
+        raise TypeError(f"q: Fp8Blocks expected, got {type(q).__name__}")
+    _expect_fp8("q", q, (q.rows, q.cols))
+    rows, cols = q.shape
+    y = torch.empty((rows, cols), dtype=dtype, device=q.device)
+    dt = _elt(y, "dtype")
+    dev = _device_index(q.device)
+    _call(lib.grouter_dequantize_fp8, "grouter_dequantize_fp8", dev, q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, cols, dt, y.data_ptr())
+    return y
+
+
+def _rows_of(what: str, x, cols: int, on: torch.device) -> int:
+    """Rows of an argument that is Fp8Blocks or a bf16 matrix, with `cols` columns on device `on`; others raise."""
+    if isinstance(x, Fp8Blocks):
+        _expect_fp8(what, x, (x.rows, cols), on)
+        return x.rows
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16:
+        raise TypeError(f"{what}: Fp8Blocks or a bfloat16 matrix expected")
+    if x.dim() != 2 or x.shape[1] != cols or x.device != on:
+        raise ValueError(f"{what}: a matrix of {cols} columns on {on} is expected, got {tuple(x.shape)} on {x.device}")
+    return x.shape[0]
+
+
+def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+               status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """grouter_linear_fp8_fwd: x W^T + bias + residual, x [T,K] as Fp8Blocks or bf16 (rows may be strided; put into 8 bits by this call),
+    W [N,K] as Fp8Blocks (quantize_fp8 with square), bias and residual bf16 -> y bf16 [T,N]."""
+    lib = load_library()
+    if not isinstance(W, Fp8Blocks):
+        raise TypeError(f"W: Fp8Blocks expected, got {type(W).__name__}")
+    on = W.device
+    N, K = W.shape
+    _expect_fp8("W", W, (N, K))
+    T = _rows_of("x", x, K, on)
+    bf = torch.bfloat16
+    if not (_fits(bias, (N,), bf, on) and _fits(residual, (T, N), bf, on) and _fits(status, (1,), torch.int32, on)):
+        _expect("bias", bias, (N,), bf, like=W.codes)
+        _expect("residual", residual, (T, N), bf, like=W.codes)
+        _expect("status", status, (1,), torch.int32, like=W.codes)
+    dev = _device_index(on)
+    if not isinstance(x, Fp8Blocks):
+        x = quantize_fp8(x)[0]
+    y = torch.empty((T, N), dtype=bf, device=on)
+    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, x.codes.data_ptr(), x.scales.data_ptr(), W.codes.data_ptr(), W.scales.data_ptr(),
+          _ptr(bias), _ptr(residual), T, K, N, y.data_ptr(), _status_ptr(status, dev))
+    return y
+
+
+def linear_fp8_backward(dy: torch.Tensor, xt: Optional[Fp8Blocks], Wt: Optional[Fp8Blocks], want_dx: bool = True, want_dW: bool = True,
+                        want_bias: bool = False, dW_dtype: torch.dtype = torch.bfloat16, dW: Optional[torch.Tensor] = None,
+                        db: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """grouter_linear_fp8_bwd: dy [T,N] bf16, xt = x^T [K,T] (for dW) and Wt = W^T [K,N] (for dx), the transposed codes of quantize_fp8 ->
+    (dx bf16 [T,K], dW [N,K] of dW_dtype, db f32 [N]), None for what is not wanted.  dy is put into 8 bits by this call.  The residual's
+    gradient is dy.  dW, db: tensors to write the gradients into (dW bf16 or f32)."""
+    lib = load_library()
+    if dy.dim() != 2:
+        raise ValueError("dy: a matrix is expected")
+    T, N = dy.shape
+    want_dW = want_dW or dW is not None
+    if (want_dx and Wt is None) or (want_dW and xt is None):
+        raise ValueError("Wt is needed for dx, xt for dW")
+    if not (want_dx or want_dW or want_bias or db is not None):
+        raise ValueError("at least one gradient has to be wanted")
+    for name, q in (("xt", xt), ("Wt", Wt)):
+        if q is not None and not isinstance(q, Fp8Blocks):
+            raise TypeError(f"{name}: Fp8Blocks expected, got {type(q).__name__}")
+    K = Wt.rows if Wt is not None else xt.rows if xt is not None else 8
+    bf, on = torch.bfloat16, dy.device
+    _expect_fp8("xt", xt, (K, T), on)
+    _expect_fp8("Wt", Wt, (K, N), on)
+    if not (_fits(dy, (T, N), bf, on) and _fits(db, (N,), torch.float32, on) and _fits(status, (1,), torch.int32, on)):
+        _expect("dy", dy, (T, N), bf)
+        _expect("db", db, (N,), torch.float32, like=dy)
+        _expect("status", status, (1,), torch.int32, like=dy)
+    if dW is not None:
+        dW_dtype = dW.dtype
+        _expect("dW", dW, (N, K), like=dy)
+    if dW_dtype != bf and dW_dtype != torch.float32:
+        raise TypeError(f"dW: bfloat16 or float32 expected, got {dW_dtype}")
+    dev = _device_index(on)
+    dx = dy.new_empty((T, K)) if want_dx else None
+    if dW is None and want_dW:
+        dW = dy.new_empty((N, K), dtype=dW_dtype)
+    if db is None and want_bias:
+        db = dy.new_empty(N, dtype=torch.float32)
+    ws = dy.new_empty(_bytes(lib.grouter_linear_fp8_bwd_workspace_bytes, dev, T, K, N), dtype=torch.uint8)
+    codes = lambda q: (None, None) if q is None else (q.codes.data_ptr(), q.scales.data_ptr())  # noqa: E731
+    _call(lib.grouter_linear_fp8_bwd, "grouter_linear_fp8_bwd", dev, dy.data_ptr(), *codes(xt), *codes(Wt), T, K, N, _ptr(dx), _ptr(dW),
+          F32 if dW_dtype == torch.float32 else BF16, _ptr(db), ws.data_ptr(), _status_ptr(status, dev))
+    return dx, dW, db
+
+
+def _gated_shapes(x: torch.Tensor, W_gu: torch.Tensor, W_d: torch.Tensor):
+    if x.dim() != 2 or W_gu.dim() != 2 or W_d.dim() != 2:
+        raise ValueError("x, W_gu and W_d: matrices are expected")
+    return x.shape[0], x.shape[1], W_d.shape[1]
+
+
+def gated_ffn(x: torch.Tensor, W_gu: torch.Tensor, W_d: torch.Tensor, act: int = ACT_SILU, residual: Optional[torch.Tensor] = None,
+              save_pre: bool = False, status: Optional[torch.Tensor] = None):
+    """grouter_gated_ffn_fwd: (act(g) * u) W_d^T + residual with [g | u] = x W_gu^T, x [T,d], W_gu [2H,d] (gate rows first), W_d [d,H], all
+    bf16 -> (y [T,d], [g | u] [T,2H] or None)."""
+    lib = load_library()
+    T, d, H = _gated_shapes(x, W_gu, W_d)
+    bf, on = torch.bfloat16, x.device
+    if not (_fits(x, (T, d), bf, on) and _fits(W_gu, (2 * H, d), bf, on) and _fits(W_d, (d, H), bf, on) and _fits(residual, (T, d), bf, on) and
+            _fits(status, (1,), torch.int32, on)):
+        _expect("x", x, (T, d), bf)
+        _expect("W_d", W_d, (d, H), bf, like=x)
+        _expect("W_gu", W_gu, (2 * H, d), bf, like=x)
+        _expect("residual", residual, (T, d), bf, like=x)
+        _expect("status", status, (1,), torch.int32, like=x)
+    dev = _device_index(on)
+    h, y = x.new_empty((T, H)), x.new_empty((T, d))
+    pre = x.new_empty((T, 2 * H)) if save_pre else None
+    _call(lib.grouter_gated_ffn_fwd, "grouter_gated_ffn_fwd", dev, x.data_ptr(), W_gu.data_ptr(), W_d.data_ptr(), _ptr(residual), T, d, H, act,
+          h.data_ptr(), y.data_ptr(), _ptr(pre), _status_ptr(status, dev))
+    return y, pre
+
+
+def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, W_gu: torch.Tensor, W_d: torch.Tensor, pre: torch.Tensor, act: int = ACT_SILU,
+                       want_dx: bool = True, want_dW: bool = True, dW_dtype: torch.dtype = torch.bfloat16, dW_gu: Optional[torch.Tensor] = None,
+                       dW_d: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """grouter_gated_ffn_bwd; pre: the forward's [g | u] -> (dx bf16 [T,d], dW_gu [2H,d], dW_d [d,H] of dW_dtype), None for what is not
+    wanted.  The residual's gradient is dy.  dW_gu, dW_d: tensors to write the gradients into (both bf16 or both f32)."""
+    lib = load_library()
+    T, d, H = _gated_shapes(x, W_gu, W_d)
+    bf, on = torch.bfloat16, x.device
+    if not (_fits(x, (T, d), bf, on) and _fits(W_gu, (2 * H, d), bf, on) and _fits(W_d, (d, H), bf, on) and _fits(dy, (T, d), bf, on) and
+            _fits(pre, (T, 2 * H), bf, on) and _fits(status, (1,), torch.int32, on)):
+        _expect("x", x, (T, d), bf)
+        _expect("W_d", W_d, (d, H), bf, like=x)
+        _expect("W_gu", W_gu, (2 * H, d), bf, like=x)
+        _expect("dy", dy, (T, d), bf, like=x)
+        _expect("pre", pre, (T, 2 * H), bf, like=x)
+        _expect("status", status, (1,), torch.int32, like=x)
+    if not (want_dx or want_dW or dW_gu is not None or dW_d is not None):
+        raise ValueError("at least one gradient has to be wanted")
+    given = [t for t in (dW_gu, dW_d) if t is not None]
+    if given:
+        dW_dtype = given[0].dtype
+        _expect("dW_gu", dW_gu, (2 * H, d), dW_dtype, like=x)
+        _expect("dW_d", dW_d, (d, H), dW_dtype, like=x)
+    if dW_dtype != bf and dW_dtype != torch.float32:
+        raise TypeError(f"dW: bfloat16 or float32 expected, got {dW_dtype}")
+    dev = _device_index(on)
+    dx = torch.empty_like(x) if want_dx else None
+    if want_dW:
+        dW_gu = x.new_empty((2 * H, d), dtype=dW_dtype) if dW_gu is None else dW_gu
+        dW_d = x.new_empty((d, H), dtype=dW_dtype) if dW_d is None else dW_d
+    ws = x.new_empty(_bytes(lib.grouter_gated_ffn_bwd_workspace_bytes, dev, T, d, H), dtype=torch.uint8)
+    _call(lib.grouter_gated_ffn_bwd, "grouter_gated_ffn_bwd", dev, dy.data_ptr(), x.data_ptr(), W_gu.data_ptr(), W_d.data_ptr(), pre.data_ptr(), T, d, H,
+          act, _ptr(dx), _ptr(dW_gu), _ptr(dW_d), F32 if dW_dtype == torch.float32 else BF16, ws.data_ptr(), _status_ptr(status, dev))
+    return dx, dW_gu, dW_d
+
+
+def gated_ffn_fp8(x, W_g: Fp8Blocks, W_u: Fp8Blocks, W_d: Fp8Blocks, act: int = ACT_SILU, residual: Optional[torch.Tensor] = None,
+                  status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """grouter_gated_ffn_fp8_fwd: the block's forward pass in 8 bits.  x [T,d] as Fp8Blocks or bf16 (rows may be strided; put into 8 bits by
+    this call), W_g, W_u [H,d] and W_d [d,H] as Fp8Blocks (quantize_fp8 with square), residual bf16 -> y bf16 [T,d].  The hidden state
+    goes from product to product as codes."""
+    lib = load_library()
+    if not isinstance(W_d, Fp8Blocks):
+        raise TypeError(f"W_d: Fp8Blocks expected, got {type(W_d).__name__}")
+    on = W_d.device
+    d, H = W_d.shape
+    for name, W, shape in (("W_g", W_g, (H, d)), ("W_u", W_u, (H, d)), ("W_d", W_d, (d, H))):
+        if W is None:
+            raise TypeError(f"{name}: Fp8Blocks expected")
+        _expect_fp8(name, W, shape, on)
+    T = _rows_of("x", x, d, on)
+    bf = torch.bfloat16
+    if not (_fits(residual, (T, d), bf, on) and _fits(status, (1,), torch.int32, on)):
+        _expect("residual", residual, (T, d), bf, like=W_d.codes)
+        _expect("status", status, (1,), torch.int32, like=W_d.codes)
+    dev = _device_index(on)
+    if not isinstance(x, Fp8Blocks):
+        x = quantize_fp8(x)[0]
+    h = Fp8Blocks.empty(T, H, on)
+    y = torch.empty((T, d), dtype=bf, device=on)
+    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, x.codes.data_ptr(), x.scales.data_ptr(), W_g.codes.data_ptr(),
+          W_g.scales.data_ptr(), W_u.codes.data_ptr(), W_u.scales.data_ptr(), W_d.codes.data_ptr(), W_d.scales.data_ptr(), _ptr(residual), T, d, H, act,
+          h.codes.data_ptr(), h.scales.data_ptr(), y.data_ptr(), _status_ptr(status, dev))
+    return y
 
 
 def dense_gemm(A: torch.Tensor, a_mn_major: bool, B: torch.Tensor, b_mn_major: bool, M: int, N: int, K: int) -> torch.Tensor:

@@ -50,4 +50,39 @@ __device__ __forceinline__ float2 act_back2(float2 g, float2 z) {
   return g;
 }
 
+// v = act(v) for an activation that is known at run time only.
+template <int N>
+__device__ __forceinline__ void act_values(float (&v)[N], int act) {
+  if (act == GROUTER_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_value<GROUTER_ACT_RELU>(v[i]);
+  } else if (act == GROUTER_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_value<GROUTER_ACT_SILU>(v[i]);
+  } else if (act == GROUTER_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_value<GROUTER_ACT_GELU>(v[i]);
+  }
+}
+
+// Backward of act(g) u from its gradient dg: a = act(g), and dg becomes the gate's, dg u act'(g).
+template <int ACT, int N>
+__device__ __forceinline__ void act_gate_back(float (&dg)[N], const float (&g)[N], const float (&u)[N], float (&a)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const float2 d = act_back2<ACT>(mul2(make_float2(dg[i], dg[i + 1]), make_float2(u[i], u[i + 1])), make_float2(g[i], g[i + 1]));
+    dg[i] = d.x;
+    dg[i + 1] = d.y;
+    a[i] = act_value<ACT>(g[i]);
+    a[i + 1] = act_value<ACT>(g[i + 1]);
+  }
+}
+template <int N>
+__device__ __forceinline__ void act_gate_backward(float (&dg)[N], const float (&g)[N], const float (&u)[N], float (&a)[N], int act) {
+  if (act == GROUTER_ACT_RELU) act_gate_back<GROUTER_ACT_RELU, N>(dg, g, u, a);
+  else if (act == GROUTER_ACT_SILU) act_gate_back<GROUTER_ACT_SILU, N>(dg, g, u, a);
+  else if (act == GROUTER_ACT_GELU) act_gate_back<GROUTER_ACT_GELU, N>(dg, g, u, a);
+  else act_gate_back<GROUTER_ACT_NONE, N>(dg, g, u, a);
+}
+
 }  // namespace grouter

@@ -176,7 +176,8 @@ cudaError_t launch_reduce_rows(grouter_ctx* ctx, const __nv_bfloat16* src, __nv_
                                int n_part, float* dgates, cudaStream_t st);
 
 // MODE_DOWN_ADD: the down product with the combine folded into its epilogue (fp32 reductions into a [T, d] accumulator).
-enum GemmMode { MODE_UP = 0, MODE_DOWN = 1, MODE_DH = 2, MODE_DX = 3, MODE_WGRAD_D = 4, MODE_WGRAD_GU = 5, MODE_DENSE = 6, MODE_DOWN_ADD = 7, MODE_LINEAR = 8 };
+enum GemmMode { MODE_UP = 0, MODE_DOWN = 1, MODE_DH = 2, MODE_DX = 3, MODE_WGRAD_D = 4, MODE_WGRAD_GU = 5, MODE_DENSE = 6, MODE_DOWN_ADD = 7, MODE_LINEAR = 8,
+                MODE_GLU = 9, MODE_GLU_BACK = 10 };
 
 cudaError_t launch_grouped_gemm(grouter_ctx* ctx, GemmMode mode, const Workspace& ws, const void* gates, const void* W_gu,
                                 const void* W_d, float* dW_gu, float* dW_d, cudaStream_t st);
@@ -186,6 +187,9 @@ cudaError_t launch_zero_split_dw(grouter_ctx* ctx, float* dW_gu, float* dW_d, cu
 cudaError_t launch_idle(int microseconds, cudaStream_t st);
 // Tensor map of a row-major bf16 matrix [rows, cols] for 128-byte-swizzled tiles of 64 columns x box_rows rows.
 bool make_bf16_tile_map(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+// ... of any matrix: elements of `type`, rows `pitch` elements apart, tiles of box_cols x box_rows.
+bool make_tile_map(CUtensorMap* tm, CUtensorMapDataType type, int element_bytes, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch,
+                   uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle);
 // Measures one bounded wait that cannot succeed (see grouter_wait_selftest).
 cudaError_t launch_wait_selftest(grouter_ctx* ctx, unsigned long long limit_ns, unsigned long long* d_waited_ns, cudaStream_t st);
 // C = A * B (fp32).  A contraction longer than k_chunk (a multiple of 64) is cut into ceil(K / k_chunk) partial products, stored
@@ -201,6 +205,22 @@ struct LinearGemm {
   int32_t* status;
 };
 cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st);
+// Forward (A = x [T,K], W = W_gu [2H,K]): H = act(G) U and, with pre, [G|U] -> pre [T,2H].  Backward (A = dy [T,K], W = W_d [K,H]): with
+// dH = A W and the saved pre, [dG|dU] -> dpre [T,2H], and H once more.
+struct GatedGemm {
+  const void *A, *W;
+  void *pre, *dpre, *h;
+  int T, K, H, act;
+  bool backward;
+  int32_t* status;
+};
+cudaError_t launch_gated_gemm(const GatedGemm& g, cudaStream_t st);
+// act(A W^T + bias) + residual by whichever of the two kernels is ahead at these sizes (linear.cu).
+cudaError_t launch_product(const LinearGemm& g, cudaStream_t st);
+// dW [N,K] of GROUTER_BF16 / GROUTER_F32 = dz^T x for dz [T,N], x [T,K] (linear.cu); pieces: weight_gradient_bytes.
+size_t weight_gradient_bytes(int T, int K, int N);
+cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
+                                   cudaStream_t st);
 // The same product for few rows of A (tokens; K-major): the contraction cut over a cluster of `splits` CTAs (linear_small_splits).
 int linear_small_splits(int T, int N, int K);
 cudaError_t launch_linear_small(const LinearGemm& g, int splits, cudaStream_t st);

@@ -1,0 +1,501 @@
+// Products of matrices in 8 bits (fp8.cuh) on the sm_100a tensor cores, scales applied on the way.
+//
+//   LINEAR  C = A B^T + bias + residual        C_mn = sum_b 2^(ea(m,b) + eb(n,b)) sum_{k in block b} ca_mk cb_nk, bf16 or f32 out
+//   GLU     [G|U] = A [Wg;Wu]^T,  H = act(G) U, out as codes with a scale for 128 columns: the next product's operand
+//
+// The CTA-pair pipeline of the bf16 products (gemm.cu): tiles of 256 x 256, five 32 KB stages in each CTA, here 128 deep; warp 0
+// loads, warp 1 of the leader issues, warps 2-9 empty the accumulator.  A block of 128 is exactly one step, so its scale is one byte a
+// row, and four steps' bytes are the 512-byte atom that lies in memory: every fourth step brings one atom of A's rows and the two of
+// all 256 of B's rows (both CTAs multiply with all of B) into shared memory and from there into TMEM.
+// TMEM: two accumulators of 256 columns would be all of it.  They overlap by the 32 columns that two sets of scales need: accumulator
+// 1 starts at column 224.  Whoever reads the shared columns of a tile reads them first and says so (`over`), and the next tile's
+// products wait for that, while its operands arrive.
+// Every wait is bounded, as in gemm.cu.
+#include "act.cuh"
+#include "fp8.cuh"
+#include "fp8_gemm.cuh"
+#include "ptx.cuh"
+
+namespace grouter {
+
+namespace {
+
+constexpr int F8_BM = 128, F8_PM = 256, F8_BN = 256, F8_BNH = 128, F8_BK = 128;
+constexpr int F8_STAGES = 5;
+constexpr int F8_A_BYTES = F8_BM * F8_BK, F8_B_BYTES = F8_BNH * F8_BK;       // 16 KB each
+constexpr int F8_STAGE_BYTES = F8_A_BYTES + F8_B_BYTES;
+constexpr int F8_SCALE_BYTES = 3 * FP8_ATOM;          // A's rows of this CTA, B's first and second 128 rows
+constexpr int F8_EPI_WARPS = 8;
+constexpr int F8_THREADS = 64 + 32 * F8_EPI_WARPS;
+constexpr int F8_BLOCK_BYTES = 32 * 64;               // one staging block: 32 rows x 64 bytes
+constexpr int F8_EPI_BLOCKS = 3;
+constexpr int F8_STAGING = F8_EPI_WARPS * F8_EPI_BLOCKS * F8_BLOCK_BYTES;
+constexpr int F8_SMEM = F8_STAGES * (F8_STAGE_BYTES + F8_SCALE_BYTES) + F8_STAGING + 1024 /*align*/ + 256 /*barriers*/;
+constexpr uint32_t F8_ACC1 = 224, F8_SCALES = 480, F8_SCALE_SET = 16;       // TMEM columns: accumulator 1, the two sets of scales (A +0, B +8)
+constexpr int F8_RASTER = 8;
+
+enum F8Mode { F8_LINEAR = 0, F8_GLU = 1 };
+
+struct F8Params {
+  int M, N, K;                   // GLU: N = hidden columns
+  int tiles_m, tiles_n, across;  // across: scale atoms of a row of 128s
+  const __nv_bfloat16 *bias, *residual;
+  int out_f32, act;
+  uint8_t* out_scales;           // GLU
+  int32_t* status;
+  unsigned long long wait_limit_ns;
+};
+
+struct F8Tile {
+  int row0, col0, m_valid, n_valid;
+};
+
+template <int MODE>
+__device__ __forceinline__ F8Tile f8_tile(const F8Params& p, int t, int rank) {
+  // bands of tile rows, down the band first, as for the bf16 products: the pairs in flight share rows of A and columns of B
+  const int band = t / (F8_RASTER * p.tiles_n), in_band = t - band * F8_RASTER * p.tiles_n;
+  const int rows = min(F8_RASTER, p.tiles_m - band * F8_RASTER);
+  const int nt = in_band / rows, mt = band * F8_RASTER + (in_band - nt * rows);
+  constexpr int cols = MODE == F8_GLU ? F8_BNH : F8_BN;
+  F8Tile ti;
+  ti.row0 = mt * F8_PM + rank * F8_BM;
+  ti.col0 = nt * cols;
+  ti.m_valid = min(F8_BM, p.M - ti.row0);
+  ti.n_valid = min(cols, p.N - ti.col0);
+  return ti;
+}
+
+// tmB, tmSB: B and its scales; GLU: the gate's weights, and tmB1, tmSB1 those of the other projection.
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8_THREADS, 1)
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmB,
+                const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmSB1,
+                const __grid_constant__ CUtensorMap tmC, const F8Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  // the same offsets in both CTAs of the pair: descriptors and multicast commits name both
+  const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t staging = smem_base + F8_STAGES * F8_STAGE_BYTES;
+  const uint32_t scale_base = staging + F8_STAGING;
+  const uint32_t bar_base = scale_base + F8_STAGES * F8_SCALE_BYTES;
+  //   full[s] leader only, one arrival with the bytes of both CTAs      empty[s] each CTA, by the leader's commit
+  //   tmem_full[a] each CTA, by the leader's commit                      tmem_empty[a] leader only, one arrival an epilogue warp
+  //   over: leader only, one arrival of the eight warps that read the columns which both accumulators have
+  //   scales[b]: leader only, the products that read set b are done      top[quad]: GLU, the two warps that share rows have their maxima in place
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (F8_STAGES + s); };
+  auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * F8_STAGES + a); };
+  auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * F8_STAGES + 2 + a); };
+  const uint32_t over_bar = bar_base + 8u * (2 * F8_STAGES + 4);
+  auto scales_bar = [&](int b) { return bar_base + 8u * (2 * F8_STAGES + 5 + b); };
+  auto top_bar = [&](int q) { return bar_base + 8u * (2 * F8_STAGES + 7 + q); };
+  __shared__ uint32_t s_tmem_base;
+  __shared__ int s_abort;
+  __shared__ uint32_t s_top[MODE == F8_GLU ? 2 : 1][2][F8_BM];      // [tile parity][half of the columns][row]
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)ptx::cluster_ctarank();
+  const int pair_id = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < F8_STAGES; ++s) {
+      ptx::mbar_init(full_bar(s), 1);
+      ptx::mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(tfull_bar(a), 1);
+      ptx::mbar_init(tempty_bar(a), 2 * F8_EPI_WARPS);
+      ptx::mbar_init(scales_bar(a), 1);
+    }
+    ptx::mbar_init(over_bar, F8_EPI_WARPS);
+    for (int q = 0; q < 4; ++q) ptx::mbar_init(top_bar(q), 2);
+    ptx::fence_mbar_init();
+    ptx::prefetch_tensormap(&tmA);
+    ptx::prefetch_tensormap(&tmSA);
+    ptx::prefetch_tensormap(&tmB);
+    ptx::prefetch_tensormap(&tmSB);
+    ptx::prefetch_tensormap(&tmC);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(ptx::smem_u32(&s_tmem_base), 512);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync_all();      // the peer's barriers are initialised and its TMEM is allocated
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = s_tmem_base;
+  volatile int* abort_flag = &s_abort;
+  after_previous_kernel();      // set up while the kernel before was still ending; from here on its results are read
+  let_next_kernel_start();
+
+  const int n_tiles = p.tiles_m * p.tiles_n, steps = (p.K + F8_BK - 1) / F8_BK;
+
+  if (warp == 0) {
+    // ===================== TMA producer (both CTAs) =====================
+    if (lane == 0) {
+      const uint64_t keep_a = ptx::l2_policy_evict_normal(), keep_b = ptx::l2_policy_evict_last();
+      int s = 0;
+      uint32_t ph = 0;
+      for (int t = pair_id; t < n_tiles && !*abort_flag; t += n_pairs) {
+        const F8Tile ti = f8_tile<MODE>(p, t, rank);
+        const CUtensorMap* b_map = MODE == F8_GLU && rank == 1 ? &tmB1 : &tmB;
+        const int b_row = MODE == F8_GLU ? ti.col0 : ti.col0 + rank * F8_BNH;
+        const int sa_atom = (ti.row0 >> 7) * p.across, sb_atom = (ti.col0 >> 7) * p.across;
+        bool ok = true;
+        for (int ks = 0; ks < steps; ++ks) {
+          if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          const bool scales = (ks & 3) == 0;
+          const uint32_t sa = smem_base + s * F8_STAGE_BYTES, sb = sa + F8_A_BYTES, sc = scale_base + s * F8_SCALE_BYTES;
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), 2 * (F8_STAGE_BYTES + (scales ? F8_SCALE_BYTES : 0)));
+          const uint32_t fb = ptx::map_to_cta(full_bar(s), 0);      // both CTAs' bytes complete on the leader's barrier
+          if (scales) {
+            const int g = ks >> 2;
+            ptx::tma_load_2d_pair(sc, &tmSA, fb, 0, sa_atom + g, keep_a);
+            ptx::tma_load_2d_pair(sc + FP8_ATOM, &tmSB, fb, 0, sb_atom + g, keep_b);
+            if (MODE == F8_GLU) ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &tmSB1, fb, 0, sb_atom + g, keep_b);
+            else ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &tmSB, fb, 0, sb_atom + p.across + g, keep_b);      // beyond the last row: zeros
+          }
+          ptx::tma_load_2d_pair(sa, &tmA, fb, ks * F8_BK, ti.row0, keep_a);      // box {128 k, 128 rows}
+          ptx::tma_load_2d_pair(sb, b_map, fb, ks * F8_BK, b_row, keep_b);
+          if (++s == F8_STAGES) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        if (!ok) break;
+      }
+      // every stage release the leader has multicast to this CTA must have landed before the CTA may exit
+      for (int i = 0; i < F8_STAGES && !*abort_flag; ++i) {
+        if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
+        if (++s == F8_STAGES) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ===================== MMA issuer (leader CTA only) =====================
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = ptx::make_idesc_fp8_scaled(F8_PM, F8_BN);
+      constexpr uint16_t both = 3, leader = 1;
+      const uint64_t da0 = ptx::make_smem_desc_sw128(smem_base, 16, 1024), db0 = ptx::make_smem_desc_sw128(smem_base + F8_A_BYTES, 16, 1024);
+      const uint32_t a_hi = (uint32_t)(da0 >> 32), b_hi = (uint32_t)(db0 >> 32);
+      int s = 0, acc = 0, set = 0;
+      uint32_t ph = 0, acc_ph = 0, over_ph = 0, set_ph = 0;
+      bool first = true;
+      for (int t = pair_id; t < n_tiles && !*abort_flag; t += n_pairs) {
+        if (!ptx::mbar_wait_bounded(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
+        if (!first) {
+          if (!ptx::mbar_wait_bounded(over_bar, over_ph, abort_flag, p.wait_limit_ns)) break;
+          over_ph ^= 1u;
+        }
+        first = false;
+        ptx::tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (acc ? F8_ACC1 : 0u);
+        bool ok = true;
+        for (int ks = 0; ks < steps; ++ks) {
+          if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          const uint32_t t_sa = tmem_base + F8_SCALES + set * F8_SCALE_SET, t_sb = t_sa + 8;
+          ptx::tc_fence_after();
+          if ((ks & 3) == 0) {
+            if (!ptx::mbar_wait_bounded(scales_bar(set), set_ph ^ 1u, abort_flag, p.wait_limit_ns)) {
+              ok = false;
+              break;
+            }
+            ptx::tc_fence_after();
+            const uint64_t ds = ptx::make_smem_desc_scales(scale_base + s * F8_SCALE_BYTES);
+            ptx::tmem_copy_scales_pair(t_sa, ds);
+            ptx::tmem_copy_scales_pair(t_sb, ds + (FP8_ATOM >> 4));
+            ptx::tmem_copy_scales_pair(t_sb + 4, ds + (2 * FP8_ATOM >> 4));
+          }
+          const uint32_t a_lo = (uint32_t)da0 + s * (F8_STAGE_BYTES >> 4), b_lo = (uint32_t)db0 + s * (F8_STAGE_BYTES >> 4);
+          const uint32_t id = ptx::scale_byte(idesc, ks & 3);
+#pragma unroll
+          for (int kk = 0; kk < F8_BK / 32; ++kk)
+            ptx::umma_fp8_pair(d_tmem, a_lo + kk * 2, a_hi, b_lo + kk * 2, b_hi, id, t_sa, t_sb, (ks | kk) != 0 ? 1u : 0u);
+          ptx::umma_commit_pair(empty_bar(s), both);      // stage (and its scales) reusable in both CTAs once these have read it
+          if ((ks & 3) == 3 || ks == steps - 1) {
+            ptx::umma_commit_pair(scales_bar(set), leader);
+            set ^= 1;
+            if (set == 0) set_ph ^= 1u;
+          }
+          if (++s == F8_STAGES) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        if (!ok) break;
+        ptx::umma_commit_pair(tfull_bar(acc), both);
+        if (++acc == 2) {
+          acc = 0;
+          acc_ph ^= 1u;
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ===================== epilogue (warps 2..9 of both CTAs) =====================
+    // Thread (quad, lane) owns row quad * 32 + lane; results leave through three staging blocks of 32 rows x 64 bytes (64-byte swizzle)
+    // in turn, as TMA tile stores that clip at the tensor's bounds.
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const int r = quad * 32 + lane;
+    const uint32_t block0 = staging + (uint32_t)(warp - 2) * (F8_EPI_BLOCKS * F8_BLOCK_BYTES);
+    const uint32_t row_off = (uint32_t)lane * 64u, sw = (uint32_t)((lane >> 1) & 3);
+    const uint64_t stream_out = ptx::l2_policy_evict_first();
+    int block = 0;
+    auto stage_begin = [&]() {            // the next block is free once all but the two newest stores have been read
+      if (lane == 0) ptx::bulk_wait_read2();
+      __syncwarp();
+    };
+    auto stage_put = [&](int q, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {      // 16-byte unit q of this row
+      ptx::st_shared_v4(block0 + block * F8_BLOCK_BYTES + row_off + (((uint32_t)q ^ sw) << 4), a, b, c, d);
+    };
+    auto stage_send = [&](int x, int y) {
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        ptx::tma_store_2d(&tmC, block0 + block * F8_BLOCK_BYTES, x, y, stream_out);
+        ptx::bulk_commit();
+      }
+      block = block == F8_EPI_BLOCKS - 1 ? 0 : block + 1;
+    };
+    const uint32_t leader_over = ptx::map_to_cta(over_bar, 0);
+    const uint32_t leader_tempty[2] = {ptx::map_to_cta(tempty_bar(0), 0), ptx::map_to_cta(tempty_bar(1), 0)};
+    int acc = 0, parity = 0;
+    uint32_t acc_ph = 0, top_ph = 0;
+    for (int t = pair_id; t < n_tiles && !*abort_flag; t += n_pairs) {
+      const F8Tile ti = f8_tile<MODE>(p, t, rank);
+      const int y0 = ti.row0 + quad * 32;
+      const bool rows_here = ti.m_valid > quad * 32;       // warp-uniform
+      if (!ptx::mbar_wait_bounded(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
+      ptx::tc_fence_after();
+      const uint32_t t_row = tmem_base + (acc ? F8_ACC1 : 0u) + ((uint32_t)(quad * 32) << 16);
+      // the shared columns are the last 32 of accumulator 0 and the first 32 of accumulator 1
+      const bool has_over = acc == 0 ? half == 1 : half == 0;
+      auto say_over = [&]() {
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster(leader_over);
+      };
+      if constexpr (MODE == F8_LINEAR) {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+          const int c0 = half * 128 + (half ? 3 - i : i) * 32;      // the shared columns first
+          const int n_left = ti.n_valid - c0;
+          const bool any = rows_here && n_left > 0;                 // warp-uniform
+          uint4 res[4];
+          if (any && p.residual != nullptr) {
+            const __nv_bfloat16* at = p.residual + ((size_t)ti.row0 + r) * p.N + ti.col0 + c0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              res[q] = r < ti.m_valid && q * 8 < n_left ? *reinterpret_cast<const uint4*>(at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
+          }
+          float v[32];
+          if (any) {
+            uint32_t ra[32];
+            ptx::tmem_ld32(t_row + c0, ra);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(ra[k]);
+          }
+          if (i == 0 && has_over) say_over();
+          if (!any) continue;
+          if (p.bias != nullptr) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (q * 8 < n_left) {
+                Pack<__nv_bfloat16, 8> b[1];
+                *reinterpret_cast<uint4*>(&b[0]) = __ldg(reinterpret_cast<const uint4*>(p.bias + ti.col0 + c0 + q * 8));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const float2 f = pair_at(b, k);
+                  v[q * 8 + 2 * k] += f.x;
+                  v[q * 8 + 2 * k + 1] += f.y;
+                }
+              }
+            }
+          }
+          if (p.residual != nullptr) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              Pack<__nv_bfloat16, 8> b[1];
+              *reinterpret_cast<uint4*>(&b[0]) = res[q];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 f = pair_at(b, k);
+                v[q * 8 + 2 * k] += f.x;
+                v[q * 8 + 2 * k + 1] += f.y;
+              }
+            }
+          }
+          if (p.out_f32) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (n_left > 16 * h) {
+                stage_begin();
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                  stage_put(q, __float_as_uint(v[h * 16 + q * 4]), __float_as_uint(v[h * 16 + q * 4 + 1]), __float_as_uint(v[h * 16 + q * 4 + 2]),
+                            __float_as_uint(v[h * 16 + q * 4 + 3]));
+                stage_send(ti.col0 + c0 + 16 * h, y0);
+              }
+            }
+          } else {
+            stage_begin();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const Pack<__nv_bfloat16, 8> o = make_pack<__nv_bfloat16, 8>(v + q * 8);
+              const uint4 w = *reinterpret_cast<const uint4*>(&o);
+              stage_put(q, w.x, w.y, w.z, w.w);
+            }
+            stage_send(ti.col0 + c0, y0);
+          }
+        }
+      } else {
+        // accumulator columns 0..127 = gate, 128..255 = up; this warp: 64 of each, which with the other half's 64 share a scale
+        const bool any = rows_here && ti.n_valid > 0;
+        float h[64];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int cc = half ? 1 - i : i;                 // the shared columns first
+          if (any) {
+            uint32_t rg[32], ru[32];
+            ptx::tmem_ld32(t_row + half * 64 + cc * 32, rg);
+            ptx::tmem_ld32(t_row + 128 + half * 64 + cc * 32, ru);
+            ptx::tmem_ld_wait();
+            float v[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(rg[k]);
+            act_values(v, p.act);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              v[k] *= __uint_as_float(ru[k]);
+              top = max(top, finite_magnitude(v[k]));
+              h[i * 32 + k] = v[k];
+            }
+          }
+          if (i == 0 && has_over) say_over();
+        }
+        s_top[parity][half][r] = top;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(top_bar(quad));
+        if (!ptx::mbar_wait_bounded(top_bar(quad), top_ph, abort_flag, p.wait_limit_ns)) break;
+        top = max(top, s_top[parity][half ^ 1][r]);
+        parity ^= 1;
+        top_ph ^= 1u;
+        if (any) {
+          const uint32_t e = fp8_exponent(top);
+          const float inv = fp8_inverse(e);
+          stage_begin();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            // unit q holds columns 16q .. 16q + 15; the second half keeps its two chunks the other way round
+            const int at = (q & 1) * 16, first = (q >> 1) * 32, second = 32 - first;
+            float w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = half ? h[second + at + k] : h[first + at + k];
+            stage_put(q, fp8_quad(w, inv), fp8_quad(w + 4, inv), fp8_quad(w + 8, inv), fp8_quad(w + 12, inv));
+          }
+          stage_send(ti.col0 + half * 64, y0);
+          if (half == 0 && r < ti.m_valid) p.out_scales[fp8_scale_at(ti.row0 + r, ti.col0 >> 7, fp8_atoms_across(p.N))] = (uint8_t)e;
+        }
+      }
+      // all TMEM reads of this warp are complete (wait::ld above): hand the accumulator back
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(leader_tempty[acc]);
+      if (++acc == 2) {
+        acc = 0;
+        acc_ph ^= 1u;
+      }
+    }
+    if (lane == 0) ptx::bulk_wait0();   // every tile store of this warp has landed
+    __syncwarp();
+  }
+
+  // ---- teardown ----
+  if (*abort_flag) {
+    if (threadIdx.x == 0) atomicOr(p.status, STATUS_TIMEOUT);
+    // give copies and barrier arrivals still in flight towards either CTA's shared memory time to land
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (ptx::globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync_all();      // neither CTA leaves while the other may still touch its shared memory or TMEM
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+struct F8Maps {
+  CUtensorMap A, SA, B, SB, B1, SB1, C;
+};
+
+template <int MODE>
+cudaError_t f8_launch(const F8Maps& m, const F8Params& p, cudaStream_t st) {
+  static bool configured[64] = {};        // the opt-in to more than 48 KB of dynamic shared memory, once per device
+  auto kern = fp8_gemm_kernel<MODE>;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev < 0 || dev >= 64 || !configured[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F8_SMEM);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) configured[dev] = true;
+  }
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  const int cap = current_sms() & ~1;
+  return launch_dependent(kern, dim3((unsigned)(2 * tiles < cap ? 2 * tiles : cap)), dim3(F8_THREADS), F8_SMEM, st, m.A, m.SA, m.B, m.SB, m.B1, m.SB1,
+                          m.C, p);
+}
+
+}  // namespace
+
+bool make_fp8_maps(CUtensorMap* codes, CUtensorMap* scales, const Fp8Operand& x, int rows, int cols, uint32_t box_rows) {
+  const uint64_t atoms = (uint64_t)cdiv(rows, 128) * fp8_atoms_across(cols);
+  return make_tile_map(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.codes, rows, cols, fp8_pitch(cols), 128, box_rows, CU_TENSOR_MAP_SWIZZLE_128B) &&
+         make_tile_map(scales, CU_TENSOR_MAP_DATA_TYPE_INT32, 4, x.scales, atoms, 128, 128, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st) {
+  F8Params p{};
+  p.M = g.M; p.N = g.N; p.K = g.K;
+  p.tiles_m = cdiv(g.M, F8_PM);
+  p.across = (int)fp8_atoms_across(g.K);
+  p.act = g.act;
+  p.status = g.status;
+  p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
+  F8Maps m;
+  bool ok = make_fp8_maps(&m.A, &m.SA, g.A, g.M, g.K, F8_BM) && make_fp8_maps(&m.B, &m.SB, g.B, g.N, g.K, F8_BNH);
+  if (g.B1.codes) {
+    p.tiles_n = cdiv(g.N, F8_BNH);
+    p.out_scales = static_cast<uint8_t*>(g.out_scales);
+    // the columns up to the pitch are written too: zeros
+    ok = ok && make_fp8_maps(&m.B1, &m.SB1, g.B1, g.N, g.K, F8_BNH) &&
+         make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, g.C, g.M, fp8_pitch(g.N), fp8_pitch(g.N), 64, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+    return ok ? f8_launch<F8_GLU>(m, p, st) : cudaErrorInvalidValue;
+  }
+  p.tiles_n = cdiv(g.N, F8_BN);
+  p.bias = static_cast<const __nv_bfloat16*>(g.bias);
+  p.residual = static_cast<const __nv_bfloat16*>(g.residual);
+  p.out_f32 = g.out_f32;
+  m.B1 = m.B;
+  m.SB1 = m.SB;
+  ok = ok && (g.out_f32 ? make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, g.C, g.M, g.N, g.N, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
+                        : make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, g.C, g.M, g.N, g.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+  return ok ? f8_launch<F8_LINEAR>(m, p, st) : cudaErrorInvalidValue;
+}
+
+}  // namespace grouter

@@ -1,0 +1,25 @@
+// Products of matrices in 8 bits, as the operators launch them.
+#pragma once
+#include "common.cuh"
+
+namespace grouter {
+
+struct Fp8Operand {
+  const void *codes, *scales;             // [rows, fp8_pitch(cols)], packed scales (fp8.cuh)
+};
+// C [M,N] = A B^T + bias + residual, bf16 or f32; with B1: act(A B^T) (A B1^T) as codes C and out_scales.
+struct Fp8Gemm {
+  Fp8Operand A, B, B1;
+  const void *bias, *residual;            // bf16 or null
+  void *C, *out_scales;
+  int M, N, K, act, out_f32;
+  int32_t* status;
+};
+cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
+// Tensor maps of a matrix's codes (tiles of 128 columns x box_rows) and of its scales (one 512-byte atom).
+bool make_fp8_maps(CUtensorMap* codes, CUtensorMap* scales, const Fp8Operand& x, int rows, int cols, uint32_t box_rows);
+// Codes of the rows of x and, with codes_t, of its columns; column_sums: with codes_t, f32 [ceil(rows / 128), cols] of the tiles' sums.
+cudaError_t launch_quantize(const void* x, int64_t ldx, int dtype, int rows, int cols, bool square, void* codes, void* scales, void* codes_t,
+                            void* scales_t, float* column_sums, cudaStream_t st);
+
+}  // namespace grouter

@@ -1,0 +1,199 @@
+// Gated feed-forward block, and the linear layer in 8 bits: the calls around their products.
+//
+//   forward    p = x W_gu^T = [g | u]     h = act(g) u     y = h W_d^T + r          x [T,d], W_gu [2H,d], W_d [d,H]
+//   backward   dh = dy W_d     du = dh act(g)     dg = dh u act'(g)     dp = [dg | du]
+//              dx = dp W_gu     dW_gu = dp^T x     dW_d = dy^T h
+//   8 bits     the same forward pass on codes and scales (fp8.cuh), h leaving as codes: y = q(act(q(x) Wg^T) (q(x) Wu^T)) Wd^T + r
+//   linear     y = q(x) q(W)^T + b + r     dx = q(dy) q(W)     dW = q(dy^T) q(x^T)^T     db = sum_t dy_t
+//
+// Both projections, the activation and the product are one kernel (gemm.cu, MODE_GLU; fp8_gemm.cu, F8_GLU): a tile holds 128 gate and the
+// 128 up columns that belong to them, so h is formed on the accumulators.  dh never leaves the chip either: its product's epilogue
+// (MODE_GLU_BACK) writes dp and h, which is cheaper to form again from p than to keep.
+#include "fp8.cuh"
+#include "fp8_gemm.cuh"
+
+namespace grouter {
+namespace {
+
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+inline bool fits_int(int64_t v) { return v <= INT32_MAX - 256; }
+
+struct GatedWorkspace {
+  size_t dp, h, pieces, bytes;
+};
+GatedWorkspace gated_workspace(int T, int d, int H) {
+  GatedWorkspace w{};
+  w.h = up256((size_t)T * 2 * H * 2);
+  w.pieces = w.h + up256((size_t)T * H * 2);
+  const size_t gu = weight_gradient_bytes(T, d, 2 * H), down = weight_gradient_bytes(T, H, d);
+  w.bytes = w.pieces + (gu > down ? gu : down) + 256;
+  return w;
+}
+
+int gated_check(int32_t T, int32_t d, int32_t H, int32_t act) {
+  if (T < 0 || d < 1 || H < 1 || act < GROUTER_ACT_NONE || act > GROUTER_ACT_GELU) return GROUTER_ERR_INVALID_ARG;
+  if (d % 8 || H % 8 || !fits_int(T) || !fits_int(d) || !fits_int(2 * (int64_t)H)) return GROUTER_ERR_UNSUPPORTED;
+  return GROUTER_OK;
+}
+
+struct Fp8Workspace {
+  size_t rows, row_scales, cols, col_scales, sums, bytes;
+};
+// Codes of dy and of its transpose, and the partial sums of its columns.
+Fp8Workspace fp8_workspace(int T, int N) {
+  Fp8Workspace w{};
+  w.row_scales = up256((size_t)T * fp8_pitch(N));
+  w.cols = w.row_scales + up256(grouter_fp8_scale_bytes(T, N));
+  w.col_scales = w.cols + up256((size_t)N * fp8_pitch(T));
+  w.sums = w.col_scales + up256(grouter_fp8_scale_bytes(N, T));
+  w.bytes = w.sums + up256(((size_t)T + 127) / 128 * N * 4) + 256;
+  return w;
+}
+
+int fp8_check(int32_t T, int32_t K, int32_t N) {
+  if (T < 0 || K < 1 || N < 1) return GROUTER_ERR_INVALID_ARG;
+  if (N % 8 || !fits_int(T) || !fits_int(K) || !fits_int(N)) return GROUTER_ERR_UNSUPPORTED;
+  // the scales' atoms are counted in 32 bits
+  const int64_t most = 1 << 30;
+  if (((int64_t)T / 128 + 2) * fp8_atoms_across(K) > most || ((int64_t)N / 128 + 2) * fp8_atoms_across(K) > most) return GROUTER_ERR_UNSUPPORTED;
+  return GROUTER_OK;
+}
+
+}  // namespace
+}  // namespace grouter
+
+using namespace grouter;
+
+extern "C" {
+
+int grouter_gated_ffn_fwd(const void* x, const void* W_gu, const void* W_d, const void* residual, int32_t T, int32_t d, int32_t H, int32_t act,
+                          void* h, void* y, void* pre, int32_t* status, void* stream) {
+  if (const int e = gated_check(T, d, H, act)) return e;
+  if (!W_gu || !W_d || !status || (T > 0 && (!x || !h || !y))) return GROUTER_ERR_INVALID_ARG;
+  if (!aligned_to(x, 16) || !aligned_to(W_gu, 16) || !aligned_to(W_d, 16) || !aligned_to(residual, 16) || !aligned_to(h, 16) || !aligned_to(y, 16) ||
+      !aligned_to(pre, 16) || !aligned_to(status, 4))
+    return GROUTER_ERR_MISALIGNED;
+  if (T == 0) return GROUTER_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  GatedGemm g{};
+  g.A = x; g.W = W_gu; g.pre = pre; g.h = h; g.T = T; g.K = d; g.H = H; g.act = act; g.status = status;
+  if (launch_gated_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  LinearGemm l{};
+  l.A = h; l.B = W_d; l.residual = residual; l.C = y; l.M = T; l.N = d; l.K = H; l.act = GROUTER_ACT_NONE; l.status = status;
+  return launch_product(l, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+}
+
+size_t grouter_gated_ffn_bwd_workspace_bytes(int32_t T, int32_t d, int32_t H) {
+  if (gated_check(T, d, H, GROUTER_ACT_NONE) != GROUTER_OK) return 0;
+  return gated_workspace(T, d, H).bytes;
+}
+
+int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const void* W_d, const void* pre, int32_t T, int32_t d, int32_t H,
+                          int32_t act, void* dx, void* dW_gu, void* dW_d, int32_t dW_dtype, void* workspace, int32_t* status, void* stream) {
+  if (const int e = gated_check(T, d, H, act)) return e;
+  if (!status || (!dx && !dW_gu && !dW_d) || (dW_dtype != GROUTER_BF16 && dW_dtype != GROUTER_F32)) return GROUTER_ERR_INVALID_ARG;
+  if (T > 0 && (!dy || !W_d || !pre || !workspace || (dx && !W_gu) || (dW_gu && !x))) return GROUTER_ERR_INVALID_ARG;
+  if (!aligned_to(dy, 16) || !aligned_to(x, 16) || !aligned_to(W_gu, 16) || !aligned_to(W_d, 16) || !aligned_to(pre, 16) || !aligned_to(dx, 16) ||
+      !aligned_to(dW_gu, 16) || !aligned_to(dW_d, 16) || !aligned_to(workspace, 256) || !aligned_to(status, 4))
+    return GROUTER_ERR_MISALIGNED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (T == 0) {           // sums over no tokens
+    const size_t el = dW_dtype == GROUTER_F32 ? 4 : 2;
+    if (dW_gu && cudaMemsetAsync(dW_gu, 0, (size_t)2 * H * d * el, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (dW_d && cudaMemsetAsync(dW_d, 0, (size_t)d * H * el, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    return GROUTER_OK;
+  }
+  const GatedWorkspace w = gated_workspace(T, d, H);
+  char* ws = static_cast<char*>(workspace);
+  GatedGemm g{};
+  g.A = dy; g.W = W_d; g.pre = const_cast<void*>(pre); g.dpre = ws + w.dp; g.h = ws + w.h; g.T = T; g.K = d; g.H = H; g.act = act;
+  g.backward = true; g.status = status;
+  if (launch_gated_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (dx) {
+    LinearGemm l{};
+    l.A = ws + w.dp; l.B = W_gu; l.b_mn = 1; l.C = dx; l.M = T; l.N = d; l.K = 2 * H; l.act = GROUTER_ACT_NONE; l.status = status;
+    if (launch_product(l, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  }
+  if (dW_gu && launch_weight_gradient(ws + w.dp, x, T, d, 2 * H, dW_gu, dW_dtype, ws + w.pieces, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (dW_d && launch_weight_gradient(dy, ws + w.h, T, H, d, dW_d, dW_dtype, ws + w.pieces, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  return GROUTER_OK;
+}
+
+int grouter_linear_fp8_fwd(const void* x, const void* x_scales, const void* W, const void* W_scales, const void* bias, const void* residual, int32_t T,
+                           int32_t K, int32_t N, void* y, int32_t* status, void* stream) {
+  if (const int e = fp8_check(T, K, N)) return e;
+  if (!W || !W_scales || !status || (T > 0 && (!x || !x_scales || !y))) return GROUTER_ERR_INVALID_ARG;
+  if (!aligned_to(x, 16) || !aligned_to(x_scales, 16) || !aligned_to(W, 16) || !aligned_to(W_scales, 16) || !aligned_to(bias, 16) ||
+      !aligned_to(residual, 16) || !aligned_to(y, 16) || !aligned_to(status, 4))
+    return GROUTER_ERR_MISALIGNED;
+  if (T == 0) return GROUTER_OK;
+  Fp8Gemm g{};
+  g.A = {x, x_scales}; g.B = {W, W_scales}; g.bias = bias; g.residual = residual; g.C = y; g.M = T; g.N = N; g.K = K; g.status = status;
+  return launch_fp8_gemm(g, static_cast<cudaStream_t>(stream)) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+}
+
+size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N) {
+  if (fp8_check(T, K, N) != GROUTER_OK) return 0;
+  return fp8_workspace(T, N).bytes;
+}
+
+int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales, const void* Wt, const void* Wt_scales, int32_t T, int32_t K, int32_t N,
+                           void* dx, void* dW, int32_t dW_dtype, float* db, void* workspace, int32_t* status, void* stream) {
+  if (const int e = fp8_check(T, K, N)) return e;
+  if (K % 8) return GROUTER_ERR_UNSUPPORTED;
+  if (!status || (!dx && !dW && !db) || (dW_dtype != GROUTER_BF16 && dW_dtype != GROUTER_F32)) return GROUTER_ERR_INVALID_ARG;
+  if (T > 0 && (!dy || !workspace || (dx && (!Wt || !Wt_scales)) || (dW && (!xt || !xt_scales)))) return GROUTER_ERR_INVALID_ARG;
+  if (!aligned_to(dy, 16) || !aligned_to(xt, 16) || !aligned_to(xt_scales, 16) || !aligned_to(Wt, 16) || !aligned_to(Wt_scales, 16) || !aligned_to(dx, 16) ||
+      !aligned_to(dW, 16) || !aligned_to(db, 4) || !aligned_to(workspace, 256) || !aligned_to(status, 4))
+    return GROUTER_ERR_MISALIGNED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (T == 0) {           // sums over no tokens
+    if (dW && cudaMemsetAsync(dW, 0, (size_t)N * K * (dW_dtype == GROUTER_F32 ? 4 : 2), st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (db && cudaMemsetAsync(db, 0, (size_t)N * 4, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    return GROUTER_OK;
+  }
+  const Fp8Workspace w = fp8_workspace(T, N);
+  char* ws = static_cast<char*>(workspace);
+  // the sums are taken on the way to the transposed codes, which a bias alone does not need
+  const int tiles = (T + 127) / 128;
+  float* sums = db ? (tiles == 1 ? db : reinterpret_cast<float*>(ws + w.sums)) : nullptr;
+  const bool columns = dW || db;
+  if (launch_quantize(dy, N, GROUTER_BF16, T, N, false, dx ? ws : nullptr, ws + w.row_scales, columns ? ws + w.cols : nullptr, ws + w.col_scales, sums,
+                      st) != cudaSuccess)
+    return GROUTER_ERR_CUDA;
+  if (db && tiles > 1 && launch_sum_rows(sums, tiles, N, db, N, nullptr, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  Fp8Gemm g{};
+  g.status = status;
+  if (dx) {
+    g.A = {ws, ws + w.row_scales}; g.B = {Wt, Wt_scales}; g.C = dx; g.M = T; g.N = K; g.K = N;
+    if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  }
+  if (dW) {
+    g.A = {ws + w.cols, ws + w.col_scales}; g.B = {xt, xt_scales}; g.C = dW; g.M = N; g.N = K; g.K = T; g.out_f32 = dW_dtype == GROUTER_F32;
+    if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  }
+  return GROUTER_OK;
+}
+
+int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, const void* W_g, const void* W_g_scales, const void* W_u, const void* W_u_scales,
+                              const void* W_d, const void* W_d_scales, const void* residual, int32_t T, int32_t d, int32_t H, int32_t act, void* h,
+                              void* h_scales, void* y, int32_t* status, void* stream) {
+  if (const int e = gated_check(T, d, H, act)) return e;
+  if (fp8_check(T, d, H) || fp8_check(T, H, d)) return GROUTER_ERR_UNSUPPORTED;
+  if (!W_g || !W_g_scales || !W_u || !W_u_scales || !W_d || !W_d_scales || !status || (T > 0 && (!x || !x_scales || !h || !h_scales || !y)))
+    return GROUTER_ERR_INVALID_ARG;
+  for (const void* q : {x, x_scales, W_g, W_g_scales, W_u, W_u_scales, W_d, W_d_scales, residual, (const void*)h, (const void*)h_scales, (const void*)y})
+    if (!aligned_to(q, 16)) return GROUTER_ERR_MISALIGNED;
+  if (!aligned_to(status, 4)) return GROUTER_ERR_MISALIGNED;
+  if (T == 0) return GROUTER_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Fp8Gemm g{};
+  g.A = {x, x_scales}; g.B = {W_g, W_g_scales}; g.B1 = {W_u, W_u_scales}; g.C = h; g.out_scales = h_scales; g.M = T; g.N = H; g.K = d; g.act = act;
+  g.status = status;
+  if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  Fp8Gemm l{};
+  l.A = {h, h_scales}; l.B = {W_d, W_d_scales}; l.residual = residual; l.C = y; l.M = T; l.N = d; l.K = H; l.status = status;
+  return launch_fp8_gemm(l, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -9,6 +9,8 @@
 //   WGRAD_GU  dW_gu[e] = [dG|dU]_e^T * Xp_e
 //   DENSE     C = A * B on plain matrices, fp32 out (component check; partial products of a linear layer's weight gradient)
 //   LINEAR    C = act(A * B + bias) + residual on plain matrices, bf16 out (the linear layer's forward pass and gradients)
+//   GLU       [G|U] = x * W_gu^T     epilogue: H = act(G) * U                   (gated feed-forward block, forward)
+//   GLU_BACK  dH    = dy * W_d       epilogue: dG, dU and, from the saved G and U, H again
 //
 // Tile: 256 x 256 x 64 per CTA pair (a cluster of two CTAs on neighbouring SMs, one pair-wide tcgen05.mma with
 // M = 256).  Each CTA owns 128 rows of the tile and half of B's 256 columns, so per 64-deep k-step it stages
@@ -75,12 +77,12 @@ struct GemmParams {
   const int32_t* pad_begin;    // [E] first pad row of each expert's padded segment
   const void* gates;
   int32_t gate_is_f32;
-  const __nv_bfloat16* in_G;   // DH
-  const __nv_bfloat16* in_U;   // DH
+  const __nv_bfloat16* in_G;   // DH, GLU_BACK (where rows of G and U are 2F elements apart)
+  const __nv_bfloat16* in_U;   // DH, GLU_BACK
   const __nv_bfloat16* bias;   // LINEAR: [N] or null
   const __nv_bfloat16* residual;   // LINEAR: [M, N] or null
-  int32_t act;                 // LINEAR: GROUTER_ACT_*
-  int32_t save_pre;            // LINEAR: also store A * B + bias (tensor map C1)
+  int32_t act;                 // LINEAR, GLU, GLU_BACK: GROUTER_ACT_*
+  int32_t save_pre;            // LINEAR: also store A * B + bias (tensor map C1); GLU: also store G and U (C0, C1)
   float* out_f;                // DH: dgate_part; weight gradients / DENSE: the fp32 output [E, M, N]; DOWN_ADD: Y accumulator [T, d]
   int32_t* status;
   unsigned int* tile_counter;  // device scalar, zero at launch (unused by DENSE, which has no context to keep one)
@@ -89,6 +91,9 @@ struct GemmParams {
 };
 
 constexpr int RASTER_ROWS = 8;
+
+// Products of plain matrices: no plan, and no context to keep a tile counter in.
+__host__ __device__ constexpr bool is_plain(int mode) { return mode == MODE_DENSE || mode == MODE_LINEAR || mode == MODE_GLU || mode == MODE_GLU_BACK; }
 
 struct Tile {     // one CTA's share of a pair tile
   int a_x, a_y;   // TMA coordinates of this CTA's A rows at k-step 0
@@ -106,7 +111,7 @@ template <int MODE>
 __device__ __forceinline__ int total_tiles(const GemmParams& p) {
   if (MODE == MODE_WGRAD_D || MODE == MODE_WGRAD_GU) return __ldg(p.n_wchunks) * p.tiles_m * p.tiles_n;
   if (MODE == MODE_DENSE) return p.tiles_m * p.tiles_n * ((p.K + p.k_chunk - 1) / p.k_chunk);
-  if (MODE == MODE_LINEAR) return p.tiles_m * p.tiles_n;
+  if (MODE == MODE_LINEAR || MODE == MODE_GLU || MODE == MODE_GLU_BACK) return p.tiles_m * p.tiles_n;
   return __ldg(p.n_pair_tiles) * p.tiles_n;
 }
 
@@ -182,7 +187,7 @@ __device__ __forceinline__ Tile decode_tile(const GemmParams& p, int t, int rank
     // barriers: its boxes lie beyond the last row, where TMA fills zeros without touching memory, and the epilogue
     // ignores the accumulator.
     ti.a_y = ti.b_y = ti.num_k > 0 ? k0 : (int)p.R_pad_max;
-  } else {  // DENSE, LINEAR
+  } else {  // DENSE, LINEAR, GLU, GLU_BACK
     // Tiles in bands of RASTER_ROWS tile rows, down the band first: the pairs in flight then share a few tile rows of A and
     // a few tile columns of B, whichever of the two matrices is the larger one.
     const int per = p.tiles_m * p.tiles_n;
@@ -192,13 +197,13 @@ __device__ __forceinline__ Tile decode_tile(const GemmParams& p, int t, int rank
     const int nt = in_band / rows, mt = band * RASTER_ROWS + (in_band - nt * rows);
     ti.e = piece;                     // DENSE: which of the partial products (their matrices follow one another)
     ti.row0 = mt * PM + rank * BM;
-    ti.col0 = nt * BN;
+    ti.col0 = nt * (MODE == MODE_GLU ? BNH : BN);
     ti.m_valid = min(BM, p.M - ti.row0);
-    ti.n_valid = min(BN, p.N - ti.col0);
+    ti.n_valid = min(MODE == MODE_GLU ? BNH : BN, p.N - ti.col0);
     ti.a_x = ti.row0;                 // MN-major A: x; K-major A: y (set below)
     ti.a_y = ti.row0;
     ti.b_x = ti.col0 + rank * BNH;    // MN-major B: x; K-major B: y
-    ti.b_y = ti.col0 + rank * BNH;
+    ti.b_y = ti.col0 + rank * (MODE == MODE_GLU ? p.F : BNH);    // GLU: W_gu as [2F, K]; leader stages 128 gate rows, peer the 128 up rows
     ti.k_base = MODE == MODE_DENSE ? piece * p.k_chunk : 0;
     ti.num_k = ((MODE == MODE_DENSE ? min(p.k_chunk, p.K - ti.k_base) : p.K) + BK - 1) / BK;
   }
@@ -249,7 +254,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
   auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + a); };
   auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + 2 + a); };
-  // Tile queue (all modes but DENSE and LINEAR).  The pair takes its tiles from a grid-wide counter instead of a fixed stride: the
+  // Tile queue (all modes but those on plain matrices).  The pair takes its tiles from a grid-wide counter instead of a fixed stride: the
   // pairs then always work on neighbouring tiles of the list, whatever their individual pace, so the operand rows the
   // neighbours share are fetched from DRAM once.  The leader's producer draws the numbers (two tiles ahead, so the
   // round trip of the atomic is never waited for) and writes them into a ring of TQ 8-byte slots {sequence, tile} in
@@ -258,7 +263,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   // stage through the operand ring (the producer is at most STAGES tiles ahead of the issuer), and the issuer starts a
   // tile only after every epilogue warp has finished the tile two before it, so the oldest number still unread is at
   // most STAGES + 3 tiles older than the newest one written (STAGES + 4 <= TQ slots in use).
-  constexpr bool PLAIN = MODE == MODE_DENSE || MODE == MODE_LINEAR;   // plain matrices, no context to keep a tile counter in
+  constexpr bool PLAIN = is_plain(MODE);
   constexpr bool DYN = !PLAIN;
   constexpr int TQ = 16;
   static_assert(STAGES + 4 <= TQ && (TQ & (TQ - 1)) == 0, "tile queue too short for the operand ring");
@@ -287,8 +292,8 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     ptx::prefetch_tensormap(&tmA);
     ptx::prefetch_tensormap(&tmB);
     ptx::prefetch_tensormap(&tmC0);
-    if (MODE == MODE_UP || MODE == MODE_DH || MODE == MODE_LINEAR) ptx::prefetch_tensormap(&tmC1);
-    if (MODE == MODE_UP) ptx::prefetch_tensormap(&tmC2);
+    if (MODE == MODE_UP || MODE == MODE_DH || MODE == MODE_LINEAR || MODE == MODE_GLU || MODE == MODE_GLU_BACK) ptx::prefetch_tensormap(&tmC1);
+    if (MODE == MODE_UP || MODE == MODE_GLU || MODE == MODE_GLU_BACK) ptx::prefetch_tensormap(&tmC2);
   }
   if (warp == 1) {
     ptx::tmem_alloc_pair(ptx::smem_u32(&s_tmem_base), TMEM_COLS);
@@ -527,11 +532,11 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         ptx::bulk_commit();
       }
     };
-    // DH: saved pre-activations G and U of one 32-column chunk of this thread's row (zeros beyond F)
+    // DH, GLU_BACK: saved pre-activations G and U of one 32-column chunk of this thread's row (zeros beyond F)
     auto load_gu = [&](const Tile& ti, int c, uint4 (&g4)[4], uint4 (&u4)[4]) {
       const int c0 = half * 128 + c * 32;
-      const int n_left = ti.m_valid > 0 ? ti.n_valid - c0 : 0;
-      const size_t gi = ((size_t)ti.row0 + r) * p.F + ti.col0 + c0;
+      const int n_left = (PLAIN ? r < ti.m_valid : ti.m_valid > 0) ? ti.n_valid - c0 : 0;
+      const size_t gi = ((size_t)ti.row0 + r) * (PLAIN ? 2 * p.F : p.F) + ti.col0 + c0;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if (q * 8 < n_left) {
@@ -560,7 +565,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const Tile ti = decode_tile<MODE>(p, t, rank);
       const bool live = ti.m_valid > 0;    // false: this CTA only lent its half of B to the pair
       uint4 g4[4], u4[4];
-      if (MODE == MODE_DH) load_gu(ti, 0, g4, u4);   // in flight while the main loop of this tile finishes
+      if (MODE == MODE_DH || MODE == MODE_GLU_BACK) load_gu(ti, 0, g4, u4);   // in flight while the main loop of this tile finishes
       if (MODE == MODE_LINEAR && p.residual != nullptr) {
         load_residual(ti, 0, g4);
         load_residual(ti, 1, u4);
@@ -770,6 +775,90 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             }
           }
         }
+      } else if (MODE == MODE_GLU) {
+        // accumulator columns as in UP: 0..127 = gate, 128..255 = up; this warp: 64 of each
+        if (ti.m_valid > quad * 32 && ti.n_valid - half * 64 > 0) {
+          const int x = ti.col0 + half * 64;
+          uint32_t ph[32];                 // H of the 64 columns, packed bf16 pairs
+#pragma unroll
+          for (int cc = 0; cc < 2; ++cc) {
+            uint32_t rg[32], ru[32];
+            ptx::tmem_ld32(t_row + half * 64 + cc * 32, rg);
+            ptx::tmem_ld32(t_row + 128 + half * 64 + cc * 32, ru);
+            ptx::tmem_ld_wait();
+            float g[32], u[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              g[i] = __uint_as_float(rg[i]);
+              u[i] = __uint_as_float(ru[i]);
+            }
+            if (p.save_pre) {
+              if (cc == 0) stage_wait_all();
+              stage_put_bf16(blk_a, cc * 4, g);
+              stage_put_bf16(blk_b, cc * 4, u);
+            }
+            act_values(g, p.act);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ph[cc * 16 + i] = pack_bf16(g[2 * i] * u[2 * i], g[2 * i + 1] * u[2 * i + 1]);
+          }
+          uint32_t sb = blk_a;
+          if (p.save_pre) {
+            stage_send_2d(blk_a, &tmC0, x, y0);
+            stage_send_2d(blk_b, &tmC1, x, y0);
+            stage_wait_older();            // block a has been read (the store of block b may still be reading)
+          } else {
+            flip ^= 1u;
+            sb = flip ? blk_a : blk_b;     // not the block of the previous store
+            stage_wait_older();
+          }
+#pragma unroll
+          for (int q = 0; q < 8; ++q) stage_put(sb, q, ph[q * 4], ph[q * 4 + 1], ph[q * 4 + 2], ph[q * 4 + 3]);
+          stage_send_2d(sb, &tmC2, x, y0);
+        }
+      } else if (MODE == MODE_GLU_BACK) {
+        uint32_t ph[32];                   // H of a 64-column block, packed bf16 pairs
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {                // four 32-column chunks; chunks 2c, 2c+1 fill one pair of blocks
+          const int cb = half * 128 + (c >> 1) * 64;
+          const int c0 = half * 128 + c * 32;
+          const bool any = ti.m_valid > quad * 32 && ti.n_valid - cb > 0;      // warp-uniform: the block holds results
+          uint4 cg[4], cu[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            cg[q] = g4[q];
+            cu[q] = u4[q];
+          }
+          if (c < 3) load_gu(ti, c + 1, g4, u4);     // next chunk's loads fly during this chunk's arithmetic
+          if (any) {
+            uint32_t ra[32];
+            ptx::tmem_ld32(t_row + c0, ra);
+            ptx::tmem_ld_wait();
+            if ((c & 1) == 0) stage_wait_all();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float g[8], u[8], a[8], dg[8], du[8];
+              unpack8(cg[q], g);
+              unpack8(cu[q], u);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) dg[i] = __uint_as_float(ra[q * 8 + i]);
+              act_gate_backward(dg, g, u, a, p.act);           // a = act(g), du = dH a, dg = dH u act'(g)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) du[i] = __uint_as_float(ra[q * 8 + i]) * a[i];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) ph[(c & 1) * 16 + q * 4 + i] = pack_bf16(a[2 * i] * u[2 * i], a[2 * i + 1] * u[2 * i + 1]);
+              stage_put(blk_a, (c & 1) * 4 + q, pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]), pack_bf16(dg[4], dg[5]), pack_bf16(dg[6], dg[7]));
+              stage_put(blk_b, (c & 1) * 4 + q, pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]), pack_bf16(du[4], du[5]), pack_bf16(du[6], du[7]));
+            }
+            if ((c & 1) == 1) {
+              stage_send_2d(blk_a, &tmC0, ti.col0 + cb, y0);   // dG: columns [0,F) of [dG|dU]
+              stage_send_2d(blk_b, &tmC1, ti.col0 + cb, y0);   // dU: columns [F,2F)
+              stage_wait_older();
+#pragma unroll
+              for (int q = 0; q < 8; ++q) stage_put(blk_a, q, ph[q * 4], ph[q * 4 + 1], ph[q * 4 + 2], ph[q * 4 + 3]);
+              stage_send_2d(blk_a, &tmC2, ti.col0 + cb, y0);
+            }
+          }
+        }
       } else {  // WGRAD_D, WGRAD_GU, DENSE: fp32 tile straight from TMEM to global memory (stored, or added for a partial sum)
         if (ti.m_valid > quad * 32 && (have_acc || !ti.add)) {
 #pragma unroll
@@ -876,6 +965,19 @@ bool make_bf16_tile_map(CUtensorMap* tm, const void* base, uint64_t rows, uint64
   return make_map(tm, base, rows, cols, box_rows);
 }
 
+bool make_tile_map(CUtensorMap* tm, CUtensorMapDataType type, int element_bytes, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch,
+                   uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  cuuint64_t gdim[2] = {cols, rows};
+  cuuint64_t gstr[1] = {pitch * element_bytes};
+  cuuint32_t box[2] = {box_cols, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = fn(tm, type, 2, const_cast<void*>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 struct Maps {
   CUtensorMap A, B, C0, C1, C2;
 };
@@ -892,7 +994,7 @@ static cudaError_t launch_tc(const Maps& m, const GemmParams& p, int grid, cudaS
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  if constexpr (MODE == MODE_DENSE || MODE == MODE_LINEAR)
+  if constexpr (is_plain(MODE))
     return launch_dependent(kern, dim3(grid), dim3(GEMM_THREADS), GEMM_SMEM, st, m.A, m.B, m.C0, m.C1, m.C2, p);
   kern<<<grid, GEMM_THREADS, GEMM_SMEM, st>>>(m.A, m.B, m.C0, m.C1, m.C2, p);
   return cudaGetLastError();
@@ -900,7 +1002,7 @@ static cudaError_t launch_tc(const Maps& m, const GemmParams& p, int grid, cudaS
 
 template <int MODE, bool A_MN, bool B_MN>
 static cudaError_t launch_t(const Maps& m, const GemmParams& p, int grid, cudaStream_t st) {
-  if constexpr (MODE != MODE_DENSE && MODE != MODE_LINEAR) {
+  if constexpr (!is_plain(MODE)) {
     if (p.cycles != nullptr) return launch_tc<MODE, A_MN, B_MN, true>(m, p, grid, st);
   }
   return launch_tc<MODE, A_MN, B_MN, false>(m, p, grid, st);
@@ -1121,6 +1223,36 @@ cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st) {
   if (g.a_mn) return g.b_mn ? launch_t<MODE_LINEAR, true, true>(m, p, grid, st) : cudaErrorInvalidValue;
   if (g.b_mn) return launch_t<MODE_LINEAR, false, true>(m, p, grid, st);
   return launch_t<MODE_LINEAR, false, false>(m, p, grid, st);
+}
+
+cudaError_t launch_gated_gemm(const GatedGemm& g, cudaStream_t st) {
+  GemmParams p{};
+  p.M = g.T; p.N = g.H; p.K = g.K; p.F = g.H;
+  p.tiles_m = cdiv(g.T, PM);
+  p.status = g.status;
+  p.act = g.act;
+  p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
+  const __nv_bfloat16* pre = static_cast<const __nv_bfloat16*>(g.pre);
+  const uint64_t H = (uint64_t)g.H;
+  Maps m;
+  bool ok = make_map(&m.A, g.A, g.T, g.K, 128);
+  if (!g.backward) {
+    p.tiles_n = cdiv(g.H, BNH);
+    p.save_pre = pre != nullptr;
+    ok = ok && make_map(&m.B, g.W, 2 * H, g.K, 128) && make_map(&m.C2, g.h, g.T, H, 32);
+    m.C0 = m.C1 = m.C2;
+    if (pre) ok = ok && make_map(&m.C0, pre, g.T, H, 32, 2 * H) && make_map(&m.C1, pre + H, g.T, H, 32, 2 * H);
+    if (!ok) return cudaErrorInvalidValue;
+    return launch_t<MODE_GLU, false, false>(m, p, plain_grid((int64_t)p.tiles_m * p.tiles_n), st);
+  }
+  p.tiles_n = cdiv(g.H, BN);
+  p.in_G = pre;
+  p.in_U = pre + H;
+  __nv_bfloat16* dpre = static_cast<__nv_bfloat16*>(g.dpre);
+  ok = ok && make_map(&m.B, g.W, g.K, H, 64) && make_map(&m.C0, dpre, g.T, H, 32, 2 * H) && make_map(&m.C1, dpre + H, g.T, H, 32, 2 * H) &&
+       make_map(&m.C2, g.h, g.T, H, 32);
+  if (!ok) return cudaErrorInvalidValue;
+  return launch_t<MODE_GLU_BACK, false, true>(m, p, plain_grid((int64_t)p.tiles_m * p.tiles_n), st);
 }
 
 }  // namespace grouter

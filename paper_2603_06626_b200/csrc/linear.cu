@@ -145,8 +145,7 @@ LinearWorkspace linear_workspace(int T, int K, int N, int act) {
   w.dz = 0;
   w.sums = w.dz + (act == GROUTER_ACT_NONE ? 0 : up256((size_t)T * N * 2));
   w.pieces = w.sums + up256((size_t)dz_row_blocks(T, N) * N * 4);
-  const int s = dw_pieces(T, K, N);
-  w.bytes = w.pieces + (s > 1 ? up256((size_t)s * N * K * 4) : 0) + 256;
+  w.bytes = w.pieces + weight_gradient_bytes(T, K, N) + 256;
   return w;
 }
 
@@ -169,6 +168,14 @@ cudaError_t launch_dz(int act, const void* dy, const void* z, int T, int N, void
   }
 }
 
+int linear_check(int32_t T, int32_t K, int32_t N, int32_t act) {
+  if (T < 0 || K < 1 || N < 1 || act < GROUTER_ACT_NONE || act > GROUTER_ACT_GELU) return GROUTER_ERR_INVALID_ARG;
+  if (K % 8 || N % 8 || T > INT32_MAX - 256 || K > INT32_MAX - 256 || N > INT32_MAX - 256) return GROUTER_ERR_UNSUPPORTED;
+  return GROUTER_OK;
+}
+
+}  // namespace
+
 // y or dx: the CTA-pair core, or the kernel for few tokens.  Both sides in rounds of the machine times 64-deep steps a round,
 // measured over T = 1 .. 4096 and weights of 128 x 128 to 4096 x 4096: a step takes 0.33 us on 256 x 256 tiles (5.7 us around them)
 // and 0.45 us on two 128 x 128 tiles an SM (7.5 us around them, and as much again for every further round); up to 64 tokens the
@@ -184,13 +191,30 @@ cudaError_t launch_product(const LinearGemm& g, cudaStream_t st) {
   return launch_linear_gemm(g, st);
 }
 
-int linear_check(int32_t T, int32_t K, int32_t N, int32_t act) {
-  if (T < 0 || K < 1 || N < 1 || act < GROUTER_ACT_NONE || act > GROUTER_ACT_GELU) return GROUTER_ERR_INVALID_ARG;
-  if (K % 8 || N % 8 || T > INT32_MAX - 256 || K > INT32_MAX - 256 || N > INT32_MAX - 256) return GROUTER_ERR_UNSUPPORTED;
-  return GROUTER_OK;
+size_t weight_gradient_bytes(int T, int K, int N) {
+  const int s = dw_pieces(T, K, N);
+  return s > 1 ? up256((size_t)s * N * K * 4) : 0;
 }
 
-}  // namespace
+cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
+                                   cudaStream_t st) {
+  const int count = dw_pieces(T, K, N);
+  if (count == 1 && dW_dtype == GROUTER_BF16) {
+    LinearGemm g{};
+    g.A = dz; g.a_mn = 1; g.B = x; g.b_mn = 1; g.C = dW; g.M = N; g.N = K; g.K = T; g.act = GROUTER_ACT_NONE; g.status = status;
+    return launch_linear_gemm(g, st);
+  }
+  float* out = static_cast<float*>(count == 1 ? dW : pieces);
+  const int chunk = dw_chunk(T, count);
+  if (const cudaError_t e = launch_dense_gemm(dz, 1, x, 1, out, N, K, T, chunk, status, st)) return e;
+  if (count == 1) return cudaSuccess;
+  const int64_t n4 = (int64_t)N * K / 4, want = (n4 + 255) / 256, cap = (int64_t)current_sms() * 8;
+  const int grid = (int)(want < cap ? want : cap), real = cdiv(T, chunk);      // whole 64-token steps may leave the last piece out
+  return dW_dtype == GROUTER_F32 ? launch_dependent(sum_pieces_kernel<float>, dim3(grid), dim3(256), 0, st, out, real, n4, static_cast<float*>(dW))
+                                 : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, out, real, n4,
+                                                    static_cast<__nv_bfloat16*>(dW));
+}
+
 }  // namespace grouter
 
 using namespace grouter;
@@ -246,25 +270,7 @@ int grouter_linear_bwd(const void* dy, const void* x, const void* W, const void*
     if (launch_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   if (dW) {
-    const int pieces = dw_pieces(T, K, N);
-    if (pieces == 1 && dW_dtype == GROUTER_BF16) {
-      LinearGemm g{};
-      g.A = dz; g.a_mn = 1; g.B = x; g.b_mn = 1; g.C = dW; g.M = N; g.N = K; g.K = T; g.act = GROUTER_ACT_NONE; g.status = status;
-      if (launch_linear_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-    } else {
-      float* out = pieces == 1 ? static_cast<float*>(dW) : reinterpret_cast<float*>(ws + w.pieces);
-      const int chunk = dw_chunk(T, pieces);
-      if (launch_dense_gemm(dz, 1, x, 1, out, N, K, T, chunk, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-      if (pieces > 1) {
-        const int64_t n4 = (int64_t)N * K / 4, want = (n4 + 255) / 256, cap = (int64_t)current_sms() * 8;
-        const int grid = (int)(want < cap ? want : cap), real = cdiv(T, chunk);      // whole 64-token steps may leave the last piece out
-        const cudaError_t e =
-            dW_dtype == GROUTER_F32
-                ? launch_dependent(sum_pieces_kernel<float>, dim3(grid), dim3(256), 0, st, out, real, n4, static_cast<float*>(dW))
-                : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, out, real, n4, static_cast<__nv_bfloat16*>(dW));
-        if (e != cudaSuccess) return GROUTER_ERR_CUDA;
-      }
-    }
+    if (launch_weight_gradient(dz, x, T, K, N, dW, dW_dtype, ws + w.pieces, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   return GROUTER_OK;
 }

@@ -293,5 +293,57 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N, bool a_mn, 
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// ---------------- block-scaled 8-bit form (kind::mxf8f6f4) ----------------
+// Operands e4m3, one 8-bit power-of-two scale for every row of A and of B and 32 elements of the contraction, applied to the products
+// before they are added up.  The scales of an instruction are bytes in TMEM: those of rows 32c .. 32c + 31 in column c (from the given
+// address on), lanes 0 .. 31 and again in the other three lane quadrants; which byte of the 32-bit cells is said by the instruction
+// descriptor.  So one cell serves four instructions, here four 128-deep steps.
+//   bits 4-5 byte of B's scales   bits 7-9, 10-12 A, B format (0 = e4m3)   bits 17-22 N>>3   bit 23 scale type (1 = power of two)
+//   bits 24-28 M>>4               bits 29-30 byte of A's scales
+__host__ __device__ constexpr uint32_t make_idesc_fp8_scaled(int M, int N) {
+  return ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t scale_byte(uint32_t idesc, int byte) { return idesc | ((uint32_t)byte << 4) | ((uint32_t)byte << 29); }
+
+__device__ __forceinline__ void umma_fp8_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                              uint32_t tmem_sa, uint32_t tmem_sb, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b64 da, db;\n"
+      "mov.b64 da, {%1, %2};\n"
+      "mov.b64 db, {%3, %4};\n"
+      "setp.ne.b32 p, %8, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n"
+      "}\n" ::"r"(tmem_d),
+      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_fp8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t tmem_sa, uint32_t tmem_sb,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %6, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
+      "}\n" ::"r"(tmem_d),
+      "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate)
+      : "memory");
+}
+// 32 rows of 16 bytes from shared memory into four TMEM columns of every lane quadrant; ordered before the same thread's later MMAs.
+// Pair form: each CTA of the pair from its own shared memory into its own TMEM.
+__device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// Descriptor of 512 bytes without swizzle: rows of 16 bytes one after the other, groups of eight 128 bytes apart.
+__device__ __forceinline__ uint64_t make_smem_desc_scales(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+// the shared-memory sources of all committed groups but the two most recent ones have been read
+__device__ __forceinline__ void bulk_wait_read2() { asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory"); }
+
 }  // namespace ptx
 }  // namespace grouter

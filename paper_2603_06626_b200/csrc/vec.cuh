@@ -41,7 +41,7 @@ inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<u
 
 // Elements of T in one 16-byte access.
 template <typename T>
-constexpr int vec16() { return 16 / (int)sizeof(T); }
+__host__ __device__ constexpr int vec16() { return 16 / (int)sizeof(T); }
 
 // VE elements as they lie in memory, fetched in one access where that is a power-of-two size up to 16 bytes.
 template <typename T, int VE>
