@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libgrouter.so")
 LIB_DEBUG = os.path.join(PKG, "libgrouter_debug.so")
 SOURCES = ["api.cu", "plan.cu", "permute.cu", "gemm.cu", "route.cu", "stats.cu", "ep.cu", "norm.cu", "balance.cu", "linear.cu", "linear_small.cu", "adamw.cu",
-           "quant.cu", "rmsnorm.cu", "gated.cu", "fp8_gemm.cu"]
+           "quant.cu", "rmsnorm.cu", "gated.cu", "fp8_gemm.cu", "fp8_small.cu"]
 
 
 def _newest_source_mtime() -> float:

@@ -65,24 +65,52 @@ __device__ __forceinline__ void act_values(float (&v)[N], int act) {
   }
 }
 
-// Backward of act(g) u from its gradient dg: a = act(g), and dg becomes the gate's, dg u act'(g).
+// Value and slope of two elements: one exponential and one reciprocal each.
+template <int ACT>
+__device__ __forceinline__ void act_value_slope2(float2 z, float2& value, float2& slope) {
+  if (ACT == GROUTER_ACT_RELU) {
+    value = make_float2(act_value<ACT>(z.x), act_value<ACT>(z.y));
+    slope = make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
+  } else if (ACT == GROUTER_ACT_SILU) {        // s,  s + z s (1 - s)
+    const float2 s = make_float2(logistic(z.x), logistic(z.y));
+    value = mul2(z, s);
+    slope = fma2(value, fma2(s, both(-1.f), both(1.f)), s);
+  } else if (ACT == GROUTER_ACT_GELU) {        // s,  s + z s (1 - s) u',  as in act_back2
+    const float2 zc = make_float2(fminf(fmaxf(z.x, -12.f), 12.f), fminf(fmaxf(z.y, -12.f), 12.f));
+    const float2 q = mul2(zc, zc);
+    const float2 u = mul2(zc, fma2(q, both(1.5957691216057308f * 0.044715f), both(1.5957691216057308f)));
+    const float2 s = make_float2(logistic(u.x), logistic(u.y));
+    value = mul2(z, s);
+    slope = fma2(mul2(value, fma2(s, both(-1.f), both(1.f))), fma2(q, both(1.5957691216057308f * 0.134145f), both(1.5957691216057308f)), s);
+  } else {
+    value = z;
+    slope = both(1.f);
+  }
+}
+// h = act(g) u and, from h's gradient dh, dg = dh u act'(g) and du = dh act(g).
 template <int ACT, int N>
-__device__ __forceinline__ void act_gate_back(float (&dg)[N], const float (&g)[N], const float (&u)[N], float (&a)[N]) {
+__device__ __forceinline__ void gate_back(const float (&dh)[N], const float (&g)[N], const float (&u)[N], float (&h)[N], float (&dg)[N], float (&du)[N]) {
 #pragma unroll
   for (int i = 0; i < N; i += 2) {
-    const float2 d = act_back2<ACT>(mul2(make_float2(dg[i], dg[i + 1]), make_float2(u[i], u[i + 1])), make_float2(g[i], g[i + 1]));
-    dg[i] = d.x;
-    dg[i + 1] = d.y;
-    a[i] = act_value<ACT>(g[i]);
-    a[i + 1] = act_value<ACT>(g[i + 1]);
+    const float2 d = make_float2(dh[i], dh[i + 1]), up = make_float2(u[i], u[i + 1]);
+    float2 a, slope;
+    act_value_slope2<ACT>(make_float2(g[i], g[i + 1]), a, slope);
+    const float2 o0 = mul2(a, up), o1 = mul2(mul2(d, up), slope), o2 = mul2(d, a);
+    h[i] = o0.x;
+    h[i + 1] = o0.y;
+    dg[i] = o1.x;
+    dg[i + 1] = o1.y;
+    du[i] = o2.x;
+    du[i + 1] = o2.y;
   }
 }
 template <int N>
-__device__ __forceinline__ void act_gate_backward(float (&dg)[N], const float (&g)[N], const float (&u)[N], float (&a)[N], int act) {
-  if (act == GROUTER_ACT_RELU) act_gate_back<GROUTER_ACT_RELU, N>(dg, g, u, a);
-  else if (act == GROUTER_ACT_SILU) act_gate_back<GROUTER_ACT_SILU, N>(dg, g, u, a);
-  else if (act == GROUTER_ACT_GELU) act_gate_back<GROUTER_ACT_GELU, N>(dg, g, u, a);
-  else act_gate_back<GROUTER_ACT_NONE, N>(dg, g, u, a);
+__device__ __forceinline__ void gate_backward(const float (&dh)[N], const float (&g)[N], const float (&u)[N], float (&h)[N], float (&dg)[N], float (&du)[N],
+                                              int act) {
+  if (act == GROUTER_ACT_RELU) gate_back<GROUTER_ACT_RELU, N>(dh, g, u, h, dg, du);
+  else if (act == GROUTER_ACT_SILU) gate_back<GROUTER_ACT_SILU, N>(dh, g, u, h, dg, du);
+  else if (act == GROUTER_ACT_GELU) gate_back<GROUTER_ACT_GELU, N>(dh, g, u, h, dg, du);
+  else gate_back<GROUTER_ACT_NONE, N>(dh, g, u, h, dg, du);
 }
 
 }  // namespace grouter

@@ -27,39 +27,45 @@ __device__ __forceinline__ int64_t fp8_scale_at(int64_t row, int block, int64_t 
   return ((row >> 7) * atoms_across + (block >> 2)) * FP8_ATOM + (r & 31) * 16 + (r >> 5) * 4 + (block & 3);
 }
 
-// Magnitude as bits, in which finite numbers are ordered; 0 for what is not finite.
-__device__ __forceinline__ uint32_t finite_magnitude(float v) {
-  const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
-}
-// e + 127 from the bits of the largest magnitude: its exponent less 8, one more where its mantissa is above 1.75 (448 = 1.75 * 2^8).
-__device__ __forceinline__ uint32_t fp8_exponent(uint32_t top) {
-  const int e = (int)((top + 0x1fffffu) >> 23) - 8;
+// The largest magnitude is looked for among all numbers first (NaN falls out of a maximum by itself): only where it comes out infinite
+// are the finite ones picked, and infinities told from 448 when codes are made.
+__device__ __forceinline__ float larger(float top, float v) { return fmaxf(top, fabsf(v)); }
+__device__ __forceinline__ bool not_finite(float top) { return __float_as_uint(top) >= 0x7f800000u; }
+__device__ __forceinline__ float larger_finite(float top, float v) { return not_finite(fabsf(v)) ? top : larger(top, v); }
+
+// e + 127 of the largest magnitude: its exponent less 8, one more where its mantissa is above 1.75 (448 = 1.75 * 2^8).
+__device__ __forceinline__ uint32_t fp8_exponent(float top) {
+  const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8;
   return e < 1 ? 1u : (uint32_t)e;
 }
 __device__ __forceinline__ float fp8_inverse(uint32_t exponent) { return __uint_as_float((254u - exponent) << 23); }   // 2^-e
 __device__ __forceinline__ float fp8_scale(uint32_t exponent) { return __uint_as_float(exponent << 23); }              // 2^e
 
-// Two values, already divided by the scale, as codes; infinities (which the conversion would make 448) as NaN.
-__device__ __forceinline__ uint32_t fp8_pair(float a, float b) {
-  const float inf = __uint_as_float(0x7f800000u), nan = __uint_as_float(0x7fffffffu);
-  if (fabsf(a) == inf) a = nan;
-  if (fabsf(b) == inf) b = nan;
-  return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+// Two values as codes.  INF: some may be infinite, which the conversion by itself would make 448; they become NaN.
+template <bool INF>
+__device__ __forceinline__ uint32_t fp8_pair(float2 v, float2 inverse) {
+  v = mul2(v, inverse);
+  if (INF) {
+    const float nan = __uint_as_float(0x7fffffffu);
+    if (not_finite(fabsf(v.x))) v.x = nan;
+    if (not_finite(fabsf(v.y))) v.y = nan;
+  }
+  return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
 }
+template <bool INF>
 __device__ __forceinline__ uint32_t fp8_quad(const float* v, float inverse) {
-  return fp8_pair(v[0] * inverse, v[1] * inverse) | fp8_pair(v[2] * inverse, v[3] * inverse) << 16;
+  return fp8_pair<INF>(make_float2(v[0], v[1]), both(inverse)) | fp8_pair<INF>(make_float2(v[2], v[3]), both(inverse)) << 16;
 }
 __device__ __forceinline__ float2 fp8_values(uint32_t two) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3);
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+// Largest of the LANES neighbouring lanes' magnitudes, the same in each of them.  Bits of numbers that are not negative are in order.
 template <int LANES>
-__device__ __forceinline__ uint32_t lanes_max_bits(uint32_t v) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+__device__ __forceinline__ float lanes_top(float v) {
+  if constexpr (LANES == 32) return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
+  else return lanes_max<LANES>(v);
 }
 
 }  // namespace grouter

@@ -90,7 +90,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   auto top_bar = [&](int q) { return bar_base + 8u * (2 * F8_STAGES + 7 + q); };
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
-  __shared__ uint32_t s_top[MODE == F8_GLU ? 2 : 1][2][F8_BM];      // [tile parity][half of the columns][row]
+  __shared__ float s_top[MODE == F8_GLU ? 2 : 1][2][F8_BM];         // [tile parity][half of the columns][row]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)ptx::cluster_ctarank();
@@ -275,6 +275,18 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const F8Tile ti = f8_tile<MODE>(p, t, rank);
       const int y0 = ti.row0 + quad * 32;
       const bool rows_here = ti.m_valid > quad * 32;       // warp-uniform
+      // the residual of this thread's row and 128 columns, on its way while the tile is multiplied
+      uint4 res[4][4];
+      if (MODE == F8_LINEAR && p.residual != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c0 = half * 128 + (half ? 3 - i : i) * 32;
+          const __nv_bfloat16* at = p.residual + ((size_t)ti.row0 + r) * p.N + ti.col0 + c0;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            res[i][q] = r < ti.m_valid && c0 + q * 8 < ti.n_valid ? *reinterpret_cast<const uint4*>(at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
       if (!ptx::mbar_wait_bounded(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = tmem_base + (acc ? F8_ACC1 : 0u) + ((uint32_t)(quad * 32) << 16);
@@ -286,18 +298,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         if (lane == 0) ptx::mbar_arrive_cluster(leader_over);
       };
       if constexpr (MODE == F8_LINEAR) {
-#pragma unroll 1
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int c0 = half * 128 + (half ? 3 - i : i) * 32;      // the shared columns first
           const int n_left = ti.n_valid - c0;
           const bool any = rows_here && n_left > 0;                 // warp-uniform
-          uint4 res[4];
-          if (any && p.residual != nullptr) {
-            const __nv_bfloat16* at = p.residual + ((size_t)ti.row0 + r) * p.N + ti.col0 + c0;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              res[q] = r < ti.m_valid && q * 8 < n_left ? *reinterpret_cast<const uint4*>(at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
-          }
           float v[32];
           if (any) {
             uint32_t ra[32];
@@ -327,7 +332,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               Pack<__nv_bfloat16, 8> b[1];
-              *reinterpret_cast<uint4*>(&b[0]) = res[q];
+              *reinterpret_cast<uint4*>(&b[0]) = res[i][q];
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const float2 f = pair_at(b, k);
@@ -362,34 +367,40 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       } else {
         // accumulator columns 0..127 = gate, 128..255 = up; this warp: 64 of each, which with the other half's 64 share a scale
         const bool any = rows_here && ti.n_valid > 0;
-        float h[64];
-        uint32_t top = 0;
+        float h[64], top = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int cc = half ? 1 - i : i;                 // the shared columns first
+          uint32_t rg[32], ru[32];
           if (any) {
-            uint32_t rg[32], ru[32];
             ptx::tmem_ld32(t_row + half * 64 + cc * 32, rg);
             ptx::tmem_ld32(t_row + 128 + half * 64 + cc * 32, ru);
             ptx::tmem_ld_wait();
+          }
+          if (i == 0 && has_over) say_over();
+          if (any) {
             float v[32];
 #pragma unroll
             for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(rg[k]);
             act_values(v, p.act);
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
-              v[k] *= __uint_as_float(ru[k]);
-              top = max(top, finite_magnitude(v[k]));
-              h[i * 32 + k] = v[k];
+              h[i * 32 + k] = v[k] * __uint_as_float(ru[k]);
+              top = larger(top, h[i * 32 + k]);
             }
           }
-          if (i == 0 && has_over) say_over();
+        }
+        const bool inf = any && not_finite(top);           // rare: the maximum is taken again without
+        if (inf) {
+          top = 0.f;
+#pragma unroll
+          for (int k = 0; k < 64; ++k) top = larger_finite(top, h[k]);
         }
         s_top[parity][half][r] = top;
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(top_bar(quad));
         if (!ptx::mbar_wait_bounded(top_bar(quad), top_ph, abort_flag, p.wait_limit_ns)) break;
-        top = max(top, s_top[parity][half ^ 1][r]);
+        top = fmaxf(top, s_top[parity][half ^ 1][r]);
         parity ^= 1;
         top_ph ^= 1u;
         if (any) {
@@ -403,7 +414,15 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             float w[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k] = half ? h[second + at + k] : h[first + at + k];
-            stage_put(q, fp8_quad(w, inv), fp8_quad(w + 4, inv), fp8_quad(w + 8, inv), fp8_quad(w + 12, inv));
+            uint32_t c[4];
+            if (inf) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) c[k] = fp8_quad<true>(w + 4 * k, inv);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) c[k] = fp8_quad<false>(w + 4 * k, inv);
+            }
+            stage_put(q, c[0], c[1], c[2], c[3]);
           }
           stage_send(ti.col0 + half * 64, y0);
           if (half == 0 && r < ti.m_valid) p.out_scales[fp8_scale_at(ti.row0 + r, ti.col0 >> 7, fp8_atoms_across(p.N))] = (uint8_t)e;

@@ -16,6 +16,9 @@ struct Fp8Gemm {
   int32_t* status;
 };
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
+// The same for few rows of A (tokens), bf16 or codes out: the contraction cut over a cluster of `splits` CTAs (fp8_small_splits).
+int fp8_small_splits(int T, int N, int K, bool glu);
+cudaError_t launch_fp8_small(const Fp8Gemm& g, int splits, cudaStream_t st);
 // Tensor maps of a matrix's codes (tiles of 128 columns x box_rows) and of its scales (one 512-byte atom).
 bool make_fp8_maps(CUtensorMap* codes, CUtensorMap* scales, const Fp8Operand& x, int rows, int cols, uint32_t box_rows);
 // Codes of the rows of x and, with codes_t, of its columns; column_sums: with codes_t, f32 [ceil(rows / 128), cols] of the tiles' sums.

@@ -59,6 +59,16 @@ int fp8_check(int32_t T, int32_t K, int32_t N) {
   return GROUTER_OK;
 }
 
+// Whichever of the two kernels is ahead at these sizes.
+cudaError_t fp8_product(const Fp8Gemm& g, cudaStream_t st) {
+  if (!g.out_f32 && g.M <= 64) return launch_fp8_small(g, fp8_small_splits(g.M, g.N, g.K, g.B1.codes != nullptr), st);
+  return launch_fp8_gemm(g, st);
+}
+cudaError_t gated_product(const GatedGemm& g, cudaStream_t st) {
+  if (g.T <= 64) return launch_gated_small(g, linear_small_splits(g.T, 2 * g.H, g.K), st);
+  return launch_gated_gemm(g, st);
+}
+
 }  // namespace
 }  // namespace grouter
 
@@ -77,7 +87,7 @@ int grouter_gated_ffn_fwd(const void* x, const void* W_gu, const void* W_d, cons
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   GatedGemm g{};
   g.A = x; g.W = W_gu; g.pre = pre; g.h = h; g.T = T; g.K = d; g.H = H; g.act = act; g.status = status;
-  if (launch_gated_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (gated_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   LinearGemm l{};
   l.A = h; l.B = W_d; l.residual = residual; l.C = y; l.M = T; l.N = d; l.K = H; l.act = GROUTER_ACT_NONE; l.status = status;
   return launch_product(l, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
@@ -129,7 +139,7 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, const void* W, c
   if (T == 0) return GROUTER_OK;
   Fp8Gemm g{};
   g.A = {x, x_scales}; g.B = {W, W_scales}; g.bias = bias; g.residual = residual; g.C = y; g.M = T; g.N = N; g.K = K; g.status = status;
-  return launch_fp8_gemm(g, static_cast<cudaStream_t>(stream)) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+  return fp8_product(g, static_cast<cudaStream_t>(stream)) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N) {
@@ -166,11 +176,11 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
   g.status = status;
   if (dx) {
     g.A = {ws, ws + w.row_scales}; g.B = {Wt, Wt_scales}; g.C = dx; g.M = T; g.N = K; g.K = N;
-    if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   if (dW) {
     g.A = {ws + w.cols, ws + w.col_scales}; g.B = {xt, xt_scales}; g.C = dW; g.M = N; g.N = K; g.K = T; g.out_f32 = dW_dtype == GROUTER_F32;
-    if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   return GROUTER_OK;
 }
@@ -190,10 +200,10 @@ int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, const void* W
   Fp8Gemm g{};
   g.A = {x, x_scales}; g.B = {W_g, W_g_scales}; g.B1 = {W_u, W_u_scales}; g.C = h; g.out_scales = h_scales; g.M = T; g.N = H; g.K = d; g.act = act;
   g.status = status;
-  if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   Fp8Gemm l{};
   l.A = {h, h_scales}; l.B = {W_d, W_d_scales}; l.residual = residual; l.C = y; l.M = T; l.N = d; l.K = H; l.status = status;
-  return launch_fp8_gemm(l, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+  return fp8_product(l, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
 }  // extern "C"

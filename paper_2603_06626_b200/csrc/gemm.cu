@@ -836,16 +836,14 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             if ((c & 1) == 0) stage_wait_all();
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              float g[8], u[8], a[8], dg[8], du[8];
+              float dh[8], g[8], u[8], h[8], dg[8], du[8];
               unpack8(cg[q], g);
               unpack8(cu[q], u);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) dg[i] = __uint_as_float(ra[q * 8 + i]);
-              act_gate_backward(dg, g, u, a, p.act);           // a = act(g), du = dH a, dg = dH u act'(g)
+              for (int i = 0; i < 8; ++i) dh[i] = __uint_as_float(ra[q * 8 + i]);
+              gate_backward(dh, g, u, h, dg, du, p.act);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) du[i] = __uint_as_float(ra[q * 8 + i]) * a[i];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) ph[(c & 1) * 16 + q * 4 + i] = pack_bf16(a[2 * i] * u[2 * i], a[2 * i + 1] * u[2 * i + 1]);
+              for (int i = 0; i < 4; ++i) ph[(c & 1) * 16 + q * 4 + i] = pack_bf16(h[2 * i], h[2 * i + 1]);
               stage_put(blk_a, (c & 1) * 4 + q, pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]), pack_bf16(dg[4], dg[5]), pack_bf16(dg[6], dg[7]));
               stage_put(blk_b, (c & 1) * 4 + q, pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]), pack_bf16(du[4], du[5]), pack_bf16(du[6], du[7]));
             }

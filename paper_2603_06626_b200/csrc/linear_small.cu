@@ -12,6 +12,9 @@
 // tokens 18; 128 x 128 with one token 4.1 us, which is what launch, set-up and the cluster's two barriers take.  A CTA has eight steps
 // and a ring of six, so its first load and its epilogue are most of its time.
 //
+// GATED: the up-projection of the gated feed-forward block, H = act(x Wg^T) * (x Wu^T).  A CTA's 128 weight rows are 64 of the gate and the
+// 64 of the other projection that belong to them, so it has both accumulators of an output in its partial tile.
+//
 // Roles in a CTA: warp 0 loads (TMA, ring of STAGES 64-deep steps), warp 1 issues the MMAs, warps 2-5 bring the accumulator to
 // shared memory; all six share the epilogue.  Every wait is bounded, as in the CTA-pair core: on give-up the CTA raises
 // STATUS_TIMEOUT, still meets the cluster's barriers, frees its TMEM and returns.
@@ -41,7 +44,7 @@ struct LinearSmallParams {
   unsigned long long wait_limit_ns;
 };
 
-template <int TN, bool A_MN>
+template <int TN, bool A_MN, bool GATED>
 __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                                                                      const LinearSmallParams p) {
   constexpr int STAGES = ls_stages(TN), STAGE_BYTES = ls_stage_bytes(TN), A_BYTES = LS_BM * LS_BK * 2;
@@ -55,7 +58,8 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
   cg::cluster_group cl = cg::this_cluster();
   const int S = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int tile = blockIdx.x / S;
-  const int n0 = tile * LS_BM, t0 = blockIdx.y * TN;
+  constexpr int OUT = GATED ? LS_BM / 2 : LS_BM;      // outputs of a CTA
+  const int n0 = tile * OUT, t0 = blockIdx.y * TN;
   const int ks0 = (int)((int64_t)p.nk * rank / S), ks1 = (int)((int64_t)p.nk * (rank + 1) / S);
   const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   float* part = reinterpret_cast<float*>(smem_raw + (smem_base - ptx::smem_u32(smem_raw)));
@@ -90,7 +94,10 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
         if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
         const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + A_BYTES;
         ptx::mbar_arrive_expect_tx(full_bar(s), (uint32_t)STAGE_BYTES);
-        if (!A_MN) {
+        if (GATED) {
+          ptx::tma_load_2d(sa, &tmA, full_bar(s), ks * LS_BK, n0);             // 2 x box {64 k, 64 rows}; rows beyond the last read as zeros
+          ptx::tma_load_2d(sa + A_BYTES / 2, &tmA, full_bar(s), ks * LS_BK, p.N + n0);
+        } else if (!A_MN) {
           ptx::tma_load_2d(sa, &tmA, full_bar(s), ks * LS_BK, n0);             // box {64 k, 128 rows}; rows beyond N read as zeros
         } else {
           ptx::tma_load_2d(sa, &tmA, full_bar(s), n0, ks * LS_BK);             // 2 x box {64 rows, 64 k}
@@ -155,7 +162,7 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
   ptx::tc_fence_before();
   cl.sync();                                           // all partial tiles of the cluster are in place (or their CTAs gave up)
   const bool failed = *abort_flag != 0;
-  const int tv = min(TN, p.T - t0), nv = min(LS_BM, p.N - n0);
+  const int tv = min(TN, p.T - t0), nv = min(OUT, p.N - n0);
   auto load4 = [&](const __nv_bfloat16* q, float (&f)[4]) {
     const uint2 u = *reinterpret_cast<const uint2*>(q);
     const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
@@ -172,9 +179,46 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
     *reinterpret_cast<uint2*>(q) = u;
   };
   // A thread keeps its four outputs n .. n + 3 and goes down the tokens, a whole cluster's threads sharing them.
-  static_assert(LS_THREADS % (LS_BM / 4) == 0, "a thread's outputs stay the same from step to step");
-  const int n = (threadIdx.x % (LS_BM / 4)) * 4, per_step = LS_THREADS / (LS_BM / 4);
-  if (n < nv) {                                        // N is a multiple of 8: four outputs at a time are all there or none
+  static_assert(LS_THREADS % (OUT / 4) == 0, "a thread's outputs stay the same from step to step");
+  const int n = (threadIdx.x % (OUT / 4)) * 4, per_step = LS_THREADS / (OUT / 4);
+  if (GATED && n < nv) {
+    const float* parts[LS_MAX_SPLITS];
+#pragma unroll
+    for (int r = 0; r < LS_MAX_SPLITS; ++r) parts[r] = cl.map_shared_rank(part, r < S ? r : 0) + n;
+    for (int t = rank * per_step + threadIdx.x / (OUT / 4); t < tv; t += S * per_step) {
+      float4 q[LS_MAX_SPLITS][2];
+#pragma unroll
+      for (int r = 0; r < LS_MAX_SPLITS; ++r) {
+        if (r < S) {
+          q[r][0] = *reinterpret_cast<const float4*>(parts[r] + t * LS_PITCH);
+          q[r][1] = *reinterpret_cast<const float4*>(parts[r] + t * LS_PITCH + OUT);
+        }
+      }
+      float g[4] = {q[0][0].x, q[0][0].y, q[0][0].z, q[0][0].w}, u[4] = {q[0][1].x, q[0][1].y, q[0][1].z, q[0][1].w};
+#pragma unroll
+      for (int r = 1; r < LS_MAX_SPLITS; ++r) {
+        if (r < S) {
+          g[0] += q[r][0].x;
+          g[1] += q[r][0].y;
+          g[2] += q[r][0].z;
+          g[3] += q[r][0].w;
+          u[0] += q[r][1].x;
+          u[1] += q[r][1].y;
+          u[2] += q[r][1].z;
+          u[3] += q[r][1].w;
+        }
+      }
+      if (p.pre) {
+        __nv_bfloat16* to = p.pre + (int64_t)(t0 + t) * 2 * p.N + n0 + n;
+        store4(to, g);
+        store4(to + p.N, u);
+      }
+      act_values(g, p.act);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] *= u[i];
+      store4(p.out + (int64_t)(t0 + t) * p.N + n0 + n, g);
+    }
+  } else if (n < nv) {                                        // N is a multiple of 8: four outputs at a time are all there or none
     float bias[4] = {0.f, 0.f, 0.f, 0.f};
     if (p.bias) load4(p.bias + n0 + n, bias);
     auto finish = [&](int t, float4 a) {
@@ -239,10 +283,10 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
 
 namespace {
 
-template <int TN, bool A_MN>
+template <int TN, bool A_MN, bool GATED>
 cudaError_t small_launch(const LinearGemm& g, int splits, cudaStream_t st) {
   static bool configured[64] = {};       // the opt-in to more than 48 KB of dynamic shared memory, once per device
-  auto kern = linear_small_kernel<TN, A_MN>;
+  auto kern = linear_small_kernel<TN, A_MN, GATED>;
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev < 0 || dev >= 64 || !configured[dev]) {
@@ -252,7 +296,9 @@ cudaError_t small_launch(const LinearGemm& g, int splits, cudaStream_t st) {
   }
   // here the weight is the M side: g.B of the product as the other kernel sees it
   CUtensorMap a, b;
-  const bool ok = (A_MN ? make_bf16_tile_map(&a, g.B, g.K, g.N, 64) : make_bf16_tile_map(&a, g.B, g.N, g.K, LS_BM)) &&
+  const bool ok = (GATED  ? make_bf16_tile_map(&a, g.B, 2 * (uint64_t)g.N, g.K, LS_BM / 2)
+                   : A_MN ? make_bf16_tile_map(&a, g.B, g.K, g.N, 64)
+                          : make_bf16_tile_map(&a, g.B, g.N, g.K, LS_BM)) &&
                   make_bf16_tile_map(&b, g.A, g.M, g.K, TN);
   if (!ok) return cudaErrorInvalidValue;
   LinearSmallParams p{};
@@ -267,7 +313,8 @@ cudaError_t small_launch(const LinearGemm& g, int splits, cudaStream_t st) {
   p.status = g.status;
   p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)((g.N + LS_BM - 1) / LS_BM * splits), (unsigned)((g.M + TN - 1) / TN));
+  constexpr int OUT = GATED ? LS_BM / 2 : LS_BM;
+  cfg.gridDim = dim3((unsigned)((g.N + OUT - 1) / OUT * splits), (unsigned)((g.M + TN - 1) / TN));
   cfg.blockDim = dim3(LS_THREADS);
   cfg.dynamicSmemBytes = ls_smem(TN);
   cfg.stream = st;
@@ -282,12 +329,12 @@ cudaError_t small_launch(const LinearGemm& g, int splits, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, kern, a, b, p);
 }
 
-template <bool A_MN>
+template <bool A_MN, bool GATED>
 cudaError_t small_by_tokens(const LinearGemm& g, int splits, cudaStream_t st) {
-  if (g.M <= 16) return small_launch<16, A_MN>(g, splits, st);
-  if (g.M <= 32) return small_launch<32, A_MN>(g, splits, st);
-  if (g.M <= 64) return small_launch<64, A_MN>(g, splits, st);
-  return small_launch<128, A_MN>(g, splits, st);
+  if (g.M <= 16) return small_launch<16, A_MN, GATED>(g, splits, st);
+  if (g.M <= 32) return small_launch<32, A_MN, GATED>(g, splits, st);
+  if (g.M <= 64) return small_launch<64, A_MN, GATED>(g, splits, st);
+  return small_launch<128, A_MN, GATED>(g, splits, st);
 }
 
 }  // namespace
@@ -302,7 +349,13 @@ int linear_small_splits(int T, int N, int K) {
 }
 
 cudaError_t launch_linear_small(const LinearGemm& g, int splits, cudaStream_t st) {
-  return g.b_mn ? small_by_tokens<true>(g, splits, st) : small_by_tokens<false>(g, splits, st);
+  return g.b_mn ? small_by_tokens<true, false>(g, splits, st) : small_by_tokens<false, false>(g, splits, st);
+}
+
+cudaError_t launch_gated_small(const GatedGemm& g, int splits, cudaStream_t st) {
+  LinearGemm l{};
+  l.A = g.A; l.B = g.W; l.C = g.h; l.pre = g.pre; l.M = g.T; l.N = g.H; l.K = g.K; l.act = g.act; l.status = g.status;
+  return small_by_tokens<false, true>(l, splits, st);
 }
 
 }  // namespace grouter

@@ -128,18 +128,30 @@ __global__ void __launch_bounds__(rms_forward_threads(LANES)) rms_forward_kernel
     if constexpr (FP8) {
       constexpr int GROUP = FP8_BLOCK / VE;      // lanes that share a scale
       static_assert(LANES >= GROUP && GROUP <= 32, "a block of columns lies in one warp");
-      uint32_t top = 0;
+      float top = 0.f;
       if (c < end) {
 #pragma unroll
-        for (int i = 0; i < VE; ++i) top = max(top, finite_magnitude(o[i]));
+        for (int i = 0; i < VE; ++i) top = larger(top, o[i]);
       }
-      top = lanes_max_bits<GROUP>(top);
+      top = lanes_top<GROUP>(top);
+      const bool inf = __any_sync(0xffffffffu, not_finite(top));
+      if (inf) {
+        top = 0.f;
+        if (c < end) {
+#pragma unroll
+          for (int i = 0; i < VE; ++i) top = larger_finite(top, o[i]);
+        }
+        top = lanes_top<GROUP>(top);
+      }
       const uint32_t e = fp8_exponent(top);
       const float inv = fp8_inverse(e);
       if (c < end) {
         uint8_t* to = static_cast<uint8_t*>(p.y) + row * d + c;
-        if constexpr (VE == 8) *reinterpret_cast<uint2*>(to) = make_uint2(fp8_quad(o, inv), fp8_quad(o + 4, inv));
-        else *reinterpret_cast<uint32_t*>(to) = fp8_quad(o, inv);
+        uint32_t q[VE / 4];
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) q[i / 4] = inf ? fp8_quad<true>(o + i, inv) : fp8_quad<false>(o + i, inv);
+        if constexpr (VE == 8) *reinterpret_cast<uint2*>(to) = make_uint2(q[0], q[1]);
+        else *reinterpret_cast<uint32_t*>(to) = q[0];
         if (at % GROUP == 0) p.scales[fp8_scale_at(row, c / FP8_BLOCK, across)] = (uint8_t)e;
       }
     }
