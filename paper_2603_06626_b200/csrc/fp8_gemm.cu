@@ -179,8 +179,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     }
     __syncwarp();
   } else if (warp == 1) {
-    // ===================== MMA issuer (leader CTA only) =====================
-    if (lane == 0 && rank == 0) {
+    // ===================== MMA issuer (leader CTA only): the warp together, one lane issues =====================
+    if (rank == 0) {
+      const bool issues = ptx::elect_one();
       constexpr uint32_t idesc = ptx::make_idesc_fp8_scaled(F8_PM, F8_BN);
       constexpr uint16_t both = 3, leader = 1;
       const uint64_t da0 = ptx::make_smem_desc_sw128(smem_base, 16, 1024), db0 = ptx::make_smem_desc_sw128(smem_base + F8_A_BYTES, 16, 1024);
@@ -188,10 +189,10 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       int s = 0, acc = 0, set = 0;
       uint32_t ph = 0, acc_ph = 0, over_ph = 0, set_ph = 0;
       bool first = true;
-      for (int t = pair_id; t < n_tiles && !*abort_flag; t += n_pairs) {
-        if (!ptx::mbar_wait_bounded(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
+      for (int t = pair_id; t < n_tiles && !__any_sync(0xffffffffu, *abort_flag); t += n_pairs) {
+        if (!ptx::mbar_wait_bounded_warp(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
         if (!first) {
-          if (!ptx::mbar_wait_bounded(over_bar, over_ph, abort_flag, p.wait_limit_ns)) break;
+          if (!ptx::mbar_wait_bounded_warp(over_bar, over_ph, abort_flag, p.wait_limit_ns)) break;
           over_ph ^= 1u;
         }
         first = false;
@@ -199,31 +200,37 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const uint32_t d_tmem = tmem_base + (acc ? F8_ACC1 : 0u);
         bool ok = true;
         for (int ks = 0; ks < steps; ++ks) {
-          if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
+          if (!ptx::mbar_wait_bounded_warp(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           const uint32_t t_sa = tmem_base + F8_SCALES + set * F8_SCALE_SET, t_sb = t_sa + 8;
-          ptx::tc_fence_after();
           if ((ks & 3) == 0) {
-            if (!ptx::mbar_wait_bounded(scales_bar(set), set_ph ^ 1u, abort_flag, p.wait_limit_ns)) {
+            if (!ptx::mbar_wait_bounded_warp(scales_bar(set), set_ph ^ 1u, abort_flag, p.wait_limit_ns)) {
               ok = false;
               break;
             }
             ptx::tc_fence_after();
             const uint64_t ds = ptx::make_smem_desc_scales(scale_base + s * F8_SCALE_BYTES);
-            ptx::tmem_copy_scales_pair(t_sa, ds);
-            ptx::tmem_copy_scales_pair(t_sb, ds + (FP8_ATOM >> 4));
-            ptx::tmem_copy_scales_pair(t_sb + 4, ds + (2 * FP8_ATOM >> 4));
+            if (issues) {
+              ptx::tmem_copy_scales_pair(t_sa, ds);
+              ptx::tmem_copy_scales_pair(t_sb, ds + (FP8_ATOM >> 4));
+              ptx::tmem_copy_scales_pair(t_sb + 4, ds + (2 * FP8_ATOM >> 4));
+            }
+            __syncwarp();
           }
           const uint32_t a_lo = (uint32_t)da0 + s * (F8_STAGE_BYTES >> 4), b_lo = (uint32_t)db0 + s * (F8_STAGE_BYTES >> 4);
           const uint32_t id = ptx::scale_byte(idesc, ks & 3);
+          const bool last_of_set = (ks & 3) == 3 || ks == steps - 1;
+          if (issues) {
 #pragma unroll
-          for (int kk = 0; kk < F8_BK / 32; ++kk)
-            ptx::umma_fp8_pair(d_tmem, a_lo + kk * 2, a_hi, b_lo + kk * 2, b_hi, id, t_sa, t_sb, (ks | kk) != 0 ? 1u : 0u);
-          ptx::umma_commit_pair(empty_bar(s), both);      // stage (and its scales) reusable in both CTAs once these have read it
-          if ((ks & 3) == 3 || ks == steps - 1) {
-            ptx::umma_commit_pair(scales_bar(set), leader);
+            for (int kk = 0; kk < F8_BK / 32; ++kk)
+              ptx::umma_fp8_pair(d_tmem, a_lo + kk * 2, a_hi, b_lo + kk * 2, b_hi, id, t_sa, t_sb, (ks | kk) != 0 ? 1u : 0u);
+            ptx::umma_commit_pair(empty_bar(s), both);      // stage (and its scales) reusable in both CTAs once these have read it
+            if (last_of_set) ptx::umma_commit_pair(scales_bar(set), leader);
+          }
+          __syncwarp();
+          if (last_of_set) {
             set ^= 1;
             if (set == 0) set_ph ^= 1u;
           }
@@ -233,7 +240,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           }
         }
         if (!ok) break;
-        ptx::umma_commit_pair(tfull_bar(acc), both);
+        if (issues) ptx::umma_commit_pair(tfull_bar(acc), both);
+        __syncwarp();
         if (++acc == 2) {
           acc = 0;
           acc_ph ^= 1u;

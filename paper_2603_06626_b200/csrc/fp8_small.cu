@@ -129,13 +129,14 @@ fp8_small_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
+    {
+      const bool issues = ptx::elect_one();      // the warp stays together, one lane issues
       constexpr uint32_t idesc = ptx::make_idesc_fp8_scaled(FS_BM, TN);
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
       for (int ks = ks0; ks < ks1; ++ks) {
-        if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
+        if (!ptx::mbar_wait_bounded_warp(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
           ok = false;
           break;
         }
@@ -143,23 +144,26 @@ fp8_small_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         const uint32_t at = smem_base + s * OPERANDS, id = ptx::scale_byte(idesc, ks & 3);
         const uint64_t ds = ptx::make_smem_desc_scales(scale_base + s * (TILES + 1) * FP8_ATOM);
         const uint32_t t_s = tmem_base + SCALES + s * (TILES + 1) * 4;
+        if (issues) {
 #pragma unroll
-        for (int i = 0; i <= TILES; ++i) ptx::tmem_copy_scales(t_s + 4 * i, ds + (i * FP8_ATOM >> 4));
+          for (int i = 0; i <= TILES; ++i) ptx::tmem_copy_scales(t_s + 4 * i, ds + (i * FP8_ATOM >> 4));
 #pragma unroll
-        for (int kk = 0; kk < FS_BK / 32; ++kk) {
-          const uint64_t dx = ptx::make_smem_desc_sw128(at + X_AT + kk * 32, 16, 1024);
+          for (int kk = 0; kk < FS_BK / 32; ++kk) {
+            const uint64_t dx = ptx::make_smem_desc_sw128(at + X_AT + kk * 32, 16, 1024);
 #pragma unroll
-          for (int i = 0; i < TILES; ++i)
-            ptx::umma_fp8(tmem_base + i * TN, ptx::make_smem_desc_sw128(at + i * W_BYTES + kk * 32, 16, 1024), dx, id, t_s + 4 * i, t_s + 4 * TILES,
-                          ks > ks0 || kk > 0 ? 1u : 0u);
+            for (int i = 0; i < TILES; ++i)
+              ptx::umma_fp8(tmem_base + i * TN, ptx::make_smem_desc_sw128(at + i * W_BYTES + kk * 32, 16, 1024), dx, id, t_s + 4 * i, t_s + 4 * TILES,
+                            ks > ks0 || kk > 0 ? 1u : 0u);
+          }
+          ptx::umma_commit(empty_bar(s));
         }
-        ptx::umma_commit(empty_bar(s));
+        __syncwarp();
         if (++s == STAGES) {
           s = 0;
           ph ^= 1u;
         }
       }
-      if (ok) ptx::umma_commit(done_bar);
+      if (ok && issues) ptx::umma_commit(done_bar);
     }
     __syncwarp();
   } else if (warp < 6) {

@@ -422,8 +422,9 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     }
     __syncwarp();
   } else if (warp == 1) {
-    // ===================== MMA issuer (leader CTA only) =====================
-    if (lane == 0 && rank == 0) {
+    // ===================== MMA issuer (leader CTA only): the warp together, one lane issues =====================
+    if (rank == 0) {
+      const bool issues = ptx::elect_one();
       constexpr uint32_t idesc = ptx::make_idesc_bf16(PM, BN, A_MN, B_MN);
       // K-major: 8-row groups are 1024 B apart (SBO); 16 K-elements = 32 B further along the row.
       // MN-major: 64-wide MN atoms are one 8 KB box apart (LBO), 8-k groups 1024 B apart (SBO);
@@ -444,10 +445,12 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       constexpr bool count = COUNT;
       long long c_acc = 0, c_full = 0, n_tiles_done = 0, n_ksteps = 0;
       const long long c_begin = count ? clock64() : 0;
-      for (int t = DYN ? next_tile() : pair_id; t < n_tiles && !*abort_flag; t = DYN ? next_tile() : t + n_pairs) {
+      // one lane's view of tile and abort flag for all: the warp must not part
+      auto same_tile = [&](int v) { return __shfl_sync(0xffffffffu, *abort_flag ? n_tiles : v, 0); };
+      for (int t = same_tile(DYN ? next_tile() : pair_id); t < n_tiles; t = same_tile(DYN ? next_tile() : t + n_pairs)) {
         const Tile ti = decode_tile<MODE>(p, t, 0);
         const long long c_t0 = count ? clock64() : 0;
-        if (!ptx::mbar_wait_bounded(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
+        if (!ptx::mbar_wait_bounded_warp(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
         if (count) {
           c_acc += clock64() - c_t0;
           n_tiles_done += 1;
@@ -458,16 +461,18 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         bool ok = true;
         for (int ks = 0; ks < ti.steps; ++ks) {
           const long long c_k0 = count ? clock64() : 0;
-          if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
+          if (!ptx::mbar_wait_bounded_warp(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           if (count) c_full += clock64() - c_k0;
-          ptx::tc_fence_after();
+          if (issues) {
 #pragma unroll
-          for (int kk = 0; kk < BK / 16; ++kk)
-            ptx::umma_bf16_pair_split(d_tmem, a_lo + kk * (a_kadv >> 4), a_hi, b_lo + kk * (b_kadv >> 4), b_hi, idesc, (ks | kk) != 0 ? 1u : 0u);
-          ptx::umma_commit_pair(empty_bar(s), both);  // stage reusable in both CTAs once these MMAs have read it
+            for (int kk = 0; kk < BK / 16; ++kk)
+              ptx::umma_bf16_pair_split(d_tmem, a_lo + kk * (a_kadv >> 4), a_hi, b_lo + kk * (b_kadv >> 4), b_hi, idesc, (ks | kk) != 0 ? 1u : 0u);
+            ptx::umma_commit_pair(empty_bar(s), both);  // stage reusable in both CTAs once these MMAs have read it
+          }
+          __syncwarp();
           a_lo += STAGE_BYTES >> 4;
           b_lo += STAGE_BYTES >> 4;
           if (++s == STAGES) {
@@ -478,13 +483,14 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           }
         }
         if (!ok) break;
-        ptx::umma_commit_pair(tfull_bar(acc), both);
+        if (issues) ptx::umma_commit_pair(tfull_bar(acc), both);
+        __syncwarp();
         if (++acc == 2) {
           acc = 0;
           acc_ph ^= 1u;
         }
       }
-      if (count) {
+      if (count && issues) {
         atomicAdd(p.cycles + 0, (unsigned long long)(clock64() - c_begin));
         atomicAdd(p.cycles + 1, (unsigned long long)c_full);
         atomicAdd(p.cycles + 2, (unsigned long long)c_acc);

@@ -112,7 +112,8 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
+    {
+      const bool issues = ptx::elect_one();      // the warp stays together, one lane issues
       constexpr uint32_t idesc = ptx::make_idesc_bf16(LS_BM, TN, A_MN, false);
       // operand layouts as in the CTA-pair core (gemm.cu)
       constexpr uint32_t a_lbo = A_MN ? A_BYTES / 2 : 16, a_kadv = A_MN ? 2048 : 32;
@@ -120,25 +121,28 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
       uint32_t ph = 0;
       bool ok = true;
       for (int ks = ks0; ks < ks1; ++ks) {
-        if (!ptx::mbar_wait_bounded(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
+        if (!ptx::mbar_wait_bounded_warp(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
           ok = false;
           break;
         }
         ptx::tc_fence_after();
         const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + A_BYTES;
+        if (issues) {
 #pragma unroll
-        for (int kk = 0; kk < LS_BK / 16; ++kk) {
-          const uint64_t da = ptx::make_smem_desc_sw128(sa + kk * a_kadv, a_lbo, 1024);
-          const uint64_t db = ptx::make_smem_desc_sw128(sb + kk * 32, 16, 1024);
-          ptx::umma_bf16(tmem_base, da, db, idesc, ks > ks0 || kk > 0 ? 1u : 0u);
+          for (int kk = 0; kk < LS_BK / 16; ++kk) {
+            const uint64_t da = ptx::make_smem_desc_sw128(sa + kk * a_kadv, a_lbo, 1024);
+            const uint64_t db = ptx::make_smem_desc_sw128(sb + kk * 32, 16, 1024);
+            ptx::umma_bf16(tmem_base, da, db, idesc, ks > ks0 || kk > 0 ? 1u : 0u);
+          }
+          ptx::umma_commit(empty_bar(s));
         }
-        ptx::umma_commit(empty_bar(s));
+        __syncwarp();
         if (++s == STAGES) {
           s = 0;
           ph ^= 1u;
         }
       }
-      if (ok) ptx::umma_commit(done_bar);
+      if (ok && issues) ptx::umma_commit(done_bar);
     }
     __syncwarp();
   } else {

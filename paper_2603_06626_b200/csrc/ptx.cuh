@@ -17,6 +17,21 @@ __device__ __forceinline__ uint64_t globaltimer_ns() {
   return t;
 }
 
+// True in one lane of a converged warp, always the same one.  A warp that stays together around the few instructions of its elected
+// lane keeps their operands in uniform registers; a loop that only one lane runs has to bring every operand over for every instruction
+// (a 128-deep step of the 8-bit products: 813 cycles, so 593, of which the tensor cores need 512).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "elect.sync _|p, 0xffffffff;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(p));
+  return p != 0;
+}
+
 // ---------------- CTA pair (cluster of two) ----------------
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;
@@ -77,6 +92,11 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
       return false;
     }
   }
+}
+
+// The same wait by a whole converged warp: true where every lane's wait ended well.
+__device__ __forceinline__ bool mbar_wait_bounded_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, limit_ns));
 }
 
 // ---------------- 8-byte words polled across the CTA pair ----------------
