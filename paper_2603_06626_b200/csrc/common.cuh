@@ -224,7 +224,8 @@ cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, 
 // The same product for few rows of A (tokens; K-major): the contraction cut over a cluster of `splits` CTAs (linear_small_splits).
 int linear_small_splits(int T, int N, int K);
 cudaError_t launch_linear_small(const LinearGemm& g, int splits, cudaStream_t st);
-// launch_gated_gemm's forward product for few tokens, likewise; its CTAs are those of a linear layer with 2H outputs.
+// launch_gated_gemm's forward product for few tokens, likewise.
+int gated_small_splits(int T, int H, int K);
 cudaError_t launch_gated_small(const GatedGemm& g, int splits, cudaStream_t st);
 
 }  // namespace grouter

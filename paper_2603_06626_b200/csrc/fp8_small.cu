@@ -357,12 +357,15 @@ cudaError_t small_by_tokens(const Fp8Gemm& g, int splits, cudaStream_t st) {
 
 }  // namespace
 
-// Cuts of the contraction: as many as fit the SMs at once (two CTAs an SM, GLU one), and no CTA left with fewer than two 128-deep steps.
+// Cuts of the contraction: as many as leave a CTA an SM of its own (4096 -> 4096: one token in 4 cuts, 128 CTAs, 5.1 us, in 8 cuts two to an
+// SM 5.5; 128 tokens 8.1 and 11.2; 256 tokens 4096 -> 1536 in 4 cuts 7.9, in 8 10.1) and at least two 128-deep steps.  Clusters of
+// eight do not find room everywhere: GLU, whose CTAs fill an SM, takes them up to three quarters of the SMs (16 tiles in eights 24.9 us,
+// in fours 16.1).
 int fp8_small_splits(int T, int N, int K, bool glu) {
   const int64_t tiles = (int64_t)((N + FS_BM - 1) / FS_BM) * ((T + 127) / 128);
-  const int nk = (K + FS_BK - 1) / FS_BK, room = (glu ? 1 : 2) * current_sms();
+  const int nk = (K + FS_BK - 1) / FS_BK, room = current_sms();
   int s = 1;
-  while (s < FS_MAX_SPLITS && tiles * s * 2 <= room && nk >= 4 * s) s *= 2;
+  while (s < FS_MAX_SPLITS && tiles * s * 2 <= (glu && s == 4 ? room * 3 / 4 : room) && nk >= 4 * s) s *= 2;
   return s;
 }
 

@@ -59,14 +59,35 @@ int fp8_check(int32_t T, int32_t K, int32_t N) {
   return GROUTER_OK;
 }
 
-// Whichever of the two kernels is ahead at these sizes.
+// Which of the two kernels is ahead: both sides in microseconds, fitted to measurements over 1 to 4096 tokens and weights of 128 x 128 to
+// 8192 x 4096.  Tiles of 256 x 256 (or 128 hidden columns) on CTA pairs: a start and the steps of every round of the pairs.  Few tokens: for
+// every round of the SMs a start, the steps of one cut, a meeting of the cluster and, where h is formed, the tokens of a tile.
+// Measured (few tokens against tiles): 8 bits 4096 -> 1536, 128 tokens 6.9 and 13.8 us, 1024 tokens 18 and 14; 1024 -> 2816, 512 tokens 7.7 and
+// 7.2; 4096 -> 4096, 384 tokens 13 and 15.  Gated in 8 bits d 4096, hidden 1536: 128 tokens 12.7 and 14.5, 512 tokens 16.2 and 15.9;
+// d 1024, hidden 2816: 64 tokens 7.5 and 9.5, 128 tokens 11.7 and 7.8.  In bf16 the same: 128 tokens 17 and 26.5, 1024 tokens 34 and 26;
+// 64 tokens 6.5 and 9.4, 256 tokens 11.0 and 9.7.
+inline int rounds(int64_t tiles, int places) { return (int)((tiles + places - 1) / (places > 0 ? places : 1)); }
+inline int log2_of(int s) { return s >= 8 ? 3 : s >= 4 ? 2 : s >= 2 ? 1 : 0; }
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int token_tile(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+
 cudaError_t fp8_product(const Fp8Gemm& g, cudaStream_t st) {
-  if (!g.out_f32 && g.M <= 64) return launch_fp8_small(g, fp8_small_splits(g.M, g.N, g.K, g.B1.codes != nullptr), st);
-  return launch_fp8_gemm(g, st);
+  const bool glu = g.B1.codes != nullptr;
+  const int sms = current_sms(), splits = fp8_small_splits(g.M, g.N, g.K, glu);
+  const int64_t steps = cdiv(g.K, 128), ctas = cdiv(g.N, 128) * cdiv(g.M, 128) * splits;
+  const int tile_rounds = rounds(cdiv(g.M, 256) * cdiv(g.N, glu ? 128 : 256), sms / 2);
+  const float tiles = (glu ? 4.9f + 0.31f * steps * tile_rounds : 4.4f + 0.285f * steps * tile_rounds);
+  const float small = glu ? rounds(ctas, sms) * (2.9f + 0.045f * token_tile(g.M) + 0.45f * cdiv(steps, splits) + 0.8f * log2_of(splits))
+                          : rounds(ctas, 2 * sms) * (3.f + 0.48f * cdiv(steps, splits) + log2_of(splits));
+  const bool fits = cdiv(g.M, 128) <= 65535;      // its grid has the token tiles in y
+  return !g.out_f32 && fits && small < tiles ? launch_fp8_small(g, splits, st) : launch_fp8_gemm(g, st);
 }
 cudaError_t gated_product(const GatedGemm& g, cudaStream_t st) {
-  if (g.T <= 64) return launch_gated_small(g, linear_small_splits(g.T, 2 * g.H, g.K), st);
-  return launch_gated_gemm(g, st);
+  const int sms = current_sms(), splits = gated_small_splits(g.T, g.H, g.K);
+  const int64_t steps = cdiv(g.K, 64), ctas = cdiv(2 * (int64_t)g.H, 128) * cdiv(g.T, 128) * splits;
+  const float tiles = 5.f + 0.3f * steps * rounds(cdiv(g.T, 256) * cdiv(g.H, 128), sms / 2);
+  const float small = rounds(ctas, 2 * sms) * (2.f + 0.03f * token_tile(g.T) + 0.5f * cdiv(steps, splits));
+  return cdiv(g.T, 128) <= 65535 && small < tiles ? launch_gated_small(g, splits, st) : launch_gated_gemm(g, st);
 }
 
 }  // namespace
