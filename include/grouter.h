@@ -437,11 +437,14 @@ int grouter_dequantize_fp8(const void* codes, const void* scales, int32_t rows, 
 
 /* Linear layer in 8 bits:  y = x W^T + bias + residual  for x [T,K], W [N,K] as codes and scales (the products of a block of 128 are
  * multiplied by both scales and added up in fp32, bias and residual in fp32, y rounded once).
+ *   x_scales NULL: x is bf16, row t at x + t*ldx elements (any alignment), and is put into 8 bits by this call, in workspace
+ *   (grouter_linear_fp8_fwd_workspace_bytes(T, K) bytes, 256-byte aligned; else unused, as ldx is)
  *   bias [N] or NULL, residual [T,N] or NULL, y [T,N] out: bf16, contiguous.  residual may be y itself.
  *   status: device int32 the kernels OR bits into (2 = a bounded wait ran out); the caller zeroes it
- * Required: N a multiple of 8, everything 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
-int grouter_linear_fp8_fwd(const void* x, const void* x_scales, const void* W, const void* W_scales, const void* bias, const void* residual, int32_t T,
-                           int32_t K, int32_t N, void* y, int32_t* status, void* stream);
+ * Required: N a multiple of 8, everything else 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
+size_t grouter_linear_fp8_fwd_workspace_bytes(int32_t T, int32_t K);
+int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W, const void* W_scales, const void* bias,
+                           const void* residual, int32_t T, int32_t K, int32_t N, void* y, void* workspace, int32_t* status, void* stream);
 /* Its backward pass from dy [T,N] bf16 (contiguous), which is put into 8 bits here, by rows for dx and by columns for dW:
  *   dx = q(dy) W [T,K] bf16      dW = q(dy^T) x [N,K] of dW_dtype      db = sum over tokens of dy [N] f32 (not in 8 bits)
  *   xt, Wt: codes and scales of the transposed matrices, x^T [K,T] for dW and W^T [K,N] for dx (grouter_quantize_fp8's codes_t)
@@ -467,11 +470,13 @@ size_t grouter_gated_ffn_bwd_workspace_bytes(int32_t T, int32_t d, int32_t H);
 int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const void* W_d, const void* pre, int32_t T, int32_t d, int32_t H,
                           int32_t act, void* dx, void* dW_gu, void* dW_d, int32_t dW_dtype, void* workspace, int32_t* status, void* stream);
 /* The same block's forward pass in 8 bits:  h = act(x W_g^T) * (x W_u^T) in fp32, put into codes (128 columns a scale) as
- * grouter_quantize_fp8 does,  y = h W_d^T + residual.  x [T,d], W_g, W_u [H,d], W_d [d,H], h [T,H] out: codes and scales;
- * residual [T,d] or NULL, y [T,d]: bf16. */
-int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, const void* W_g, const void* W_g_scales, const void* W_u, const void* W_u_scales,
-                              const void* W_d, const void* W_d_scales, const void* residual, int32_t T, int32_t d, int32_t H, int32_t act, void* h,
-                              void* h_scales, void* y, int32_t* status, void* stream);
+ * grouter_quantize_fp8 does,  y = h W_d^T + residual.  x [T,d], W_g, W_u [H,d], W_d [d,H]: codes and scales; x_scales NULL: x is bf16, as
+ * for the linear layer in 8 bits.  residual [T,d] or NULL, y [T,d]: bf16.  workspace: grouter_gated_ffn_fp8_fwd_workspace_bytes(T, d, H)
+ * bytes, 256-byte aligned. */
+size_t grouter_gated_ffn_fp8_fwd_workspace_bytes(int32_t T, int32_t d, int32_t H);
+int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W_g, const void* W_g_scales, const void* W_u,
+                              const void* W_u_scales, const void* W_d, const void* W_d_scales, const void* residual, int32_t T, int32_t d, int32_t H,
+                              int32_t act, void* y, void* workspace, int32_t* status, void* stream);
 
 /* Synchronises `stream` and returns the sticky device status (GROUTER_OK,
  * GROUTER_ERR_BAD_INDEX, GROUTER_ERR_TIMEOUT) or GROUTER_ERR_CUDA; clears it. */

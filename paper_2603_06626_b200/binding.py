@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 import threading
 from typing import Optional
@@ -36,8 +37,9 @@ EXPORTS = ["grouter_create", "grouter_destroy", "grouter_workspace_bytes", "grou
            "grouter_adamw_layout_host", "grouter_adamw_step", "grouter_adamw_moments",
            "grouter_rmsnorm_fwd", "grouter_rmsnorm_bwd", "grouter_rmsnorm_bwd_workspace_bytes",
            "grouter_fp8_pitch", "grouter_fp8_scale_bytes", "grouter_quantize_fp8", "grouter_dequantize_fp8",
-           "grouter_linear_fp8_fwd", "grouter_linear_fp8_bwd", "grouter_linear_fp8_bwd_workspace_bytes",
-           "grouter_gated_ffn_fwd", "grouter_gated_ffn_bwd", "grouter_gated_ffn_bwd_workspace_bytes", "grouter_gated_ffn_fp8_fwd"]
+           "grouter_linear_fp8_fwd", "grouter_linear_fp8_fwd_workspace_bytes", "grouter_linear_fp8_bwd", "grouter_linear_fp8_bwd_workspace_bytes",
+           "grouter_gated_ffn_fwd", "grouter_gated_ffn_bwd", "grouter_gated_ffn_bwd_workspace_bytes", "grouter_gated_ffn_fp8_fwd",
+           "grouter_gated_ffn_fp8_fwd_workspace_bytes"]
 KERNEL_SLOTS = ["plan_hist", "plan_permute", "gather_X", "gemm_up_swiglu", "gemm_down", "combine_Y", "gather_dY", "gemm_dH",
                 "wgrad_down", "gemm_dX", "wgrad_gate_up", "reduce_dX", "zero_split_dW", "plan_scan"]
 
@@ -183,13 +185,15 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             ("fp8_scale_bytes", size, [i32, i32]),
             ("quantize_fp8", i32, [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp]),
             ("dequantize_fp8", i32, [vp, vp, i32, i32, i64, i32, vp, vp]),
-            ("linear_fp8_fwd", i32, [vp] * 6 + [i32] * 3 + [vp] * 3),
+            ("linear_fp8_fwd_workspace_bytes", size, [i32] * 2),
+            ("linear_fp8_fwd", i32, [vp, vp, i64] + [vp] * 4 + [i32] * 3 + [vp] * 4),
             ("linear_fp8_bwd_workspace_bytes", size, [i32] * 3),
             ("linear_fp8_bwd", i32, [vp] * 5 + [i32] * 3 + [vp, vp, i32] + [vp] * 4),
             ("gated_ffn_fwd", i32, [vp] * 4 + [i32] * 4 + [vp] * 5),
             ("gated_ffn_bwd_workspace_bytes", size, [i32] * 3),
             ("gated_ffn_bwd", i32, [vp] * 5 + [i32] * 4 + [vp] * 3 + [i32] + [vp] * 3),
-            ("gated_ffn_fp8_fwd", i32, [vp] * 9 + [i32] * 4 + [vp] * 5)):
+            ("gated_ffn_fp8_fwd_workspace_bytes", size, [i32] * 3),
+            ("gated_ffn_fp8_fwd", i32, [vp, vp, i64] + [vp] * 7 + [i32] * 4 + [vp] * 4)):
         fn = getattr(lib, "grouter_" + name)
         fn.restype, fn.argtypes = result, args
     if path == _build.LIB:
@@ -957,22 +961,24 @@ class Fp8Blocks:
         return self.scales.permute(0, 3, 2, 1, 4).reshape(128 * a, 4 * b)[:rows, :(cols + 127) // 128]
 
 
-def _expect_fp8(what: str, q: Optional[Fp8Blocks], shape, like: Optional[torch.device] = None) -> None:
-    """Raises unless q (None passes) holds a matrix of this shape in the layout that the kernels read, on the device `like`."""
+def _expect_fp8(what: str, q: Optional[Fp8Blocks], rows: int, cols: int, on: torch.device) -> None:
+    """Raises unless q (None passes) holds a matrix of this shape in the layout that the kernels read, on the device `on`."""
     if q is None:
         return
     if not isinstance(q, Fp8Blocks):
         raise TypeError(f"{what}: Fp8Blocks expected, got {type(q).__name__}")
-    rows, cols = shape
-    on = q.codes.device if like is None else like
-    if (q.cols == cols and _fits(q.codes, (rows, (cols + 15) // 16 * 16), torch.float8_e4m3fn, on) and
-            _fits(q.scales, Fp8Blocks.scale_shape(rows, cols), torch.uint8, on)):
+    c, s = q.codes, q.scales
+    if (q.cols == cols and c.shape == (rows, (cols + 15) // 16 * 16) and c.dtype == _E4M3 and c.device == on and c.is_contiguous() and
+            s.shape == ((rows + 127) // 128, (cols + 511) // 512, 32, 4, 4) and s.dtype == torch.uint8 and s.device == on and s.is_contiguous()):
         return
     if q.cols != cols:
         raise ValueError(f"{what}: {cols} columns expected, got {q.cols}")
     where = torch.empty(0, device=on)
-    _expect(f"{what}: codes", q.codes, (rows, (cols + 15) // 16 * 16), torch.float8_e4m3fn, like=where)
-    _expect(f"{what}: scales", q.scales, Fp8Blocks.scale_shape(rows, cols), torch.uint8, like=where)
+    _expect(f"{what}: codes", c, (rows, (cols + 15) // 16 * 16), _E4M3, like=where)
+    _expect(f"{what}: scales", s, Fp8Blocks.scale_shape(rows, cols), torch.uint8, like=where)
+
+
+_E4M3 = torch.float8_e4m3fn
 
 
 def quantize_fp8(x: torch.Tensor, square: bool = False, rows: bool = True, transposed: bool = False):
@@ -997,7 +1003,7 @@ def dequantize_fp8(q: Fp8Blocks, dtype: torch.dtype = torch.bfloat16) -> torch.T
     lib = load_library()
     if not isinstance(q, Fp8Blocks):
         raise TypeError(f"q: Fp8Blocks expected, got {type(q).__name__}")
-    _expect_fp8("q", q, (q.rows, q.cols))
+    _expect_fp8("q", q, q.rows, q.cols, q.device)
     rows, cols = q.shape
     y = torch.empty((rows, cols), dtype=dtype, device=q.device)
     dt = _elt(y, "dtype")
@@ -1006,16 +1012,28 @@ def dequantize_fp8(q: Fp8Blocks, dtype: torch.dtype = torch.bfloat16) -> torch.T
     return y
 
 
-def _rows_of(what: str, x, cols: int, on: torch.device) -> int:
-    """Rows of an argument that is Fp8Blocks or a bf16 matrix, with `cols` columns on device `on`; others raise."""
+def _fp8_input(what: str, x, cols: int, on: torch.device):
+    """(rows, address, address of the scales or None, row stride) of an argument that is Fp8Blocks or a bf16 matrix whose rows may be
+    strided, with `cols` columns on device `on`; others raise."""
     if isinstance(x, Fp8Blocks):
-        _expect_fp8(what, x, (x.rows, cols), on)
-        return x.rows
+        rows = x.codes.shape[0]
+        _expect_fp8(what, x, rows, cols, on)
+        return rows, x.codes.data_ptr(), x.scales.data_ptr(), 0
     if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16:
         raise TypeError(f"{what}: Fp8Blocks or a bfloat16 matrix expected")
     if x.dim() != 2 or x.shape[1] != cols or x.device != on:
         raise ValueError(f"{what}: a matrix of {cols} columns on {on} is expected, got {tuple(x.shape)} on {x.device}")
-    return x.shape[0]
+    return x.shape[0], x.data_ptr(), None, _row_stride(what, x)
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_fp8_bytes(T: int, K: int) -> int:
+    return load_library().grouter_linear_fp8_fwd_workspace_bytes(T, K)
+
+
+@functools.lru_cache(maxsize=1024)
+def _gated_fp8_bytes(T: int, d: int, H: int) -> int:
+    return load_library().grouter_gated_ffn_fp8_fwd_workspace_bytes(T, d, H)
 
 
 def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
@@ -1025,21 +1043,21 @@ def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: O
     lib = load_library()
     if not isinstance(W, Fp8Blocks):
         raise TypeError(f"W: Fp8Blocks expected, got {type(W).__name__}")
-    on = W.device
-    N, K = W.shape
-    _expect_fp8("W", W, (N, K))
-    T = _rows_of("x", x, K, on)
-    bf = torch.bfloat16
+    codes = W.codes
+    on, K, bf = codes.device, W.cols, torch.bfloat16
+    N = codes.shape[0]
+    _expect_fp8("W", W, N, K, on)
+    T, px, ps, ld = _fp8_input("x", x, K, on)
     if not (_fits(bias, (N,), bf, on) and _fits(residual, (T, N), bf, on) and _fits(status, (1,), torch.int32, on)):
-        _expect("bias", bias, (N,), bf, like=W.codes)
-        _expect("residual", residual, (T, N), bf, like=W.codes)
-        _expect("status", status, (1,), torch.int32, like=W.codes)
+        _expect("bias", bias, (N,), bf, like=codes)
+        _expect("residual", residual, (T, N), bf, like=codes)
+        _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
-    if not isinstance(x, Fp8Blocks):
-        x = quantize_fp8(x)[0]
-    y = torch.empty((T, N), dtype=bf, device=on)
-    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, x.codes.data_ptr(), x.scales.data_ptr(), W.codes.data_ptr(), W.scales.data_ptr(),
-          _ptr(bias), _ptr(residual), T, K, N, y.data_ptr(), _status_ptr(status, dev))
+    ws = None if ps is not None else x.new_empty(_linear_fp8_bytes(T, K), dtype=torch.uint8)
+    y = codes.new_empty((T, N), dtype=bf)
+    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, px, ps, ld, codes.data_ptr(), W.scales.data_ptr(),
+          None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(), T, K, N, y.data_ptr(),
+          None if ws is None else ws.data_ptr(), _status_ptr(status, dev))
     return y
 
 
@@ -1063,8 +1081,8 @@ def linear_fp8_backward(dy: torch.Tensor, xt: Optional[Fp8Blocks], Wt: Optional[
             raise TypeError(f"{name}: Fp8Blocks expected, got {type(q).__name__}")
     K = Wt.rows if Wt is not None else xt.rows if xt is not None else 8
     bf, on = torch.bfloat16, dy.device
-    _expect_fp8("xt", xt, (K, T), on)
-    _expect_fp8("Wt", Wt, (K, N), on)
+    _expect_fp8("xt", xt, K, T, on)
+    _expect_fp8("Wt", Wt, K, N, on)
     if not (_fits(dy, (T, N), bf, on) and _fits(db, (N,), torch.float32, on) and _fits(status, (1,), torch.int32, on)):
         _expect("dy", dy, (T, N), bf)
         _expect("db", db, (N,), torch.float32, like=dy)
@@ -1159,25 +1177,24 @@ def gated_ffn_fp8(x, W_g: Fp8Blocks, W_u: Fp8Blocks, W_d: Fp8Blocks, act: int = 
     lib = load_library()
     if not isinstance(W_d, Fp8Blocks):
         raise TypeError(f"W_d: Fp8Blocks expected, got {type(W_d).__name__}")
-    on = W_d.device
-    d, H = W_d.shape
-    for name, W, shape in (("W_g", W_g, (H, d)), ("W_u", W_u, (H, d)), ("W_d", W_d, (d, H))):
-        if W is None:
-            raise TypeError(f"{name}: Fp8Blocks expected")
-        _expect_fp8(name, W, shape, on)
-    T = _rows_of("x", x, d, on)
-    bf = torch.bfloat16
+    if W_g is None or W_u is None:
+        raise TypeError("W_g, W_u: Fp8Blocks expected")
+    codes = W_d.codes
+    on, H, bf = codes.device, W_d.cols, torch.bfloat16
+    d = codes.shape[0]
+    _expect_fp8("W_g", W_g, H, d, on)
+    _expect_fp8("W_u", W_u, H, d, on)
+    _expect_fp8("W_d", W_d, d, H, on)
+    T, px, ps, ld = _fp8_input("x", x, d, on)
     if not (_fits(residual, (T, d), bf, on) and _fits(status, (1,), torch.int32, on)):
-        _expect("residual", residual, (T, d), bf, like=W_d.codes)
-        _expect("status", status, (1,), torch.int32, like=W_d.codes)
+        _expect("residual", residual, (T, d), bf, like=codes)
+        _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
-    if not isinstance(x, Fp8Blocks):
-        x = quantize_fp8(x)[0]
-    h = Fp8Blocks.empty(T, H, on)
-    y = torch.empty((T, d), dtype=bf, device=on)
-    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, x.codes.data_ptr(), x.scales.data_ptr(), W_g.codes.data_ptr(),
-          W_g.scales.data_ptr(), W_u.codes.data_ptr(), W_u.scales.data_ptr(), W_d.codes.data_ptr(), W_d.scales.data_ptr(), _ptr(residual), T, d, H, act,
-          h.codes.data_ptr(), h.scales.data_ptr(), y.data_ptr(), _status_ptr(status, dev))
+    ws = codes.new_empty(_gated_fp8_bytes(T, d, H), dtype=torch.uint8)
+    y = codes.new_empty((T, d), dtype=bf)
+    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, px, ps, ld, W_g.codes.data_ptr(), W_g.scales.data_ptr(),
+          W_u.codes.data_ptr(), W_u.scales.data_ptr(), codes.data_ptr(), W_d.scales.data_ptr(), None if residual is None else residual.data_ptr(),
+          T, d, H, act, y.data_ptr(), ws.data_ptr(), _status_ptr(status, dev))
     return y
 
 

@@ -195,7 +195,7 @@ cudaError_t launch_wait_selftest(grouter_ctx* ctx, unsigned long long limit_ns, 
 // C = A * B (fp32).  A contraction longer than k_chunk (a multiple of 64) is cut into ceil(K / k_chunk) partial products, stored
 // one after the other as M x N matrices from C on.
 cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, float* C, int M, int N, int K, int k_chunk, int32_t* status,
-                              cudaStream_t st);
+                              cudaStream_t st, bool waits_at_end = false);
 // C = act(A * B + bias) + residual (bf16); pre: A * B + bias (bf16) or null.  Operands as for launch_dense_gemm; an MN-major A
 // goes with an MN-major B only.
 struct LinearGemm {
@@ -203,6 +203,7 @@ struct LinearGemm {
   void *C, *pre;
   int a_mn, b_mn, M, N, K, act;
   int32_t* status;
+  bool waits_at_end;      // works beside the end of the kernel before it, whose results it does not read (launch_linear_gemm only)
 };
 cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st);
 // Forward (A = x [T,K], W = W_gu [2H,K]): H = act(G) U and, with pre, [G|U] -> pre [T,2H].  Backward (A = dy [T,K], W = W_d [K,H]): with
@@ -221,6 +222,10 @@ cudaError_t launch_product(const LinearGemm& g, cudaStream_t st);
 size_t weight_gradient_bytes(int T, int K, int N);
 cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
                                    cudaStream_t st);
+// Its two parts: the product, and the sum of the pieces where there are several.
+cudaError_t launch_weight_product(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
+                                  bool waits_at_end, cudaStream_t st);
+cudaError_t launch_weight_sum(int T, int K, int N, void* dW, int dW_dtype, const void* pieces, cudaStream_t st);
 // The same product for few rows of A (tokens; K-major): the contraction cut over a cluster of `splits` CTAs (linear_small_splits).
 int linear_small_splits(int T, int N, int K);
 cudaError_t launch_linear_small(const LinearGemm& g, int splits, cudaStream_t st);

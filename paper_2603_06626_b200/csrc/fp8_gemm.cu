@@ -44,6 +44,7 @@ struct F8Params {
   uint8_t* out_scales;           // GLU
   int32_t* status;
   unsigned long long wait_limit_ns;
+  int waits_at_end;              // as in gemm.cu: works beside the end of the kernel before it
 };
 
 struct F8Tile {
@@ -126,7 +127,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   ptx::tc_fence_after();
   const uint32_t tmem_base = s_tmem_base;
   volatile int* abort_flag = &s_abort;
-  after_previous_kernel();      // set up while the kernel before was still ending; from here on its results are read
+  if (!p.waits_at_end) after_previous_kernel();      // set up while the kernel before was still ending; from here on its results are read
   let_next_kernel_start();
 
   const int n_tiles = p.tiles_m * p.tiles_n, steps = (p.K + F8_BK - 1) / F8_BK;
@@ -456,6 +457,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     const uint64_t t0 = ptx::globaltimer_ns();
     while (ptx::globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
   }
+  if (p.waits_at_end) after_previous_kernel();
   ptx::tc_fence_before();
   __syncthreads();
   ptx::cluster_sync_all();      // neither CTA leaves while the other may still touch its shared memory or TMEM
@@ -503,6 +505,7 @@ cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st) {
   p.across = (int)fp8_atoms_across(g.K);
   p.act = g.act;
   p.status = g.status;
+  p.waits_at_end = g.waits_at_end;
   p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
   F8Maps m;
   bool ok = make_fp8_maps(&m.A, &m.SA, g.A, g.M, g.K, F8_BM) && make_fp8_maps(&m.B, &m.SB, g.B, g.N, g.K, F8_BNH);

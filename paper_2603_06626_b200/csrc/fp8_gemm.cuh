@@ -14,6 +14,7 @@ struct Fp8Gemm {
   void *C, *out_scales;
   int M, N, K, act, out_f32;
   int32_t* status;
+  bool waits_at_end;                      // launch_fp8_gemm: works beside the end of the kernel before it, whose results it does not read
 };
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
 // The same for few rows of A (tokens), bf16 or codes out: the contraction cut over a cluster of `splits` CTAs (fp8_small_splits).

@@ -19,14 +19,14 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 inline bool fits_int(int64_t v) { return v <= INT32_MAX - 256; }
 
 struct GatedWorkspace {
-  size_t dp, h, pieces, bytes;
+  size_t dp, h, pieces_gu, pieces_d, bytes;
 };
 GatedWorkspace gated_workspace(int T, int d, int H) {
   GatedWorkspace w{};
   w.h = up256((size_t)T * 2 * H * 2);
-  w.pieces = w.h + up256((size_t)T * H * 2);
-  const size_t gu = weight_gradient_bytes(T, d, 2 * H), down = weight_gradient_bytes(T, H, d);
-  w.bytes = w.pieces + (gu > down ? gu : down) + 256;
+  w.pieces_gu = w.h + up256((size_t)T * H * 2);
+  w.pieces_d = w.pieces_gu + weight_gradient_bytes(T, d, 2 * H);      // both products are on their way at a time
+  w.bytes = w.pieces_d + weight_gradient_bytes(T, H, d) + 256;
   return w;
 }
 
@@ -47,6 +47,17 @@ Fp8Workspace fp8_workspace(int T, int N) {
   w.col_scales = w.cols + up256((size_t)N * fp8_pitch(T));
   w.sums = w.col_scales + up256(grouter_fp8_scale_bytes(N, T));
   w.bytes = w.sums + up256(((size_t)T + 127) / 128 * N * 4) + 256;
+  return w;
+}
+
+// Codes of bf16 activations [T,K], made by the call itself.
+struct Fp8Input {
+  size_t scales, bytes;
+};
+Fp8Input fp8_input(int T, int K) {
+  Fp8Input w{};
+  w.scales = up256((size_t)T * fp8_pitch(K));
+  w.bytes = w.scales + up256(grouter_fp8_scale_bytes(T, K));
   return w;
 }
 
@@ -145,22 +156,43 @@ int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const
     l.A = ws + w.dp; l.B = W_gu; l.b_mn = 1; l.C = dx; l.M = T; l.N = d; l.K = 2 * H; l.act = GROUTER_ACT_NONE; l.status = status;
     if (launch_product(l, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
-  if (dW_gu && launch_weight_gradient(ws + w.dp, x, T, d, 2 * H, dW_gu, dW_dtype, ws + w.pieces, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-  if (dW_d && launch_weight_gradient(dy, ws + w.h, T, H, d, dW_d, dW_dtype, ws + w.pieces, status, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  // The three products read what the first kernel wrote and nothing of one another: each works beside the end of the one before it, whose
+  // last round leaves pairs of SMs idle (4095 x 1024, hidden 2816: 64, 88 and 44 tiles for 74 pairs).  The first of them waits for the
+  // kernel before it at its start, as the others rely on.
+  bool beside = dx != nullptr;
+  if (dW_gu) {
+    if (launch_weight_product(ws + w.dp, x, T, d, 2 * H, dW_gu, dW_dtype, ws + w.pieces_gu, status, beside, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    beside = true;
+  }
+  if (dW_d && launch_weight_product(dy, ws + w.h, T, H, d, dW_d, dW_dtype, ws + w.pieces_d, status, beside, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (dW_gu && launch_weight_sum(T, d, 2 * H, dW_gu, dW_dtype, ws + w.pieces_gu, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  if (dW_d && launch_weight_sum(T, H, d, dW_d, dW_dtype, ws + w.pieces_d, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   return GROUTER_OK;
 }
 
-int grouter_linear_fp8_fwd(const void* x, const void* x_scales, const void* W, const void* W_scales, const void* bias, const void* residual, int32_t T,
-                           int32_t K, int32_t N, void* y, int32_t* status, void* stream) {
+size_t grouter_linear_fp8_fwd_workspace_bytes(int32_t T, int32_t K) {
+  return T < 0 || K < 1 ? 0 : fp8_input(T, K).bytes;
+}
+
+int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W, const void* W_scales, const void* bias,
+                           const void* residual, int32_t T, int32_t K, int32_t N, void* y, void* workspace, int32_t* status, void* stream) {
   if (const int e = fp8_check(T, K, N)) return e;
-  if (!W || !W_scales || !status || (T > 0 && (!x || !x_scales || !y))) return GROUTER_ERR_INVALID_ARG;
-  if (!aligned_to(x, 16) || !aligned_to(x_scales, 16) || !aligned_to(W, 16) || !aligned_to(W_scales, 16) || !aligned_to(bias, 16) ||
-      !aligned_to(residual, 16) || !aligned_to(y, 16) || !aligned_to(status, 4))
+  if (!W || !W_scales || !status || (T > 0 && (!x || !y || (!x_scales && (!workspace || ldx < K))))) return GROUTER_ERR_INVALID_ARG;
+  if (!aligned_to(x, x_scales ? 16 : 2) || !aligned_to(x_scales, 16) || !aligned_to(W, 16) || !aligned_to(W_scales, 16) || !aligned_to(bias, 16) ||
+      !aligned_to(residual, 16) || !aligned_to(y, 16) || !aligned_to(workspace, 256) || !aligned_to(status, 4))
     return GROUTER_ERR_MISALIGNED;
   if (T == 0) return GROUTER_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Fp8Operand in{x, x_scales};
+  if (!x_scales) {
+    char* ws = static_cast<char*>(workspace);
+    in = {ws, ws + fp8_input(T, K).scales};
+    if (launch_quantize(x, ldx, GROUTER_BF16, T, K, false, ws, ws + fp8_input(T, K).scales, nullptr, nullptr, nullptr, st) != cudaSuccess)
+      return GROUTER_ERR_CUDA;
+  }
   Fp8Gemm g{};
-  g.A = {x, x_scales}; g.B = {W, W_scales}; g.bias = bias; g.residual = residual; g.C = y; g.M = T; g.N = N; g.K = K; g.status = status;
-  return fp8_product(g, static_cast<cudaStream_t>(stream)) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
+  g.A = in; g.B = {W, W_scales}; g.bias = bias; g.residual = residual; g.C = y; g.M = T; g.N = N; g.K = K; g.status = status;
+  return fp8_product(g, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N) {
@@ -201,25 +233,37 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
   }
   if (dW) {
     g.A = {ws + w.cols, ws + w.col_scales}; g.B = {xt, xt_scales}; g.C = dW; g.M = N; g.N = K; g.K = T; g.out_f32 = dW_dtype == GROUTER_F32;
-    if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    g.waits_at_end = dx != nullptr;          // of dx's product, which waited for the codes, it needs nothing
+    if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   return GROUTER_OK;
 }
 
-int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, const void* W_g, const void* W_g_scales, const void* W_u, const void* W_u_scales,
-                              const void* W_d, const void* W_d_scales, const void* residual, int32_t T, int32_t d, int32_t H, int32_t act, void* h,
-                              void* h_scales, void* y, int32_t* status, void* stream) {
+size_t grouter_gated_ffn_fp8_fwd_workspace_bytes(int32_t T, int32_t d, int32_t H) {
+  return T < 0 || d < 1 || H < 1 ? 0 : fp8_input(T, d).bytes + fp8_input(T, H).bytes;
+}
+
+int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W_g, const void* W_g_scales, const void* W_u,
+                              const void* W_u_scales, const void* W_d, const void* W_d_scales, const void* residual, int32_t T, int32_t d, int32_t H,
+                              int32_t act, void* y, void* workspace, int32_t* status, void* stream) {
   if (const int e = gated_check(T, d, H, act)) return e;
   if (fp8_check(T, d, H) || fp8_check(T, H, d)) return GROUTER_ERR_UNSUPPORTED;
-  if (!W_g || !W_g_scales || !W_u || !W_u_scales || !W_d || !W_d_scales || !status || (T > 0 && (!x || !x_scales || !h || !h_scales || !y)))
+  if (!W_g || !W_g_scales || !W_u || !W_u_scales || !W_d || !W_d_scales || !status || (T > 0 && (!x || !y || !workspace || (!x_scales && ldx < d))))
     return GROUTER_ERR_INVALID_ARG;
-  for (const void* q : {x, x_scales, W_g, W_g_scales, W_u, W_u_scales, W_d, W_d_scales, residual, (const void*)h, (const void*)h_scales, (const void*)y})
+  for (const void* q : {x_scales ? x : nullptr, x_scales, W_g, W_g_scales, W_u, W_u_scales, W_d, W_d_scales, residual, (const void*)y})
     if (!aligned_to(q, 16)) return GROUTER_ERR_MISALIGNED;
-  if (!aligned_to(status, 4)) return GROUTER_ERR_MISALIGNED;
+  if (!aligned_to(x, 2) || !aligned_to(workspace, 256) || !aligned_to(status, 4)) return GROUTER_ERR_MISALIGNED;
   if (T == 0) return GROUTER_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  char *ws = static_cast<char*>(workspace), *h = ws + fp8_input(T, d).bytes, *h_scales = h + fp8_input(T, H).scales;
+  Fp8Operand in{x, x_scales};
+  if (!x_scales) {
+    in = {ws, ws + fp8_input(T, d).scales};
+    if (launch_quantize(x, ldx, GROUTER_BF16, T, d, false, ws, ws + fp8_input(T, d).scales, nullptr, nullptr, nullptr, st) != cudaSuccess)
+      return GROUTER_ERR_CUDA;
+  }
   Fp8Gemm g{};
-  g.A = {x, x_scales}; g.B = {W_g, W_g_scales}; g.B1 = {W_u, W_u_scales}; g.C = h; g.out_scales = h_scales; g.M = T; g.N = H; g.K = d; g.act = act;
+  g.A = in; g.B = {W_g, W_g_scales}; g.B1 = {W_u, W_u_scales}; g.C = h; g.out_scales = h_scales; g.M = T; g.N = H; g.K = d; g.act = act;
   g.status = status;
   if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   Fp8Gemm l{};

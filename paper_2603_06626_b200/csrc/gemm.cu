@@ -77,8 +77,8 @@ struct GemmParams {
   const int32_t* pad_begin;    // [E] first pad row of each expert's padded segment
   const void* gates;
   int32_t gate_is_f32;
-  const __nv_bfloat16* in_G;   // DH, GLU_BACK (where rows of G and U are 2F elements apart)
-  const __nv_bfloat16* in_U;   // DH, GLU_BACK
+  const __nv_bfloat16* in_G;   // DH
+  const __nv_bfloat16* in_U;   // DH
   const __nv_bfloat16* bias;   // LINEAR: [N] or null
   const __nv_bfloat16* residual;   // LINEAR: [M, N] or null
   int32_t act;                 // LINEAR, GLU, GLU_BACK: GROUTER_ACT_*
@@ -88,11 +88,20 @@ struct GemmParams {
   unsigned int* tile_counter;  // device scalar, zero at launch (unused by DENSE, which has no context to keep one)
   unsigned long long* cycles;  // null, or GEMM_CYCLE_COUNTERS counters every issuer adds its account to
   unsigned long long wait_limit_ns;   // how long any one wait (barrier, tile queue) may last before the CTA gives up
+  // DENSE, LINEAR: nothing of the kernel before this one on the stream is read, and nothing it reads is written: this kernel works beside its
+  // end and waits for it before it ends itself.  The kernel before must have waited for its own predecessors before it let this one start.
+  int32_t waits_at_end;
 };
 
 constexpr int RASTER_ROWS = 8;
 
 // Products of plain matrices: no plan, and no context to keep a tile counter in.
+// GLU_BACK keeps one stage less: its epilogue warps have saved activations on their way into shared memory as well.
+__host__ __device__ constexpr int stages_of(int mode) { return mode == MODE_GLU_BACK ? STAGES - 1 : STAGES; }
+constexpr int GB_BLOCK = 32 * 64;               // one block there: 32 rows x 32 columns
+constexpr int GB_SET = 3 * GB_BLOCK;            // G, U and H of a chunk; two sets per epilogue warp
+static_assert(STAGE_BYTES + EPI_WARPS * 2 * EPI_STAGE_BYTES == EPI_WARPS * 2 * GB_SET, "what the stage left goes to the epilogue");
+
 __host__ __device__ constexpr bool is_plain(int mode) { return mode == MODE_DENSE || mode == MODE_LINEAR || mode == MODE_GLU || mode == MODE_GLU_BACK; }
 
 struct Tile {     // one CTA's share of a pair tile
@@ -238,36 +247,37 @@ template <int MODE, bool A_MN, bool B_MN, bool COUNT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
 grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                     const __grid_constant__ CUtensorMap tmC0, const __grid_constant__ CUtensorMap tmC1,
-                    const __grid_constant__ CUtensorMap tmC2, const GemmParams p) {
+                    const __grid_constant__ CUtensorMap tmC2, const __grid_constant__ CUtensorMap tmD, const GemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   // The dynamic shared memory starts at the same offset in both CTAs of the pair, so every address derived
   // below names the same location in either CTA (the MMA descriptors and multicast commits rely on that).
   const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t stage_base = smem_base + STAGES * STAGE_BYTES;          // epilogue staging, 2 x 4 KB per warp
-  const uint32_t bar_base = stage_base + EPI_WARPS * 2 * EPI_STAGE_BYTES;
-  // barriers (8 bytes each): full[STAGES], empty[STAGES], tmem_full[2], tmem_empty[2]; then the tile queue's slots
+  constexpr int NS = stages_of(MODE);
+  const uint32_t stage_base = smem_base + NS * STAGE_BYTES;              // epilogue staging, 2 x 4 KB per warp (GLU_BACK: 2 x 6 KB)
+  const uint32_t bar_base = smem_base + STAGES * STAGE_BYTES + EPI_WARPS * 2 * EPI_STAGE_BYTES;
+  // barriers (8 bytes each): full[NS], empty[NS], tmem_full[2], tmem_empty[2]; then the tile queue's slots
   //   full[s]       leader only: one arrival (leader's producer, with the byte count of BOTH CTAs' loads)
   //   empty[s]      each CTA: one arrival per round, delivered to both CTAs by the leader's multicast commit
   //   tmem_full[a]  each CTA: one arrival per tile, delivered to both CTAs by the leader's multicast commit
   //   tmem_empty[a] leader only: 2 * EPI_WARPS arrivals, one per epilogue warp of either CTA
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
-  auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + a); };
-  auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + 2 + a); };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (NS + s); };
+  auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * NS + a); };
+  auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * NS + 2 + a); };
   // Tile queue (all modes but those on plain matrices).  The pair takes its tiles from a grid-wide counter instead of a fixed stride: the
   // pairs then always work on neighbouring tiles of the list, whatever their individual pace, so the operand rows the
   // neighbours share are fetched from DRAM once.  The leader's producer draws the numbers (two tiles ahead, so the
   // round trip of the atomic is never waited for) and writes them into a ring of TQ 8-byte slots {sequence, tile} in
   // both CTAs; the other roles poll their CTA's copy: slot i % TQ holds the pair's i-th tile once its sequence word
   // reads i + 1.  Nobody acknowledges a slot, because nobody can fall TQ tiles behind: every tile passes at least one
-  // stage through the operand ring (the producer is at most STAGES tiles ahead of the issuer), and the issuer starts a
+  // stage through the operand ring (the producer is at most NS tiles ahead of the issuer), and the issuer starts a
   // tile only after every epilogue warp has finished the tile two before it, so the oldest number still unread is at
-  // most STAGES + 3 tiles older than the newest one written (STAGES + 4 <= TQ slots in use).
+  // most NS + 3 tiles older than the newest one written (NS + 4 <= TQ slots in use).
   constexpr bool PLAIN = is_plain(MODE);
   constexpr bool DYN = !PLAIN;
   constexpr int TQ = 16;
-  static_assert(STAGES + 4 <= TQ && (TQ & (TQ - 1)) == 0, "tile queue too short for the operand ring");
-  auto tq_slot = [&](int i) { return bar_base + 8u * (2 * STAGES + 4) + 8u * (uint32_t)(i & (TQ - 1)); };
+  static_assert(NS + 4 <= TQ && (TQ & (TQ - 1)) == 0, "tile queue too short for the operand ring");
+  auto tq_slot = [&](int i) { return bar_base + 8u * (2 * NS + 4) + 8u * (uint32_t)(i & (TQ - 1)); };
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
 
@@ -279,7 +289,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
   if (threadIdx.x == 0) {
     s_abort = 0;
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < NS; ++s) {
       ptx::mbar_init(full_bar(s), 1);
       ptx::mbar_init(empty_bar(s), 1);
     }
@@ -287,7 +297,10 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       ptx::mbar_init(tfull_bar(a), 1);
       ptx::mbar_init(tempty_bar(a), 2 * EPI_WARPS);
     }
-    for (int q = 0; q < TQ; ++q) ptx::st_shared_volatile_v2(tq_slot(q), 0u, 0u);   // sequence 0: nothing published
+    if (DYN)
+      for (int q = 0; q < TQ; ++q) ptx::st_shared_volatile_v2(tq_slot(q), 0u, 0u);   // sequence 0: nothing published
+    if (MODE == MODE_GLU_BACK)      // no queue: its place holds the barriers of the sets, two per epilogue warp
+      for (int q = 0; q < 2 * EPI_WARPS; ++q) ptx::mbar_init(tq_slot(q), 1);
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmA);
     ptx::prefetch_tensormap(&tmB);
@@ -306,7 +319,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   const uint32_t tmem_base = s_tmem_base;
   volatile int* abort_flag = &s_abort;
   if constexpr (PLAIN) {              // set up while the kernel before was still ending (launch_tc); from here on its results are read
-    after_previous_kernel();
+    if (!p.waits_at_end) after_previous_kernel();
     let_next_kernel_start();
   }
 
@@ -395,7 +408,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             ptx::tma_load_2d_pair(sb, &tmB, fb, ti.b_x, by, keep_b);                       // 2 x box {64 n, 64 k}
             ptx::tma_load_2d_pair(sb + ATOM_BYTES, &tmB, fb, ti.b_x + 64, by, keep_b);
           }
-          if (++s == STAGES) {
+          if (++s == NS) {
             s = 0;
             ph ^= 1u;
           }
@@ -412,9 +425,9 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         }
       }
       // every stage release the leader has multicast to this CTA must have landed before the CTA may exit
-      for (int i = 0; i < STAGES && !*abort_flag; ++i) {
+      for (int i = 0; i < NS && !*abort_flag; ++i) {
         if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
-        if (++s == STAGES) {
+        if (++s == NS) {
           s = 0;
           ph ^= 1u;
         }
@@ -475,7 +488,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           __syncwarp();
           a_lo += STAGE_BYTES >> 4;
           b_lo += STAGE_BYTES >> 4;
-          if (++s == STAGES) {
+          if (++s == NS) {
             s = 0;
             ph ^= 1u;
             a_lo = (uint32_t)da0;
@@ -538,11 +551,11 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         ptx::bulk_commit();
       }
     };
-    // DH, GLU_BACK: saved pre-activations G and U of one 32-column chunk of this thread's row (zeros beyond F)
+    // DH: saved pre-activations G and U of one 32-column chunk of this thread's row (zeros beyond F)
     auto load_gu = [&](const Tile& ti, int c, uint4 (&g4)[4], uint4 (&u4)[4]) {
       const int c0 = half * 128 + c * 32;
-      const int n_left = (PLAIN ? r < ti.m_valid : ti.m_valid > 0) ? ti.n_valid - c0 : 0;
-      const size_t gi = ((size_t)ti.row0 + r) * (PLAIN ? 2 * p.F : p.F) + ti.col0 + c0;
+      const int n_left = ti.m_valid > 0 ? ti.n_valid - c0 : 0;
+      const size_t gi = ((size_t)ti.row0 + r) * p.F + ti.col0 + c0;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if (q * 8 < n_left) {
@@ -563,6 +576,33 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       for (int q = 0; q < 4; ++q)
         q4[q] = q * 8 < n_left ? *reinterpret_cast<const uint4*>(p.residual + at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
     };
+    // GLU_BACK: G and U of 32 rows x 32 columns come by TMA into a set of blocks of this warp's own, dG and dU take their places there and
+    // H a third block.  The set of the next chunk is on its way while this one is worked on, the first two of a tile while the tile is
+    // multiplied (loaded row by row into registers, one chunk ahead, every chunk waited some 3000 cycles: 4095 x 1024, hidden 2816
+    // backward 173 us).  Chunks are numbered in the order of the warp's work; only those that hold results count.
+    const uint32_t gb_base = stage_base + (uint32_t)(warp - 2) * (2 * GB_SET);
+    int gb_next_t = pair_id, gb_next_c = 0, gb_i = 0;       // the chunk to be loaded next; chunks worked on so far
+    auto gb_live = [&](const Tile& ti, int c) { return ti.m_valid > quad * 32 && ti.n_valid > half * 128 + c * 32; };
+    auto gb_load = [&](int set) {
+      for (; gb_next_t < n_tiles; gb_next_t += n_pairs, gb_next_c = 0) {
+        const Tile ti = decode_tile<MODE>(p, gb_next_t, rank);
+        if (gb_next_c < 4 && gb_live(ti, gb_next_c)) {
+          if (lane == 0) {
+            const uint32_t to = gb_base + set * GB_SET, bar = tq_slot((warp - 2) * 2 + set);
+            const int x = ti.col0 + half * 128 + gb_next_c * 32, y = ti.row0 + quad * 32;
+            ptx::mbar_arrive_expect_tx(bar, 2 * GB_BLOCK);
+            ptx::tma_load_2d(to, &tmD, bar, x, y);
+            ptx::tma_load_2d(to + GB_BLOCK, &tmD, bar, p.F + x, y);
+          }
+          ++gb_next_c;
+          return;
+        }
+      }
+    };
+    if (MODE == MODE_GLU_BACK) {
+      gb_load(0);
+      gb_load(1);
+    }
     const uint32_t leader_tempty[2] = {ptx::map_to_cta(tempty_bar(0), 0), ptx::map_to_cta(tempty_bar(1), 0)};
     int acc = 0;
     uint32_t acc_ph = 0;
@@ -571,7 +611,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const Tile ti = decode_tile<MODE>(p, t, rank);
       const bool live = ti.m_valid > 0;    // false: this CTA only lent its half of B to the pair
       uint4 g4[4], u4[4];
-      if (MODE == MODE_DH || MODE == MODE_GLU_BACK) load_gu(ti, 0, g4, u4);   // in flight while the main loop of this tile finishes
+      if (MODE == MODE_DH) load_gu(ti, 0, g4, u4);   // in flight while the main loop of this tile finishes
       if (MODE == MODE_LINEAR && p.residual != nullptr) {
         load_residual(ti, 0, g4);
         load_residual(ti, 1, u4);
@@ -822,47 +862,48 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           stage_send_2d(sb, &tmC2, x, y0);
         }
       } else if (MODE == MODE_GLU_BACK) {
-        uint32_t ph[32];                   // H of a 64-column block, packed bf16 pairs
+        const uint32_t row_at = (uint32_t)lane * 64u, turn = (uint32_t)((lane >> 1) & 3);      // 64-byte rows, 64-byte swizzle
+        bool ok = true;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {                // four 32-column chunks; chunks 2c, 2c+1 fill one pair of blocks
-          const int cb = half * 128 + (c >> 1) * 64;
-          const int c0 = half * 128 + c * 32;
-          const bool any = ti.m_valid > quad * 32 && ti.n_valid - cb > 0;      // warp-uniform: the block holds results
-          uint4 cg[4], cu[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            cg[q] = g4[q];
-            cu[q] = u4[q];
-          }
-          if (c < 3) load_gu(ti, c + 1, g4, u4);     // next chunk's loads fly during this chunk's arithmetic
-          if (any) {
+        for (int c = 0; c < 4; ++c) {
+          if (gb_live(ti, c)) {                      // warp-uniform
+            const int set = gb_i & 1;
+            const uint32_t at = gb_base + set * GB_SET;
             uint32_t ra[32];
-            ptx::tmem_ld32(t_row + c0, ra);
+            ptx::tmem_ld32(t_row + half * 128 + c * 32, ra);
+            ok = ptx::mbar_wait_bounded_warp(tq_slot((warp - 2) * 2 + set), (uint32_t)(gb_i >> 1) & 1u, abort_flag, p.wait_limit_ns);
             ptx::tmem_ld_wait();
-            if ((c & 1) == 0) stage_wait_all();
+            if (!ok) break;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
+              const uint32_t unit = at + row_at + (((uint32_t)q ^ turn) << 4);
               float dh[8], g[8], u[8], h[8], dg[8], du[8];
-              unpack8(cg[q], g);
-              unpack8(cu[q], u);
+              unpack8(ptx::ld_shared_v4(unit), g);
+              unpack8(ptx::ld_shared_v4(unit + GB_BLOCK), u);
 #pragma unroll
               for (int i = 0; i < 8; ++i) dh[i] = __uint_as_float(ra[q * 8 + i]);
               gate_backward(dh, g, u, h, dg, du, p.act);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) ph[(c & 1) * 16 + q * 4 + i] = pack_bf16(h[2 * i], h[2 * i + 1]);
-              stage_put(blk_a, (c & 1) * 4 + q, pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]), pack_bf16(dg[4], dg[5]), pack_bf16(dg[6], dg[7]));
-              stage_put(blk_b, (c & 1) * 4 + q, pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]), pack_bf16(du[4], du[5]), pack_bf16(du[6], du[7]));
+              ptx::st_shared_v4(unit, pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]), pack_bf16(dg[4], dg[5]), pack_bf16(dg[6], dg[7]));
+              ptx::st_shared_v4(unit + GB_BLOCK, pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]), pack_bf16(du[4], du[5]), pack_bf16(du[6], du[7]));
+              ptx::st_shared_v4(unit + 2 * GB_BLOCK, pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]), pack_bf16(h[4], h[5]), pack_bf16(h[6], h[7]));
+              if (q == 1 && gb_i > 0) {              // the other set's stores, one chunk old, have been read: the next chunk takes its place
+                stage_wait_all();
+                gb_load(set ^ 1);
+              }
             }
-            if ((c & 1) == 1) {
-              stage_send_2d(blk_a, &tmC0, ti.col0 + cb, y0);   // dG: columns [0,F) of [dG|dU]
-              stage_send_2d(blk_b, &tmC1, ti.col0 + cb, y0);   // dU: columns [F,2F)
-              stage_wait_older();
-#pragma unroll
-              for (int q = 0; q < 8; ++q) stage_put(blk_a, q, ph[q * 4], ph[q * 4 + 1], ph[q * 4 + 2], ph[q * 4 + 3]);
-              stage_send_2d(blk_a, &tmC2, ti.col0 + cb, y0);
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              const int x = ti.col0 + half * 128 + c * 32;
+              ptx::tma_store_2d(&tmC0, at, x, y0, stream_out);                     // dG: columns [0,F) of [dG|dU]
+              ptx::tma_store_2d(&tmC1, at + GB_BLOCK, x, y0, stream_out);          // dU: columns [F,2F)
+              ptx::tma_store_2d(&tmC2, at + 2 * GB_BLOCK, x, y0, stream_out);      // H
+              ptx::bulk_commit();
             }
+            ++gb_i;
           }
         }
+        if (!ok) break;
       } else {  // WGRAD_D, WGRAD_GU, DENSE: fp32 tile straight from TMEM to global memory (stored, or added for a partial sum)
         if (ti.m_valid > quad * 32 && (have_acc || !ti.add)) {
 #pragma unroll
@@ -921,6 +962,9 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // give copies and barrier arrivals still in flight towards either CTA's shared memory time to land
     const uint64_t t0 = ptx::globaltimer_ns();
     while (ptx::globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+  }
+  if constexpr (PLAIN) {
+    if (p.waits_at_end) after_previous_kernel();
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -983,7 +1027,7 @@ bool make_tile_map(CUtensorMap* tm, CUtensorMapDataType type, int element_bytes,
 }
 
 struct Maps {
-  CUtensorMap A, B, C0, C1, C2;
+  CUtensorMap A, B, C0, C1, C2, D;      // D: GLU_BACK
 };
 
 template <int MODE, bool A_MN, bool B_MN, bool COUNT>
@@ -999,8 +1043,8 @@ static cudaError_t launch_tc(const Maps& m, const GemmParams& p, int grid, cudaS
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   if constexpr (is_plain(MODE))
-    return launch_dependent(kern, dim3(grid), dim3(GEMM_THREADS), GEMM_SMEM, st, m.A, m.B, m.C0, m.C1, m.C2, p);
-  kern<<<grid, GEMM_THREADS, GEMM_SMEM, st>>>(m.A, m.B, m.C0, m.C1, m.C2, p);
+    return launch_dependent(kern, dim3(grid), dim3(GEMM_THREADS), GEMM_SMEM, st, m.A, m.B, m.C0, m.C1, m.C2, MODE == MODE_GLU_BACK ? m.D : m.A, p);
+  kern<<<grid, GEMM_THREADS, GEMM_SMEM, st>>>(m.A, m.B, m.C0, m.C1, m.C2, m.A, p);
   return cudaGetLastError();
 }
 
@@ -1185,8 +1229,9 @@ static int plain_grid(int64_t tiles) {
 }
 
 cudaError_t launch_dense_gemm(const void* A, int a_mn, const void* B, int b_mn, float* C, int M, int N, int K, int k_chunk, int32_t* status,
-                              cudaStream_t st) {
+                              cudaStream_t st, bool waits_at_end) {
   GemmParams p{};
+  p.waits_at_end = waits_at_end;
   p.M = M; p.N = N; p.K = K;
   p.k_chunk = k_chunk;
   p.tiles_m = cdiv(M, PM);
@@ -1216,6 +1261,7 @@ cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st) {
   p.residual = static_cast<const __nv_bfloat16*>(g.residual);
   p.act = g.act;
   p.save_pre = g.pre != nullptr;
+  p.waits_at_end = g.waits_at_end;
   p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
   Maps m;
   const bool ok = (g.a_mn ? make_map(&m.A, g.A, g.K, g.M, 64) : make_map(&m.A, g.A, g.M, g.K, 128)) &&
@@ -1250,11 +1296,12 @@ cudaError_t launch_gated_gemm(const GatedGemm& g, cudaStream_t st) {
     return launch_t<MODE_GLU, false, false>(m, p, plain_grid((int64_t)p.tiles_m * p.tiles_n), st);
   }
   p.tiles_n = cdiv(g.H, BN);
-  p.in_G = pre;
-  p.in_U = pre + H;
   __nv_bfloat16* dpre = static_cast<__nv_bfloat16*>(g.dpre);
-  ok = ok && make_map(&m.B, g.W, g.K, H, 64) && make_map(&m.C0, dpre, g.T, H, 32, 2 * H) && make_map(&m.C1, dpre + H, g.T, H, 32, 2 * H) &&
-       make_map(&m.C2, g.h, g.T, H, 32);
+  auto block_map = [&](CUtensorMap* tm, const void* base, uint64_t cols, uint64_t pitch) {
+    return make_tile_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, g.T, cols, pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  };
+  ok = ok && make_map(&m.B, g.W, g.K, H, 64) && block_map(&m.C0, dpre, H, 2 * H) && block_map(&m.C1, dpre + H, H, 2 * H) &&
+       block_map(&m.C2, g.h, H, H) && block_map(&m.D, pre, 2 * H, 2 * H);
   if (!ok) return cudaErrorInvalidValue;
   return launch_t<MODE_GLU_BACK, false, true>(m, p, plain_grid((int64_t)p.tiles_m * p.tiles_n), st);
 }

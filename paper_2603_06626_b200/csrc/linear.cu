@@ -196,23 +196,33 @@ size_t weight_gradient_bytes(int T, int K, int N) {
   return s > 1 ? up256((size_t)s * N * K * 4) : 0;
 }
 
-cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
-                                   cudaStream_t st) {
+cudaError_t launch_weight_product(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
+                                  bool waits_at_end, cudaStream_t st) {
   const int count = dw_pieces(T, K, N);
   if (count == 1 && dW_dtype == GROUTER_BF16) {
     LinearGemm g{};
     g.A = dz; g.a_mn = 1; g.B = x; g.b_mn = 1; g.C = dW; g.M = N; g.N = K; g.K = T; g.act = GROUTER_ACT_NONE; g.status = status;
+    g.waits_at_end = waits_at_end;
     return launch_linear_gemm(g, st);
   }
-  float* out = static_cast<float*>(count == 1 ? dW : pieces);
-  const int chunk = dw_chunk(T, count);
-  if (const cudaError_t e = launch_dense_gemm(dz, 1, x, 1, out, N, K, T, chunk, status, st)) return e;
+  return launch_dense_gemm(dz, 1, x, 1, static_cast<float*>(count == 1 ? dW : pieces), N, K, T, dw_chunk(T, count), status, st, waits_at_end);
+}
+
+cudaError_t launch_weight_sum(int T, int K, int N, void* dW, int dW_dtype, const void* pieces, cudaStream_t st) {
+  const int count = dw_pieces(T, K, N);
   if (count == 1) return cudaSuccess;
+  const float* in = static_cast<const float*>(pieces);
   const int64_t n4 = (int64_t)N * K / 4, want = (n4 + 255) / 256, cap = (int64_t)current_sms() * 8;
-  const int grid = (int)(want < cap ? want : cap), real = cdiv(T, chunk);      // whole 64-token steps may leave the last piece out
-  return dW_dtype == GROUTER_F32 ? launch_dependent(sum_pieces_kernel<float>, dim3(grid), dim3(256), 0, st, out, real, n4, static_cast<float*>(dW))
-                                 : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, out, real, n4,
+  const int grid = (int)(want < cap ? want : cap), real = cdiv(T, dw_chunk(T, count));      // whole 64-token steps may leave the last piece out
+  return dW_dtype == GROUTER_F32 ? launch_dependent(sum_pieces_kernel<float>, dim3(grid), dim3(256), 0, st, in, real, n4, static_cast<float*>(dW))
+                                 : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, in, real, n4,
                                                     static_cast<__nv_bfloat16*>(dW));
+}
+
+cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
+                                   cudaStream_t st) {
+  const cudaError_t e = launch_weight_product(dz, x, T, K, N, dW, dW_dtype, pieces, status, false, st);
+  return e != cudaSuccess ? e : launch_weight_sum(T, K, N, dW, dW_dtype, pieces, st);
 }
 
 }  // namespace grouter

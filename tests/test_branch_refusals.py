@@ -49,10 +49,12 @@ def test_eight_bits(lib):
     assert back(q=None) == back(s=None) == back(y=None) == back(ld=63) == back(dt=2) == INVALID
     assert back(q=A + 8) == back(y=A + 1) == MISALIGNED and back(rows=0, q=None, s=None, y=None) == OK
 
-    def fwd(x=A, xs=A, W=A, Ws=A, b=A, r=A, T=4, K=64, N=64, y=A, status=A):
-        return lib.grouter_linear_fp8_fwd(x, xs, W, Ws, b, r, T, K, N, y, status, None)
-    for name in ("x", "xs", "W", "Ws", "y", "status"):
+    def fwd(x=A, xs=A, ld=0, W=A, Ws=A, b=A, r=A, T=4, K=64, N=64, y=A, ws=None, status=A):
+        return lib.grouter_linear_fp8_fwd(x, xs, ld, W, Ws, b, r, T, K, N, y, ws, status, None)
+    for name in ("x", "W", "Ws", "y", "status"):
         assert fwd(**{name: None}) == INVALID, name
+    assert fwd(xs=None, ld=64) == fwd(xs=None, ld=63, ws=A) == INVALID and fwd(xs=None, ld=64, ws=A + 16) == fwd(xs=None, ld=64, ws=A, x=A + 1) == MISALIGNED
+    assert lib.grouter_linear_fp8_fwd_workspace_bytes(4, 64) >= 4 * 64 + 512 and lib.grouter_linear_fp8_fwd_workspace_bytes(-1, 64) == 0
     assert fwd(T=-1) == fwd(K=0) == fwd(N=0) == INVALID and fwd(N=12) == fwd(T=MOST) == UNSUPPORTED
     assert fwd(x=A + 8) == fwd(xs=A + 8) == fwd(b=A + 8) == fwd(r=A + 8) == fwd(y=A + 8) == MISALIGNED
     assert fwd(T=0, x=None, xs=None, y=None) == OK
@@ -84,12 +86,14 @@ def test_gated(lib):
     assert bwd(ws=A + 16) == bwd(dd=A + 8) == MISALIGNED
     assert lib.grouter_gated_ffn_bwd_workspace_bytes(4, 64, 12) == 0
 
-    def eight(x=A, xs=A, g=A, gs=A, u=A, us=A, dn=A, ds=A, r=A, T=4, d=64, H=64, act=2, h=A, hs=A, y=A, status=A):
-        return lib.grouter_gated_ffn_fp8_fwd(x, xs, g, gs, u, us, dn, ds, r, T, d, H, act, h, hs, y, status, None)
-    for name in ("x", "xs", "g", "gs", "u", "us", "dn", "ds", "h", "hs", "y", "status"):
+    def eight(x=A, xs=A, ld=0, g=A, gs=A, u=A, us=A, dn=A, ds=A, r=A, T=4, d=64, H=64, act=2, y=A, ws=A, status=A):
+        return lib.grouter_gated_ffn_fp8_fwd(x, xs, ld, g, gs, u, us, dn, ds, r, T, d, H, act, y, ws, status, None)
+    for name in ("x", "g", "gs", "u", "us", "dn", "ds", "y", "ws", "status"):
         assert eight(**{name: None}) == INVALID, name
-    assert eight(act=9) == INVALID and eight(d=12) == UNSUPPORTED and eight(hs=A + 8) == eight(y=A + 8) == eight(us=A + 1) == MISALIGNED
-    assert eight(T=0, x=None, xs=None, h=None, hs=None, y=None) == OK
+    assert eight(act=9) == eight(xs=None, ld=63) == INVALID and eight(d=12) == UNSUPPORTED
+    assert eight(ws=A + 16) == eight(y=A + 8) == eight(us=A + 1) == eight(xs=A + 8) == eight(xs=None, ld=64, x=A + 1) == MISALIGNED
+    assert eight(T=0, x=None, xs=None, ws=None, y=None) == OK
+    assert lib.grouter_gated_ffn_fp8_fwd_workspace_bytes(4, 64, 128) >= 4 * 192 + 1024
 
 
 def _raises(kind, call):
