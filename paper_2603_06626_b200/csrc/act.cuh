@@ -104,13 +104,5 @@ __device__ __forceinline__ void gate_back(const float (&dh)[N], const float (&g)
     du[i + 1] = o2.y;
   }
 }
-template <int N>
-__device__ __forceinline__ void gate_backward(const float (&dh)[N], const float (&g)[N], const float (&u)[N], float (&h)[N], float (&dg)[N], float (&du)[N],
-                                              int act) {
-  if (act == GROUTER_ACT_RELU) gate_back<GROUTER_ACT_RELU, N>(dh, g, u, h, dg, du);
-  else if (act == GROUTER_ACT_SILU) gate_back<GROUTER_ACT_SILU, N>(dh, g, u, h, dg, du);
-  else if (act == GROUTER_ACT_GELU) gate_back<GROUTER_ACT_GELU, N>(dh, g, u, h, dg, du);
-  else gate_back<GROUTER_ACT_NONE, N>(dh, g, u, h, dg, du);
-}
 
 }  // namespace grouter

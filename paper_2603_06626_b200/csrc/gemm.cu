@@ -32,6 +32,8 @@
 //
 // Every wait (mbarriers, tile queue) is bounded; on give-up the CTA raises an abort flag, ORs STATUS_TIMEOUT into the status
 // word, leaves its loops, and the pair meets at a cluster barrier before freeing TMEM and exiting.
+#include <type_traits>
+
 #include "act.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
@@ -584,6 +586,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     int gb_next_t = pair_id, gb_next_c = 0, gb_i = 0;       // the chunk to be loaded next; chunks worked on so far
     auto gb_live = [&](const Tile& ti, int c) { return ti.m_valid > quad * 32 && ti.n_valid > half * 128 + c * 32; };
     auto gb_load = [&](int set) {
+#pragma unroll 1
       for (; gb_next_t < n_tiles; gb_next_t += n_pairs, gb_next_c = 0) {
         const Tile ti = decode_tile<MODE>(p, gb_next_t, rank);
         if (gb_next_c < 4 && gb_live(ti, gb_next_c)) {
@@ -759,8 +762,13 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           p.out_f[(size_t)(nt * 2 + half) * p.R_pad_max + (size_t)ti.row0 + r] = dgate;
         }
       } else if (MODE == MODE_LINEAR) {
+        // four 32-column chunks; chunks 2c, 2c+1 fill one staging block.  The two blocks are a loop: few tiles go through it, and code that is
+        // run once is slow.
+#pragma unroll 1
+        for (int cp = 0; cp < 4; cp += 2)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {                // four 32-column chunks; chunks 2c, 2c+1 fill one staging block
+        for (int odd = 0; odd < 2; ++odd) {
+          const int c = cp + odd;
           const int cb = half * 128 + (c >> 1) * 64;
           const int c0 = half * 128 + c * 32;
           const int n_left = ti.n_valid - c0;
@@ -768,11 +776,11 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           uint4 res[4];
           if (p.residual != nullptr) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) res[q] = c & 1 ? u4[q] : g4[q];
-            if (c < 2) load_residual(ti, c + 2, c & 1 ? u4 : g4);      // two chunks ahead of the arithmetic
+            for (int q = 0; q < 4; ++q) res[q] = odd ? u4[q] : g4[q];
+            if (c < 2) load_residual(ti, c + 2, odd ? u4 : g4);      // two chunks ahead of the arithmetic
           }
           if (any) {
-            if ((c & 1) == 0) {
+            if (odd == 0) {
               if (p.save_pre) stage_wait_all();      // both blocks are written: y through one, A * B + bias through the other
               else { flip ^= 1u; stage_wait_older(); }
             }
@@ -794,7 +802,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 }
               }
             }
-            if (p.save_pre) stage_put_bf16(blk_b, (c & 1) * 4, v);
+            if (p.save_pre) stage_put_bf16(blk_b, odd * 4, v);
             if (p.act == GROUTER_ACT_RELU) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) v[i] = act_value<GROUTER_ACT_RELU>(v[i]);
@@ -814,66 +822,84 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 for (int i = 0; i < 8; ++i) v[q * 8 + i] += f[i];
               }
             }
-            stage_put_bf16(sb, (c & 1) * 4, v);
-            if ((c & 1) == 1) {
+            stage_put_bf16(sb, odd * 4, v);
+            if (odd == 1) {
               stage_send_2d(sb, &tmC0, ti.col0 + cb, y0);
               if (p.save_pre) stage_send_2d(blk_b, &tmC1, ti.col0 + cb, y0);
             }
           }
         }
       } else if (MODE == MODE_GLU) {
-        // accumulator columns as in UP: 0..127 = gate, 128..255 = up; this warp: 64 of each
-        if (ti.m_valid > quad * 32 && ti.n_valid - half * 64 > 0) {
-          const int x = ti.col0 + half * 64;
-          uint32_t ph[32];                 // H of the 64 columns, packed bf16 pairs
-#pragma unroll
-          for (int cc = 0; cc < 2; ++cc) {
+        // accumulator columns as in UP: 0..127 = gate, 128..255 = up; this warp: 64 of each, in two chunks of 32.  Chunks leave through blocks of
+        // 32 rows x 64 bytes (64-byte swizzle); the loop stays a loop, since few tiles go through it and code that is run once is slow.
+        const uint32_t row_at = blk_a + (uint32_t)lane * 64u, turn = (uint32_t)((lane >> 1) & 3);
+        if (ti.m_valid > quad * 32) {
+#pragma unroll 1
+          for (int c = 0; c < 2; ++c) {
+            const int c0 = half * 64 + c * 32;
+            if (ti.n_valid <= c0) break;             // warp-uniform
             uint32_t rg[32], ru[32];
-            ptx::tmem_ld32(t_row + half * 64 + cc * 32, rg);
-            ptx::tmem_ld32(t_row + 128 + half * 64 + cc * 32, ru);
+            ptx::tmem_ld32(t_row + c0, rg);
+            ptx::tmem_ld32(t_row + 128 + c0, ru);
             ptx::tmem_ld_wait();
-            float g[32], u[32];
+            float g[32];
+            uint32_t pg[16], pu[16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              g[i] = __uint_as_float(rg[i]);
-              u[i] = __uint_as_float(ru[i]);
-            }
-            if (p.save_pre) {
-              if (cc == 0) stage_wait_all();
-              stage_put_bf16(blk_a, cc * 4, g);
-              stage_put_bf16(blk_b, cc * 4, u);
+            for (int i = 0; i < 32; ++i) g[i] = __uint_as_float(rg[i]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              pg[i] = pack_bf16(g[2 * i], g[2 * i + 1]);
+              pu[i] = pack_bf16(__uint_as_float(ru[2 * i]), __uint_as_float(ru[2 * i + 1]));
             }
             act_values(g, p.act);
+            stage_wait_all();                        // the stores of the chunk before, which this one's arithmetic has given time
+            if (p.save_pre) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ph[cc * 16 + i] = pack_bf16(g[2 * i] * u[2 * i], g[2 * i + 1] * u[2 * i + 1]);
-          }
-          uint32_t sb = blk_a;
-          if (p.save_pre) {
-            stage_send_2d(blk_a, &tmC0, x, y0);
-            stage_send_2d(blk_b, &tmC1, x, y0);
-            stage_wait_older();            // block a has been read (the store of block b may still be reading)
-          } else {
-            flip ^= 1u;
-            sb = flip ? blk_a : blk_b;     // not the block of the previous store
-            stage_wait_older();
-          }
+              for (int q = 0; q < 4; ++q) {
+                ptx::st_shared_v4(row_at + (((uint32_t)q ^ turn) << 4), pg[q * 4], pg[q * 4 + 1], pg[q * 4 + 2], pg[q * 4 + 3]);
+                ptx::st_shared_v4(row_at + GB_BLOCK + (((uint32_t)q ^ turn) << 4), pu[q * 4], pu[q * 4 + 1], pu[q * 4 + 2], pu[q * 4 + 3]);
+              }
+            }
 #pragma unroll
-          for (int q = 0; q < 8; ++q) stage_put(sb, q, ph[q * 4], ph[q * 4 + 1], ph[q * 4 + 2], ph[q * 4 + 3]);
-          stage_send_2d(sb, &tmC2, x, y0);
+            for (int q = 0; q < 4; ++q) {
+              uint32_t h[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int k = q * 8 + 2 * i;
+                h[i] = pack_bf16(g[k] * __uint_as_float(ru[k]), g[k + 1] * __uint_as_float(ru[k + 1]));
+              }
+              ptx::st_shared_v4(row_at + 2 * GB_BLOCK + (((uint32_t)q ^ turn) << 4), h[0], h[1], h[2], h[3]);
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              if (p.save_pre) {
+                ptx::tma_store_2d(&tmC0, blk_a, ti.col0 + c0, y0, stream_out);
+                ptx::tma_store_2d(&tmC1, blk_a + GB_BLOCK, ti.col0 + c0, y0, stream_out);
+              }
+              ptx::tma_store_2d(&tmC2, blk_a + 2 * GB_BLOCK, ti.col0 + c0, y0, stream_out);
+              ptx::bulk_commit();
+            }
+          }
         }
       } else if (MODE == MODE_GLU_BACK) {
         const uint32_t row_at = (uint32_t)lane * 64u, turn = (uint32_t)((lane >> 1) & 3);      // 64-byte rows, 64-byte swizzle
         bool ok = true;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < 4; ++c) {
-          if (gb_live(ti, c)) {                      // warp-uniform
-            const int set = gb_i & 1;
-            const uint32_t at = gb_base + set * GB_SET;
-            uint32_t ra[32];
-            ptx::tmem_ld32(t_row + half * 128 + c * 32, ra);
-            ok = ptx::mbar_wait_bounded_warp(tq_slot((warp - 2) * 2 + set), (uint32_t)(gb_i >> 1) & 1u, abort_flag, p.wait_limit_ns);
-            ptx::tmem_ld_wait();
-            if (!ok) break;
+          if (!gb_live(ti, c)) break;                // warp-uniform, as are those after it
+          const int set = gb_i & 1;
+          const uint32_t at = gb_base + set * GB_SET;
+          uint32_t ra[32];
+          ptx::tmem_ld32(t_row + half * 128 + c * 32, ra);
+          ok = ptx::mbar_wait_bounded_warp(tq_slot((warp - 2) * 2 + set), (uint32_t)(gb_i >> 1) & 1u, abort_flag, p.wait_limit_ns);
+          ptx::tmem_ld_wait();
+          if (!ok) break;
+          if (gb_i > 0) {                            // the other set's stores have been read: the next chunk takes its place
+            stage_wait_all();
+            gb_load(set ^ 1);
+          }
+          auto chunk = [&](auto act) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const uint32_t unit = at + row_at + (((uint32_t)q ^ turn) << 4);
@@ -882,26 +908,26 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
               unpack8(ptx::ld_shared_v4(unit + GB_BLOCK), u);
 #pragma unroll
               for (int i = 0; i < 8; ++i) dh[i] = __uint_as_float(ra[q * 8 + i]);
-              gate_backward(dh, g, u, h, dg, du, p.act);
+              gate_back<decltype(act)::value, 8>(dh, g, u, h, dg, du);
               ptx::st_shared_v4(unit, pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]), pack_bf16(dg[4], dg[5]), pack_bf16(dg[6], dg[7]));
               ptx::st_shared_v4(unit + GB_BLOCK, pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]), pack_bf16(du[4], du[5]), pack_bf16(du[6], du[7]));
               ptx::st_shared_v4(unit + 2 * GB_BLOCK, pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]), pack_bf16(h[4], h[5]), pack_bf16(h[6], h[7]));
-              if (q == 1 && gb_i > 0) {              // the other set's stores, one chunk old, have been read: the next chunk takes its place
-                stage_wait_all();
-                gb_load(set ^ 1);
-              }
             }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              const int x = ti.col0 + half * 128 + c * 32;
-              ptx::tma_store_2d(&tmC0, at, x, y0, stream_out);                     // dG: columns [0,F) of [dG|dU]
-              ptx::tma_store_2d(&tmC1, at + GB_BLOCK, x, y0, stream_out);          // dU: columns [F,2F)
-              ptx::tma_store_2d(&tmC2, at + 2 * GB_BLOCK, x, y0, stream_out);      // H
-              ptx::bulk_commit();
-            }
-            ++gb_i;
+          };
+          if (p.act == GROUTER_ACT_SILU) chunk(std::integral_constant<int, GROUTER_ACT_SILU>{});
+          else if (p.act == GROUTER_ACT_GELU) chunk(std::integral_constant<int, GROUTER_ACT_GELU>{});
+          else if (p.act == GROUTER_ACT_RELU) chunk(std::integral_constant<int, GROUTER_ACT_RELU>{});
+          else chunk(std::integral_constant<int, GROUTER_ACT_NONE>{});
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int x = ti.col0 + half * 128 + c * 32;
+            ptx::tma_store_2d(&tmC0, at, x, y0, stream_out);                     // dG: columns [0,F) of [dG|dU]
+            ptx::tma_store_2d(&tmC1, at + GB_BLOCK, x, y0, stream_out);          // dU: columns [F,2F)
+            ptx::tma_store_2d(&tmC2, at + 2 * GB_BLOCK, x, y0, stream_out);      // H
+            ptx::bulk_commit();
           }
+          ++gb_i;
         }
         if (!ok) break;
       } else {  // WGRAD_D, WGRAD_GU, DENSE: fp32 tile straight from TMEM to global memory (stored, or added for a partial sum)
@@ -1286,20 +1312,20 @@ cudaError_t launch_gated_gemm(const GatedGemm& g, cudaStream_t st) {
   const uint64_t H = (uint64_t)g.H;
   Maps m;
   bool ok = make_map(&m.A, g.A, g.T, g.K, 128);
+  auto block_map = [&](CUtensorMap* tm, const void* base, uint64_t cols, uint64_t pitch) {
+    return make_tile_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, g.T, cols, pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  };
   if (!g.backward) {
     p.tiles_n = cdiv(g.H, BNH);
     p.save_pre = pre != nullptr;
-    ok = ok && make_map(&m.B, g.W, 2 * H, g.K, 128) && make_map(&m.C2, g.h, g.T, H, 32);
+    ok = ok && make_map(&m.B, g.W, 2 * H, g.K, 128) && block_map(&m.C2, g.h, H, H);
     m.C0 = m.C1 = m.C2;
-    if (pre) ok = ok && make_map(&m.C0, pre, g.T, H, 32, 2 * H) && make_map(&m.C1, pre + H, g.T, H, 32, 2 * H);
+    if (pre) ok = ok && block_map(&m.C0, pre, H, 2 * H) && block_map(&m.C1, pre + H, H, 2 * H);
     if (!ok) return cudaErrorInvalidValue;
     return launch_t<MODE_GLU, false, false>(m, p, plain_grid((int64_t)p.tiles_m * p.tiles_n), st);
   }
   p.tiles_n = cdiv(g.H, BN);
   __nv_bfloat16* dpre = static_cast<__nv_bfloat16*>(g.dpre);
-  auto block_map = [&](CUtensorMap* tm, const void* base, uint64_t cols, uint64_t pitch) {
-    return make_tile_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, g.T, cols, pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-  };
   ok = ok && make_map(&m.B, g.W, g.K, H, 64) && block_map(&m.C0, dpre, H, 2 * H) && block_map(&m.C1, dpre + H, H, 2 * H) &&
        block_map(&m.C2, g.h, H, H) && block_map(&m.D, pre, 2 * H, 2 * H);
   if (!ok) return cudaErrorInvalidValue;
