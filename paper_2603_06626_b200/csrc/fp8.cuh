@@ -18,6 +18,7 @@ namespace grouter {
 
 constexpr int FP8_BLOCK = 128;
 constexpr int FP8_ATOM = 512;
+constexpr int FP8_MAX_COLS = 1 << 27;        // longest row (columns are counted in 32 bits, a grid's y takes 65535 x 8 atoms of 512)
 
 __host__ __device__ inline int64_t fp8_atoms_across(int64_t cols) { return (cols + 4 * FP8_BLOCK - 1) / (4 * FP8_BLOCK); }
 __host__ __device__ inline int64_t fp8_pitch(int64_t cols) { return (cols + 15) / 16 * 16; }

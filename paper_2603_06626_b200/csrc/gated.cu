@@ -63,7 +63,7 @@ Fp8Input fp8_input(int T, int K) {
 
 int fp8_check(int32_t T, int32_t K, int32_t N) {
   if (T < 0 || K < 1 || N < 1) return GROUTER_ERR_INVALID_ARG;
-  if (N % 8 || !fits_int(T) || !fits_int(K) || !fits_int(N)) return GROUTER_ERR_UNSUPPORTED;
+  if (N % 8 || !fits_int(T) || K > FP8_MAX_COLS || N > FP8_MAX_COLS) return GROUTER_ERR_UNSUPPORTED;
   // the scales' atoms are counted in 32 bits
   const int64_t most = 1 << 30;
   if (((int64_t)T / 128 + 2) * fp8_atoms_across(K) > most || ((int64_t)N / 128 + 2) * fp8_atoms_across(K) > most) return GROUTER_ERR_UNSUPPORTED;
@@ -196,14 +196,14 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, con
 }
 
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N) {
-  if (fp8_check(T, K, N) != GROUTER_OK) return 0;
+  if (fp8_check(T, K, N) != GROUTER_OK || T > FP8_MAX_COLS) return 0;
   return fp8_workspace(T, N).bytes;
 }
 
 int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales, const void* Wt, const void* Wt_scales, int32_t T, int32_t K, int32_t N,
                            void* dx, void* dW, int32_t dW_dtype, float* db, void* workspace, int32_t* status, void* stream) {
   if (const int e = fp8_check(T, K, N)) return e;
-  if (K % 8) return GROUTER_ERR_UNSUPPORTED;
+  if (K % 8 || T > FP8_MAX_COLS) return GROUTER_ERR_UNSUPPORTED;
   if (!status || (!dx && !dW && !db) || (dW_dtype != GROUTER_BF16 && dW_dtype != GROUTER_F32)) return GROUTER_ERR_INVALID_ARG;
   if (T > 0 && (!dy || !workspace || (dx && (!Wt || !Wt_scales)) || (dW && (!xt || !xt_scales)))) return GROUTER_ERR_INVALID_ARG;
   if (!aligned_to(dy, 16) || !aligned_to(xt, 16) || !aligned_to(xt_scales, 16) || !aligned_to(Wt, 16) || !aligned_to(Wt_scales, 16) || !aligned_to(dx, 16) ||

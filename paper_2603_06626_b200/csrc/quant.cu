@@ -1,14 +1,13 @@
 // Matrices into 8 bits and back (the format is in fp8.cuh): codes of the rows, of the transposed matrix, or both from one reading.
 //
 // Bound by HBM (2 bytes in and one out an element, two out with the transposed codes) as long as an element costs no more than the 17
-// (rows) or 22 (both) instruction slots that its bytes leave it.  So bf16 stays in pairs: magnitudes are compared two to an instruction as
-// 16-bit integers (their order is that of the numbers), infinities and NaN are looked for in the maximum only, and two elements are scaled
-// and converted by one instruction each.
-//   Rows alone: sixteen lanes (f32: 32) hold a block of 128, four rows in flight a thread.
+// (rows) or 22 (both) instruction slots that its bytes leave it; so a lane takes sixteen neighbours, over which addresses, exponent and
+// shuffles are spread.  bf16 stays in pairs: magnitudes are compared two to an instruction as 16-bit integers (their order is that of the
+// numbers), infinities and NaN are looked for in the maximum only, and two elements are scaled and converted by one instruction each.
+//   Rows alone: eight lanes hold a block of 128, a warp four blocks (whose scales are one word) of four rows.
 //   Squares or transposed codes: a CTA takes a tile of 128 x 128, which is a block of every row, a block of every column and a whole
-//     square.  For the transposed codes it waits in shared memory and is read by columns: a lane takes four neighbouring rows of a word's
-//     columns (two of bf16), so that a column's codes leave as 128 bytes of a warp; words are permuted so that neither side meets
-//     conflicts it need not have.
+//     square.  For the transposed codes it waits in shared memory and is read by columns: a lane takes eight neighbouring rows of a word's
+//     columns (two of bf16), sixteen lanes hold a column; words are permuted so that these reads meet no conflicts.
 #include "fp8.cuh"
 #include "fp8_gemm.cuh"
 
@@ -67,102 +66,123 @@ __device__ __forceinline__ float2 word_pair(const uint32_t* w, int j) {
   else return make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
 }
 
-// 16 bytes of row r from column c on; zeros outside the matrix.
-template <typename T, bool VEC>
-__device__ __forceinline__ uint4 load_row(const QuantParams& p, int64_t r, int c) {
-  uint4 v = make_uint4(0u, 0u, 0u, 0u);
-  if (r >= p.rows) return v;
-  const T* at = static_cast<const T*>(p.x) + r * p.ldx + c;
-  if constexpr (VEC) {
-    if (c < p.cols) v = ld_stream16(at);
-  } else {
-    T* e = reinterpret_cast<T*>(&v);
-#pragma unroll
-    for (int i = 0; i < vec16<T>(); ++i)
-      if (c + i < p.cols) e[i] = at[i];
-  }
-  return v;
-}
+constexpr int Q_LANE = 16;                // neighbours a lane takes
+constexpr int Q_LANES = QT / Q_LANE;      // lanes that hold a block
+template <typename T>
+__host__ __device__ constexpr int q_words() { return Q_LANE * (int)sizeof(T) / 4; }
 
-// Codes and the scale of the block that LANES neighbouring lanes hold 16 bytes each of; top: a magnitude known beforehand (a square's).
-template <typename T, bool SQUARE>
-__device__ __forceinline__ void put_row(const QuantParams& p, const uint4& v, int64_t r, int c, bool square_inf, uint32_t square, int64_t pitch, int64_t across) {
-  constexpr int VE = vec16<T>(), LANES = QT / VE;
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t top = square;
-  bool inf = square_inf;
-  if (!SQUARE) {
-    top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = word_top<T>(top, w[i]);
-    top = lanes_top_bits<LANES>(top_of_word<T>(top));
-    inf = __any_sync(0xffffffffu, bits_not_finite(top));
-    if (inf) {
-      top = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = word_top_finite<T>(top, w[i]);
-      top = lanes_top_bits<LANES>(top_of_word<T>(top));
-    }
-  }
-  const uint32_t e = fp8_exponent(__uint_as_float(top));
-  const float2 inv = both(fp8_inverse(e));
-  if (r < p.rows && c < pitch) {
-    uint32_t q[VE / 4];
-#pragma unroll
-    for (int i = 0; i < VE / 4; ++i) {
-      if (inf) q[i] = fp8_pair<true>(word_pair<T>(w, 2 * i), inv) | fp8_pair<true>(word_pair<T>(w, 2 * i + 1), inv) << 16;
-      else q[i] = fp8_pair<false>(word_pair<T>(w, 2 * i), inv) | fp8_pair<false>(word_pair<T>(w, 2 * i + 1), inv) << 16;
-    }
-    uint8_t* to = p.codes + r * pitch + c;
-    if constexpr (VE == 8) *reinterpret_cast<uint2*>(to) = make_uint2(q[0], q[1]);
-    else *reinterpret_cast<uint32_t*>(to) = q[0];
-    if ((c & (QT - 1)) == 0) p.scales[fp8_scale_at(r, c / QT, across)] = (uint8_t)e;
-  }
-}
-
-// Codes of the rows alone.  A warp takes 512 bytes of four rows (bf16: two blocks a row), neighbouring warps neighbouring columns.
-constexpr int QR_ROWS = 4;
+// Sixteen elements of a row from column c on; zeros outside the matrix.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantParams p) {
+__device__ __forceinline__ void load_lane(const T* at, int c, int cols, bool row_there, uint32_t (&w)[q_words<T>()]) {
   constexpr int VE = vec16<T>();
-  const int64_t pitch = fp8_pitch(p.cols), across = fp8_atoms_across(p.cols);
-  const int64_t chunks = (pitch + 32 * VE - 1) / (32 * VE);              // of a row
-  const int64_t unit = (int64_t)blockIdx.x * (Q_THREADS / 32) + (threadIdx.x >> 5);
-  const int64_t r0 = unit / chunks * QR_ROWS;
-  const int c = (int)(unit % chunks) * (32 * VE) + (threadIdx.x & 31) * VE;
+#pragma unroll
+  for (int i = 0; i < Q_LANE / VE; ++i) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (VEC) {
+      if (row_there && c + i * VE < cols) v = ld_stream16(at + i * VE);
+    } else {
+      T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+      for (int k = 0; k < VE; ++k)
+        if (row_there && c + i * VE + k < cols) e[k] = at[i * VE + k];
+    }
+    w[4 * i] = v.x;
+    w[4 * i + 1] = v.y;
+    w[4 * i + 2] = v.z;
+    w[4 * i + 3] = v.w;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t lane_top(const uint32_t (&w)[q_words<T>()]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < q_words<T>(); ++i) top = word_top<T>(top, w[i]);
+  return top_of_word<T>(top);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t lane_top_finite(const uint32_t (&w)[q_words<T>()]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < q_words<T>(); ++i) top = word_top_finite<T>(top, w[i]);
+  return top_of_word<T>(top);
+}
+// Exponent + 127 of the block that Q_LANES neighbouring lanes hold; inf: some element of the warp is not finite.
+template <typename T>
+__device__ __forceinline__ uint32_t block_exponent(const uint32_t (&w)[q_words<T>()], bool& inf) {
+  uint32_t top = lanes_top_bits<Q_LANES>(lane_top<T>(w));
+  inf = __any_sync(0xffffffffu, bits_not_finite(top));
+  if (inf) top = lanes_top_bits<Q_LANES>(lane_top_finite<T>(w));
+  return fp8_exponent(__uint_as_float(top));
+}
+template <typename T, bool INF>
+__device__ __forceinline__ uint4 lane_codes(const uint32_t (&w)[q_words<T>()], float2 inv) {
+  uint32_t q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = fp8_pair<INF>(word_pair<T>(w, 2 * i), inv) | fp8_pair<INF>(word_pair<T>(w, 2 * i + 1), inv) << 16;
+  return make_uint4(q[0], q[1], q[2], q[3]);
+}
+
+// Where a warp of the kernels over rows works: four rows from r0 on, 512 columns (an atom's) from `chunk` on.  A block's eight warps are
+// 2^across_log2 beside one another, the others below.
+constexpr int QR_ROWS = 4;
+struct RowsPlace {
+  int r0, chunk;
+};
+__device__ __forceinline__ RowsPlace rows_place(int across_log2) {
+  const int warp = threadIdx.x >> 5, across = 1 << across_log2;
+  return {((int)blockIdx.x * ((Q_THREADS / 32) >> across_log2) + (warp >> across_log2)) * QR_ROWS, (int)blockIdx.y * across + (warp & (across - 1))};
+}
+
+// Codes of the rows alone.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantParams p, int across_log2) {
+  const RowsPlace at = rows_place(across_log2);
+  const int lane = threadIdx.x & 31, c = at.chunk * 4 * QT + lane * Q_LANE;
+  const int pitch = (int)fp8_pitch(p.cols), across = (int)fp8_atoms_across(p.cols);
   after_previous_kernel();
   let_next_kernel_start();
-  if (r0 >= p.rows) return;               // whole warps
-  uint4 v[QR_ROWS];
+  if (at.r0 >= p.rows || at.chunk >= across) return;             // whole warps
+  const T* x = static_cast<const T*>(p.x) + at.r0 * p.ldx + c;
+  uint32_t w[QR_ROWS][q_words<T>()];
 #pragma unroll
-  for (int n = 0; n < QR_ROWS; ++n) v[n] = load_row<T, VEC>(p, r0 + n, c);
+  for (int n = 0; n < QR_ROWS; ++n) load_lane<T, VEC>(x + n * p.ldx, c, p.cols, at.r0 + n < p.rows, w[n]);
+  uint8_t* to = p.codes + (int64_t)at.r0 * pitch + c;
+  uint8_t* scale = p.scales + fp8_scale_at(at.r0, 4 * at.chunk + lane / Q_LANES, across);      // of the rows below: 16 bytes on each
+  const bool here = c < pitch, says = here && (lane & (Q_LANES - 1)) == 0;
 #pragma unroll
-  for (int n = 0; n < QR_ROWS; ++n) put_row<T, false>(p, v[n], r0 + n, c, false, 0u, pitch, across);
+  for (int n = 0; n < QR_ROWS; ++n) {
+    bool inf;
+    const uint32_t e = block_exponent<T>(w[n], inf);
+    const float2 inv = both(fp8_inverse(e));
+    const uint4 q = inf ? lane_codes<T, true>(w[n], inv) : lane_codes<T, false>(w[n], inv);
+    if (at.r0 + n < p.rows) {
+      if (here) *reinterpret_cast<uint4*>(to + (int64_t)n * pitch) = q;
+      if (says) scale[16 * n] = (uint8_t)e;
+    }
+  }
 }
 
 template <typename T, bool VEC, bool SQUARE>
-__global__ void __launch_bounds__(Q_THREADS) quantize_tile_kernel(const QuantParams p) {
-  constexpr int VE = vec16<T>(), LANES = QT / VE;                        // elements an access, lanes a row
-  constexpr int STEP = Q_THREADS / LANES, NR = QT / STEP;                // rows a block at a time, times
-  constexpr int WORDS = QT * (int)sizeof(T) / 4;                         // of a tile row
-  extern __shared__ uint32_t s_tile[];    // [QT][WORDS], with transposed codes; word w of row r at w ^ (r / 4 % 32)
+__global__ void __launch_bounds__(Q_THREADS, sizeof(T) == 2 ? 4 : 2) quantize_tile_kernel(const QuantParams p) {
+  constexpr int W = q_words<T>(), STEP = Q_THREADS / Q_LANES, NR = QT / STEP;        // rows a block at a time, times
+  constexpr int WORDS = QT * (int)sizeof(T) / 4;                                     // of a tile row
+  extern __shared__ __align__(8) uint32_t s_tile[];    // [QT][WORDS], with transposed codes; word w of row r at w ^ (r / 8 * 2)
   __shared__ uint32_t s_top[2][Q_THREADS / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int sub = threadIdx.x / LANES, at = threadIdx.x % LANES;
-  const int64_t tr = blockIdx.x / p.tiles_c;
-  const int tc = (int)(blockIdx.x - tr * p.tiles_c);
-  const int64_t r0 = tr * QT;
-  const int c0 = tc * QT, c = c0 + at * VE;
+  const int sub = threadIdx.x / Q_LANES, at = threadIdx.x % Q_LANES;
+  const int tiles_c = (int)p.tiles_c, tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+  const int r0 = tr * QT, c0 = tc * QT, c = c0 + at * Q_LANE;
   after_previous_kernel();
   let_next_kernel_start();
-  uint4 v[NR];
+  uint32_t v[NR][W];
+  const T* x = static_cast<const T*>(p.x) + (int64_t)(r0 + sub) * p.ldx + c;
 #pragma unroll
-  for (int n = 0; n < NR; ++n) v[n] = load_row<T, VEC>(p, r0 + n * STEP + sub, c);
+  for (int n = 0; n < NR; ++n) load_lane<T, VEC>(x + n * STEP * p.ldx, c, p.cols, r0 + n * STEP + sub < p.rows, v[n]);
   uint32_t square = 0;
   bool square_inf = false;
   if (SQUARE) {
     auto block_top = [&](uint32_t t, int which) {
-      t = lanes_top_bits<32>(top_of_word<T>(t));
+      t = lanes_top_bits<32>(t);
       if (lane == 0) s_top[which][warp] = t;
       __syncthreads();
       t = s_top[which][0];
@@ -171,132 +191,157 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_tile_kernel(const QuantPar
       return t;
     };
 #pragma unroll
-    for (int n = 0; n < NR; ++n) square = word_top<T>(word_top<T>(word_top<T>(word_top<T>(square, v[n].x), v[n].y), v[n].z), v[n].w);
+    for (int n = 0; n < NR; ++n) square = max(square, lane_top<T>(v[n]));
     square = block_top(square, 0);
     square_inf = bits_not_finite(square);
     if (square_inf) {                     // the whole block alike
       square = 0;
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
-        square = word_top_finite<T>(word_top_finite<T>(word_top_finite<T>(word_top_finite<T>(square, v[n].x), v[n].y), v[n].z), v[n].w);
+      for (int n = 0; n < NR; ++n) square = max(square, lane_top_finite<T>(v[n]));
       square = block_top(square, 1);
     }
   }
   if (p.codes_t) {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      const int r = n * STEP + sub, turn = r >> 2;
+      const int r = n * STEP + sub, turn = (r >> 3) * 2;
       uint32_t* row = s_tile + r * WORDS;
-      row[(at * 4 + 0) ^ turn] = v[n].x;
-      row[(at * 4 + 1) ^ turn] = v[n].y;
-      row[(at * 4 + 2) ^ turn] = v[n].z;
-      row[(at * 4 + 3) ^ turn] = v[n].w;
+#pragma unroll
+      for (int i = 0; i < W; i += 2) *reinterpret_cast<uint2*>(row + ((at * W + i) ^ turn)) = make_uint2(v[n][i], v[n][i + 1]);
     }
   }
   if (p.codes) {
-    const int64_t pitch = fp8_pitch(p.cols), across = fp8_atoms_across(p.cols);
+    const int pitch = (int)fp8_pitch(p.cols);
+    const int64_t across = fp8_atoms_across(p.cols);
+    uint8_t* to = p.codes + (int64_t)(r0 + sub) * pitch + c;
+    uint8_t* scale = p.scales + (tr * across + (tc >> 2)) * FP8_ATOM + (tc & 3);
+    const bool here = c < pitch;
 #pragma unroll
-    for (int n = 0; n < NR; ++n) put_row<T, SQUARE>(p, v[n], r0 + n * STEP + sub, c, square_inf, square, pitch, across);
+    for (int n = 0; n < NR; ++n) {
+      const int r = n * STEP + sub;
+      bool inf = square_inf;
+      const uint32_t e = SQUARE ? fp8_exponent(__uint_as_float(square)) : block_exponent<T>(v[n], inf);
+      const float2 inv = both(fp8_inverse(e));
+      const uint4 q = inf ? lane_codes<T, true>(v[n], inv) : lane_codes<T, false>(v[n], inv);
+      if (r0 + r < p.rows && here) {
+        *reinterpret_cast<uint4*>(to + (int64_t)(n * STEP) * pitch) = q;
+        if (at == 0) scale[(r & 31) * 16 + (r >> 5) * 4] = (uint8_t)e;
+      }
+    }
   }
   if (p.codes_t) {
     __syncthreads();
-    constexpr int CPW = 4 / (int)sizeof(T);
-    const int64_t pitch = fp8_pitch(p.rows), across = fp8_atoms_across(p.rows);
-    const bool here = r0 + 4 * lane < pitch;
-#pragma unroll 4
-    for (int wc = warp; wc < WORDS; wc += Q_THREADS / 32) {
-      uint32_t q[4];
+    constexpr int CPW = 4 / (int)sizeof(T);             // columns of a word
+    const int64_t pitch = fp8_pitch(p.rows);
+    const int lr = lane & 15, side = lane >> 4;         // rows 8 lr .. 8 lr + 7 of the word beside
+    const bool here = r0 + 8 * lr < pitch;
+    const uint32_t* from = s_tile + 8 * lr * WORDS;
+    uint8_t* to = p.codes_t + c0 * pitch + r0 + 8 * lr;
+    uint8_t* scale = p.scales_t + (tc * fp8_atoms_across(p.rows) + (tr >> 2)) * FP8_ATOM + (tr & 3);
+#pragma unroll 2
+    for (int w2 = warp; w2 < WORDS / 2; w2 += Q_THREADS / 32) {
+      const int word = 2 * w2 + side;
+      uint32_t q[8], tops = 0;                          // tops: of the word's columns
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = s_tile[(4 * lane + i) * WORDS + (wc ^ lane)];
-      uint32_t word = 0;
+      for (int i = 0; i < 8; ++i) q[i] = from[i * WORDS + (word ^ (2 * lr))];
+      bool inf = square_inf;
       if (!SQUARE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) word = word_top<T>(word, q[i]);
+        for (int i = 0; i < 8; ++i) tops = word_top<T>(tops, q[i]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) tops = word_top<T>(tops, __shfl_xor_sync(0xffffffffu, tops, o));
+        inf = __any_sync(0xffffffffu, bits_not_finite(top_of_word<T>(tops)));
+        if (inf) {
+          tops = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) tops = word_top_finite<T>(tops, q[i]);
+#pragma unroll
+          for (int o = 8; o > 0; o >>= 1) tops = word_top<T>(tops, __shfl_xor_sync(0xffffffffu, tops, o));
+        }
       }
 #pragma unroll
       for (int j = 0; j < CPW; ++j) {
         auto half = [&](uint32_t w) { return sizeof(T) == 4 ? w : j == 0 ? w << 16 : w & 0xffff0000u; };
-        uint32_t top = square;
-        bool inf = square_inf;
-        if (!SQUARE) {
-          top = lanes_top_bits<32>(half(word));
-          inf = bits_not_finite(top);
-          if (inf) {
-            uint32_t some = 0;
+        float f[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) some = word_top_finite<float>(some, half(q[i]));
-            top = lanes_top_bits<32>(some);
-          }
-        }
-        float f[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(half(q[i]));
-        const uint32_t e = fp8_exponent(__uint_as_float(top));
+        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(half(q[i]));
+        const uint32_t e = fp8_exponent(__uint_as_float(SQUARE ? square : half(tops)));
         const float inv = fp8_inverse(e);
-        const int col = c0 + wc * CPW + j;
+        const int col = word * CPW + j;                 // within the tile
+        const bool column = c0 + col < p.cols;
         if (p.sums) {
-          const float sum = lanes_sum<32>((f[0] + f[1]) + (f[2] + f[3]));
-          if (lane == 0 && col < p.cols) p.sums[tr * p.cols + col] = sum;
+          const float sum = lanes_sum<16>(((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7])));
+          if (lr == 0 && column) p.sums[(int64_t)tr * p.cols + c0 + col] = sum;
         }
-        if (col < p.cols && here) {
-          *reinterpret_cast<uint32_t*>(p.codes_t + col * pitch + r0 + 4 * lane) = inf ? fp8_quad<true>(f, inv) : fp8_quad<false>(f, inv);
-          if (lane == 0) p.scales_t[fp8_scale_at(col, (int)tr, across)] = (uint8_t)e;
+        const uint2 codes = inf ? make_uint2(fp8_quad<true>(f, inv), fp8_quad<true>(f + 4, inv)) : make_uint2(fp8_quad<false>(f, inv), fp8_quad<false>(f + 4, inv));
+        if (column && here) {
+          *reinterpret_cast<uint2*>(to + col * pitch) = codes;
+          if (lr == 0) scale[(col & 31) * 16 + (col >> 5) * 4] = (uint8_t)e;
         }
       }
     }
   }
 }
 
-// A thread's codes fill one 16-byte store (eight to bf16, four to f32), four rows' worth of them in flight; where the output's rows are not
-// 16-byte aligned its elements are stored one by one.
+// Sixteen codes a lane, as quantize_rows_kernel; where the output's rows are not 16-byte aligned its elements are stored one by one.
 template <typename T>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int cols,
-                                                         int64_t ldy, bool vec, T* __restrict__ y) {
-  constexpr int VE = vec16<T>(), AHEAD = 4;
-  const int64_t pitch = fp8_pitch(cols), per_row = pitch / VE, total = per_row * rows, across = fp8_atoms_across(cols);
-  const int64_t step = (int64_t)gridDim.x * 256;
+__global__ void __launch_bounds__(Q_THREADS) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int cols,
+                                                               int64_t ldy, bool vec, int across_log2, T* __restrict__ y) {
+  constexpr int VE = vec16<T>();
+  const RowsPlace at = rows_place(across_log2);
+  const int lane = threadIdx.x & 31, c = at.chunk * 4 * QT + lane * Q_LANE;
+  const int pitch = (int)fp8_pitch(cols), across = (int)fp8_atoms_across(cols);
   after_previous_kernel();
   let_next_kernel_start();
-  for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += AHEAD * step) {
-    uint32_t w[AHEAD][VE / 4];
-    float s[AHEAD];
-    int64_t r[AHEAD];
-    int c[AHEAD];
+  if (at.r0 >= rows || c >= pitch) return;
+  const uint8_t* from = codes + (int64_t)at.r0 * pitch + c;
+  const uint8_t* scale = scales + fp8_scale_at(at.r0, 4 * at.chunk + lane / Q_LANES, across);
+  uint4 q[QR_ROWS];
+  float s[QR_ROWS];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int64_t i = i0 + k * step;
-      r[k] = i / per_row;
-      c[k] = (int)(i - r[k] * per_row) * VE;
-      if (i < total) {
-        const uint8_t* from = codes + r[k] * pitch + c[k];
-        if constexpr (VE == 8) *reinterpret_cast<uint2*>(w[k]) = __ldg(reinterpret_cast<const uint2*>(from));
-        else w[k][0] = __ldg(reinterpret_cast<const uint32_t*>(from));
-        s[k] = fp8_scale(__ldg(scales + fp8_scale_at(r[k], c[k] / FP8_BLOCK, across)));
-      }
+  for (int n = 0; n < QR_ROWS; ++n) {
+    if (at.r0 + n < rows) {
+      q[n] = ld_stream16(from + (int64_t)n * pitch);
+      s[n] = fp8_scale(__ldg(scale + 16 * n));
     }
+  }
+  T* to = y + at.r0 * ldy + c;
+  const bool whole = vec && c + Q_LANE <= cols;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      if (i0 + k * step >= total) break;
-      float f[VE];
+  for (int n = 0; n < QR_ROWS; ++n) {
+    if (at.r0 + n >= rows) break;
+    const uint32_t w[4] = {q[n].x, q[n].y, q[n].z, q[n].w};
+    float f[Q_LANE];
 #pragma unroll
-      for (int i = 0; i < VE; i += 2) {
-        const float2 t = mul2(fp8_values(w[k][i / 4] >> (8 * (i & 2))), both(s[k]));
-        f[i] = t.x;
-        f[i + 1] = t.y;
-      }
-      T* to = y + r[k] * ldy + c[k];
-      if (vec && c[k] + VE <= cols) {
-        st_pack<T, VE>(to, f);
-      } else {
+    for (int i = 0; i < Q_LANE; i += 2) {
+      const float2 t = mul2(fp8_values(w[i / 4] >> (8 * (i & 2))), both(s[n]));
+      f[i] = t.x;
+      f[i + 1] = t.y;
+    }
+    if (whole) {
 #pragma unroll
-        for (int i = 0; i < VE; ++i)
-          if (c[k] + i < cols) to[i] = from_f32<T>(f[i]);
-      }
+      for (int i = 0; i < Q_LANE; i += VE) st_pack<T, VE>(to + n * ldy + i, f + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < Q_LANE; ++i)
+        if (c + i < cols) to[n * ldy + i] = from_f32<T>(f[i]);
     }
   }
 }
 
 namespace {
+
+struct RowsGrid {
+  dim3 grid;
+  int across_log2;
+};
+RowsGrid rows_grid(int rows, int cols) {
+  const int chunks = (int)fp8_atoms_across(cols);
+  int l = 0;
+  while (l < 3 && (1 << l) < chunks) ++l;
+  const int64_t block_rows = ((Q_THREADS / 32) >> l) * QR_ROWS;
+  return {dim3((unsigned)((rows + block_rows - 1) / block_rows), (unsigned)((chunks + (1 << l) - 1) >> l)), l};
+}
 
 template <typename T, bool VEC, bool SQUARE>
 cudaError_t tile_launch(const QuantParams& p, cudaStream_t st) {
@@ -318,8 +363,8 @@ template <typename T, bool VEC>
 cudaError_t quantize_launch(const QuantParams& p, bool square, cudaStream_t st) {
   if (square) return tile_launch<T, VEC, true>(p, st);
   if (p.codes_t) return tile_launch<T, VEC, false>(p, st);
-  const int64_t chunks = (fp8_pitch(p.cols) + 32 * vec16<T>() - 1) / (32 * vec16<T>()), warps = ((int64_t)p.rows + QR_ROWS - 1) / QR_ROWS * chunks;
-  return launch_dependent(quantize_rows_kernel<T, VEC>, dim3((unsigned)((warps + Q_THREADS / 32 - 1) / (Q_THREADS / 32))), dim3(Q_THREADS), 0, st, p);
+  const RowsGrid g = rows_grid(p.rows, p.cols);
+  return launch_dependent(quantize_rows_kernel<T, VEC>, g.grid, dim3(Q_THREADS), 0, st, p, g.across_log2);
 }
 
 }  // namespace
@@ -357,7 +402,7 @@ size_t grouter_fp8_scale_bytes(int32_t rows, int32_t cols) {
 int grouter_quantize_fp8(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t cols, int32_t square, void* codes, void* scales,
                          void* codes_t, void* scales_t, void* stream) {
   if (rows < 0 || cols < 0 || ldx < cols || (dtype != GROUTER_BF16 && dtype != GROUTER_F32)) return GROUTER_ERR_INVALID_ARG;
-  if (rows > INT32_MAX - 256 || cols > INT32_MAX - 256) return GROUTER_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX - 256 || cols > FP8_MAX_COLS || (codes_t && rows > FP8_MAX_COLS)) return GROUTER_ERR_UNSUPPORTED;
   if (((int64_t)rows + 127) / 128 * (((int64_t)cols + 127) / 128) > INT32_MAX) return GROUTER_ERR_UNSUPPORTED;
   if ((!codes && !codes_t) || (codes && !scales) || (codes_t && !scales_t)) return rows && cols ? GROUTER_ERR_INVALID_ARG : GROUTER_OK;
   if (rows > 0 && cols > 0 && !x) return GROUTER_ERR_INVALID_ARG;
@@ -373,19 +418,19 @@ int grouter_quantize_fp8(const void* x, int64_t ldx, int32_t dtype, int32_t rows
 
 int grouter_dequantize_fp8(const void* codes, const void* scales, int32_t rows, int32_t cols, int64_t ldy, int32_t dtype, void* y, void* stream) {
   if (rows < 0 || cols < 0 || ldy < cols || (dtype != GROUTER_BF16 && dtype != GROUTER_F32)) return GROUTER_ERR_INVALID_ARG;
-  if (rows > INT32_MAX - 256 || cols > INT32_MAX - 256) return GROUTER_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX - 256 || cols > FP8_MAX_COLS) return GROUTER_ERR_UNSUPPORTED;
   if (rows == 0 || cols == 0) return GROUTER_OK;
   if (!codes || !scales || !y) return GROUTER_ERR_INVALID_ARG;
   if (!aligned_to(codes, 16) || !aligned_to(scales, 16) || !aligned_to(y, dtype == GROUTER_F32 ? 4 : 2)) return GROUTER_ERR_MISALIGNED;
-  const int64_t work = fp8_pitch(cols) / (dtype == GROUTER_F32 ? 4 : 8) * rows, want = (work + 255) / 256, cap = (int64_t)current_sms() * 8;
-  const dim3 grid((unsigned)(want < cap ? want : cap > 0 ? cap : 1));
+  const RowsGrid g = rows_grid(rows, cols);
   const bool vec = aligned_to(y, 16) && ldy % (dtype == GROUTER_F32 ? 4 : 8) == 0;
   const uint8_t *q = static_cast<const uint8_t*>(codes), *s = static_cast<const uint8_t*>(scales);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == GROUTER_F32
-          ? launch_dependent(dequantize_kernel<float>, grid, dim3(256), 0, st, q, s, rows, cols, ldy, vec, static_cast<float*>(y))
-          : launch_dependent(dequantize_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, q, s, rows, cols, ldy, vec, static_cast<__nv_bfloat16*>(y));
+          ? launch_dependent(dequantize_kernel<float>, g.grid, dim3(Q_THREADS), 0, st, q, s, rows, cols, ldy, vec, g.across_log2, static_cast<float*>(y))
+          : launch_dependent(dequantize_kernel<__nv_bfloat16>, g.grid, dim3(Q_THREADS), 0, st, q, s, rows, cols, ldy, vec, g.across_log2,
+                             static_cast<__nv_bfloat16*>(y));
   return e == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
