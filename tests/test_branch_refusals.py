@@ -174,3 +174,11 @@ def test_the_binding_checks_the_gated_blocks_arguments():
     _raises(ValueError, lambda: B.gated_ffn_fp8(x[:, :32], g, u, dn))
     _raises(TypeError, lambda: B.gated_ffn_fp8(x.float(), g, u, dn))
     _raises(ValueError, lambda: B.gated_ffn_fp8(x, g, u, dn, residual=x[:3]))
+
+
+def test_the_dense_block_names_the_size_it_refuses():
+    from paper_2603_06626_b200.dense import DenseBlock, Projection8
+    with pytest.raises(ValueError, match="hidden"):
+        DenseBlock(256, 200, device="cpu")
+    with pytest.raises(ValueError, match="n:"):
+        Projection8(256, 8, device="cpu")
