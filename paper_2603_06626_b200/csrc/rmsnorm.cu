@@ -179,7 +179,7 @@ struct RmsBackward {
 
 // Every thread copies its own elements of the coming rows into shared memory and reads back only those: the ring needs no barrier.
 // Rows that are not 16-byte aligned: plain loads, no ring.
-template <typename T, int VE, int TPR, bool DH>
+template <typename T, typename W, int VE, int TPR, bool DH>
 __global__ void __launch_bounds__(rms_backward_threads(TPR), rms_backward_per_sm(TPR)) rms_backward_kernel(const RmsBackward p) {
   constexpr int NV = RMS_EPT / VE, PAIRS = RMS_EPT / 2, NS = DH ? 3 : 2;
   constexpr int THREADS = rms_backward_threads(TPR), RPB = THREADS / TPR;
@@ -201,10 +201,7 @@ __global__ void __launch_bounds__(rms_backward_threads(TPR), rms_backward_per_sm
 #pragma unroll
       for (int i = 0; i < VE; ++i) t[i] = 0.f;
       const int c = (n * TPR + lane) * VE;
-      if (c < d) {
-        if (p.w_f32) load_weights<float, VE>(static_cast<const float*>(p.w), c, t);
-        else load_weights<__nv_bfloat16, VE>(static_cast<const __nv_bfloat16*>(p.w), c, t);
-      }
+      if (c < d) load_weights<W, VE>(static_cast<const W*>(p.w), c, t);
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
         const int k = n * VE + i;
@@ -345,11 +342,15 @@ int rms_tpr(int d) {
   while (tpr * RMS_EPT < d) tpr *= 2;
   return tpr;
 }
-// Blocks of the backward pass: enough to fill the GPU, no more than there are rows for.  Each leaves one partial row.
+// Blocks of the backward pass: each leaves a partial row, which has to be written and read again, so a block works on RMS_WALK rows before
+// every SM gets another one (1000 x 1024 bf16: 7.0 us, a row a block 9.4; 1001 x 1023 f32 8.9 and 10.0), and all SMs have equally many
+// (2000 x 2048 with 592 blocks 8.3 us, with 500 11.1).
+constexpr int RMS_WALK = 4;
 int rms_backward_blocks(int rows, int d) {
   const int tpr = rms_tpr(d), rpb = rms_backward_threads(tpr) / tpr;
   const int want = (rows + rpb - 1) / rpb, cap = current_sms() * rms_backward_per_sm(tpr);
-  return std::max(1, std::min(want, cap));
+  const int sms = std::max(1, current_sms()), a_sm = (want + RMS_WALK * sms - 1) / (RMS_WALK * sms);
+  return std::max(1, std::min({want, cap, a_sm * sms}));
 }
 
 template <typename T, int VE, int NP, int LANES, bool FP8>
@@ -396,13 +397,13 @@ cudaError_t forward_by_type(const RmsForward& a, bool fp8, cudaStream_t st) {
   return forward_by_width<T, 1, false>(a, st);
 }
 
-template <typename T, int VE, int TPR, bool DH>
+template <typename T, typename W, int VE, int TPR, bool DH>
 cudaError_t backward_launch(const RmsBackward& a, int blocks, cudaStream_t st) {
   constexpr int threads = rms_backward_threads(TPR);
   constexpr int ring = VE == vec16<T>() ? rms_ring(sizeof(T), TPR, DH) * (DH ? 3 : 2) * (RMS_EPT / VE) * threads * 16 : 0;
   constexpr int cols = threads * RMS_EPT * (int)sizeof(float);
   constexpr int smem = ring > cols ? ring : cols;      // up to 192 KB
-  auto kern = rms_backward_kernel<T, VE, TPR, DH>;
+  auto kern = rms_backward_kernel<T, W, VE, TPR, DH>;
   static bool configured[64] = {};                     // the opt-in is a per-device setting
   int dev = 0;
   cudaGetDevice(&dev);
@@ -414,22 +415,26 @@ cudaError_t backward_launch(const RmsBackward& a, int blocks, cudaStream_t st) {
   return launch_dependent(kern, dim3(blocks), dim3(threads), smem, st, a);
 }
 
-template <typename T, int VE, bool DH>
+template <typename T, typename W, int VE, bool DH>
 cudaError_t backward_by_width(const RmsBackward& a, int blocks, cudaStream_t st) {
   switch (rms_tpr(a.d)) {
-    case 8: return backward_launch<T, VE, 8, DH>(a, blocks, st);
-    case 16: return backward_launch<T, VE, 16, DH>(a, blocks, st);
-    case 32: return backward_launch<T, VE, 32, DH>(a, blocks, st);
-    case 64: return backward_launch<T, VE, 64, DH>(a, blocks, st);
-    case 128: return backward_launch<T, VE, 128, DH>(a, blocks, st);
-    case 256: return backward_launch<T, VE, 256, DH>(a, blocks, st);
-    case 512: return backward_launch<T, VE, 512, DH>(a, blocks, st);
-    default: return backward_launch<T, VE, 1024, DH>(a, blocks, st);
+    case 8: return backward_launch<T, W, VE, 8, DH>(a, blocks, st);
+    case 16: return backward_launch<T, W, VE, 16, DH>(a, blocks, st);
+    case 32: return backward_launch<T, W, VE, 32, DH>(a, blocks, st);
+    case 64: return backward_launch<T, W, VE, 64, DH>(a, blocks, st);
+    case 128: return backward_launch<T, W, VE, 128, DH>(a, blocks, st);
+    case 256: return backward_launch<T, W, VE, 256, DH>(a, blocks, st);
+    case 512: return backward_launch<T, W, VE, 512, DH>(a, blocks, st);
+    default: return backward_launch<T, W, VE, 1024, DH>(a, blocks, st);
   }
 }
-template <typename T, int VE>
+template <typename T, typename W, int VE>
 cudaError_t backward_by_stream(const RmsBackward& a, int blocks, cudaStream_t st) {
-  return a.dh ? backward_by_width<T, VE, true>(a, blocks, st) : backward_by_width<T, VE, false>(a, blocks, st);
+  return a.dh ? backward_by_width<T, W, VE, true>(a, blocks, st) : backward_by_width<T, W, VE, false>(a, blocks, st);
+}
+template <typename T, int VE>
+cudaError_t backward_by_weights(const RmsBackward& a, int blocks, cudaStream_t st) {
+  return a.w_f32 ? backward_by_stream<T, float, VE>(a, blocks, st) : backward_by_stream<T, __nv_bfloat16, VE>(a, blocks, st);
 }
 template <typename T>
 cudaError_t backward_by_type(const RmsBackward& a, int blocks, cudaStream_t st) {
@@ -438,9 +443,9 @@ cudaError_t backward_by_type(const RmsBackward& a, int blocks, cudaStream_t st) 
     return a.d % ve == 0 && a.ldh % ve == 0 && aligned_to(a.h, b) && aligned_to(a.dy, b) && aligned_to(a.dh, b) && aligned_to(a.dx, b) &&
            aligned_to(a.w, wb);
   };
-  if (fits(vec16<T>())) return backward_by_stream<T, vec16<T>()>(a, blocks, st);
-  if (fits(2)) return backward_by_stream<T, 2>(a, blocks, st);
-  return backward_by_stream<T, 1>(a, blocks, st);
+  if (fits(vec16<T>())) return backward_by_weights<T, vec16<T>()>(a, blocks, st);
+  if (fits(2)) return backward_by_weights<T, 2>(a, blocks, st);
+  return backward_by_weights<T, 1>(a, blocks, st);
 }
 
 int rms_check(int32_t rows, int32_t d, int64_t ldx, int32_t dtype, int32_t w_dtype) {
