@@ -69,4 +69,80 @@ __device__ __forceinline__ float lanes_top(float v) {
   else return lanes_max<LANES>(v);
 }
 
+// ---- blocks as the quantizing kernels hold them: sixteen neighbours a lane, as they lie in memory, eight lanes a block ----
+// Magnitudes in progress: of one f32 (as itself) or of two bf16 (as 16-bit halves of a word).
+template <typename T>
+__device__ __forceinline__ uint32_t word_top(uint32_t top, uint32_t w) {
+  if constexpr (sizeof(T) == 4) return max(top, w & 0x7fffffffu);
+  else return __vmaxu2(top, w & 0x7fff7fffu);
+}
+// ... without what is not finite
+template <typename T>
+__device__ __forceinline__ uint32_t word_top_finite(uint32_t top, uint32_t w) {
+  if constexpr (sizeof(T) == 4) {
+    w &= 0x7fffffffu;
+    return w < 0x7f800000u ? max(top, w) : top;
+  } else {
+    w &= 0x7fff7fffu;
+    if ((w & 0xffffu) >= 0x7f80u) w &= 0xffff0000u;
+    if (w >= 0x7f800000u) w &= 0xffffu;
+    return __vmaxu2(top, w);
+  }
+}
+// the larger half of a pair, as the bits of an f32
+template <typename T>
+__device__ __forceinline__ uint32_t top_of_word(uint32_t top) {
+  if constexpr (sizeof(T) == 4) return top;
+  else return max(top << 16, top & 0xffff0000u);
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_top_bits(uint32_t v) {
+  if constexpr (LANES == 32) return __reduce_max_sync(0xffffffffu, v);
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ bool bits_not_finite(uint32_t top) { return top >= 0x7f800000u; }
+// Elements 2j and 2j + 1 of some words, as f32.
+template <typename T>
+__device__ __forceinline__ float2 word_pair(const uint32_t* w, int j) {
+  if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+  else return make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+}
+
+constexpr int Q_LANE = 16;                // neighbours a lane takes
+constexpr int Q_LANES = FP8_BLOCK / Q_LANE;      // lanes that hold a block
+template <typename T>
+__host__ __device__ constexpr int q_words() { return Q_LANE * (int)sizeof(T) / 4; }
+
+template <typename T>
+__device__ __forceinline__ uint32_t lane_top(const uint32_t (&w)[q_words<T>()]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < q_words<T>(); ++i) top = word_top<T>(top, w[i]);
+  return top_of_word<T>(top);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t lane_top_finite(const uint32_t (&w)[q_words<T>()]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < q_words<T>(); ++i) top = word_top_finite<T>(top, w[i]);
+  return top_of_word<T>(top);
+}
+// Exponent + 127 of the block that Q_LANES neighbouring lanes hold; inf: some element of the warp is not finite.
+template <typename T>
+__device__ __forceinline__ uint32_t block_exponent(const uint32_t (&w)[q_words<T>()], bool& inf) {
+  uint32_t top = lanes_top_bits<Q_LANES>(lane_top<T>(w));
+  inf = __any_sync(0xffffffffu, bits_not_finite(top));
+  if (inf) top = lanes_top_bits<Q_LANES>(lane_top_finite<T>(w));
+  return fp8_exponent(__uint_as_float(top));
+}
+template <typename T, bool INF>
+__device__ __forceinline__ uint4 lane_codes(const uint32_t (&w)[q_words<T>()], float2 inv) {
+  uint32_t q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = fp8_pair<INF>(word_pair<T>(w, 2 * i), inv) | fp8_pair<INF>(word_pair<T>(w, 2 * i + 1), inv) << 16;
+  return make_uint4(q[0], q[1], q[2], q[3]);
+}
+
 }  // namespace grouter

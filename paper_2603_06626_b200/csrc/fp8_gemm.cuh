@@ -10,6 +10,8 @@ struct Fp8Operand {
 // C [M,N] = A B^T + bias + residual, bf16 or f32; with B1: act(A B^T) (A B1^T) as codes C and out_scales.
 struct Fp8Gemm {
   Fp8Operand A, B, B1;
+  const void* x;                          // A as bf16, row t at x + t * ldx, instead of codes (launch_fp8_small, up to 16 rows); else null
+  int64_t ldx;
   const void *bias, *residual;            // bf16 or null
   void *C, *out_scales;
   int M, N, K, act, out_f32;

@@ -82,7 +82,8 @@ inline int log2_of(int s) { return s >= 8 ? 3 : s >= 4 ? 2 : s >= 2 ? 1 : 0; }
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int token_tile(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
 
-cudaError_t fp8_product(const Fp8Gemm& g, cudaStream_t st) {
+// A as codes, or (g.x) as bf16, which a kernel of its own puts into the place that g.A names unless the product can do it on the way.
+cudaError_t fp8_product(Fp8Gemm g, cudaStream_t st) {
   const bool glu = g.B1.codes != nullptr;
   const int sms = current_sms(), splits = fp8_small_splits(g.M, g.N, g.K, glu);
   const int64_t steps = cdiv(g.K, 128), ctas = cdiv(g.N, 128) * cdiv(g.M, 128) * splits;
@@ -91,7 +92,14 @@ cudaError_t fp8_product(const Fp8Gemm& g, cudaStream_t st) {
   const float small = glu ? rounds(ctas, sms) * (2.9f + 0.045f * token_tile(g.M) + 0.45f * cdiv(steps, splits) + 0.8f * log2_of(splits))
                           : rounds(ctas, 2 * sms) * (3.f + 0.48f * cdiv(steps, splits) + log2_of(splits));
   const bool fits = cdiv(g.M, 128) <= 65535;      // its grid has the token tiles in y
-  return !g.out_f32 && fits && small < tiles ? launch_fp8_small(g, splits, st) : launch_fp8_gemm(g, st);
+  const bool few = !g.out_f32 && fits && small < tiles;
+  if (g.x && !(few && g.M <= 16 && g.K % 8 == 0 && g.ldx % 8 == 0 && aligned_to(g.x, 16))) {
+    if (const cudaError_t e = launch_quantize(g.x, g.ldx, GROUTER_BF16, g.M, g.K, false, const_cast<void*>(g.A.codes), const_cast<void*>(g.A.scales),
+                                              nullptr, nullptr, nullptr, st))
+      return e;
+    g.x = nullptr;
+  }
+  return few ? launch_fp8_small(g, splits, st) : launch_fp8_gemm(g, st);
 }
 cudaError_t gated_product(const GatedGemm& g, cudaStream_t st) {
   const int sms = current_sms(), splits = gated_small_splits(g.T, g.H, g.K);
@@ -183,15 +191,15 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, con
     return GROUTER_ERR_MISALIGNED;
   if (T == 0) return GROUTER_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  Fp8Operand in{x, x_scales};
+  Fp8Gemm g{};
+  g.A = {x, x_scales};
   if (!x_scales) {
     char* ws = static_cast<char*>(workspace);
-    in = {ws, ws + fp8_input(T, K).scales};
-    if (launch_quantize(x, ldx, GROUTER_BF16, T, K, false, ws, ws + fp8_input(T, K).scales, nullptr, nullptr, nullptr, st) != cudaSuccess)
-      return GROUTER_ERR_CUDA;
+    g.A = {ws, ws + fp8_input(T, K).scales};
+    g.x = x;
+    g.ldx = ldx;
   }
-  Fp8Gemm g{};
-  g.A = in; g.B = {W, W_scales}; g.bias = bias; g.residual = residual; g.C = y; g.M = T; g.N = N; g.K = K; g.status = status;
+  g.B = {W, W_scales}; g.bias = bias; g.residual = residual; g.C = y; g.M = T; g.N = N; g.K = K; g.status = status;
   return fp8_product(g, st) == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
 
@@ -256,14 +264,14 @@ int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, 
   if (T == 0) return GROUTER_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char *ws = static_cast<char*>(workspace), *h = ws + fp8_input(T, d).bytes, *h_scales = h + fp8_input(T, H).scales;
-  Fp8Operand in{x, x_scales};
-  if (!x_scales) {
-    in = {ws, ws + fp8_input(T, d).scales};
-    if (launch_quantize(x, ldx, GROUTER_BF16, T, d, false, ws, ws + fp8_input(T, d).scales, nullptr, nullptr, nullptr, st) != cudaSuccess)
-      return GROUTER_ERR_CUDA;
-  }
   Fp8Gemm g{};
-  g.A = in; g.B = {W_g, W_g_scales}; g.B1 = {W_u, W_u_scales}; g.C = h; g.out_scales = h_scales; g.M = T; g.N = H; g.K = d; g.act = act;
+  g.A = {x, x_scales};
+  if (!x_scales) {
+    g.A = {ws, ws + fp8_input(T, d).scales};
+    g.x = x;
+    g.ldx = ldx;
+  }
+  g.B = {W_g, W_g_scales}; g.B1 = {W_u, W_u_scales}; g.C = h; g.out_scales = h_scales; g.M = T; g.N = H; g.K = d; g.act = act;
   g.status = status;
   if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   Fp8Gemm l{};

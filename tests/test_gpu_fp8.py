@@ -140,6 +140,23 @@ def test_rows_that_are_not_finite_stay_alone():
         assert torch.isnan(y[3]).all() and torch.equal(y[keep], clean[keep])
 
 
+@pytest.mark.parametrize("T", [1, 5, 8, 9, 16, 17, 40])
+@pytest.mark.parametrize("K,N,pad", [(8, 8, 0), (72, 264, 8), (520, 136, 0), (1000, 392, 24), (4096, 1032, 0), (2056, 64, 3)])
+def test_tokens_as_they_are_and_as_codes_give_the_same(T, K, N, pad):
+    """Few tokens are put into 8 bits on their way into the product, others by a kernel before it: the codes are the same ones."""
+    from paper_2603_06626_b200 import binding as B
+    rng = np.random.default_rng(T + K)
+    x = _rand(rng, T, K + pad)[:, :K]
+    x[T // 2, K // 2] = 0
+    if T > 4:
+        x[3, 1], x[2, K - 1], x[1, 0] = float("nan"), float("inf"), float("-inf")
+    W, b = B.quantize_fp8(_rand(rng, N, K, std=K ** -0.5), square=True)[0], _rand(rng, 1, N)[0]
+    y = B.linear_fp8(x, W, bias=b)
+    assert torch.equal(y.view(torch.int16), B.linear_fp8(B.quantize_fp8(x)[0], W, bias=b).view(torch.int16))
+    bad = torch.isnan(y).any(1).cpu()
+    assert bad[1:4].all() and int(bad.sum()) == 3 if T > 4 else not bad.any()
+
+
 def _backward(T, K, N, dtype=torch.bfloat16, bias=True):
     from paper_2603_06626_b200 import binding as B
     rng = np.random.default_rng(T + K + N)

@@ -210,6 +210,32 @@ def test_eight_bits_of_more_tiles_than_pairs():
     _eight(2600, 520, 1032, residual=True)
 
 
+@pytest.mark.parametrize("T", [1, 7, 16, 17, 300])
+def test_eight_bits_of_tokens_and_of_codes_are_the_same(T):
+    from paper_2603_06626_b200 import binding as B
+    rng = np.random.default_rng(T)
+    d, H = 1032, 264
+    x, (Wgu, Wd) = _bf(rng, T, d + 8)[:, :d], _weights(rng, d, H)
+    W8 = [B.quantize_fp8(W.contiguous(), square=True)[0] for W in (Wgu[:H], Wgu[H:], Wd)]
+    y = B.gated_ffn_fp8(x, *W8, act=B.ACT_GELU)
+    assert torch.equal(y, B.gated_ffn_fp8(B.quantize_fp8(x)[0], *W8, act=B.ACT_GELU))
+
+
+@pytest.mark.parametrize("T", [4, 300])
+def test_a_hidden_state_beyond_the_largest_number(T):
+    """g u overflows in one row: an infinity there has the code of NaN, the row's output is NaN and no other row's changes."""
+    from paper_2603_06626_b200 import binding as B
+    rng = np.random.default_rng(9)
+    Wgu, Wd = _weights(rng, 264, 200)
+    W8 = [B.quantize_fp8(W.contiguous(), square=True)[0] for W in (Wgu[:200], Wgu[200:], Wd)]
+    x = _bf(rng, T, 264)
+    clean = B.gated_ffn_fp8(x, *W8)
+    x[1] *= 2.0 ** 90
+    y = B.gated_ffn_fp8(x, *W8)
+    keep = torch.arange(T, device="cuda:0") != 1
+    assert torch.isnan(y[1]).all() and torch.equal(y[keep], clean[keep])
+
+
 def test_streams_and_graphs():
     from paper_2603_06626_b200 import binding as B
     rng = np.random.default_rng(7)
