@@ -225,6 +225,8 @@ cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, 
 // Its two parts: the product, and the sum of the pieces where there are several.
 cudaError_t launch_weight_product(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,
                                   bool waits_at_end, cudaStream_t st);
+// out [n] of dtype = the sum of `count` f32 arrays of n values, `stride` values apart, in order; n and stride multiples of 4.
+cudaError_t launch_sum_pieces(const void* pieces, int count, int64_t n, int64_t stride, void* out, int dtype, cudaStream_t st);
 cudaError_t launch_weight_sum(int T, int K, int N, void* dW, int dW_dtype, const void* pieces, cudaStream_t st);
 // The same product for few rows of A (tokens; K-major): the contraction cut over a cluster of `splits` CTAs (linear_small_splits).
 int linear_small_splits(int T, int N, int K);

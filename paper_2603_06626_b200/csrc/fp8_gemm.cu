@@ -39,6 +39,8 @@ enum F8Mode { F8_LINEAR = 0, F8_GLU = 1 };
 struct F8Params {
   int M, N, K;                   // GLU: N = hidden columns
   int tiles_m, tiles_n, across;  // across: scale atoms of a row of 128s
+  int pieces, piece_steps;       // LINEAR, f32 out: the contraction cut into pieces of so many steps, a multiple of four, each with a matrix of its own
+  int piece_rows;                // ... of so many rows, M rounded up to whole staging blocks
   const __nv_bfloat16 *bias, *residual;
   int out_f32, act;
   uint8_t* out_scales;           // GLU
@@ -49,11 +51,14 @@ struct F8Params {
 
 struct F8Tile {
   int row0, col0, m_valid, n_valid;
+  int step0, steps, out_row;     // first step, steps; row of the output's first row of the piece
 };
 
 template <int MODE>
 __device__ __forceinline__ F8Tile f8_tile(const F8Params& p, int t, int rank) {
   // bands of tile rows, down the band first, as for the bf16 products: the pairs in flight share rows of A and columns of B
+  const int per = p.tiles_m * p.tiles_n, piece = MODE == F8_LINEAR ? t / per : 0;
+  t -= piece * per;
   const int band = t / (F8_RASTER * p.tiles_n), in_band = t - band * F8_RASTER * p.tiles_n;
   const int rows = min(F8_RASTER, p.tiles_m - band * F8_RASTER);
   const int nt = in_band / rows, mt = band * F8_RASTER + (in_band - nt * rows);
@@ -63,6 +68,9 @@ __device__ __forceinline__ F8Tile f8_tile(const F8Params& p, int t, int rank) {
   ti.col0 = nt * cols;
   ti.m_valid = min(F8_BM, p.M - ti.row0);
   ti.n_valid = min(cols, p.N - ti.col0);
+  ti.step0 = piece * p.piece_steps;
+  ti.steps = min(p.piece_steps, (p.K + F8_BK - 1) / F8_BK - ti.step0);
+  ti.out_row = piece * p.piece_rows;
   return ti;
 }
 
@@ -130,7 +138,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   if (!p.waits_at_end) after_previous_kernel();      // set up while the kernel before was still ending; from here on its results are read
   let_next_kernel_start();
 
-  const int n_tiles = p.tiles_m * p.tiles_n, steps = (p.K + F8_BK - 1) / F8_BK;
+  const int n_tiles = p.tiles_m * p.tiles_n * p.pieces;
 
   if (warp == 0) {
     // ===================== TMA producer (both CTAs) =====================
@@ -144,7 +152,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const int b_row = MODE == F8_GLU ? ti.col0 : ti.col0 + rank * F8_BNH;
         const int sa_atom = (ti.row0 >> 7) * p.across, sb_atom = (ti.col0 >> 7) * p.across;
         bool ok = true;
-        for (int ks = 0; ks < steps; ++ks) {
+        for (int ks = 0; ks < ti.steps; ++ks) {
           if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.wait_limit_ns)) {
             ok = false;
             break;
@@ -154,14 +162,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), 2 * (F8_STAGE_BYTES + (scales ? F8_SCALE_BYTES : 0)));
           const uint32_t fb = ptx::map_to_cta(full_bar(s), 0);      // both CTAs' bytes complete on the leader's barrier
           if (scales) {
-            const int g = ks >> 2;
+            const int g = (ti.step0 + ks) >> 2;
             ptx::tma_load_2d_pair(sc, &tmSA, fb, 0, sa_atom + g, keep_a);
             ptx::tma_load_2d_pair(sc + FP8_ATOM, &tmSB, fb, 0, sb_atom + g, keep_b);
             if (MODE == F8_GLU) ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &tmSB1, fb, 0, sb_atom + g, keep_b);
             else ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &tmSB, fb, 0, sb_atom + p.across + g, keep_b);      // beyond the last row: zeros
           }
-          ptx::tma_load_2d_pair(sa, &tmA, fb, ks * F8_BK, ti.row0, keep_a);      // box {128 k, 128 rows}
-          ptx::tma_load_2d_pair(sb, b_map, fb, ks * F8_BK, b_row, keep_b);
+          ptx::tma_load_2d_pair(sa, &tmA, fb, (ti.step0 + ks) * F8_BK, ti.row0, keep_a);      // box {128 k, 128 rows}
+          ptx::tma_load_2d_pair(sb, b_map, fb, (ti.step0 + ks) * F8_BK, b_row, keep_b);
           if (++s == F8_STAGES) {
             s = 0;
             ph ^= 1u;
@@ -199,6 +207,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         first = false;
         ptx::tc_fence_after();
         const uint32_t d_tmem = tmem_base + (acc ? F8_ACC1 : 0u);
+        const int steps = f8_tile<MODE>(p, t, 0).steps;
         bool ok = true;
         for (int ks = 0; ks < steps; ++ks) {
           if (!ptx::mbar_wait_bounded_warp(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
@@ -359,7 +368,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 for (int q = 0; q < 4; ++q)
                   stage_put(q, __float_as_uint(v[h * 16 + q * 4]), __float_as_uint(v[h * 16 + q * 4 + 1]), __float_as_uint(v[h * 16 + q * 4 + 2]),
                             __float_as_uint(v[h * 16 + q * 4 + 3]));
-                stage_send(ti.col0 + c0 + 16 * h, y0);
+                stage_send(ti.col0 + c0 + 16 * h, ti.out_row + y0);
               }
             }
           } else {
@@ -484,7 +493,7 @@ cudaError_t f8_launch(const F8Maps& m, const F8Params& p, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.pieces;
   const int cap = current_sms() & ~1;
   return launch_dependent(kern, dim3((unsigned)(2 * tiles < cap ? 2 * tiles : cap)), dim3(F8_THREADS), F8_SMEM, st, m.A, m.SA, m.B, m.SB, m.B1, m.SB1,
                           m.C, p);
@@ -503,6 +512,8 @@ cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st) {
   p.M = g.M; p.N = g.N; p.K = g.K;
   p.tiles_m = cdiv(g.M, F8_PM);
   p.across = (int)fp8_atoms_across(g.K);
+  p.pieces = 1;
+  p.piece_steps = cdiv(g.K, F8_BK);
   p.act = g.act;
   p.status = g.status;
   p.waits_at_end = g.waits_at_end;
@@ -521,9 +532,15 @@ cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st) {
   p.bias = static_cast<const __nv_bfloat16*>(g.bias);
   p.residual = static_cast<const __nv_bfloat16*>(g.residual);
   p.out_f32 = g.out_f32;
+  if (g.pieces > 1) {
+    p.pieces = g.pieces;
+    p.piece_steps = g.piece_steps;
+    p.piece_rows = fp8_piece_rows(g.M);
+  }
   m.B1 = m.B;
   m.SB1 = m.SB;
-  ok = ok && (g.out_f32 ? make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, g.C, g.M, g.N, g.N, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
+  ok = ok && (g.out_f32 ? make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, g.C, p.pieces > 1 ? (uint64_t)p.pieces * p.piece_rows : g.M, g.N, g.N,
+                                        16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
                         : make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, g.C, g.M, g.N, g.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
   return ok ? f8_launch<F8_LINEAR>(m, p, st) : cudaErrorInvalidValue;
 }

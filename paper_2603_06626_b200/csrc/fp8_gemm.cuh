@@ -16,9 +16,11 @@ struct Fp8Gemm {
   void *C, *out_scales;
   int M, N, K, act, out_f32;
   int32_t* status;
+  int pieces, piece_steps;                // with out_f32, over 1: C [pieces][fp8_piece_rows(M)][N] of partial products over piece_steps 128-deep steps each
   bool waits_at_end;                      // launch_fp8_gemm: works beside the end of the kernel before it, whose results it does not read
 };
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
+inline int fp8_piece_rows(int M) { return (M + 31) / 32 * 32; }
 // The same for few rows of A (tokens), bf16 or codes out: the contraction cut over a cluster of `splits` CTAs (fp8_small_splits).
 int fp8_small_splits(int T, int N, int K, bool glu);
 cudaError_t launch_fp8_small(const Fp8Gemm& g, int splits, cudaStream_t st);

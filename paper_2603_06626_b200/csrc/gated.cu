@@ -36,17 +36,42 @@ int gated_check(int32_t T, int32_t d, int32_t H, int32_t act) {
   return GROUTER_OK;
 }
 
+// Pieces the contraction of the weight gradient over T tokens is cut into, and their length in 128-deep steps, whole groups of four (a scale
+// atom).  Cost in steps of a 256 x 256 tile (0.3 us): rounds of the CTA pairs times steps a round, of which four pass between two tiles; a sum
+// over pieces takes 10 steps and reads its matrices at 8 TB/s (the backward pass of 16384 tokens, 1024 x 1024: 99 -> 66 us, 65536 tokens, 256 x
+// 256: 183 -> 52; 16384 tokens, 1408 x 2048 in three pieces or one: 120 either way).
+struct Fp8Pieces {
+  int count, steps;
+};
+Fp8Pieces fp8_pieces(int T, int K, int N) {
+  const int pairs = current_sms() / 2 > 0 ? current_sms() / 2 : 1, steps = T > 0 ? (T + 127) / 128 : 1;
+  const int64_t tiles = (((int64_t)N + 255) / 256) * (((int64_t)K + 255) / 256);
+  Fp8Pieces best{1, steps};
+  float best_cost = 0.f;
+  for (int s = 1; s <= 16 && (s == 1 || steps / s >= 8); ++s) {
+    const int each = s == 1 ? steps : ((steps + s - 1) / s + 3) / 4 * 4, count = (steps + each - 1) / each;
+    const float cost = (float)((tiles * count + pairs - 1) / pairs) * (each + 4) + (count > 1 ? 10.f + (float)count * N * K * (4.f / 8e6f / 0.3f) : 0.f);
+    if (s == 1 || cost < best_cost) {
+      best = {count, each};
+      best_cost = cost;
+    }
+  }
+  return best;
+}
+
 struct Fp8Workspace {
-  size_t rows, row_scales, cols, col_scales, sums, bytes;
+  size_t rows, row_scales, cols, col_scales, sums, pieces, bytes;
 };
 // Codes of dy and of its transpose, and the partial sums of its columns.
-Fp8Workspace fp8_workspace(int T, int N) {
+Fp8Workspace fp8_workspace(int T, int K, int N) {
   Fp8Workspace w{};
   w.row_scales = up256((size_t)T * fp8_pitch(N));
   w.cols = w.row_scales + up256(grouter_fp8_scale_bytes(T, N));
   w.col_scales = w.cols + up256((size_t)N * fp8_pitch(T));
   w.sums = w.col_scales + up256(grouter_fp8_scale_bytes(N, T));
-  w.bytes = w.sums + up256(((size_t)T + 127) / 128 * N * 4) + 256;
+  w.pieces = w.sums + up256(((size_t)T + 127) / 128 * N * 4);
+  const int count = fp8_pieces(T, K, N).count;
+  w.bytes = w.pieces + (count > 1 ? up256((size_t)count * fp8_piece_rows(N) * K * 4) : 0) + 256;
   return w;
 }
 
@@ -205,7 +230,7 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, con
 
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N) {
   if (fp8_check(T, K, N) != GROUTER_OK || T > FP8_MAX_COLS) return 0;
-  return fp8_workspace(T, N).bytes;
+  return fp8_workspace(T, K, N).bytes;
 }
 
 int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales, const void* Wt, const void* Wt_scales, int32_t T, int32_t K, int32_t N,
@@ -223,7 +248,7 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
     if (db && cudaMemsetAsync(db, 0, (size_t)N * 4, st) != cudaSuccess) return GROUTER_ERR_CUDA;
     return GROUTER_OK;
   }
-  const Fp8Workspace w = fp8_workspace(T, N);
+  const Fp8Workspace w = fp8_workspace(T, K, N);
   char* ws = static_cast<char*>(workspace);
   // the sums are taken on the way to the transposed codes, which a bias alone does not need
   const int tiles = (T + 127) / 128;
@@ -242,7 +267,16 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
   if (dW) {
     g.A = {ws + w.cols, ws + w.col_scales}; g.B = {xt, xt_scales}; g.C = dW; g.M = N; g.N = K; g.K = T; g.out_f32 = dW_dtype == GROUTER_F32;
     g.waits_at_end = dx != nullptr;          // of dx's product, which waited for the codes, it needs nothing
+    const Fp8Pieces pieces = fp8_pieces(T, K, N);
+    if (pieces.count > 1) {
+      g.C = ws + w.pieces;
+      g.out_f32 = 1;
+      g.pieces = pieces.count;
+      g.piece_steps = pieces.steps;
+    }
     if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    if (pieces.count > 1 && launch_sum_pieces(ws + w.pieces, pieces.count, (int64_t)N * K, (int64_t)fp8_piece_rows(N) * K, dW, dW_dtype, st) != cudaSuccess)
+      return GROUTER_ERR_CUDA;
   }
   return GROUTER_OK;
 }

@@ -82,15 +82,15 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz_kernel(const __nv_bfloat
   }
 }
 
-// out = sum of `pieces` matrices of n4 x 4 values, in order.
+// out = sum of `pieces` matrices of n4 x 4 values, `stride` x 4 values apart, in order.
 template <typename T>
-__global__ void __launch_bounds__(256) sum_pieces_kernel(const float* __restrict__ in, int pieces, int64_t n4, T* __restrict__ out) {
+__global__ void __launch_bounds__(256) sum_pieces_kernel(const float* __restrict__ in, int pieces, int64_t n4, int64_t stride, T* __restrict__ out) {
   after_previous_kernel();
   let_next_kernel_start();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
     float4 a = __ldcs(reinterpret_cast<const float4*>(in) + i);
     for (int q = 1; q < pieces; ++q) {
-      const float4 b = __ldcs(reinterpret_cast<const float4*>(in) + q * n4 + i);
+      const float4 b = __ldcs(reinterpret_cast<const float4*>(in) + q * stride + i);
       a.x += b.x;
       a.y += b.y;
       a.z += b.z;
@@ -208,15 +208,20 @@ cudaError_t launch_weight_product(const void* dz, const void* x, int T, int K, i
   return launch_dense_gemm(dz, 1, x, 1, static_cast<float*>(count == 1 ? dW : pieces), N, K, T, dw_chunk(T, count), status, st, waits_at_end);
 }
 
+cudaError_t launch_sum_pieces(const void* pieces, int count, int64_t n, int64_t stride, void* out, int dtype, cudaStream_t st) {
+  const float* in = static_cast<const float*>(pieces);
+  const int64_t want = (n / 4 + 255) / 256, cap = (int64_t)current_sms() * 8;
+  const dim3 grid((unsigned)(want < cap ? want : cap));
+  return dtype == GROUTER_F32
+             ? launch_dependent(sum_pieces_kernel<float>, grid, dim3(256), 0, st, in, count, n / 4, stride / 4, static_cast<float*>(out))
+             : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, in, count, n / 4, stride / 4, static_cast<__nv_bfloat16*>(out));
+}
+
 cudaError_t launch_weight_sum(int T, int K, int N, void* dW, int dW_dtype, const void* pieces, cudaStream_t st) {
   const int count = dw_pieces(T, K, N);
   if (count == 1) return cudaSuccess;
-  const float* in = static_cast<const float*>(pieces);
-  const int64_t n4 = (int64_t)N * K / 4, want = (n4 + 255) / 256, cap = (int64_t)current_sms() * 8;
-  const int grid = (int)(want < cap ? want : cap), real = cdiv(T, dw_chunk(T, count));      // whole 64-token steps may leave the last piece out
-  return dW_dtype == GROUTER_F32 ? launch_dependent(sum_pieces_kernel<float>, dim3(grid), dim3(256), 0, st, in, real, n4, static_cast<float*>(dW))
-                                 : launch_dependent(sum_pieces_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, in, real, n4,
-                                                    static_cast<__nv_bfloat16*>(dW));
+  // whole 64-token steps may leave the last piece out
+  return launch_sum_pieces(pieces, cdiv(T, dw_chunk(T, count)), (int64_t)N * K, (int64_t)N * K, dW, dW_dtype, st);
 }
 
 cudaError_t launch_weight_gradient(const void* dz, const void* x, int T, int K, int N, void* dW, int dW_dtype, void* pieces, int32_t* status,

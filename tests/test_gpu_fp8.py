@@ -183,6 +183,13 @@ def test_backward(T, K, N):
     _backward(T, K, N, torch.float32, False)
 
 
+@pytest.mark.parametrize("T,K,N", [(8200, 264, 136), (5000, 1032, 520), (20001, 16, 24)])
+def test_backward_of_many_tokens_and_a_small_weight(T, K, N):
+    """The weight gradient's contraction is cut into pieces that are added up: one more rounding for each piece, which the bound's 32 covers."""
+    _backward(T, K, N)
+    _backward(T, K, N, torch.float32, False)
+
+
 def test_gradients_one_by_one_and_into_given_tensors():
     from paper_2603_06626_b200 import binding as B
     rng = np.random.default_rng(9)
