@@ -426,8 +426,8 @@ int grouter_rmsnorm_bwd(const void* dy, const void* h, int64_t ldh, const void* 
  * grouter_quantize_fp8: x [rows, cols] of dtype, row r at x + r*ldx elements, any alignment -> codes and scales of its rows (codes NULL:
  *   not wanted) and codes_t, scales_t [cols, ...] of the transposed matrix's (NULL: not wanted), whose blocks run along x's rows.
  *   square != 0: one scale for 128 x 128 elements, the same in both forms (weights).
- * grouter_dequantize_fp8: y [rows, cols] of dtype, row r at y + r*ldy elements: the values that codes and scales stand for (exact
- *   in both types; what was rounded up to 2^128 is an infinity).
+ * grouter_dequantize_fp8: y [rows, cols] of dtype, row r at y + r*ldy elements: the values that codes and scales stand for (exact,
+ *   but that in bf16 those below 2^-126 are rounded to its multiples of 2^-133; what was rounded up to 2^128 is an infinity).
  * codes and scales are 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
 size_t grouter_fp8_pitch(int32_t cols);
 size_t grouter_fp8_scale_bytes(int32_t rows, int32_t cols);
@@ -439,7 +439,7 @@ int grouter_dequantize_fp8(const void* codes, const void* scales, int32_t rows, 
  * multiplied by both scales and added up in fp32, bias and residual in fp32, y rounded once).
  *   x_scales NULL: x is bf16, row t at x + t*ldx elements (any alignment), and is put into 8 bits by this call, in workspace
  *   (grouter_linear_fp8_fwd_workspace_bytes(T, K) bytes, 256-byte aligned; else unused, as ldx is)
- *   bias [N] or NULL, residual [T,N] or NULL, y [T,N] out: bf16, contiguous.  residual may be y itself.
+ *   bias [N] or NULL, residual [T,N] or NULL, y [T,N] out: bf16, contiguous.  residual may be y itself; y overlaps no other input.
  *   status: device int32 the kernels OR bits into (2 = a bounded wait ran out); the caller zeroes it
  * Required: N a multiple of 8, everything else 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, MISALIGNED, CUDA. */
 size_t grouter_linear_fp8_fwd_workspace_bytes(int32_t T, int32_t K);
@@ -448,8 +448,9 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, con
 /* Its backward pass from dy [T,N] bf16 (contiguous), which is put into 8 bits here, by rows for dx and by columns for dW:
  *   dx = q(dy) W [T,K] bf16      dW = q(dy^T) x [N,K] of dW_dtype      db = sum over tokens of dy [N] f32 (not in 8 bits)
  *   xt, Wt: codes and scales of the transposed matrices, x^T [K,T] for dW and W^T [K,N] for dx (grouter_quantize_fp8's codes_t)
- * Outputs that are not wanted are NULL (at least one is wanted).  K and N multiples of 8.  Results are bit-reproducible.  workspace:
- * grouter_linear_fp8_bwd_workspace_bytes(T, K, N) bytes (of the current device), 256-byte aligned.  T = 0 zeroes dW and db.  Errors as above. */
+ * Outputs that are not wanted are NULL (at least one is wanted).  K and N multiples of 8.  Results are bit-reproducible.  Outputs must not
+ * overlap the inputs.  workspace: grouter_linear_fp8_bwd_workspace_bytes(T, K, N) bytes (of the current device), 256-byte aligned.  T = 0
+ * zeroes dW and db.  Errors as above. */
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N);
 int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales, const void* Wt, const void* Wt_scales, int32_t T, int32_t K, int32_t N,
                            void* dx, void* dW, int32_t dW_dtype, float* db, void* workspace, int32_t* status, void* stream);
@@ -464,14 +465,14 @@ int grouter_gated_ffn_fwd(const void* x, const void* W_gu, const void* W_d, cons
 /* Its backward pass:  dh = dy W_d,  dpre = [dh * u * act'(g) | dh * act(g)] (relu'(0) = 0),
  *   dx = dpre W_gu [T,d] bf16      dW_gu = dpre^T x [2H,d],  dW_d = dy^T h [d,H] of dW_dtype
  * Outputs that are not wanted are NULL (at least one is wanted); the residual's gradient is dy.  h is formed again from pre; h and dpre
- * enter the products rounded to bf16, dh does not leave fp32.  Results are bit-reproducible.  workspace:
+ * enter the products rounded to bf16, dh does not leave fp32.  Results are bit-reproducible.  Outputs must not overlap the inputs.  workspace:
  * grouter_gated_ffn_bwd_workspace_bytes(T, d, H) bytes (of the current device), 256-byte aligned.  T = 0 zeroes dW_gu and dW_d. */
 size_t grouter_gated_ffn_bwd_workspace_bytes(int32_t T, int32_t d, int32_t H);
 int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const void* W_d, const void* pre, int32_t T, int32_t d, int32_t H,
                           int32_t act, void* dx, void* dW_gu, void* dW_d, int32_t dW_dtype, void* workspace, int32_t* status, void* stream);
 /* The same block's forward pass in 8 bits:  h = act(x W_g^T) * (x W_u^T) in fp32, put into codes (128 columns a scale) as
  * grouter_quantize_fp8 does,  y = h W_d^T + residual.  x [T,d], W_g, W_u [H,d], W_d [d,H]: codes and scales; x_scales NULL: x is bf16, as
- * for the linear layer in 8 bits.  residual [T,d] or NULL, y [T,d]: bf16.  workspace: grouter_gated_ffn_fp8_fwd_workspace_bytes(T, d, H)
+ * for the linear layer in 8 bits.  residual [T,d] or NULL (may be y itself), y [T,d]: bf16.  workspace: grouter_gated_ffn_fp8_fwd_workspace_bytes(T, d, H)
  * bytes, 256-byte aligned. */
 size_t grouter_gated_ffn_fp8_fwd_workspace_bytes(int32_t T, int32_t d, int32_t H);
 int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W_g, const void* W_g_scales, const void* W_u,
