@@ -4,7 +4,8 @@
 // (rows) or 22 (both) instruction slots that its bytes leave it; so a lane takes sixteen neighbours, over which addresses, exponent and
 // shuffles are spread.  bf16 stays in pairs: magnitudes are compared two to an instruction as 16-bit integers (their order is that of the
 // numbers), infinities and NaN are looked for in the maximum only, and two elements are scaled and converted by one instruction each.
-//   Rows alone: eight lanes hold a block of 128, a warp four blocks (whose scales are one word) of four rows.
+// Measured: 32768 x 4096 bf16 to codes of the rows 61 us (6.6 TB/s), of both forms 121, back to bf16 61; f32 both forms 316.
+//   Rows alone: eight lanes hold a block of 128, a warp four blocks (whose scales are one word) of two rows.
 //   Squares or transposed codes: a CTA takes a tile of 128 x 128, which is a block of every row, a block of every column and a whole
 //     square.  For the transposed codes it waits in shared memory and is read by columns: a lane takes eight neighbouring rows of a word's
 //     columns (two of bf16), sixteen lanes hold a column; words are permuted so that these reads meet no conflicts.
@@ -47,33 +48,38 @@ __device__ __forceinline__ void load_lane(const T* at, int c, int cols, bool row
     w[4 * i + 3] = v.w;
   }
 }
-// Where a warp of the kernels over rows works: four rows from r0 on, 512 columns (an atom's) from `chunk` on.  A block's eight warps are
-// 2^across_log2 beside one another, the others below.
-constexpr int QR_ROWS = 4;
-struct RowsPlace {
-  int r0, chunk;
+// Where a lane of the kernels over rows works: QR_ROWS rows from r0 on, 512 columns (an atom's) from `chunk` on with the other lanes of its warp;
+// where rows are no longer than 256 or 128 elements, half a warp or a quarter does (200000 x 96 to codes 29.3 -> 10.0 us).  A block's eight warps
+// are 2^across_log2 beside one another, the others below.
+constexpr int QR_ROWS = 2;                // one, two, four: 8 x 4096 to codes 1.3, 1.5, 2.0 us, 65536 x 256 8.2, 7.8, 8.3, 32768 x 4096 in f32 108, 108, 114
+struct RowsShape {
+  int across_log2, lanes_log2;
 };
-__device__ __forceinline__ RowsPlace rows_place(int across_log2) {
-  const int warp = threadIdx.x >> 5, across = 1 << across_log2;
-  return {((int)blockIdx.x * ((Q_THREADS / 32) >> across_log2) + (warp >> across_log2)) * QR_ROWS, (int)blockIdx.y * across + (warp & (across - 1))};
+struct RowsPlace {
+  int warp_r0, r0, chunk, lane;           // lane: within those that share rows
+};
+__device__ __forceinline__ RowsPlace rows_place(RowsShape shape) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, across = 1 << shape.across_log2;
+  const int w0 = (((int)blockIdx.x * ((Q_THREADS / 32) >> shape.across_log2) + (warp >> shape.across_log2)) << (5 - shape.lanes_log2)) * QR_ROWS;
+  return {w0, w0 + (lane >> shape.lanes_log2) * QR_ROWS, (int)blockIdx.y * across + (warp & (across - 1)), lane & ((1 << shape.lanes_log2) - 1)};
 }
 
 // Codes of the rows alone.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantParams p, int across_log2) {
-  const RowsPlace at = rows_place(across_log2);
-  const int lane = threadIdx.x & 31, c = at.chunk * 4 * QT + lane * Q_LANE;
+__global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantParams p, RowsShape shape) {
+  const RowsPlace at = rows_place(shape);
+  const int c = at.chunk * 4 * QT + at.lane * Q_LANE;
   const int pitch = (int)fp8_pitch(p.cols), across = (int)fp8_atoms_across(p.cols);
   after_previous_kernel();
   let_next_kernel_start();
-  if (at.r0 >= p.rows || at.chunk >= across) return;             // whole warps
+  if (at.warp_r0 >= p.rows || at.chunk >= across) return;        // whole warps
   const T* x = static_cast<const T*>(p.x) + at.r0 * p.ldx + c;
   uint32_t w[QR_ROWS][q_words<T>()];
 #pragma unroll
   for (int n = 0; n < QR_ROWS; ++n) load_lane<T, VEC>(x + n * p.ldx, c, p.cols, at.r0 + n < p.rows, w[n]);
   uint8_t* to = p.codes + (int64_t)at.r0 * pitch + c;
-  uint8_t* scale = p.scales + fp8_scale_at(at.r0, 4 * at.chunk + lane / Q_LANES, across);      // of the rows below: 16 bytes on each
-  const bool here = c < pitch, says = here && (lane & (Q_LANES - 1)) == 0;
+  uint8_t* scale = p.scales + fp8_scale_at(at.r0, 4 * at.chunk + at.lane / Q_LANES, across);      // of the rows below: 16 bytes on each
+  const bool here = c < pitch, says = here && (at.lane & (Q_LANES - 1)) == 0;
 #pragma unroll
   for (int n = 0; n < QR_ROWS; ++n) {
     bool inf;
@@ -208,48 +214,63 @@ __global__ void __launch_bounds__(Q_THREADS, sizeof(T) == 2 ? 4 : 2) quantize_ti
   }
 }
 
-// Sixteen codes a lane, as quantize_rows_kernel; where the output's rows are not 16-byte aligned its elements are stored one by one.
+// Rows of 512 columns a warp, as quantize_rows_kernel, but a lane has as many neighbouring codes as fill 16 bytes of the output: a warp's
+// stores then fill whole lines (with sixteen codes a lane every other 16 bytes: 32768 x 4096 to bf16 71 us, so 61).  The four scales of a
+// row are one word.  Where the output's rows are not 16-byte aligned its elements are stored one by one.
 template <typename T>
 __global__ void __launch_bounds__(Q_THREADS) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int cols,
-                                                               int64_t ldy, bool vec, int across_log2, T* __restrict__ y) {
-  constexpr int VE = vec16<T>();
-  const RowsPlace at = rows_place(across_log2);
-  const int lane = threadIdx.x & 31, c = at.chunk * 4 * QT + lane * Q_LANE;
+                                                               int64_t ldy, bool vec, RowsShape shape, T* __restrict__ y) {
+  constexpr int VE = vec16<T>(), WORDS = VE / 4, NJ = 4 * QT / (32 * VE);
+  const RowsPlace at = rows_place(shape);
+  const int span = VE << shape.lanes_log2, c = at.chunk * 4 * QT + at.lane * VE;
   const int pitch = (int)fp8_pitch(cols), across = (int)fp8_atoms_across(cols);
   after_previous_kernel();
   let_next_kernel_start();
-  if (at.r0 >= rows || c >= pitch) return;
+  if (at.r0 >= rows || at.chunk >= across) return;
   const uint8_t* from = codes + (int64_t)at.r0 * pitch + c;
-  const uint8_t* scale = scales + fp8_scale_at(at.r0, 4 * at.chunk + lane / Q_LANES, across);
-  uint4 q[QR_ROWS];
-  float s[QR_ROWS];
-#pragma unroll
-  for (int n = 0; n < QR_ROWS; ++n) {
-    if (at.r0 + n < rows) {
-      q[n] = ld_stream16(from + (int64_t)n * pitch);
-      s[n] = fp8_scale(__ldg(scale + 16 * n));
-    }
-  }
-  T* to = y + at.r0 * ldy + c;
-  const bool whole = vec && c + Q_LANE <= cols;
+  const uint8_t* scale = scales + fp8_scale_at(at.r0, 4 * at.chunk, across);
+  uint32_t q[QR_ROWS][NJ][WORDS], four[QR_ROWS];
 #pragma unroll
   for (int n = 0; n < QR_ROWS; ++n) {
     if (at.r0 + n >= rows) break;
-    const uint32_t w[4] = {q[n].x, q[n].y, q[n].z, q[n].w};
-    float f[Q_LANE];
+    four[n] = __ldg(reinterpret_cast<const uint32_t*>(scale + 16 * n));
 #pragma unroll
-    for (int i = 0; i < Q_LANE; i += 2) {
-      const float2 t = mul2(fp8_values(w[i / 4] >> (8 * (i & 2))), both(s[n]));
-      f[i] = t.x;
-      f[i + 1] = t.y;
+    for (int j = 0; j < NJ; ++j) {
+      if (c + j * span >= pitch) break;
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(from + (int64_t)n * pitch + j * span);
+      if constexpr (WORDS == 2) {
+        const uint2 two = __ldcs(reinterpret_cast<const uint2*>(w));
+        q[n][j][0] = two.x;
+        q[n][j][1] = two.y;
+      } else {
+        q[n][j][0] = __ldcs(w);
+      }
     }
-    if (whole) {
+  }
+  T* to = y + at.r0 * ldy + c;
 #pragma unroll
-      for (int i = 0; i < Q_LANE; i += VE) st_pack<T, VE>(to + n * ldy + i, f + i);
-    } else {
+  for (int n = 0; n < QR_ROWS; ++n) {
+    if (at.r0 + n >= rows) break;
 #pragma unroll
-      for (int i = 0; i < Q_LANE; ++i)
-        if (c + i < cols) to[n * ldy + i] = from_f32<T>(f[i]);
+    for (int j = 0; j < NJ; ++j) {
+      const int first = c + j * span;
+      if (first >= cols) break;
+      const int block = (j * span + at.lane * VE) / QT;
+      const float s = fp8_scale(four[n] >> (8 * block) & 0xffu);
+      float f[VE];
+#pragma unroll
+      for (int i = 0; i < VE; i += 2) {
+        const float2 t = mul2(fp8_values(q[n][j][i / 4] >> (8 * (i & 2))), both(s));
+        f[i] = t.x;
+        f[i + 1] = t.y;
+      }
+      if (vec && first + VE <= cols) {
+        st_pack<T, VE>(to + n * ldy + j * span, f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+          if (first + i < cols) to[n * ldy + j * span + i] = from_f32<T>(f[i]);
+      }
     }
   }
 }
@@ -258,14 +279,14 @@ namespace {
 
 struct RowsGrid {
   dim3 grid;
-  int across_log2;
+  RowsShape shape;
 };
 RowsGrid rows_grid(int rows, int cols) {
-  const int chunks = (int)fp8_atoms_across(cols);
+  const int chunks = (int)fp8_atoms_across(cols), lanes = cols <= QT ? 3 : cols <= 2 * QT ? 4 : 5;
   int l = 0;
   while (l < 3 && (1 << l) < chunks) ++l;
-  const int64_t block_rows = ((Q_THREADS / 32) >> l) * QR_ROWS;
-  return {dim3((unsigned)((rows + block_rows - 1) / block_rows), (unsigned)((chunks + (1 << l) - 1) >> l)), l};
+  const int64_t block_rows = (((Q_THREADS / 32) >> l) << (5 - lanes)) * QR_ROWS;
+  return {dim3((unsigned)((rows + block_rows - 1) / block_rows), (unsigned)((chunks + (1 << l) - 1) >> l)), {l, lanes}};
 }
 
 template <typename T, bool VEC, bool SQUARE>
@@ -289,7 +310,7 @@ cudaError_t quantize_launch(const QuantParams& p, bool square, cudaStream_t st) 
   if (square) return tile_launch<T, VEC, true>(p, st);
   if (p.codes_t) return tile_launch<T, VEC, false>(p, st);
   const RowsGrid g = rows_grid(p.rows, p.cols);
-  return launch_dependent(quantize_rows_kernel<T, VEC>, g.grid, dim3(Q_THREADS), 0, st, p, g.across_log2);
+  return launch_dependent(quantize_rows_kernel<T, VEC>, g.grid, dim3(Q_THREADS), 0, st, p, g.shape);
 }
 
 }  // namespace
@@ -353,8 +374,8 @@ int grouter_dequantize_fp8(const void* codes, const void* scales, int32_t rows, 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == GROUTER_F32
-          ? launch_dependent(dequantize_kernel<float>, g.grid, dim3(Q_THREADS), 0, st, q, s, rows, cols, ldy, vec, g.across_log2, static_cast<float*>(y))
-          : launch_dependent(dequantize_kernel<__nv_bfloat16>, g.grid, dim3(Q_THREADS), 0, st, q, s, rows, cols, ldy, vec, g.across_log2,
+          ? launch_dependent(dequantize_kernel<float>, g.grid, dim3(Q_THREADS), 0, st, q, s, rows, cols, ldy, vec, g.shape, static_cast<float*>(y))
+          : launch_dependent(dequantize_kernel<__nv_bfloat16>, g.grid, dim3(Q_THREADS), 0, st, q, s, rows, cols, ldy, vec, g.shape,
                              static_cast<__nv_bfloat16*>(y));
   return e == cudaSuccess ? GROUTER_OK : GROUTER_ERR_CUDA;
 }
