@@ -379,7 +379,9 @@ cudaError_t forward_by_width(const RmsForward& a, cudaStream_t st) {
   if constexpr (VE * sizeof(T) < 16) {
     return forward_spread<T, VE, FP8, 8, 4, 512>(a, st);
   } else {
-    return (int64_t)a.rows * a.d <= (1 << 21) ? forward_spread<T, VE, FP8, 2, 1, 512>(a, st) : forward_spread<T, VE, FP8, 4, 4, 256>(a, st);
+    // two accesses a lane as long as a block of 256 holds the row: more warps with less each are ahead of four (16384 x 2048 to codes 38.1 and
+    // 40.1 us, to bf16 41.9 and 42.8; 4096 x 16384 to codes 77.7 and 86.6) and of one (42.2, 42.3)
+    return (int64_t)a.rows * a.d <= (1 << 21) ? forward_spread<T, VE, FP8, 2, 1, 512>(a, st) : forward_spread<T, VE, FP8, 2, 2, 256>(a, st);
   }
 }
 
