@@ -137,6 +137,33 @@ __device__ __forceinline__ uint32_t block_exponent(const uint32_t (&w)[q_words<T
   if (inf) top = lanes_top_bits<Q_LANES>(lane_top_finite<T>(w));
   return fp8_exponent(__uint_as_float(top));
 }
+// The same of two rows' blocks at once: two bf16 maxima are halves of a word, so that the lanes compare both with one shuffle.
+template <typename T>
+__device__ __forceinline__ void block_exponents(const uint32_t (&w)[2][q_words<T>()], uint32_t (&e)[2], bool& inf) {
+  if constexpr (sizeof(T) == 4) {
+    bool inf1;
+    e[0] = block_exponent<T>(w[0], inf);
+    e[1] = block_exponent<T>(w[1], inf1);
+    inf = inf || inf1;
+  } else {
+    uint32_t top[2] = {0, 0};
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int i = 0; i < q_words<T>(); ++i) top[r] = word_top<T>(top[r], w[r][i]);
+    uint32_t t = __vmaxu2(__byte_perm(top[0], top[1], 0x5410), __byte_perm(top[0], top[1], 0x7632));
+#pragma unroll
+    for (int o = Q_LANES / 2; o > 0; o >>= 1) t = __vmaxu2(t, __shfl_xor_sync(0xffffffffu, t, o));
+    uint32_t bits[2] = {t << 16, t & 0xffff0000u};
+    inf = __any_sync(0xffffffffu, bits_not_finite(bits[0]) || bits_not_finite(bits[1]));
+    if (inf) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) bits[r] = lanes_top_bits<Q_LANES>(lane_top_finite<T>(w[r]));
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) e[r] = fp8_exponent(__uint_as_float(bits[r]));
+  }
+}
 template <typename T, bool INF>
 __device__ __forceinline__ uint4 lane_codes(const uint32_t (&w)[q_words<T>()], float2 inv) {
   uint32_t q[4];

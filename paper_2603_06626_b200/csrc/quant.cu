@@ -4,11 +4,12 @@
 // (rows) or 22 (both) instruction slots that its bytes leave it; so a lane takes sixteen neighbours, over which addresses, exponent and
 // shuffles are spread.  bf16 stays in pairs: magnitudes are compared two to an instruction as 16-bit integers (their order is that of the
 // numbers), infinities and NaN are looked for in the maximum only, and two elements are scaled and converted by one instruction each.
-// Measured: 32768 x 4096 bf16 to codes of the rows 61 us (6.6 TB/s), of both forms 121, back to bf16 61; f32 both forms 316.
+// Measured: 32768 x 4096 bf16 to codes of the rows 60 us (6.7 TB/s), of both forms 93 (5.8), back to bf16 61; f32 both forms 201.
 //   Rows alone: eight lanes hold a block of 128, a warp four blocks (whose scales are one word) of two rows.
 //   Squares or transposed codes: a CTA takes a tile of 128 x 128, which is a block of every row, a block of every column and a whole
-//     square.  For the transposed codes it waits in shared memory and is read by columns: a lane takes eight neighbouring rows of a word's
-//     columns (two of bf16), sixteen lanes hold a column; words are permuted so that these reads meet no conflicts.
+//     square.  For the transposed codes it waits in shared memory and is read by columns: a lane takes sixteen neighbouring rows of a word's
+//     columns (two of bf16), eight lanes hold a column (with eight rows and sixteen lanes 32768 x 4096 121 us, f32 316); words are permuted so
+//     that these reads meet no conflicts.
 #include "fp8.cuh"
 #include "fp8_gemm.cuh"
 
@@ -80,15 +81,16 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantPar
   uint8_t* to = p.codes + (int64_t)at.r0 * pitch + c;
   uint8_t* scale = p.scales + fp8_scale_at(at.r0, 4 * at.chunk + at.lane / Q_LANES, across);      // of the rows below: 16 bytes on each
   const bool here = c < pitch, says = here && (at.lane & (Q_LANES - 1)) == 0;
+  bool inf;
+  uint32_t e[QR_ROWS];
+  block_exponents<T>(w, e, inf);
 #pragma unroll
   for (int n = 0; n < QR_ROWS; ++n) {
-    bool inf;
-    const uint32_t e = block_exponent<T>(w[n], inf);
-    const float2 inv = both(fp8_inverse(e));
+    const float2 inv = both(fp8_inverse(e[n]));
     const uint4 q = inf ? lane_codes<T, true>(w[n], inv) : lane_codes<T, false>(w[n], inv);
     if (at.r0 + n < p.rows) {
       if (here) *reinterpret_cast<uint4*>(to + (int64_t)n * pitch) = q;
-      if (says) scale[16 * n] = (uint8_t)e;
+      if (says) scale[16 * n] = (uint8_t)e[n];
     }
   }
 }
@@ -97,7 +99,7 @@ template <typename T, bool VEC, bool SQUARE>
 __global__ void __launch_bounds__(Q_THREADS, sizeof(T) == 2 ? 4 : 2) quantize_tile_kernel(const QuantParams p) {
   constexpr int W = q_words<T>(), STEP = Q_THREADS / Q_LANES, NR = QT / STEP;        // rows a block at a time, times
   constexpr int WORDS = QT * (int)sizeof(T) / 4;                                     // of a tile row
-  extern __shared__ __align__(8) uint32_t s_tile[];    // [QT][WORDS], with transposed codes; word w of row r at w ^ (r / 8 * 2)
+  extern __shared__ __align__(16) uint32_t s_tile[];   // [QT][WORDS], with transposed codes; word w of row r at place(w, r)
   __shared__ uint32_t s_top[2][Q_THREADS / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int sub = threadIdx.x / Q_LANES, at = threadIdx.x % Q_LANES;
@@ -105,10 +107,12 @@ __global__ void __launch_bounds__(Q_THREADS, sizeof(T) == 2 ? 4 : 2) quantize_ti
   const int r0 = tr * QT, c0 = tc * QT, c = c0 + at * Q_LANE;
   after_previous_kernel();
   let_next_kernel_start();
-  uint32_t v[NR][W];
+  // four words at a time stay together, and no two of a warp's go to the same banks, neither when rows are written nor when columns are read
+  auto place = [](int w, int r16) { return w ^ ((r16 ^ (w >> 5 & 3)) << 2); };
+  uint32_t v[NR / 2][2][W];
   const T* x = static_cast<const T*>(p.x) + (int64_t)(r0 + sub) * p.ldx + c;
 #pragma unroll
-  for (int n = 0; n < NR; ++n) load_lane<T, VEC>(x + n * STEP * p.ldx, c, p.cols, r0 + n * STEP + sub < p.rows, v[n]);
+  for (int n = 0; n < NR; ++n) load_lane<T, VEC>(x + n * STEP * p.ldx, c, p.cols, r0 + n * STEP + sub < p.rows, v[n / 2][n & 1]);
   uint32_t square = 0;
   bool square_inf = false;
   if (SQUARE) {
@@ -122,23 +126,24 @@ __global__ void __launch_bounds__(Q_THREADS, sizeof(T) == 2 ? 4 : 2) quantize_ti
       return t;
     };
 #pragma unroll
-    for (int n = 0; n < NR; ++n) square = max(square, lane_top<T>(v[n]));
+    for (int n = 0; n < NR; ++n) square = max(square, lane_top<T>(v[n / 2][n & 1]));
     square = block_top(square, 0);
     square_inf = bits_not_finite(square);
     if (square_inf) {                     // the whole block alike
       square = 0;
 #pragma unroll
-      for (int n = 0; n < NR; ++n) square = max(square, lane_top_finite<T>(v[n]));
+      for (int n = 0; n < NR; ++n) square = max(square, lane_top_finite<T>(v[n / 2][n & 1]));
       square = block_top(square, 1);
     }
   }
   if (p.codes_t) {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      const int r = n * STEP + sub, turn = (r >> 3) * 2;
+      const int r = n * STEP + sub;
       uint32_t* row = s_tile + r * WORDS;
+      const uint32_t* w = v[n / 2][n & 1];
 #pragma unroll
-      for (int i = 0; i < W; i += 2) *reinterpret_cast<uint2*>(row + ((at * W + i) ^ turn)) = make_uint2(v[n][i], v[n][i + 1]);
+      for (int i = 0; i < W; i += 4) *reinterpret_cast<uint4*>(row + place(at * W + i, r >> 4)) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
     }
   }
   if (p.codes) {
@@ -148,65 +153,76 @@ __global__ void __launch_bounds__(Q_THREADS, sizeof(T) == 2 ? 4 : 2) quantize_ti
     uint8_t* scale = p.scales + (tr * across + (tc >> 2)) * FP8_ATOM + (tc & 3);
     const bool here = c < pitch;
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const int r = n * STEP + sub;
+    for (int m = 0; m < NR / 2; ++m) {
       bool inf = square_inf;
-      const uint32_t e = SQUARE ? fp8_exponent(__uint_as_float(square)) : block_exponent<T>(v[n], inf);
-      const float2 inv = both(fp8_inverse(e));
-      const uint4 q = inf ? lane_codes<T, true>(v[n], inv) : lane_codes<T, false>(v[n], inv);
-      if (r0 + r < p.rows && here) {
-        *reinterpret_cast<uint4*>(to + (int64_t)(n * STEP) * pitch) = q;
-        if (at == 0) scale[(r & 31) * 16 + (r >> 5) * 4] = (uint8_t)e;
+      uint32_t e[2];
+      if (SQUARE) e[0] = e[1] = fp8_exponent(__uint_as_float(square));
+      else block_exponents<T>(v[m], e, inf);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int r = (2 * m + k) * STEP + sub;
+        const float2 inv = both(fp8_inverse(e[k]));
+        const uint4 q = inf ? lane_codes<T, true>(v[m][k], inv) : lane_codes<T, false>(v[m][k], inv);
+        if (r0 + r < p.rows && here) {
+          *reinterpret_cast<uint4*>(to + (int64_t)((2 * m + k) * STEP) * pitch) = q;
+          if (at == 0) scale[(r & 31) * 16 + (r >> 5) * 4] = (uint8_t)e[k];
+        }
       }
     }
   }
   if (p.codes_t) {
     __syncthreads();
     constexpr int CPW = 4 / (int)sizeof(T);             // columns of a word
+    constexpr int UNROLL = sizeof(T) == 2 ? 2 : 1;      // f32: four times no faster
     const int64_t pitch = fp8_pitch(p.rows);
-    const int lr = lane & 15, side = lane >> 4;         // rows 8 lr .. 8 lr + 7 of the word beside
-    const bool here = r0 + 8 * lr < pitch;
-    const uint32_t* from = s_tile + 8 * lr * WORDS;
-    uint8_t* to = p.codes_t + c0 * pitch + r0 + 8 * lr;
+    const int lr = lane & 7, side = lane >> 3;          // rows 16 lr .. 16 lr + 15 of one of four neighbouring words
+    const bool here = r0 + 16 * lr < pitch;
+    const uint32_t* from = s_tile + 16 * lr * WORDS;
+    uint8_t* to = p.codes_t + c0 * pitch + r0 + 16 * lr;
     uint8_t* scale = p.scales_t + (tc * fp8_atoms_across(p.rows) + (tr >> 2)) * FP8_ATOM + (tr & 3);
-#pragma unroll 2
-    for (int w2 = warp; w2 < WORDS / 2; w2 += Q_THREADS / 32) {
-      const int word = 2 * w2 + side;
-      uint32_t q[8], tops = 0;                          // tops: of the word's columns
+#pragma unroll UNROLL
+    for (int w4 = warp; w4 < WORDS / 4; w4 += Q_THREADS / 32) {
+      const int word = 4 * w4 + side;
+      uint32_t q[16], tops = 0;                         // tops: of the word's columns
 #pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] = from[i * WORDS + (word ^ (2 * lr))];
+      for (int i = 0; i < 16; ++i) q[i] = from[i * WORDS + place(word, lr)];
       bool inf = square_inf;
       if (!SQUARE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tops = word_top<T>(tops, q[i]);
+        for (int i = 0; i < 16; ++i) tops = word_top<T>(tops, q[i]);
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) tops = word_top<T>(tops, __shfl_xor_sync(0xffffffffu, tops, o));
+        for (int o = 4; o > 0; o >>= 1) tops = word_top<T>(tops, __shfl_xor_sync(0xffffffffu, tops, o));
         inf = __any_sync(0xffffffffu, bits_not_finite(top_of_word<T>(tops)));
         if (inf) {
           tops = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) tops = word_top_finite<T>(tops, q[i]);
+          for (int i = 0; i < 16; ++i) tops = word_top_finite<T>(tops, q[i]);
 #pragma unroll
-          for (int o = 8; o > 0; o >>= 1) tops = word_top<T>(tops, __shfl_xor_sync(0xffffffffu, tops, o));
+          for (int o = 4; o > 0; o >>= 1) tops = word_top<T>(tops, __shfl_xor_sync(0xffffffffu, tops, o));
         }
       }
 #pragma unroll
       for (int j = 0; j < CPW; ++j) {
         auto half = [&](uint32_t w) { return sizeof(T) == 4 ? w : j == 0 ? w << 16 : w & 0xffff0000u; };
-        float f[8];
+        float f[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(half(q[i]));
+        for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(half(q[i]));
         const uint32_t e = fp8_exponent(__uint_as_float(SQUARE ? square : half(tops)));
         const float inv = fp8_inverse(e);
         const int col = word * CPW + j;                 // within the tile
         const bool column = c0 + col < p.cols;
         if (p.sums) {
-          const float sum = lanes_sum<16>(((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7])));
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) sum += (f[i] + f[i + 1]) + (f[i + 2] + f[i + 3]);
+          sum = lanes_sum<8>(sum);
           if (lr == 0 && column) p.sums[(int64_t)tr * p.cols + c0 + col] = sum;
         }
-        const uint2 codes = inf ? make_uint2(fp8_quad<true>(f, inv), fp8_quad<true>(f + 4, inv)) : make_uint2(fp8_quad<false>(f, inv), fp8_quad<false>(f + 4, inv));
+        uint32_t codes[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[i] = inf ? fp8_quad<true>(f + 4 * i, inv) : fp8_quad<false>(f + 4 * i, inv);
         if (column && here) {
-          *reinterpret_cast<uint2*>(to + col * pitch) = codes;
+          *reinterpret_cast<uint4*>(to + col * pitch) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
           if (lr == 0) scale[(col & 31) * 16 + (col >> 5) * 4] = (uint8_t)e;
         }
       }
