@@ -34,20 +34,55 @@ constexpr int F8_SMEM = F8_STAGES * (F8_STAGE_BYTES + F8_SCALE_BYTES) + F8_STAGI
 constexpr uint32_t F8_ACC1 = 224, F8_SCALES = 480, F8_SCALE_SET = 16;       // TMEM columns: accumulator 1, the two sets of scales (A +0, B +8)
 constexpr int F8_RASTER = 8;
 
-enum F8Mode { F8_LINEAR = 0, F8_GLU = 1 };
+enum F8Mode { F8_LINEAR = 0, F8_GLU = 1, F8_TWO = 2 };      // TWO: two LINEAR products in one launch
 
-struct F8Params {
+struct F8Product {
   int M, N, K;                   // GLU: N = hidden columns
   int tiles_m, tiles_n, across;  // across: scale atoms of a row of 128s
-  int pieces, piece_steps;       // LINEAR, f32 out: the contraction cut into pieces of so many steps, a multiple of four, each with a matrix of its own
+  int pieces, piece_steps;       // f32 out: the contraction cut into pieces of so many steps, a multiple of four, each with a matrix of its own
   int piece_rows;                // ... of so many rows, M rounded up to whole staging blocks
+  int tiles;                     // of all pieces
   const __nv_bfloat16 *bias, *residual;
-  int out_f32, act;
+  int out_f32;
+};
+struct F8Maps {
+  CUtensorMap A, SA, B, SB, C;
+};
+struct F8Params {
+  F8Maps maps[2];                // GLU: B and SB of the second are the other projection
+  F8Product of[2];
+  int ahead;                     // TWO: tiles of the second product that a pair has time for while others have one more of the first
+  int act;
   uint8_t* out_scales;           // GLU
   int32_t* status;
   unsigned long long wait_limit_ns;
   int waits_at_end;              // as in gemm.cu: works beside the end of the kernel before it
 };
+
+// The i-th tile of a pair; false behind its last.  TWO: the first product's tiles go round the pairs; the second's, whose contraction is shorter,
+// first to those pairs that the last round leaves without a tile, `ahead` each, then round all of them.
+template <int MODE>
+__device__ __forceinline__ bool f8_pick(const F8Params& p, int i, int pair, int n_pairs, int& which, int& t) {
+  which = 0;
+  t = pair + i * n_pairs;
+  if (MODE != F8_TWO) return t < p.of[0].tiles;
+  if (t < p.of[0].tiles) return true;
+  which = 1;
+  const int late = p.of[0].tiles % n_pairs;          // pairs with one more
+  int r = i - p.of[0].tiles / n_pairs - (pair < late ? 1 : 0);
+  if (late > 0) {
+    if (pair >= late && r < p.ahead) {
+      t = r * (n_pairs - late) + pair - late;
+      return t < p.of[1].tiles;
+    }
+    t = p.ahead * (n_pairs - late);
+    if (pair >= late) r -= p.ahead;
+  } else {
+    t = 0;
+  }
+  t += r * n_pairs + pair;
+  return t < p.of[1].tiles;
+}
 
 struct F8Tile {
   int row0, col0, m_valid, n_valid;
@@ -55,9 +90,9 @@ struct F8Tile {
 };
 
 template <int MODE>
-__device__ __forceinline__ F8Tile f8_tile(const F8Params& p, int t, int rank) {
+__device__ __forceinline__ F8Tile f8_tile(const F8Product& p, int t, int rank) {
   // bands of tile rows, down the band first, as for the bf16 products: the pairs in flight share rows of A and columns of B
-  const int per = p.tiles_m * p.tiles_n, piece = MODE == F8_LINEAR ? t / per : 0;
+  const int per = p.tiles_m * p.tiles_n, piece = MODE == F8_GLU ? 0 : t / per;
   t -= piece * per;
   const int band = t / (F8_RASTER * p.tiles_n), in_band = t - band * F8_RASTER * p.tiles_n;
   const int rows = min(F8_RASTER, p.tiles_m - band * F8_RASTER);
@@ -74,12 +109,8 @@ __device__ __forceinline__ F8Tile f8_tile(const F8Params& p, int t, int rank) {
   return ti;
 }
 
-// tmB, tmSB: B and its scales; GLU: the gate's weights, and tmB1, tmSB1 those of the other projection.
 template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8_THREADS, 1)
-fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmB,
-                const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmSB1,
-                const __grid_constant__ CUtensorMap tmC, const F8Params p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_constant__ F8Params p) {
   extern __shared__ uint8_t smem_raw[];
   // the same offsets in both CTAs of the pair: descriptors and multicast commits name both
   const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -119,11 +150,10 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     ptx::mbar_init(over_bar, F8_EPI_WARPS);
     for (int q = 0; q < 4; ++q) ptx::mbar_init(top_bar(q), 2);
     ptx::fence_mbar_init();
-    ptx::prefetch_tensormap(&tmA);
-    ptx::prefetch_tensormap(&tmSA);
-    ptx::prefetch_tensormap(&tmB);
-    ptx::prefetch_tensormap(&tmSB);
-    ptx::prefetch_tensormap(&tmC);
+    for (int i = 0; i < (MODE == F8_TWO ? 2 : 1); ++i) {
+      const F8Maps& m = p.maps[i];
+      for (const CUtensorMap* map : {&m.A, &m.SA, &m.B, &m.SB, &m.C}) ptx::prefetch_tensormap(map);
+    }
   }
   if (warp == 1) {
     ptx::tmem_alloc_pair(ptx::smem_u32(&s_tmem_base), 512);
@@ -138,19 +168,20 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   if (!p.waits_at_end) after_previous_kernel();      // set up while the kernel before was still ending; from here on its results are read
   let_next_kernel_start();
 
-  const int n_tiles = p.tiles_m * p.tiles_n * p.pieces;
-
   if (warp == 0) {
     // ===================== TMA producer (both CTAs) =====================
     if (lane == 0) {
       const uint64_t keep_a = ptx::l2_policy_evict_normal(), keep_b = ptx::l2_policy_evict_last();
       int s = 0;
       uint32_t ph = 0;
-      for (int t = pair_id; t < n_tiles && !*abort_flag; t += n_pairs) {
-        const F8Tile ti = f8_tile<MODE>(p, t, rank);
-        const CUtensorMap* b_map = MODE == F8_GLU && rank == 1 ? &tmB1 : &tmB;
+      int which, t;
+      for (int i = 0; f8_pick<MODE>(p, i, pair_id, n_pairs, which, t) && !*abort_flag; ++i) {
+        const F8Tile ti = f8_tile<MODE>(p.of[which], t, rank);
+        const F8Maps& m = p.maps[which];
+        const int across = p.of[which].across;
+        const CUtensorMap* b_map = MODE == F8_GLU && rank == 1 ? &p.maps[1].B : &m.B;
         const int b_row = MODE == F8_GLU ? ti.col0 : ti.col0 + rank * F8_BNH;
-        const int sa_atom = (ti.row0 >> 7) * p.across, sb_atom = (ti.col0 >> 7) * p.across;
+        const int sa_atom = (ti.row0 >> 7) * across, sb_atom = (ti.col0 >> 7) * across;
         bool ok = true;
         for (int ks = 0; ks < ti.steps; ++ks) {
           if (!ptx::mbar_wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.wait_limit_ns)) {
@@ -163,12 +194,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           const uint32_t fb = ptx::map_to_cta(full_bar(s), 0);      // both CTAs' bytes complete on the leader's barrier
           if (scales) {
             const int g = (ti.step0 + ks) >> 2;
-            ptx::tma_load_2d_pair(sc, &tmSA, fb, 0, sa_atom + g, keep_a);
-            ptx::tma_load_2d_pair(sc + FP8_ATOM, &tmSB, fb, 0, sb_atom + g, keep_b);
-            if (MODE == F8_GLU) ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &tmSB1, fb, 0, sb_atom + g, keep_b);
-            else ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &tmSB, fb, 0, sb_atom + p.across + g, keep_b);      // beyond the last row: zeros
+            ptx::tma_load_2d_pair(sc, &m.SA, fb, 0, sa_atom + g, keep_a);
+            ptx::tma_load_2d_pair(sc + FP8_ATOM, &m.SB, fb, 0, sb_atom + g, keep_b);
+            if (MODE == F8_GLU) ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &p.maps[1].SB, fb, 0, sb_atom + g, keep_b);
+            else ptx::tma_load_2d_pair(sc + 2 * FP8_ATOM, &m.SB, fb, 0, sb_atom + across + g, keep_b);      // beyond the last row: zeros
           }
-          ptx::tma_load_2d_pair(sa, &tmA, fb, (ti.step0 + ks) * F8_BK, ti.row0, keep_a);      // box {128 k, 128 rows}
+          ptx::tma_load_2d_pair(sa, &m.A, fb, (ti.step0 + ks) * F8_BK, ti.row0, keep_a);      // box {128 k, 128 rows}
           ptx::tma_load_2d_pair(sb, b_map, fb, (ti.step0 + ks) * F8_BK, b_row, keep_b);
           if (++s == F8_STAGES) {
             s = 0;
@@ -198,7 +229,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       int s = 0, acc = 0, set = 0;
       uint32_t ph = 0, acc_ph = 0, over_ph = 0, set_ph = 0;
       bool first = true;
-      for (int t = pair_id; t < n_tiles && !__any_sync(0xffffffffu, *abort_flag); t += n_pairs) {
+      int which, t;
+      for (int i = 0; f8_pick<MODE>(p, i, pair_id, n_pairs, which, t) && !__any_sync(0xffffffffu, *abort_flag); ++i) {
         if (!ptx::mbar_wait_bounded_warp(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.wait_limit_ns)) break;
         if (!first) {
           if (!ptx::mbar_wait_bounded_warp(over_bar, over_ph, abort_flag, p.wait_limit_ns)) break;
@@ -207,7 +239,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         first = false;
         ptx::tc_fence_after();
         const uint32_t d_tmem = tmem_base + (acc ? F8_ACC1 : 0u);
-        const int steps = f8_tile<MODE>(p, t, 0).steps;
+        const int steps = f8_tile<MODE>(p.of[which], t, 0).steps;
         bool ok = true;
         for (int ks = 0; ks < steps; ++ks) {
           if (!ptx::mbar_wait_bounded_warp(full_bar(s), ph, abort_flag, p.wait_limit_ns)) {
@@ -276,30 +308,31 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     auto stage_put = [&](int q, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {      // 16-byte unit q of this row
       ptx::st_shared_v4(block0 + block * F8_BLOCK_BYTES + row_off + (((uint32_t)q ^ sw) << 4), a, b, c, d);
     };
-    auto stage_send = [&](int x, int y) {
+    auto stage_send = [&](const CUtensorMap* to, int x, int y) {
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        ptx::tma_store_2d(&tmC, block0 + block * F8_BLOCK_BYTES, x, y, stream_out);
+        ptx::tma_store_2d(to, block0 + block * F8_BLOCK_BYTES, x, y, stream_out);
         ptx::bulk_commit();
       }
       block = block == F8_EPI_BLOCKS - 1 ? 0 : block + 1;
     };
     const uint32_t leader_over = ptx::map_to_cta(over_bar, 0);
     const uint32_t leader_tempty[2] = {ptx::map_to_cta(tempty_bar(0), 0), ptx::map_to_cta(tempty_bar(1), 0)};
-    int acc = 0, parity = 0;
+    int acc = 0, parity = 0, which, t;
     uint32_t acc_ph = 0, top_ph = 0;
-    for (int t = pair_id; t < n_tiles && !*abort_flag; t += n_pairs) {
-      const F8Tile ti = f8_tile<MODE>(p, t, rank);
+    for (int nth = 0; f8_pick<MODE>(p, nth, pair_id, n_pairs, which, t) && !*abort_flag; ++nth) {
+      const F8Product& of = p.of[which];
+      const F8Tile ti = f8_tile<MODE>(of, t, rank);
       const int y0 = ti.row0 + quad * 32;
       const bool rows_here = ti.m_valid > quad * 32;       // warp-uniform
       // the residual of this thread's row and 128 columns, on its way while the tile is multiplied
       uint4 res[4][4];
-      if (MODE == F8_LINEAR && p.residual != nullptr) {
+      if (MODE != F8_GLU && of.residual != nullptr) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int c0 = half * 128 + (half ? 3 - i : i) * 32;
-          const __nv_bfloat16* at = p.residual + ((size_t)ti.row0 + r) * p.N + ti.col0 + c0;
+          const __nv_bfloat16* at = of.residual + ((size_t)ti.row0 + r) * of.N + ti.col0 + c0;
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             res[i][q] = r < ti.m_valid && c0 + q * 8 < ti.n_valid ? *reinterpret_cast<const uint4*>(at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
@@ -315,7 +348,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive_cluster(leader_over);
       };
-      if constexpr (MODE == F8_LINEAR) {
+      if constexpr (MODE != F8_GLU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int c0 = half * 128 + (half ? 3 - i : i) * 32;      // the shared columns first
@@ -331,12 +364,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           }
           if (i == 0 && has_over) say_over();
           if (!any) continue;
-          if (p.bias != nullptr) {
+          if (of.bias != nullptr) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               if (q * 8 < n_left) {
                 Pack<__nv_bfloat16, 8> b[1];
-                *reinterpret_cast<uint4*>(&b[0]) = __ldg(reinterpret_cast<const uint4*>(p.bias + ti.col0 + c0 + q * 8));
+                *reinterpret_cast<uint4*>(&b[0]) = __ldg(reinterpret_cast<const uint4*>(of.bias + ti.col0 + c0 + q * 8));
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                   const float2 f = pair_at(b, k);
@@ -346,7 +379,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               }
             }
           }
-          if (p.residual != nullptr) {
+          if (of.residual != nullptr) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               Pack<__nv_bfloat16, 8> b[1];
@@ -359,7 +392,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               }
             }
           }
-          if (p.out_f32) {
+          if (of.out_f32) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               if (n_left > 16 * h) {
@@ -368,7 +401,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 for (int q = 0; q < 4; ++q)
                   stage_put(q, __float_as_uint(v[h * 16 + q * 4]), __float_as_uint(v[h * 16 + q * 4 + 1]), __float_as_uint(v[h * 16 + q * 4 + 2]),
                             __float_as_uint(v[h * 16 + q * 4 + 3]));
-                stage_send(ti.col0 + c0 + 16 * h, ti.out_row + y0);
+                stage_send(&p.maps[which].C, ti.col0 + c0 + 16 * h, ti.out_row + y0);
               }
             }
           } else {
@@ -379,7 +412,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               const uint4 w = *reinterpret_cast<const uint4*>(&o);
               stage_put(q, w.x, w.y, w.z, w.w);
             }
-            stage_send(ti.col0 + c0, y0);
+            stage_send(&p.maps[which].C, ti.col0 + c0, y0);
           }
         }
       } else {
@@ -442,8 +475,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             }
             stage_put(q, c[0], c[1], c[2], c[3]);
           }
-          stage_send(ti.col0 + half * 64, y0);
-          if (half == 0 && r < ti.m_valid) p.out_scales[fp8_scale_at(ti.row0 + r, ti.col0 >> 7, fp8_atoms_across(p.N))] = (uint8_t)e;
+          stage_send(&p.maps[which].C, ti.col0 + half * 64, y0);
+          if (half == 0 && r < ti.m_valid) p.out_scales[fp8_scale_at(ti.row0 + r, ti.col0 >> 7, fp8_atoms_across(of.N))] = (uint8_t)e;
         }
       }
       // all TMEM reads of this warp are complete (wait::ld above): hand the accumulator back
@@ -478,12 +511,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 
 inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-struct F8Maps {
-  CUtensorMap A, SA, B, SB, B1, SB1, C;
-};
-
 template <int MODE>
-cudaError_t f8_launch(const F8Maps& m, const F8Params& p, cudaStream_t st) {
+cudaError_t f8_launch(const F8Params& p, cudaStream_t st) {
   static bool configured[64] = {};        // the opt-in to more than 48 KB of dynamic shared memory, once per device
   auto kern = fp8_gemm_kernel<MODE>;
   int dev = 0;
@@ -493,10 +522,9 @@ cudaError_t f8_launch(const F8Maps& m, const F8Params& p, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.pieces;
+  const int64_t tiles = (int64_t)p.of[0].tiles + (MODE == F8_TWO ? p.of[1].tiles : 0);
   const int cap = current_sms() & ~1;
-  return launch_dependent(kern, dim3((unsigned)(2 * tiles < cap ? 2 * tiles : cap)), dim3(F8_THREADS), F8_SMEM, st, m.A, m.SA, m.B, m.SB, m.B1, m.SB1,
-                          m.C, p);
+  return launch_dependent(kern, dim3((unsigned)(2 * tiles < cap ? 2 * tiles : cap)), dim3(F8_THREADS), F8_SMEM, st, p);
 }
 
 }  // namespace
@@ -507,42 +535,69 @@ bool make_fp8_maps(CUtensorMap* codes, CUtensorMap* scales, const Fp8Operand& x,
          make_tile_map(scales, CU_TENSOR_MAP_DATA_TYPE_INT32, 4, x.scales, atoms, 128, 128, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st) {
-  F8Params p{};
-  p.M = g.M; p.N = g.N; p.K = g.K;
-  p.tiles_m = cdiv(g.M, F8_PM);
-  p.across = (int)fp8_atoms_across(g.K);
-  p.pieces = 1;
-  p.piece_steps = cdiv(g.K, F8_BK);
-  p.act = g.act;
-  p.status = g.status;
-  p.waits_at_end = g.waits_at_end;
-  p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
-  F8Maps m;
-  bool ok = make_fp8_maps(&m.A, &m.SA, g.A, g.M, g.K, F8_BM) && make_fp8_maps(&m.B, &m.SB, g.B, g.N, g.K, F8_BNH);
-  if (g.B1.codes) {
-    p.tiles_n = cdiv(g.N, F8_BNH);
-    p.out_scales = static_cast<uint8_t*>(g.out_scales);
-    // the columns up to the pitch are written too: zeros
-    ok = ok && make_fp8_maps(&m.B1, &m.SB1, g.B1, g.N, g.K, F8_BNH) &&
-         make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, g.C, g.M, fp8_pitch(g.N), fp8_pitch(g.N), 64, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-    return ok ? f8_launch<F8_GLU>(m, p, st) : cudaErrorInvalidValue;
-  }
-  p.tiles_n = cdiv(g.N, F8_BN);
-  p.bias = static_cast<const __nv_bfloat16*>(g.bias);
-  p.residual = static_cast<const __nv_bfloat16*>(g.residual);
-  p.out_f32 = g.out_f32;
+namespace {
+
+bool f8_linear(const Fp8Gemm& g, F8Maps* m, F8Product* of) {
+  *of = {};
+  of->M = g.M; of->N = g.N; of->K = g.K;
+  of->tiles_m = cdiv(g.M, F8_PM);
+  of->tiles_n = cdiv(g.N, F8_BN);
+  of->across = (int)fp8_atoms_across(g.K);
+  of->pieces = 1;
+  of->piece_steps = cdiv(g.K, F8_BK);
+  of->bias = static_cast<const __nv_bfloat16*>(g.bias);
+  of->residual = static_cast<const __nv_bfloat16*>(g.residual);
+  of->out_f32 = g.out_f32;
   if (g.pieces > 1) {
-    p.pieces = g.pieces;
-    p.piece_steps = g.piece_steps;
-    p.piece_rows = fp8_piece_rows(g.M);
+    of->pieces = g.pieces;
+    of->piece_steps = g.piece_steps;
+    of->piece_rows = fp8_piece_rows(g.M);
   }
-  m.B1 = m.B;
-  m.SB1 = m.SB;
-  ok = ok && (g.out_f32 ? make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, g.C, p.pieces > 1 ? (uint64_t)p.pieces * p.piece_rows : g.M, g.N, g.N,
-                                        16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
-                        : make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, g.C, g.M, g.N, g.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
-  return ok ? f8_launch<F8_LINEAR>(m, p, st) : cudaErrorInvalidValue;
+  of->tiles = of->tiles_m * of->tiles_n * of->pieces;
+  return make_fp8_maps(&m->A, &m->SA, g.A, g.M, g.K, F8_BM) && make_fp8_maps(&m->B, &m->SB, g.B, g.N, g.K, F8_BNH) &&
+         (g.out_f32 ? make_tile_map(&m->C, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, g.C, of->pieces > 1 ? (uint64_t)of->pieces * of->piece_rows : g.M, g.N, g.N,
+                                    16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
+                    : make_tile_map(&m->C, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, g.C, g.M, g.N, g.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+}
+F8Params f8_params(const Fp8Gemm& g) {
+  F8Params p;
+  p.of[1] = {};
+  p.ahead = 0;
+  p.act = g.act;
+  p.out_scales = static_cast<uint8_t*>(g.out_scales);
+  p.status = g.status;
+  p.wait_limit_ns = DEFAULT_WAIT_LIMIT_NS;
+  p.waits_at_end = g.waits_at_end;
+  return p;
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st) {
+  F8Params p = f8_params(g);
+  if (!g.B1.codes) return f8_linear(g, &p.maps[0], &p.of[0]) ? f8_launch<F8_LINEAR>(p, st) : cudaErrorInvalidValue;
+  F8Product& of = p.of[0];
+  of = {};
+  of.M = g.M; of.N = g.N; of.K = g.K;
+  of.tiles_m = cdiv(g.M, F8_PM);
+  of.tiles_n = cdiv(g.N, F8_BNH);
+  of.across = (int)fp8_atoms_across(g.K);
+  of.pieces = 1;
+  of.piece_steps = cdiv(g.K, F8_BK);
+  of.tiles = of.tiles_m * of.tiles_n;
+  F8Maps& m = p.maps[0];
+  // the columns up to the pitch are written too
+  const bool ok = make_fp8_maps(&m.A, &m.SA, g.A, g.M, g.K, F8_BM) && make_fp8_maps(&m.B, &m.SB, g.B, g.N, g.K, F8_BNH) &&
+                  make_fp8_maps(&p.maps[1].B, &p.maps[1].SB, g.B1, g.N, g.K, F8_BNH) &&
+                  make_tile_map(&m.C, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, g.C, g.M, fp8_pitch(g.N), fp8_pitch(g.N), 64, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  return ok ? f8_launch<F8_GLU>(p, st) : cudaErrorInvalidValue;
+}
+
+cudaError_t launch_fp8_gemms(const Fp8Gemm& a, const Fp8Gemm& b, cudaStream_t st) {
+  F8Params p = f8_params(a);
+  if (!f8_linear(a, &p.maps[0], &p.of[0]) || !f8_linear(b, &p.maps[1], &p.of[1])) return cudaErrorInvalidValue;
+  p.ahead = fp8_tile_cost(p.of[0].piece_steps) / fp8_tile_cost(p.of[1].piece_steps);
+  return f8_launch<F8_TWO>(p, st);
 }
 
 }  // namespace grouter

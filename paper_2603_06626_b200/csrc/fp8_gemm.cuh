@@ -20,6 +20,10 @@ struct Fp8Gemm {
   bool waits_at_end;                      // launch_fp8_gemm: works beside the end of the kernel before it, whose results it does not read
 };
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
+// Two products that need nothing of one another, bf16 or f32 out, in one launch; a is the one with the longer contraction (or pieces).
+cudaError_t launch_fp8_gemms(const Fp8Gemm& a, const Fp8Gemm& b, cudaStream_t st);
+// What a tile of so many 128-deep steps takes, in steps: four of them pass between two tiles.
+inline int fp8_tile_cost(int steps) { return steps + 4; }
 inline int fp8_piece_rows(int M) { return (M + 31) / 32 * 32; }
 // The same for few rows of A (tokens), bf16 or codes out: the contraction cut over a cluster of `splits` CTAs (fp8_small_splits).
 int fp8_small_splits(int T, int N, int K, bool glu);

@@ -37,20 +37,25 @@ int gated_check(int32_t T, int32_t d, int32_t H, int32_t act) {
 }
 
 // Pieces the contraction of the weight gradient over T tokens is cut into, and their length in 128-deep steps, whole groups of four (a scale
-// atom).  Cost in steps of a 256 x 256 tile (0.3 us): rounds of the CTA pairs times steps a round, of which four pass between two tiles; a sum
-// over pieces takes 10 steps and reads its matrices at 8 TB/s (the backward pass of 16384 tokens, 1024 x 1024: 99 -> 66 us, 65536 tokens, 256 x
-// 256: 183 -> 52; 16384 tokens, 1408 x 2048 in three pieces or one: 120 either way).
+// atom).  Cost in steps of a 256 x 256 tile (0.3 us): rounds of the CTA pairs times what a tile takes or, with dx's product in the same launch,
+// the share of a pair in all of it; a sum over pieces takes 10 steps and reads its matrices at 8 TB/s (alone: the backward pass of 16384
+// tokens, 1024 x 1024: 99 -> 66 us, 65536 tokens, 256 x 256: 183 -> 52).
 struct Fp8Pieces {
   int count, steps;
 };
-Fp8Pieces fp8_pieces(int T, int K, int N) {
-  const int pairs = current_sms() / 2 > 0 ? current_sms() / 2 : 1, steps = T > 0 ? (T + 127) / 128 : 1;
-  const int64_t tiles = (((int64_t)N + 255) / 256) * (((int64_t)K + 255) / 256);
+Fp8Pieces fp8_pieces(int T, int K, int N, bool with_dx) {
+  const int pairs = current_sms() / 2 > 0 ? current_sms() / 2 : 1, steps = T > 0 ? (T + 127) / 128 : 1, dx_steps = (N + 127) / 128;
+  const int64_t tiles = (((int64_t)N + 255) / 256) * (((int64_t)K + 255) / 256), dx_tiles = (((int64_t)T + 255) / 256) * (((int64_t)K + 255) / 256);
   Fp8Pieces best{1, steps};
   float best_cost = 0.f;
   for (int s = 1; s <= 16 && (s == 1 || steps / s >= 8); ++s) {
     const int each = s == 1 ? steps : ((steps + s - 1) / s + 3) / 4 * 4, count = (steps + each - 1) / each;
-    const float cost = (float)((tiles * count + pairs - 1) / pairs) * (each + 4) + (count > 1 ? 10.f + (float)count * N * K * (4.f / 8e6f / 0.3f) : 0.f);
+    float cost = (float)((tiles * count + pairs - 1) / pairs) * fp8_tile_cost(each);
+    if (with_dx) {
+      const float all = ((float)tiles * count * fp8_tile_cost(each) + (float)dx_tiles * fp8_tile_cost(dx_steps)) / pairs;
+      cost = all > cost ? all : cost;
+    }
+    if (count > 1) cost += 10.f + (float)count * N * K * (4.f / 8e6f / 0.3f);
     if (s == 1 || cost < best_cost) {
       best = {count, each};
       best_cost = cost;
@@ -70,7 +75,7 @@ Fp8Workspace fp8_workspace(int T, int K, int N) {
   w.col_scales = w.cols + up256((size_t)N * fp8_pitch(T));
   w.sums = w.col_scales + up256(grouter_fp8_scale_bytes(N, T));
   w.pieces = w.sums + up256(((size_t)T + 127) / 128 * N * 4);
-  const int count = fp8_pieces(T, K, N).count;
+  const int alone = fp8_pieces(T, K, N, false).count, both = fp8_pieces(T, K, N, true).count, count = alone > both ? alone : both;
   w.bytes = w.pieces + (count > 1 ? up256((size_t)count * fp8_piece_rows(N) * K * 4) : 0) + 256;
   return w;
 }
@@ -107,17 +112,23 @@ inline int log2_of(int s) { return s >= 8 ? 3 : s >= 4 ? 2 : s >= 2 ? 1 : 0; }
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int token_tile(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
 
-// A as codes, or (g.x) as bf16, which a kernel of its own puts into the place that g.A names unless the product can do it on the way.
-cudaError_t fp8_product(Fp8Gemm g, cudaStream_t st) {
+// Whether the kernel for few tokens is ahead, in `splits` cuts.
+bool fp8_few(const Fp8Gemm& g, int& splits) {
   const bool glu = g.B1.codes != nullptr;
-  const int sms = current_sms(), splits = fp8_small_splits(g.M, g.N, g.K, glu);
+  const int sms = current_sms();
+  splits = fp8_small_splits(g.M, g.N, g.K, glu);
   const int64_t steps = cdiv(g.K, 128), ctas = cdiv(g.N, 128) * cdiv(g.M, 128) * splits;
   const int tile_rounds = rounds(cdiv(g.M, 256) * cdiv(g.N, glu ? 128 : 256), sms / 2);
   const float tiles = (glu ? 4.9f + 0.31f * steps * tile_rounds : 4.4f + 0.285f * steps * tile_rounds);
   const float small = glu ? rounds(ctas, sms) * (2.9f + 0.045f * token_tile(g.M) + 0.45f * cdiv(steps, splits) + 0.8f * log2_of(splits))
                           : rounds(ctas, 2 * sms) * (3.f + 0.48f * cdiv(steps, splits) + log2_of(splits));
   const bool fits = cdiv(g.M, 128) <= 65535;      // its grid has the token tiles in y
-  const bool few = !g.out_f32 && fits && small < tiles;
+  return !g.out_f32 && fits && small < tiles;
+}
+// A as codes, or (g.x) as bf16, which a kernel of its own puts into the place that g.A names unless the product can do it on the way.
+cudaError_t fp8_product(Fp8Gemm g, cudaStream_t st) {
+  int splits;
+  const bool few = fp8_few(g, splits);
   if (g.x && !(few && g.M <= 16 && g.K % 8 == 0 && g.ldx % 8 == 0 && aligned_to(g.x, 16))) {
     if (const cudaError_t e = launch_quantize(g.x, g.ldx, GROUTER_BF16, g.M, g.K, false, const_cast<void*>(g.A.codes), const_cast<void*>(g.A.scales),
                                               nullptr, nullptr, nullptr, st))
@@ -258,26 +269,32 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
                       st) != cudaSuccess)
     return GROUTER_ERR_CUDA;
   if (db && tiles > 1 && launch_sum_rows(sums, tiles, N, db, N, nullptr, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-  Fp8Gemm g{};
-  g.status = status;
-  if (dx) {
-    g.A = {ws, ws + w.row_scales}; g.B = {Wt, Wt_scales}; g.C = dx; g.M = T; g.N = K; g.K = N;
-    if (fp8_product(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  Fp8Gemm to_x{}, to_w{};
+  to_x.A = {ws, ws + w.row_scales}; to_x.B = {Wt, Wt_scales}; to_x.C = dx; to_x.M = T; to_x.N = K; to_x.K = N; to_x.status = status;
+  to_w.A = {ws + w.cols, ws + w.col_scales}; to_w.B = {xt, xt_scales}; to_w.C = dW; to_w.M = N; to_w.N = K; to_w.K = T; to_w.status = status;
+  to_w.out_f32 = dW_dtype == GROUTER_F32;
+  // Both on tiles go in one launch: the gradient of a weight has few of them, of long contractions, and leaves pairs of SMs without one, which
+  // work on dx's meanwhile (16384 tokens, 1408 x 2048: 48 tiles of 128 steps and 512 of 11 on 74 pairs: the backward pass 105 us, one after the other 112).
+  int splits;
+  const bool together = dx && dW && !fp8_few(to_x, splits);
+  const Fp8Pieces pieces = fp8_pieces(T, K, N, together);
+  if (pieces.count > 1) {
+    to_w.C = ws + w.pieces;
+    to_w.out_f32 = 1;
+    to_w.pieces = pieces.count;
+    to_w.piece_steps = pieces.steps;
   }
-  if (dW) {
-    g.A = {ws + w.cols, ws + w.col_scales}; g.B = {xt, xt_scales}; g.C = dW; g.M = N; g.N = K; g.K = T; g.out_f32 = dW_dtype == GROUTER_F32;
-    g.waits_at_end = dx != nullptr;          // of dx's product, which waited for the codes, it needs nothing
-    const Fp8Pieces pieces = fp8_pieces(T, K, N);
-    if (pieces.count > 1) {
-      g.C = ws + w.pieces;
-      g.out_f32 = 1;
-      g.pieces = pieces.count;
-      g.piece_steps = pieces.steps;
-    }
-    if (launch_fp8_gemm(g, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-    if (pieces.count > 1 && launch_sum_pieces(ws + w.pieces, pieces.count, (int64_t)N * K, (int64_t)fp8_piece_rows(N) * K, dW, dW_dtype, st) != cudaSuccess)
-      return GROUTER_ERR_CUDA;
+  if (together) {
+    const bool w_first = pieces.steps >= cdiv(N, 128);
+    if (launch_fp8_gemms(w_first ? to_w : to_x, w_first ? to_x : to_w, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+  } else {
+    if (dx && fp8_product(to_x, st) != cudaSuccess) return GROUTER_ERR_CUDA;
+    to_w.waits_at_end = dx != nullptr;       // of dx's product, which waited for the codes, it needs nothing
+    if (dW && launch_fp8_gemm(to_w, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
+  if (dW && pieces.count > 1 &&
+      launch_sum_pieces(ws + w.pieces, pieces.count, (int64_t)N * K, (int64_t)fp8_piece_rows(N) * K, dW, dW_dtype, st) != cudaSuccess)
+    return GROUTER_ERR_CUDA;
   return GROUTER_OK;
 }
 

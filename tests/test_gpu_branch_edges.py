@@ -120,3 +120,16 @@ def test_weights_with_a_scale_for_every_row(T, K, N):
     want = g @ Wtr.T
     assert (np.abs(f64(dx) - want) <= (N / 16 + 32) * U * (np.abs(g) @ np.abs(Wtr).T) + 2.0 ** -8 * np.abs(want)).all()
     B.check_status()
+
+
+@pytest.mark.parametrize("T,K,N", [(700, 264, 2056), (1500, 1032, 4104), (9000, 1544, 2056), (40000, 72, 264), (6001, 2056, 24)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_both_gradients_in_one_launch(T, K, N, dtype):
+    """Either product may be the one with the longer contraction, with fewer tiles than pairs of SMs or several rounds; dx does not depend on
+    whether dW is wanted, and bounds as for each alone."""
+    from paper_2603_06626_b200 import binding as B
+    from tests.test_gpu_fp8 import _backward
+    _backward(T, K, N, dtype=dtype, bias=False)
+    dy, W = _bf(T, T, N), B.quantize_fp8(_bf(1, N, K, std=K ** -0.5), square=True, rows=False, transposed=True)[1]
+    xt = B.quantize_fp8(_bf(2, T, K), rows=False, transposed=True)[1]
+    assert torch.equal(B.linear_fp8_backward(dy, xt, W, dW_dtype=dtype)[0], B.linear_fp8_backward(dy, None, W, want_dW=False)[0])
