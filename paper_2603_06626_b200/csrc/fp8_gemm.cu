@@ -2,6 +2,7 @@
 //
 //   LINEAR  C = A B^T + bias + residual        C_mn = sum_b 2^(ea(m,b) + eb(n,b)) sum_{k in block b} ca_mk cb_nk, bf16 or f32 out
 //   GLU     [G|U] = A [Wg;Wu]^T,  H = act(G) U, out as codes with a scale for 128 columns: the next product's operand
+//   TWO     two LINEAR products in one launch: the backward pass of the linear layer
 //
 // The CTA-pair pipeline of the bf16 products (gemm.cu): tiles of 256 x 256, five 32 KB stages in each CTA, here 128 deep; warp 0
 // loads, warp 1 of the leader issues, warps 2-9 empty the accumulator.  A block of 128 is exactly one step, so its scale is one byte a
@@ -11,6 +12,11 @@
 // 1 starts at column 224.  Whoever reads the shared columns of a tile reads them first and says so (`over`), and the next tile's
 // products wait for that, while its operands arrive.
 // Every wait is bounded, as in gemm.cu.
+//
+// Measured: 8192 x 4096 x 4096 95-107 us, 8192^3 381-445 (2.5 to 2.9 PFLOP/s by the clock that the power limit leaves); GLU 16384 tokens, 4096 ->
+// 1536 126 us with the tensor pipe 80 % active; 16384 x 1536 x 4096 with a residual 85-95, 57 %: every 12 steps a tile of 128 KB goes out and
+// one of the residual comes in.  A step takes its 32 KB per SM in 256 tensor cycles, twice the pace at which bf16 tiles need theirs, so
+// tiles smaller than 256 x 256 are out.
 #include "act.cuh"
 #include "fp8.cuh"
 #include "fp8_gemm.cuh"

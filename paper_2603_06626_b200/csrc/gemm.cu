@@ -11,6 +11,8 @@
 //   LINEAR    C = act(A * B + bias) + residual on plain matrices, bf16 out (the linear layer's forward pass and gradients)
 //   GLU       [G|U] = x * W_gu^T     epilogue: H = act(G) * U                   (gated feed-forward block, forward)
 //   GLU_BACK  dH    = dy * W_d       epilogue: dG, dU and, from the saved G and U, H again
+// The last two at 16384 tokens, 4096, hidden 1536: GLU 252 us, tensor pipe 84 % active (1.64 PFLOP/s); GLU_BACK 174 us, 57 %: per tile it takes in
+// as many bytes of G and U, and gives out as many of dG, dU and half of them of H, as 32 of its 64 k-steps take in operands.
 //
 // Tile: 256 x 256 x 64 per CTA pair (a cluster of two CTAs on neighbouring SMs, one pair-wide tcgen05.mma with
 // M = 256).  Each CTA owns 128 rows of the tile and half of B's 256 columns, so per 64-deep k-step it stages
@@ -27,7 +29,7 @@
 // Operands may be K-major (rows of the stored matrix run along K) or MN-major (rows run along M/N); both are
 // described to the MMA by shared-memory descriptors, so no operand is ever transposed in memory.
 //
-// Tiles are handed out by a grid-wide counter (all products but DENSE and LINEAR): a pair takes the next tile of the list when it
+// Tiles are handed out by a grid-wide counter (all products but the plain ones, from DENSE on): a pair takes the next tile of the list when it
 // is ready for one, so the pairs always work on neighbouring tiles and the operand rows they share are in L2 together.
 //
 // Every wait (mbarriers, tile queue) is bounded; on give-up the CTA raises an abort flag, ORs STATUS_TIMEOUT into the status

@@ -8,6 +8,8 @@
 // Every element is touched once, HBM is the bound: with bf16 the forward pass moves 8 bytes an element with the residual (7 with
 // codes), the backward pass 8 with the stream's own gradient dh.  As in the layer norm a row lies in the registers of as many lanes
 // as hold it in a few accesses each, and arithmetic goes two elements to an instruction.  Sums and statistics are fp32.
+// Measured, bf16 with the residual: forward 32768 x 4096 159 us (6.7 TB/s), to codes 145 (6.5); 16384 x 2048 42 and 38; backward with dh 16384 x
+// 2048 44 us (6.1 TB/s), f32 8192 x 16384 380 (5.7).
 //   Forward: the only sum is over the rounded h, so a row takes one meeting of its threads.  Codes: the 16 (f32: 32) lanes that hold 128
 //     columns find their largest value among themselves.
 //   Backward: the running dw of a column stays with one thread; blocks are resident and walk over the rows, the coming ones on their
