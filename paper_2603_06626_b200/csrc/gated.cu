@@ -107,6 +107,8 @@ int fp8_check(int32_t T, int32_t K, int32_t N) {
 // 7.2; 4096 -> 4096, 384 tokens 13 and 15.  Gated in 8 bits d 4096, hidden 1536: 128 tokens 12.7 and 14.5, 512 tokens 16.2 and 15.9;
 // d 1024, hidden 2816: 64 tokens 7.5 and 9.5, 128 tokens 11.7 and 7.8.  In bf16 the same: 128 tokens 17 and 26.5, 1024 tokens 34 and 26;
 // 64 tokens 6.5 and 9.4, 256 tokens 11.0 and 9.7.
+// Up to 64 tokens it always is, by more the larger the weight (whole gated block, d 2048, hidden 8192: 8 tokens 23 and 65 us, 64 tokens 30 and 33;
+// d 8192, hidden 8192: 66 and 90, 73 and 82; 8 bits 4096 -> 22016: 13 and 39, 15 and 17).
 inline int rounds(int64_t tiles, int places) { return (int)((tiles + places - 1) / (places > 0 ? places : 1)); }
 inline int log2_of(int s) { return s >= 8 ? 3 : s >= 4 ? 2 : s >= 2 ? 1 : 0; }
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -123,7 +125,7 @@ bool fp8_few(const Fp8Gemm& g, int& splits) {
   const float small = glu ? rounds(ctas, sms) * (2.9f + 0.045f * token_tile(g.M) + 0.45f * cdiv(steps, splits) + 0.8f * log2_of(splits))
                           : rounds(ctas, 2 * sms) * (3.f + 0.48f * cdiv(steps, splits) + log2_of(splits));
   const bool fits = cdiv(g.M, 128) <= 65535;      // its grid has the token tiles in y
-  return !g.out_f32 && fits && small < tiles;
+  return !g.out_f32 && fits && (g.M <= 64 || small < tiles);
 }
 // A as codes, or (g.x) as bf16, which a kernel of its own puts into the place that g.A names unless the product can do it on the way.
 cudaError_t fp8_product(Fp8Gemm g, cudaStream_t st) {
@@ -142,7 +144,7 @@ cudaError_t gated_product(const GatedGemm& g, cudaStream_t st) {
   const int64_t steps = cdiv(g.K, 64), ctas = cdiv(2 * (int64_t)g.H, 128) * cdiv(g.T, 128) * splits;
   const float tiles = 5.f + 0.3f * steps * rounds(cdiv(g.T, 256) * cdiv(g.H, 128), sms / 2);
   const float small = rounds(ctas, 2 * sms) * (2.f + 0.03f * token_tile(g.T) + 0.5f * cdiv(steps, splits));
-  return cdiv(g.T, 128) <= 65535 && small < tiles ? launch_gated_small(g, splits, st) : launch_gated_gemm(g, st);
+  return cdiv(g.T, 128) <= 65535 && (g.T <= 64 || small < tiles) ? launch_gated_small(g, splits, st) : launch_gated_gemm(g, st);
 }
 
 }  // namespace

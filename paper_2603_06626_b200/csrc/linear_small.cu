@@ -356,13 +356,14 @@ cudaError_t launch_linear_small(const LinearGemm& g, int splits, cudaStream_t st
   return g.b_mn ? small_by_tokens<true, false>(g, splits, st) : small_by_tokens<false, false>(g, splits, st);
 }
 
-// As linear_small_splits, but one CTA an SM: each streams twice as long (24 tiles of 64 tokens, 4096 deep: in 4 cuts 11.7 us, in 8 13.0; 128 tokens
-// 14.0 and 17.5; one token 8.9 and 8.4).
+// As linear_small_splits, but one CTA an SM, which streams twice as long (24 tiles of 64 tokens, 4096 deep: in 4 cuts 11.7 us, in 8 13.0; 128 tokens
+// 14.0 and 17.5; one token 8.9 and 8.4), unless that leaves a CTA 64 steps or more (d 8192, hidden 4096, both products: 128 tokens in 2 cuts 55
+// us, in 4 48; hidden 8192 in 1 cut 93, in 2 79; one token 69 and 66; 2048 deep, 128 tiles, 8 tokens in 1 cut 23.2, in 2 24.3).
 int gated_small_splits(int T, int H, int K) {
   const int64_t tiles = (int64_t)((2 * (int64_t)H + LS_BM - 1) / LS_BM) * ((T + 127) / 128);
-  const int nk = (K + LS_BK - 1) / LS_BK, room = current_sms();
+  const int nk = (K + LS_BK - 1) / LS_BK, sms = current_sms();
   int s = 1;
-  while (s < LS_MAX_SPLITS && tiles * s * 2 <= room && nk >= 8 * s) s *= 2;
+  while (s < LS_MAX_SPLITS && tiles * s * 2 <= (nk >= 64 * s ? 2 * sms : sms) && nk >= 8 * s) s *= 2;
   return s;
 }
 
