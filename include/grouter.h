@@ -448,9 +448,10 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, con
 /* Its backward pass from dy [T,N] bf16 (contiguous), which is put into 8 bits here, by rows for dx and by columns for dW:
  *   dx = q(dy) W [T,K] bf16      dW = q(dy^T) x [N,K] of dW_dtype      db = sum over tokens of dy [N] f32 (not in 8 bits)
  *   xt, Wt: codes and scales of the transposed matrices, x^T [K,T] for dW and W^T [K,N] for dx (grouter_quantize_fp8's codes_t)
- * Outputs that are not wanted are NULL (at least one is wanted).  K and N multiples of 8.  Results are bit-reproducible.  Outputs must not
- * overlap the inputs.  workspace: grouter_linear_fp8_bwd_workspace_bytes(T, K, N) bytes (of the current device), 256-byte aligned.  T = 0
- * zeroes dW and db.  Errors as above. */
+ * Outputs that are not wanted are NULL (at least one is wanted).  K and N multiples of 8.  Results are bit-reproducible (dW's
+ * sums may be cut differently in a call that wants dx too).  Outputs must not overlap the inputs.  workspace:
+ * grouter_linear_fp8_bwd_workspace_bytes(T, K, N) bytes (of the current device), 256-byte aligned.  T = 0 zeroes dW and db.  Errors as
+ * above. */
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N);
 int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales, const void* Wt, const void* Wt_scales, int32_t T, int32_t K, int32_t N,
                            void* dx, void* dW, int32_t dW_dtype, float* db, void* workspace, int32_t* status, void* stream);

@@ -597,6 +597,12 @@ def _bytes(fn, index: int, *args) -> int:
         return fn(*args)
 
 
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name: str, index: int, *sizes: int) -> int:
+    """_bytes of a call that is made over and over with the same sizes."""
+    return _bytes(getattr(load_library(), name), index, *sizes)
+
+
 _status_words = {}
 _status_lock = threading.Lock()
 
@@ -917,7 +923,7 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
     dx = torch.empty_like(dy)
     if dw is None:
         dw = h.new_empty(d, dtype=f32)
-    ws = h.new_empty(_bytes(lib.grouter_rmsnorm_bwd_workspace_bytes, dev, T, d), dtype=torch.uint8)
+    ws = h.new_empty(_workspace_bytes("grouter_rmsnorm_bwd_workspace_bytes", dev, T, d), dtype=torch.uint8)
     _call(lib.grouter_rmsnorm_bwd, "grouter_rmsnorm_bwd", dev, dy.data_ptr(), h.data_ptr(), ldh, _ptr(dh), weight.data_ptr(), rstd.data_ptr(), T, d,
           dt, wt, dx.data_ptr(), dw.data_ptr(), ws.data_ptr())
     return dx, dw
@@ -1026,16 +1032,6 @@ def _fp8_input(what: str, x, cols: int, on: torch.device):
     return x.shape[0], x.data_ptr(), None, _row_stride(what, x)
 
 
-@functools.lru_cache(maxsize=1024)
-def _linear_fp8_bytes(T: int, K: int) -> int:
-    return load_library().grouter_linear_fp8_fwd_workspace_bytes(T, K)
-
-
-@functools.lru_cache(maxsize=1024)
-def _gated_fp8_bytes(T: int, d: int, H: int) -> int:
-    return load_library().grouter_gated_ffn_fp8_fwd_workspace_bytes(T, d, H)
-
-
 def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
                status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """grouter_linear_fp8_fwd: x W^T + bias + residual, x [T,K] as Fp8Blocks or bf16 (rows may be strided; put into 8 bits by this call),
@@ -1053,7 +1049,7 @@ def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: O
         _expect("residual", residual, (T, N), bf, like=codes)
         _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
-    ws = None if ps is not None else x.new_empty(_linear_fp8_bytes(T, K), dtype=torch.uint8)
+    ws = None if ps is not None else x.new_empty(_workspace_bytes("grouter_linear_fp8_fwd_workspace_bytes", dev, T, K), dtype=torch.uint8)
     y = codes.new_empty((T, N), dtype=bf)
     _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, px, ps, ld, codes.data_ptr(), W.scales.data_ptr(),
           None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(), T, K, N, y.data_ptr(),
@@ -1098,7 +1094,7 @@ def linear_fp8_backward(dy: torch.Tensor, xt: Optional[Fp8Blocks], Wt: Optional[
         dW = dy.new_empty((N, K), dtype=dW_dtype)
     if db is None and want_bias:
         db = dy.new_empty(N, dtype=torch.float32)
-    ws = dy.new_empty(_bytes(lib.grouter_linear_fp8_bwd_workspace_bytes, dev, T, K, N), dtype=torch.uint8)
+    ws = dy.new_empty(_workspace_bytes("grouter_linear_fp8_bwd_workspace_bytes", dev, T, K, N), dtype=torch.uint8)
     codes = lambda q: (None, None) if q is None else (q.codes.data_ptr(), q.scales.data_ptr())  # noqa: E731
     _call(lib.grouter_linear_fp8_bwd, "grouter_linear_fp8_bwd", dev, dy.data_ptr(), *codes(xt), *codes(Wt), T, K, N, _ptr(dx), _ptr(dW),
           F32 if dW_dtype == torch.float32 else BF16, _ptr(db), ws.data_ptr(), _status_ptr(status, dev))
@@ -1163,7 +1159,7 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, W_gu: torch.Tensor, W_
     if want_dW:
         dW_gu = x.new_empty((2 * H, d), dtype=dW_dtype) if dW_gu is None else dW_gu
         dW_d = x.new_empty((d, H), dtype=dW_dtype) if dW_d is None else dW_d
-    ws = x.new_empty(_bytes(lib.grouter_gated_ffn_bwd_workspace_bytes, dev, T, d, H), dtype=torch.uint8)
+    ws = x.new_empty(_workspace_bytes("grouter_gated_ffn_bwd_workspace_bytes", dev, T, d, H), dtype=torch.uint8)
     _call(lib.grouter_gated_ffn_bwd, "grouter_gated_ffn_bwd", dev, dy.data_ptr(), x.data_ptr(), W_gu.data_ptr(), W_d.data_ptr(), pre.data_ptr(), T, d, H,
           act, _ptr(dx), _ptr(dW_gu), _ptr(dW_d), F32 if dW_dtype == torch.float32 else BF16, ws.data_ptr(), _status_ptr(status, dev))
     return dx, dW_gu, dW_d
@@ -1190,7 +1186,7 @@ def gated_ffn_fp8(x, W_g: Fp8Blocks, W_u: Fp8Blocks, W_d: Fp8Blocks, act: int = 
         _expect("residual", residual, (T, d), bf, like=codes)
         _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
-    ws = codes.new_empty(_gated_fp8_bytes(T, d, H), dtype=torch.uint8)
+    ws = codes.new_empty(_workspace_bytes("grouter_gated_ffn_fp8_fwd_workspace_bytes", dev, T, d, H), dtype=torch.uint8)
     y = codes.new_empty((T, d), dtype=bf)
     _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, px, ps, ld, W_g.codes.data_ptr(), W_g.scales.data_ptr(),
           W_u.codes.data_ptr(), W_u.scales.data_ptr(), codes.data_ptr(), W_d.scales.data_ptr(), None if residual is None else residual.data_ptr(),

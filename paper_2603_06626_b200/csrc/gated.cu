@@ -100,7 +100,7 @@ int fp8_check(int32_t T, int32_t K, int32_t N) {
   return GROUTER_OK;
 }
 
-// Which of the two kernels is ahead: both sides in microseconds, fitted to measurements over 1 to 4096 tokens and weights of 128 x 128 to
+// Which of the two kernels is ahead: both sides in microseconds, fitted to measurements over 65 to 4096 tokens and weights of 128 x 128 to
 // 8192 x 4096.  Tiles of 256 x 256 (or 128 hidden columns) on CTA pairs: a start and the steps of every round of the pairs.  Few tokens: for
 // every round of the SMs a start, the steps of one cut, a meeting of the cluster and, where h is formed, the tokens of a tile.
 // Measured (few tokens against tiles): 8 bits 4096 -> 1536, 128 tokens 6.9 and 13.8 us, 1024 tokens 18 and 14; 1024 -> 2816, 512 tokens 7.7 and
