@@ -932,17 +932,58 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
 class Fp8Blocks:
     """A matrix [rows, cols] in 8 bits: codes [rows, cols rounded up to 16] float8_e4m3fn, zeros behind the last column, and scales, a
     power of two for 128 neighbours of a row, as uint8 exponents + 127 [ceil(rows / 128), ceil(cols / 512), 32, 4, 4]: the scale of row r,
-    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h)."""
+    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h).  They are looked at when they are
+    set, not in every call: neither tensor's storage, shape or strides are to be changed afterwards."""
 
-    __slots__ = ("codes", "scales", "cols")
+    __slots__ = ("_codes", "_scales", "_cols", "_is")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
-        self.codes, self.scales, self.cols = codes, scales, int(cols)
+        self._codes, self._scales, self._cols = codes, scales, int(cols)
+        self._look()
+
+    def _look(self) -> None:
+        codes, scales, cols = self._codes, self._scales, self._cols
+        rows = codes.shape[0] if codes.dim() == 2 else -1
+        # the matrix that they hold, (rows, columns, device), or None: then a call that is given this says what is wrong
+        self._is = (rows, cols, codes.device) if (
+            rows >= 0 and cols >= 0 and codes.shape[1] == (cols + 15) // 16 * 16 and codes.dtype == torch.float8_e4m3fn and codes.is_contiguous() and
+            scales.shape == self.scale_shape(rows, cols) and scales.dtype == torch.uint8 and scales.device == codes.device and
+            scales.is_contiguous()) else None
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Fp8Blocks":
-        return cls(torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device),
-                   torch.empty(cls.scale_shape(rows, cols), dtype=torch.uint8, device=device), cols)
+        q = cls.__new__(cls)
+        q._codes = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
+        q._scales = torch.empty(cls.scale_shape(rows, cols), dtype=torch.uint8, device=device)
+        q._cols, q._is = cols, (rows, cols, q._codes.device)
+        return q
+
+    @property
+    def codes(self) -> torch.Tensor:
+        return self._codes
+
+    @codes.setter
+    def codes(self, to: torch.Tensor) -> None:
+        self._codes = to
+        self._look()
+
+    @property
+    def scales(self) -> torch.Tensor:
+        return self._scales
+
+    @scales.setter
+    def scales(self, to: torch.Tensor) -> None:
+        self._scales = to
+        self._look()
+
+    @property
+    def cols(self) -> int:
+        return self._cols
+
+    @cols.setter
+    def cols(self, to: int) -> None:
+        self._cols = int(to)
+        self._look()
 
     @staticmethod
     def scale_shape(rows: int, cols: int):
@@ -973,10 +1014,9 @@ def _expect_fp8(what: str, q: Optional[Fp8Blocks], rows: int, cols: int, on: tor
         return
     if not isinstance(q, Fp8Blocks):
         raise TypeError(f"{what}: Fp8Blocks expected, got {type(q).__name__}")
-    c, s = q.codes, q.scales
-    if (q.cols == cols and c.shape == (rows, (cols + 15) // 16 * 16) and c.dtype == _E4M3 and c.device == on and c.is_contiguous() and
-            s.shape == ((rows + 127) // 128, (cols + 511) // 512, 32, 4, 4) and s.dtype == torch.uint8 and s.device == on and s.is_contiguous()):
+    if q._is == (rows, cols, on):
         return
+    c, s = q.codes, q.scales
     if q.cols != cols:
         raise ValueError(f"{what}: {cols} columns expected, got {q.cols}")
     where = torch.empty(0, device=on)
@@ -1022,14 +1062,14 @@ def _fp8_input(what: str, x, cols: int, on: torch.device):
     """(rows, address, address of the scales or None, row stride) of an argument that is Fp8Blocks or a bf16 matrix whose rows may be
     strided, with `cols` columns on device `on`; others raise."""
     if isinstance(x, Fp8Blocks):
-        rows = x.codes.shape[0]
+        rows = x._codes.shape[0]
         _expect_fp8(what, x, rows, cols, on)
-        return rows, x.codes.data_ptr(), x.scales.data_ptr(), 0
+        return rows, x._codes.data_ptr(), x._scales.data_ptr(), 0
     if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16:
         raise TypeError(f"{what}: Fp8Blocks or a bfloat16 matrix expected")
     if x.dim() != 2 or x.shape[1] != cols or x.device != on:
         raise ValueError(f"{what}: a matrix of {cols} columns on {on} is expected, got {tuple(x.shape)} on {x.device}")
-    return x.shape[0], x.data_ptr(), None, _row_stride(what, x)
+    return x.shape[0], x.data_ptr(), None, cols if x.is_contiguous() else _row_stride(what, x)
 
 
 def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
@@ -1039,7 +1079,7 @@ def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: O
     lib = load_library()
     if not isinstance(W, Fp8Blocks):
         raise TypeError(f"W: Fp8Blocks expected, got {type(W).__name__}")
-    codes = W.codes
+    codes = W._codes
     on, K, bf = codes.device, W.cols, torch.bfloat16
     N = codes.shape[0]
     _expect_fp8("W", W, N, K, on)
@@ -1050,8 +1090,8 @@ def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: O
         _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
     ws = None if ps is not None else x.new_empty(_workspace_bytes("grouter_linear_fp8_fwd_workspace_bytes", dev, T, K), dtype=torch.uint8)
-    y = codes.new_empty((T, N), dtype=bf)
-    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, px, ps, ld, codes.data_ptr(), W.scales.data_ptr(),
+    y = codes.new_empty((T, N), dtype=bf) if residual is None else torch.empty_like(residual)
+    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, px, ps, ld, codes.data_ptr(), W._scales.data_ptr(),
           None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(), T, K, N, y.data_ptr(),
           None if ws is None else ws.data_ptr(), _status_ptr(status, dev))
     return y
@@ -1175,7 +1215,7 @@ def gated_ffn_fp8(x, W_g: Fp8Blocks, W_u: Fp8Blocks, W_d: Fp8Blocks, act: int = 
         raise TypeError(f"W_d: Fp8Blocks expected, got {type(W_d).__name__}")
     if W_g is None or W_u is None:
         raise TypeError("W_g, W_u: Fp8Blocks expected")
-    codes = W_d.codes
+    codes = W_d._codes
     on, H, bf = codes.device, W_d.cols, torch.bfloat16
     d = codes.shape[0]
     _expect_fp8("W_g", W_g, H, d, on)
@@ -1187,9 +1227,9 @@ def gated_ffn_fp8(x, W_g: Fp8Blocks, W_u: Fp8Blocks, W_d: Fp8Blocks, act: int = 
         _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
     ws = codes.new_empty(_workspace_bytes("grouter_gated_ffn_fp8_fwd_workspace_bytes", dev, T, d, H), dtype=torch.uint8)
-    y = codes.new_empty((T, d), dtype=bf)
-    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, px, ps, ld, W_g.codes.data_ptr(), W_g.scales.data_ptr(),
-          W_u.codes.data_ptr(), W_u.scales.data_ptr(), codes.data_ptr(), W_d.scales.data_ptr(), None if residual is None else residual.data_ptr(),
+    y = codes.new_empty((T, d), dtype=bf) if residual is None else torch.empty_like(residual)
+    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, px, ps, ld, W_g._codes.data_ptr(), W_g._scales.data_ptr(),
+          W_u._codes.data_ptr(), W_u._scales.data_ptr(), codes.data_ptr(), W_d._scales.data_ptr(), None if residual is None else residual.data_ptr(),
           T, d, H, act, y.data_ptr(), ws.data_ptr(), _status_ptr(status, dev))
     return y
 

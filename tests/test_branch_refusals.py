@@ -182,3 +182,21 @@ def test_the_dense_block_names_the_size_it_refuses():
         DenseBlock(256, 200, device="cpu")
     with pytest.raises(ValueError, match="n:"):
         Projection8(256, 8, device="cpu")
+
+
+def test_a_matrix_in_8_bits_is_looked_at_whenever_a_part_of_it_is_set():
+    on, q = torch.device("cpu"), _blocks(3, 40)
+    assert q.shape == (3, 40) and q.rows == 3 and q.cols == 40 and q.codes.shape == (3, 48)
+    for good in (q, B.Fp8Blocks(q.codes, q.scales, 40), _blocks(3, 40, codes=q.codes.clone(), scales=q.scales.clone())):
+        B._expect_fp8("q", good, 3, 40, on)
+        _raises(ValueError, lambda: B._expect_fp8("q", good, 4, 40, on))
+        _raises(ValueError, lambda: B._expect_fp8("q", good, 3, 41, on))
+    wide = torch.empty(3, 96, dtype=torch.float8_e4m3fn)
+    for parts in (dict(codes=q.codes[:2]), dict(codes=wide[:, :48]), dict(codes=q.codes.view(torch.uint8)), dict(codes=q.codes[0]), dict(cols=41),
+                  dict(scales=q.scales[..., :2]), dict(scales=q.scales.transpose(3, 4)), dict(scales=q.scales.int()), dict(scales=q.scales[0])):
+        made = B.Fp8Blocks(**{"codes": q.codes, "scales": q.scales, "cols": 40, **parts})
+        for bad in (made, _blocks(3, 40, **parts)):
+            _raises((ValueError, TypeError), lambda: B._expect_fp8("q", bad, 3, 40, on))
+    back = _blocks(3, 40, cols=41)
+    back.cols = 40
+    B._expect_fp8("q", back, 3, 40, on)
