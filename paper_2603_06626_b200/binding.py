@@ -932,30 +932,22 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
 class Fp8Blocks:
     """A matrix [rows, cols] in 8 bits: codes [rows, cols rounded up to 16] float8_e4m3fn, zeros behind the last column, and scales, a
     power of two for 128 neighbours of a row, as uint8 exponents + 127 [ceil(rows / 128), ceil(cols / 512), 32, 4, 4]: the scale of row r,
-    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h).  They are looked at when they are
-    set, not in every call: neither tensor's storage, shape or strides are to be changed afterwards."""
+    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h).  They are looked at by the first
+    call that is given them, and again after one of them is set, not in every call: neither tensor's storage, shape or strides are to be
+    changed in place."""
 
     __slots__ = ("_codes", "_scales", "_cols", "_is")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         self._codes, self._scales, self._cols = codes, scales, int(cols)
-        self._look()
-
-    def _look(self) -> None:
-        codes, scales, cols = self._codes, self._scales, self._cols
-        rows = codes.shape[0] if codes.dim() == 2 else -1
-        # the matrix that they hold, (rows, columns, device), or None: then a call that is given this says what is wrong
-        self._is = (rows, cols, codes.device) if (
-            rows >= 0 and cols >= 0 and codes.shape[1] == (cols + 15) // 16 * 16 and codes.dtype == torch.float8_e4m3fn and codes.is_contiguous() and
-            scales.shape == self.scale_shape(rows, cols) and scales.dtype == torch.uint8 and scales.device == codes.device and
-            scales.is_contiguous()) else None
+        self._is = None           # what they were found to hold, (rows, columns, device)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Fp8Blocks":
         q = cls.__new__(cls)
         q._codes = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
         q._scales = torch.empty(cls.scale_shape(rows, cols), dtype=torch.uint8, device=device)
-        q._cols, q._is = cols, (rows, cols, q._codes.device)
+        q._cols, q._is = cols, None
         return q
 
     @property
@@ -965,7 +957,7 @@ class Fp8Blocks:
     @codes.setter
     def codes(self, to: torch.Tensor) -> None:
         self._codes = to
-        self._look()
+        self._is = None
 
     @property
     def scales(self) -> torch.Tensor:
@@ -974,7 +966,7 @@ class Fp8Blocks:
     @scales.setter
     def scales(self, to: torch.Tensor) -> None:
         self._scales = to
-        self._look()
+        self._is = None
 
     @property
     def cols(self) -> int:
@@ -983,7 +975,7 @@ class Fp8Blocks:
     @cols.setter
     def cols(self, to: int) -> None:
         self._cols = int(to)
-        self._look()
+        self._is = None
 
     @staticmethod
     def scale_shape(rows: int, cols: int):
@@ -1016,7 +1008,11 @@ def _expect_fp8(what: str, q: Optional[Fp8Blocks], rows: int, cols: int, on: tor
         raise TypeError(f"{what}: Fp8Blocks expected, got {type(q).__name__}")
     if q._is == (rows, cols, on):
         return
-    c, s = q.codes, q.scales
+    c, s = q._codes, q._scales
+    if (q._cols == cols and c.shape == (rows, (cols + 15) // 16 * 16) and c.dtype == _E4M3 and c.device == on and c.is_contiguous() and
+            s.shape == ((rows + 127) // 128, (cols + 511) // 512, 32, 4, 4) and s.dtype == torch.uint8 and s.device == on and s.is_contiguous()):
+        q._is = (rows, cols, on)
+        return
     if q.cols != cols:
         raise ValueError(f"{what}: {cols} columns expected, got {q.cols}")
     where = torch.empty(0, device=on)
