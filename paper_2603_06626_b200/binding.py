@@ -932,50 +932,18 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
 class Fp8Blocks:
     """A matrix [rows, cols] in 8 bits: codes [rows, cols rounded up to 16] float8_e4m3fn, zeros behind the last column, and scales, a
     power of two for 128 neighbours of a row, as uint8 exponents + 127 [ceil(rows / 128), ceil(cols / 512), 32, 4, 4]: the scale of row r,
-    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h).  They are looked at by the first
-    call that is given them, and again after one of them is set, not in every call: neither tensor's storage, shape or strides are to be
-    changed in place."""
+    block b lies at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4] (include/grouter.h).  Every call that is given one looks at the
+    layout of both tensors."""
 
-    __slots__ = ("_codes", "_scales", "_cols", "_is")
+    __slots__ = ("codes", "scales", "cols")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
-        self._codes, self._scales, self._cols = codes, scales, int(cols)
-        self._is = None           # what they were found to hold, (rows, columns, device)
+        self.codes, self.scales, self.cols = codes, scales, int(cols)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Fp8Blocks":
-        q = cls.__new__(cls)
-        q._codes = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
-        q._scales = torch.empty(cls.scale_shape(rows, cols), dtype=torch.uint8, device=device)
-        q._cols, q._is = cols, None
-        return q
-
-    @property
-    def codes(self) -> torch.Tensor:
-        return self._codes
-
-    @codes.setter
-    def codes(self, to: torch.Tensor) -> None:
-        self._codes = to
-        self._is = None
-
-    @property
-    def scales(self) -> torch.Tensor:
-        return self._scales
-
-    @scales.setter
-    def scales(self, to: torch.Tensor) -> None:
-        self._scales = to
-        self._is = None
-
-    @property
-    def cols(self) -> int:
-        return self._cols
-
-    @cols.setter
-    def cols(self, to: int) -> None:
-        self._cols = int(to)
-        self._is = None
+        return cls(torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device),
+                   torch.empty(cls.scale_shape(rows, cols), dtype=torch.uint8, device=device), cols)
 
     @staticmethod
     def scale_shape(rows: int, cols: int):
@@ -1000,24 +968,24 @@ class Fp8Blocks:
         return self.scales.permute(0, 3, 2, 1, 4).reshape(128 * a, 4 * b)[:rows, :(cols + 127) // 128]
 
 
-def _expect_fp8(what: str, q: Optional[Fp8Blocks], rows: int, cols: int, on: torch.device) -> None:
-    """Raises unless q (None passes) holds a matrix of this shape in the layout that the kernels read, on the device `on`."""
+def _expect_fp8(what: str, q: Optional[Fp8Blocks], rows: int, cols: int, on: torch.device):
+    """(codes, scales) of q, a matrix of this shape in the layout that the kernels read, on the device `on`; others raise.  (None, None) for
+    None.  The tensors that were looked at are the ones returned: a part that another thread sets meanwhile is not read by this call, and
+    what an in-place change did to one of them (resize_, t_, .data) is seen, because nothing is remembered."""
     if q is None:
-        return
+        return None, None
     if not isinstance(q, Fp8Blocks):
         raise TypeError(f"{what}: Fp8Blocks expected, got {type(q).__name__}")
-    if q._is == (rows, cols, on):
-        return
-    c, s = q._codes, q._scales
-    if (q._cols == cols and c.shape == (rows, (cols + 15) // 16 * 16) and c.dtype == _E4M3 and c.device == on and c.is_contiguous() and
-            s.shape == ((rows + 127) // 128, (cols + 511) // 512, 32, 4, 4) and s.dtype == torch.uint8 and s.device == on and s.is_contiguous()):
-        q._is = (rows, cols, on)
-        return
-    if q.cols != cols:
-        raise ValueError(f"{what}: {cols} columns expected, got {q.cols}")
+    c, s, has = q.codes, q.scales, q.cols
+    if (has == cols and c.shape == (rows, (cols + 15) // 16 * 16) and c.dtype is _E4M3 and c.device == on and c.is_contiguous() and
+            s.shape == ((rows + 127) // 128, (cols + 511) // 512, 32, 4, 4) and s.dtype is torch.uint8 and s.device == on and s.is_contiguous()):
+        return c, s
+    if has != cols:
+        raise ValueError(f"{what}: {cols} columns expected, got {has}")
     where = torch.empty(0, device=on)
     _expect(f"{what}: codes", c, (rows, (cols + 15) // 16 * 16), _E4M3, like=where)
     _expect(f"{what}: scales", s, Fp8Blocks.scale_shape(rows, cols), torch.uint8, like=where)
+    raise ValueError(f"{what}: codes or scales have another layout than expected")
 
 
 _E4M3 = torch.float8_e4m3fn
@@ -1045,27 +1013,26 @@ def dequantize_fp8(q: Fp8Blocks, dtype: torch.dtype = torch.bfloat16) -> torch.T
     lib = load_library()
     if not isinstance(q, Fp8Blocks):
         raise TypeError(f"q: Fp8Blocks expected, got {type(q).__name__}")
-    _expect_fp8("q", q, q.rows, q.cols, q.device)
     rows, cols = q.shape
-    y = torch.empty((rows, cols), dtype=dtype, device=q.device)
+    codes, scales = _expect_fp8("q", q, rows, cols, q.device)
+    y = torch.empty((rows, cols), dtype=dtype, device=codes.device)
     dt = _elt(y, "dtype")
-    dev = _device_index(q.device)
-    _call(lib.grouter_dequantize_fp8, "grouter_dequantize_fp8", dev, q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, cols, dt, y.data_ptr())
+    dev = _device_index(codes.device)
+    _call(lib.grouter_dequantize_fp8, "grouter_dequantize_fp8", dev, codes.data_ptr(), scales.data_ptr(), rows, cols, cols, dt, y.data_ptr())
     return y
 
 
 def _fp8_input(what: str, x, cols: int, on: torch.device):
-    """(rows, address, address of the scales or None, row stride) of an argument that is Fp8Blocks or a bf16 matrix whose rows may be
-    strided, with `cols` columns on device `on`; others raise."""
+    """(rows, tensor, scales or None, row stride) of an argument that is Fp8Blocks or a bf16 matrix whose rows may be strided, with
+    `cols` columns on device `on`; others raise."""
     if isinstance(x, Fp8Blocks):
-        rows = x._codes.shape[0]
-        _expect_fp8(what, x, rows, cols, on)
-        return rows, x._codes.data_ptr(), x._scales.data_ptr(), 0
+        rows = x.rows
+        return rows, *_expect_fp8(what, x, rows, cols, on), 0
     if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16:
         raise TypeError(f"{what}: Fp8Blocks or a bfloat16 matrix expected")
     if x.dim() != 2 or x.shape[1] != cols or x.device != on:
         raise ValueError(f"{what}: a matrix of {cols} columns on {on} is expected, got {tuple(x.shape)} on {x.device}")
-    return x.shape[0], x.data_ptr(), None, cols if x.is_contiguous() else _row_stride(what, x)
+    return x.shape[0], x, None, cols if x.is_contiguous() else _row_stride(what, x)
 
 
 def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
@@ -1075,20 +1042,18 @@ def linear_fp8(x, W: Fp8Blocks, bias: Optional[torch.Tensor] = None, residual: O
     lib = load_library()
     if not isinstance(W, Fp8Blocks):
         raise TypeError(f"W: Fp8Blocks expected, got {type(W).__name__}")
-    codes = W._codes
-    on, K, bf = codes.device, W.cols, torch.bfloat16
-    N = codes.shape[0]
-    _expect_fp8("W", W, N, K, on)
-    T, px, ps, ld = _fp8_input("x", x, K, on)
+    N, K, on, bf = W.rows, W.cols, W.device, torch.bfloat16
+    codes, scales = _expect_fp8("W", W, N, K, on)
+    T, x, xs, ld = _fp8_input("x", x, K, on)
     if not (_fits(bias, (N,), bf, on) and _fits(residual, (T, N), bf, on) and _fits(status, (1,), torch.int32, on)):
         _expect("bias", bias, (N,), bf, like=codes)
         _expect("residual", residual, (T, N), bf, like=codes)
         _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
-    ws = None if ps is not None else x.new_empty(_workspace_bytes("grouter_linear_fp8_fwd_workspace_bytes", dev, T, K), dtype=torch.uint8)
+    ws = None if xs is not None else x.new_empty(_workspace_bytes("grouter_linear_fp8_fwd_workspace_bytes", dev, T, K), dtype=torch.uint8)
     y = codes.new_empty((T, N), dtype=bf) if residual is None else torch.empty_like(residual)
-    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, px, ps, ld, codes.data_ptr(), W._scales.data_ptr(),
-          None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(), T, K, N, y.data_ptr(),
+    _call(lib.grouter_linear_fp8_fwd, "grouter_linear_fp8_fwd", dev, x.data_ptr(), None if xs is None else xs.data_ptr(), ld, codes.data_ptr(),
+          scales.data_ptr(), None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(), T, K, N, y.data_ptr(),
           None if ws is None else ws.data_ptr(), _status_ptr(status, dev))
     return y
 
@@ -1113,8 +1078,8 @@ def linear_fp8_backward(dy: torch.Tensor, xt: Optional[Fp8Blocks], Wt: Optional[
             raise TypeError(f"{name}: Fp8Blocks expected, got {type(q).__name__}")
     K = Wt.rows if Wt is not None else xt.rows if xt is not None else 8
     bf, on = torch.bfloat16, dy.device
-    _expect_fp8("xt", xt, K, T, on)
-    _expect_fp8("Wt", Wt, K, N, on)
+    xt, xt_scales = _expect_fp8("xt", xt, K, T, on)
+    Wt, Wt_scales = _expect_fp8("Wt", Wt, K, N, on)
     if not (_fits(dy, (T, N), bf, on) and _fits(db, (N,), torch.float32, on) and _fits(status, (1,), torch.int32, on)):
         _expect("dy", dy, (T, N), bf)
         _expect("db", db, (N,), torch.float32, like=dy)
@@ -1131,9 +1096,8 @@ def linear_fp8_backward(dy: torch.Tensor, xt: Optional[Fp8Blocks], Wt: Optional[
     if db is None and want_bias:
         db = dy.new_empty(N, dtype=torch.float32)
     ws = dy.new_empty(_workspace_bytes("grouter_linear_fp8_bwd_workspace_bytes", dev, T, K, N), dtype=torch.uint8)
-    codes = lambda q: (None, None) if q is None else (q.codes.data_ptr(), q.scales.data_ptr())  # noqa: E731
-    _call(lib.grouter_linear_fp8_bwd, "grouter_linear_fp8_bwd", dev, dy.data_ptr(), *codes(xt), *codes(Wt), T, K, N, _ptr(dx), _ptr(dW),
-          F32 if dW_dtype == torch.float32 else BF16, _ptr(db), ws.data_ptr(), _status_ptr(status, dev))
+    _call(lib.grouter_linear_fp8_bwd, "grouter_linear_fp8_bwd", dev, dy.data_ptr(), _ptr(xt), _ptr(xt_scales), _ptr(Wt), _ptr(Wt_scales), T, K, N,
+          _ptr(dx), _ptr(dW), F32 if dW_dtype == torch.float32 else BF16, _ptr(db), ws.data_ptr(), _status_ptr(status, dev))
     return dx, dW, db
 
 
@@ -1211,21 +1175,19 @@ def gated_ffn_fp8(x, W_g: Fp8Blocks, W_u: Fp8Blocks, W_d: Fp8Blocks, act: int = 
         raise TypeError(f"W_d: Fp8Blocks expected, got {type(W_d).__name__}")
     if W_g is None or W_u is None:
         raise TypeError("W_g, W_u: Fp8Blocks expected")
-    codes = W_d._codes
-    on, H, bf = codes.device, W_d.cols, torch.bfloat16
-    d = codes.shape[0]
-    _expect_fp8("W_g", W_g, H, d, on)
-    _expect_fp8("W_u", W_u, H, d, on)
-    _expect_fp8("W_d", W_d, d, H, on)
-    T, px, ps, ld = _fp8_input("x", x, d, on)
+    d, H, on, bf = W_d.rows, W_d.cols, W_d.device, torch.bfloat16
+    g, g_scales = _expect_fp8("W_g", W_g, H, d, on)
+    u, u_scales = _expect_fp8("W_u", W_u, H, d, on)
+    codes, scales = _expect_fp8("W_d", W_d, d, H, on)
+    T, x, xs, ld = _fp8_input("x", x, d, on)
     if not (_fits(residual, (T, d), bf, on) and _fits(status, (1,), torch.int32, on)):
         _expect("residual", residual, (T, d), bf, like=codes)
         _expect("status", status, (1,), torch.int32, like=codes)
     dev = _device_index(on)
     ws = codes.new_empty(_workspace_bytes("grouter_gated_ffn_fp8_fwd_workspace_bytes", dev, T, d, H), dtype=torch.uint8)
     y = codes.new_empty((T, d), dtype=bf) if residual is None else torch.empty_like(residual)
-    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, px, ps, ld, W_g._codes.data_ptr(), W_g._scales.data_ptr(),
-          W_u._codes.data_ptr(), W_u._scales.data_ptr(), codes.data_ptr(), W_d._scales.data_ptr(), None if residual is None else residual.data_ptr(),
+    _call(lib.grouter_gated_ffn_fp8_fwd, "grouter_gated_ffn_fp8_fwd", dev, x.data_ptr(), None if xs is None else xs.data_ptr(), ld, g.data_ptr(),
+          g_scales.data_ptr(), u.data_ptr(), u_scales.data_ptr(), codes.data_ptr(), scales.data_ptr(), None if residual is None else residual.data_ptr(),
           T, d, H, act, y.data_ptr(), ws.data_ptr(), _status_ptr(status, dev))
     return y
 
