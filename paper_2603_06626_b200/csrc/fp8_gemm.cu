@@ -327,7 +327,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8_THREADS, 1) fp8_g
     const uint32_t leader_tempty[2] = {ptx::map_to_cta(tempty_bar(0), 0), ptx::map_to_cta(tempty_bar(1), 0)};
     int acc = 0, parity = 0, which, t;
     uint32_t acc_ph = 0, top_ph = 0;
-    for (int nth = 0; f8_pick<MODE>(p, nth, pair_id, n_pairs, which, t) && !*abort_flag; ++nth) {
+    for (int nth = 0; f8_pick<MODE>(p, nth, pair_id, n_pairs, which, t) && !__any_sync(0xffffffffu, *abort_flag); ++nth) {
       const F8Product& of = p.of[which];
       const F8Tile ti = f8_tile<MODE>(of, t, rank);
       const int y0 = ti.row0 + quad * 32;
@@ -344,7 +344,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8_THREADS, 1) fp8_g
             res[i][q] = r < ti.m_valid && c0 + q * 8 < ti.n_valid ? *reinterpret_cast<const uint4*>(at + q * 8) : make_uint4(0u, 0u, 0u, 0u);
         }
       }
-      if (!ptx::mbar_wait_bounded(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
+      if (!ptx::mbar_wait_bounded_warp(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = tmem_base + (acc ? F8_ACC1 : 0u) + ((uint32_t)(quad * 32) << 16);
       // the shared columns are the last 32 of accumulator 0 and the first 32 of accumulator 1
@@ -456,7 +456,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8_THREADS, 1) fp8_g
         s_top[parity][half][r] = top;
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(top_bar(quad));
-        if (!ptx::mbar_wait_bounded(top_bar(quad), top_ph, abort_flag, p.wait_limit_ns)) break;
+        if (!ptx::mbar_wait_bounded_warp(top_bar(quad), top_ph, abort_flag, p.wait_limit_ns)) break;
         top = fmaxf(top, s_top[parity][half ^ 1][r]);
         parity ^= 1;
         top_ph ^= 1u;

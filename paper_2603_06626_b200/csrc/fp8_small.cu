@@ -241,7 +241,7 @@ fp8_small_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     }
     // the accumulators are complete: every load has landed and every MMA has read its stage, so the ring is free
     const int quad = warp & 3;                         // TMEM lane quadrant this warp may read
-    if (warp < 6 && ptx::mbar_wait_bounded(done_bar, 0u, abort_flag, p.wait_limit_ns)) {
+    if (warp < 6 && ptx::mbar_wait_bounded_warp(done_bar, 0u, abort_flag, p.wait_limit_ns)) {
       ptx::tc_fence_after();
       const int tv = min(TN, p.T - t0);
 #pragma unroll

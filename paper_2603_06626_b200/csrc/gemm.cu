@@ -355,6 +355,9 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     }
   };
 
+  // A whole warp's next tile: one lane's view of tile and abort flag for all, because the warp must not part.
+  auto same_tile = [&](int v) { return __shfl_sync(0xffffffffu, *abort_flag ? n_tiles : v, 0); };
+
   if (warp == 0) {
     // ===================== TMA producer (both CTAs) =====================
     if (lane == 0) {
@@ -462,8 +465,6 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       constexpr bool count = COUNT;
       long long c_acc = 0, c_full = 0, n_tiles_done = 0, n_ksteps = 0;
       const long long c_begin = count ? clock64() : 0;
-      // one lane's view of tile and abort flag for all: the warp must not part
-      auto same_tile = [&](int v) { return __shfl_sync(0xffffffffu, *abort_flag ? n_tiles : v, 0); };
       for (int t = same_tile(DYN ? next_tile() : pair_id); t < n_tiles; t = same_tile(DYN ? next_tile() : t + n_pairs)) {
         const Tile ti = decode_tile<MODE>(p, t, 0);
         const long long c_t0 = count ? clock64() : 0;
@@ -612,7 +613,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     int acc = 0;
     uint32_t acc_ph = 0;
     uint32_t flip = 0;                    // staging block the next single-block store uses (they strictly alternate)
-    for (int t = DYN ? next_tile() : pair_id; t < n_tiles && !*abort_flag; t = DYN ? next_tile() : t + n_pairs) {
+    for (int t = same_tile(DYN ? next_tile() : pair_id); t < n_tiles; t = same_tile(DYN ? next_tile() : t + n_pairs)) {
       const Tile ti = decode_tile<MODE>(p, t, rank);
       const bool live = ti.m_valid > 0;    // false: this CTA only lent its half of B to the pair
       uint4 g4[4], u4[4];
@@ -621,7 +622,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         load_residual(ti, 0, g4);
         load_residual(ti, 1, u4);
       }
-      if (!ptx::mbar_wait_bounded(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
+      if (!ptx::mbar_wait_bounded_warp(tfull_bar(acc), acc_ph, abort_flag, p.wait_limit_ns)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)acc * BN + ((uint32_t)(quad * 32) << 16);
       const bool have_acc = ti.num_k > 0;

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(LS_THREADS, 2) linear_small_kernel(const __gri
   } else {
     // the accumulator is complete: every load has landed and every MMA has read its stage, so the ring is free
     const int quad = warp & 3;                         // TMEM lane quadrant this warp may read
-    if (ptx::mbar_wait_bounded(done_bar, 0u, abort_flag, p.wait_limit_ns)) {
+    if (ptx::mbar_wait_bounded_warp(done_bar, 0u, abort_flag, p.wait_limit_ns)) {
       ptx::tc_fence_after();
       const int tv = min(TN, p.T - t0);
 #pragma unroll

@@ -96,7 +96,8 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
   }
 }
 
-// The same wait by a whole converged warp: true where every lane's wait ended well.
+// The same wait by a whole converged warp: true where every lane's wait ended well.  Whatever is done by a warp together (reads of tensor
+// memory, shuffles, __syncwarp) waits so: of lanes that give up one by one some could leave and others go on.
 __device__ __forceinline__ bool mbar_wait_bounded_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
   return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, limit_ns));
 }

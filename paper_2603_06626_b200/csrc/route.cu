@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(RF_THREADS) route_fused_kernel(const __grid_co
     const int quad = warp & 3;                       // the TMEM lane quadrant this warp may read
     const int t = row0 + quad * 32 + lane;
     const bool have = t < p.T;
-    if (ptx::mbar_wait_bounded(tfull_bar, 0u, abort_flag, p.wait_limit_ns)) {
+    if (ptx::mbar_wait_bounded_warp(tfull_bar, 0u, abort_flag, p.wait_limit_ns)) {
       ptx::tc_fence_after();
       const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16);
       float bv[RF_KEEP];
