@@ -217,7 +217,7 @@ int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const
 }
 
 size_t grouter_linear_fp8_fwd_workspace_bytes(int32_t T, int32_t K) {
-  return T < 0 || K < 1 ? 0 : fp8_input(T, K).bytes;
+  return fp8_check(T, K, 8) != GROUTER_OK ? 0 : fp8_input(T, K).bytes;
 }
 
 int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W, const void* W_scales, const void* bias,
@@ -242,7 +242,7 @@ int grouter_linear_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, con
 }
 
 size_t grouter_linear_fp8_bwd_workspace_bytes(int32_t T, int32_t K, int32_t N) {
-  if (fp8_check(T, K, N) != GROUTER_OK || T > FP8_MAX_COLS) return 0;
+  if (fp8_check(T, K, N) != GROUTER_OK || K % 8 || T > FP8_MAX_COLS) return 0;
   return fp8_workspace(T, K, N).bytes;
 }
 
@@ -301,7 +301,8 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
 }
 
 size_t grouter_gated_ffn_fp8_fwd_workspace_bytes(int32_t T, int32_t d, int32_t H) {
-  return T < 0 || d < 1 || H < 1 ? 0 : fp8_input(T, d).bytes + fp8_input(T, H).bytes;
+  if (gated_check(T, d, H, GROUTER_ACT_NONE) != GROUTER_OK || fp8_check(T, d, H) != GROUTER_OK || fp8_check(T, H, d) != GROUTER_OK) return 0;
+  return fp8_input(T, d).bytes + fp8_input(T, H).bytes;
 }
 
 int grouter_gated_ffn_fp8_fwd(const void* x, const void* x_scales, int64_t ldx, const void* W_g, const void* W_g_scales, const void* W_u,

@@ -553,7 +553,7 @@ int grouter_layernorm_fwd(const void* x, int64_t ldx, const void* w, const void*
 }
 
 size_t grouter_layernorm_bwd_workspace_bytes(int32_t rows, int32_t d) {
-  if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
+  if (norm_check(rows, d, d, GROUTER_BF16, GROUTER_BF16) != GROUTER_OK) return 0;
   // alignment is not known here: as many partial rows as rows without a ring leave
   return (size_t)std::max(norm_backward_grid(rows, d, false).parts(), 1) * 2 * d * sizeof(float);
 }

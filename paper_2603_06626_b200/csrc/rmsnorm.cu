@@ -490,7 +490,7 @@ int grouter_rmsnorm_fwd(const void* x, int64_t ldx, const void* residual, int64_
 }
 
 size_t grouter_rmsnorm_bwd_workspace_bytes(int32_t rows, int32_t d) {
-  if (rows < 0 || d < 1 || d > RMS_MAX_D) return 0;
+  if (rms_check(rows, d, d, GROUTER_BF16, GROUTER_BF16) != GROUTER_OK) return 0;
   return (size_t)rms_backward_blocks(rows, d) * d * sizeof(float);
 }
 
