@@ -203,7 +203,7 @@ struct LinearGemm {
   void *C, *pre;
   int a_mn, b_mn, M, N, K, act;
   int32_t* status;
-  bool waits_at_end;      // works beside the end of the kernel before it, whose results it does not read (launch_linear_gemm only)
+  bool waits_at_end;      // works beside the end of the kernels before it, back to the last that waited at its start (vec.cuh; launch_linear_gemm only)
 };
 cudaError_t launch_linear_gemm(const LinearGemm& g, cudaStream_t st);
 // Forward (A = x [T,K], W = W_gu [2H,K]): H = act(G) U and, with pre, [G|U] -> pre [T,2H].  Backward (A = dy [T,K], W = W_d [K,H]): with

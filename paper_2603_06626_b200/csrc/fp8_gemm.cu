@@ -62,7 +62,7 @@ struct F8Params {
   uint8_t* out_scales;           // GLU
   int32_t* status;
   unsigned long long wait_limit_ns;
-  int waits_at_end;              // as in gemm.cu: works beside the end of the kernel before it
+  int waits_at_end;              // as in gemm.cu
 };
 
 // The i-th tile of a pair; false behind its last.  TWO: the first product's tiles go round the pairs; the second's, whose contraction is shorter,

@@ -17,7 +17,7 @@ struct Fp8Gemm {
   int M, N, K, act, out_f32;
   int32_t* status;
   int pieces, piece_steps;                // with out_f32, over 1: C [pieces][fp8_piece_rows(M)][N] of partial products over piece_steps 128-deep steps each
-  bool waits_at_end;                      // launch_fp8_gemm: works beside the end of the kernel before it, whose results it does not read
+  bool waits_at_end;                      // launch_fp8_gemm: works beside the end of the kernels before it, back to the last that waited at its start (vec.cuh)
 };
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
 // Two products that need nothing of one another, bf16 or f32 out, in one launch; a is the one with the longer contraction (or pieces).

@@ -203,8 +203,9 @@ int grouter_gated_ffn_bwd(const void* dy, const void* x, const void* W_gu, const
     if (launch_product(l, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   // The three products read what the first kernel wrote and nothing of one another: each works beside the end of the one before it, whose
-  // last round leaves pairs of SMs idle (4095 x 1024, hidden 2816: 64, 88 and 44 tiles for 74 pairs).  The first of them waits for the
-  // kernel before it at its start, as the others rely on.
+  // last round leaves pairs of SMs idle (4095 x 1024, hidden 2816: 64, 88 and 44 tiles for 74 pairs).  The first of them, dx's where it is
+  // wanted, waits for the first kernel at its start; the others rely on that one's wait, dW_d's on the far side of dW_gu's, which does not wait
+  // before it lets dW_d's start (launch_dependent, vec.cuh).
   bool beside = dx != nullptr;
   if (dW_gu) {
     if (launch_weight_product(ws + w.dp, x, T, d, 2 * H, dW_gu, dW_dtype, ws + w.pieces_gu, status, beside, st) != cudaSuccess) return GROUTER_ERR_CUDA;
@@ -291,7 +292,7 @@ int grouter_linear_fp8_bwd(const void* dy, const void* xt, const void* xt_scales
     if (launch_fp8_gemms(w_first ? to_w : to_x, w_first ? to_x : to_w, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   } else {
     if (dx && fp8_product(to_x, st) != cudaSuccess) return GROUTER_ERR_CUDA;
-    to_w.waits_at_end = dx != nullptr;       // of dx's product, which waited for the codes, it needs nothing
+    to_w.waits_at_end = dx != nullptr;       // of dx's product, which waits at its start for the codes (and sums of db), it needs nothing
     if (dW && launch_fp8_gemm(to_w, st) != cudaSuccess) return GROUTER_ERR_CUDA;
   }
   if (dW && pieces.count > 1 &&

@@ -92,8 +92,8 @@ struct GemmParams {
   unsigned int* tile_counter;  // device scalar, zero at launch (unused by DENSE, which has no context to keep one)
   unsigned long long* cycles;  // null, or GEMM_CYCLE_COUNTERS counters every issuer adds its account to
   unsigned long long wait_limit_ns;   // how long any one wait (barrier, tile queue) may last before the CTA gives up
-  // DENSE, LINEAR: nothing of the kernel before this one on the stream is read, and nothing it reads is written: this kernel works beside its
-  // end and waits for it before it ends itself.  The kernel before must have waited for its own predecessors before it let this one start.
+  // DENSE, LINEAR: nothing of the kernels before this one, back to the last that waited at its start, is read, and nothing they read or write is
+  // written: this kernel works beside their end and waits for the one before it when it ends itself (launch_dependent, vec.cuh).
   int32_t waits_at_end;
 };
 

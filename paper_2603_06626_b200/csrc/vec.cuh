@@ -16,8 +16,17 @@ inline int current_sms() {
   return n;
 }
 
-// Launches a kernel that reads what the kernel before it on the stream wrote: it may be scheduled while that one still runs
-// (programmatic dependent launch), so it has to call after_previous_kernel() before it touches anything.
+// Launches a kernel that may be scheduled while the kernel before it on the stream still runs (programmatic dependent launch).  It calls
+// after_previous_kernel() before it touches anything, or, launched with waits_at_end, before it ends.
+//
+// waits_at_end: such a kernel works beside the end of a run of kernels.  For the runs that the operators launch this holds, and has to hold
+// when one of them is changed:
+//   - A run begins with a kernel that waits at its start, before it lets the next one start.  All that came before it on the stream is then
+//     complete for every kernel of the run, however early it is scheduled: each of them starts after all blocks of the one before have
+//     let it, and so, going back, after the first one's wait.
+//   - No kernel of the run reads or overwrites what another one of it writes, nor writes what another one reads.
+//   - Each kernel after the first waits for the one before it at its end, so that the last one's end is the end of all: whatever waits for
+//     that one at its start (a sum of pieces, the next call) may read what any of them wrote.
 template <typename... Params, typename... Args>
 inline cudaError_t launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg{};
@@ -32,9 +41,11 @@ inline cudaError_t launch_dependent(void (*kern)(Params...), dim3 grid, dim3 blo
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
 }
-// Waits until the kernel before this one has ended and its writes are visible.
+// Waits until the kernel before this one on the stream has ended (and so, as each waits for the one before it, all before that) and its
+// writes are visible.
 __device__ __forceinline__ void after_previous_kernel() { cudaGridDependencySynchronize(); }
-// From here on the next kernel's blocks may be scheduled (they still wait for this kernel's end before they read).
+// From here on, once every block of this kernel has come here or ended, the next kernel's blocks may be scheduled.  What they may touch before
+// this kernel's end is said at launch_dependent.
 __device__ __forceinline__ void let_next_kernel_start() { cudaTriggerProgrammaticLaunchCompletion(); }
 
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
