@@ -14,9 +14,9 @@
 // Every wait is bounded, as in gemm.cu.
 //
 // Measured: 8192 x 4096 x 4096 95-107 us, 8192^3 381-445 (2.5 to 2.9 PFLOP/s by the clock that the power limit leaves); GLU 16384 tokens, 4096 ->
-// 1536 126 us with the tensor pipe 80 % active; 16384 x 1536 x 4096 with a residual 85-95, 57 %: every 12 steps a tile of 128 KB goes out and
-// one of the residual comes in.  A step takes its 32 KB per SM in 256 tensor cycles, twice the pace at which bf16 tiles need theirs, so
-// tiles smaller than 256 x 256 are out.
+// 1536 126 us with the tensor pipe 80 % active; 16384 x 1536 x 4096 with a residual 85-100 (119 in a loop at the power
+// limit), 57 %: every 12 steps a tile of 128 KB goes out and one of the residual comes in.  A step takes its 32 KB per SM in 256 tensor
+// cycles, twice the pace at which bf16 tiles need theirs, so tiles smaller than 256 x 256 are out.
 #include "act.cuh"
 #include "fp8.cuh"
 #include "fp8_gemm.cuh"
